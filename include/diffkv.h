@@ -144,15 +144,18 @@ enum {
     DIFFKV_OP_COMPACT = 2,
     DIFFKV_OP_ALLOC = 3,
     DIFFKV_OP_GENERATION = 4,
-    DIFFKV_OP_PROMPT_SIGNIFICANCE = 5
+    DIFFKV_OP_PROMPT_SIGNIFICANCE = 5,
+    DIFFKV_OP_CHUNK_ATTENTION = 6,
+    DIFFKV_OP_CHUNK_SIGNIFICANCE = 7
 };
 
 /* Bytes of device workspace the operation needs (host out-parameter).
  * APPEND: num_seqs, num_kv_heads, total_new.  ATTENTION: num_seqs,
  * num_q_heads, num_splits (0 = automatic, -1 = balanced).
  * COMPACT / ALLOC / GENERATION: num_seqs*num_kv_heads tables.
- * PROMPT_SIGNIFICANCE: num_seqs, num_q_heads, total_new.  Unused sizes
- * are ignored. */
+ * PROMPT_SIGNIFICANCE: num_seqs, num_q_heads, total_new.
+ * CHUNK_ATTENTION / CHUNK_SIGNIFICANCE: num_seqs, num_q_heads, num_kv_heads,
+ * total_new.  Unused sizes are ignored. */
 diffkv_status diffkv_workspace_size(int32_t op, const diffkv_layout* layout,
                                     int32_t num_seqs, int32_t num_q_heads,
                                     int32_t num_kv_heads, int64_t total_new,
@@ -324,6 +327,139 @@ diffkv_status diffkv_prompt_significance(const diffkv_layout* layout, int32_t nu
                                          int32_t num_kv_heads, const uint16_t* q, const uint16_t* k,
                                          float sm_scale, const float* lse, float* score, void* ws,
                                          size_t ws_bytes, void* stream);
+
+/*
+ * Rotary positions of queries and keys, before they reach the entry points
+ * here (which all take rotated rows).  Pair i of a head's first rot_dim dims,
+ *   (x[i], x[i + rot_dim/2])  DIFFKV_ROPE_HALF,
+ *   (x[2i], x[2i + 1])        DIFFKV_ROPE_INTERLEAVED,
+ * is turned by the angle t = pos * inv_freq[i] and scaled:
+ *   a' = scale * (a cos t - b sin t),  b' = scale * (b cos t + a sin t);
+ * dims rot_dim .. head_dim-1 pass unchanged.
+ *   pos       device int32 [rows]: position of each row's token (any value)
+ *   inv_freq  device fp32 [rot_dim/2], 16-byte aligned: radians per position
+ *             (diffkv_rope_frequencies fills such a table)
+ *   rot_dim   a multiple of 16 up to head_dim (DIFFKV_E_UNSUPPORTED if it is
+ *             another even number)
+ *   q, k      device fp16: row r, head h at q + r*q_stride + h*head_dim, so that
+ *             slices of a fused projection can be passed; strides in elements,
+ *             at least heads*head_dim (any value with one row).  k and k_out are
+ *             NULL with num_kv_heads 0 (then only q is turned).
+ *   q_out, k_out  device fp16, with strides of their own; q_out == q with
+ *             the same stride turns in place, otherwise they must not overlap
+ *             the inputs.
+ * All row addresses 16-byte aligned, strides multiples of 8, else
+ * DIFFKV_E_INVAL.  Angles are taken in 64 bits, so positions of any size keep
+ * theirs; products in fp32, one rounding to fp16 (head_dim 128 only).
+ */
+enum { DIFFKV_ROPE_HALF = 0, DIFFKV_ROPE_INTERLEAVED = 1 };
+
+diffkv_status diffkv_rotate(const diffkv_layout* layout, int64_t rows, const int32_t* pos,
+                            const float* inv_freq, int32_t rot_dim, int32_t style, float scale,
+                            int32_t num_q_heads, const uint16_t* q, int64_t q_stride,
+                            uint16_t* q_out, int64_t q_out_stride,
+                            int32_t num_kv_heads, const uint16_t* k, int64_t k_stride,
+                            uint16_t* k_out, int64_t k_out_stride, void* stream);
+
+/*
+ * Frequencies of rotary positions, computed on the host in 64 bits:
+ * f_i = base^(-2i/rot_dim), i < rot_dim/2, for contexts longer than the trained
+ * ones by `factor` (>= 1):
+ *   DIFFKV_ROPE_PLAIN     f_i
+ *   DIFFKV_ROPE_LINEAR    f_i / factor
+ *   DIFFKV_ROPE_BASE      the base becomes base * factor^(rot_dim/(rot_dim-2))
+ *   DIFFKV_ROPE_BY_PARTS  f_i * (g + (1-g)/factor), g = clamp((r_i - slow)/
+ *             (fast - slow), 0, 1) with r_i = trained_len * f_i / (2 pi) turns
+ *             over the trained length, fast > slow >= 0 (arXiv 2309.00071), and
+ *             *scale = 0.1 ln(factor) + 1.
+ * *scale is 1 in the other forms.  inv_freq: host fp32 [rot_dim/2].
+ * trained_len, slow and fast are read by DIFFKV_ROPE_BY_PARTS alone.
+ * DIFFKV_E_INVAL: rot_dim not even and positive (above 2 for _BASE), base not
+ * above 0, factor below 1, a parameter not finite, a NULL pointer.
+ */
+enum { DIFFKV_ROPE_PLAIN = 0, DIFFKV_ROPE_LINEAR = 1, DIFFKV_ROPE_BASE = 2, DIFFKV_ROPE_BY_PARTS = 3 };
+
+diffkv_status diffkv_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                                      int32_t trained_len, double slow, double fast,
+                                      float* inv_freq, float* scale);
+
+/*
+ * The form of a chunk's attention scores (a NULL pointer: all off).  For a
+ * query of head hq at position p and a key at position c <= p:
+ *   x = sm_scale * q . k;
+ *   cap > 0:         x <- cap * tanh(x / cap);
+ *   slopes != NULL:  x <- x - slopes[hq] * (p - c)  (device fp32 [num_q_heads]);
+ *   window > 0:      the key is seen only if p - c < window.
+ * cap finite and >= 0, window >= 0, else DIFFKV_E_INVAL.
+ */
+typedef struct diffkv_score_form {
+    float cap;
+    int32_t window;
+    const float* slopes;
+} diffkv_score_form;
+
+/*
+ * Attention of a chunk of new tokens over the compressed cache, before the
+ * chunk is appended: a prompt's next part, drafted tokens that are checked at
+ * once, one decoded token, or any mixture over the sequences.  New token j of
+ * sequence b has position p = seq_len[b] + j; its query of head hq attends to
+ * every kept token of table b*Hkv + hq/(Hq/Hkv) (k_hat, v_hat as in
+ * diffkv_decode_attention; their positions from the pages) and to the chunk's own
+ * tokens 0 .. j in fp16:
+ *   out[row][hq] = sum_c softmax_c(x) v_c,  x as in diffkv_score_form.
+ *   new_len  device int32 [num_seqs], rows of sequence b follow those of b-1.
+ *            They must sum to total_new with every entry in [0, max_new];
+ *            lengths are clamped so that no row past total_new is read or
+ *            written, and rows that no sequence owns are left as they were.
+ *   q, k, v  device fp16: row r, head h at q + r*q_stride + h*head_dim (slices
+ *            of a fused projection can be passed), 16-byte aligned, strides in
+ *            elements, multiples of 8, at least heads*head_dim
+ *   out      device fp16 [total_new][num_q_heads][head_dim], 16-byte aligned
+ *   lse      device fp32 [total_new][num_q_heads] (natural log of the softmax
+ *            denominator) or NULL
+ *   ws       diffkv_workspace_size(DIFFKV_OP_CHUNK_ATTENTION, ...) bytes, no
+ *            clearing needed; calls that may overlap need one each
+ * The cache is read only.  A page ID outside the pool counts no tokens.
+ * sm_scale positive and finite (DIFFKV_E_INVAL otherwise).  The layouts of
+ * diffkv_layout_init's list, up to 8 query heads per KV head.
+ * Precision: q . k_hat exact up to fp32 summation, fp32 softmax statistics;
+ * weights and v_hat are rounded to fp16 (2^-11 each), products summed in fp32,
+ * and out is rounded once.  A non-finite own value reaches only the rows that
+ * see its token.
+ */
+diffkv_status diffkv_chunk_attention(const diffkv_layout* layout, const diffkv_cache* cache,
+                                     int64_t total_new, int32_t max_new, const int32_t* new_len,
+                                     int32_t num_q_heads, const uint16_t* q, int64_t q_stride,
+                                     const uint16_t* k, int64_t k_stride,
+                                     const uint16_t* v, int64_t v_stride,
+                                     float sm_scale, const diffkv_score_form* form,
+                                     uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Significance of a chunk (Sec. 4), after diffkv_chunk_attention with the same
+ * q, k and form, before the chunk is appended.  With P the attention
+ * probabilities of the chunk's n = new_len[b] queries, combined over a KV
+ * head's query heads by their maximum, X_c = sum_j max_hq P_hq[j][c]:
+ *   a kept token at position c:  score <- score + (X_c - n*score) / (N - c),
+ *            N = seq_len[b] + n: the mean over the N - c queries it has received,
+ *            in place in its page, as diffkv_update_significance does for one
+ *            query;
+ *   own token i:  score[row i][h] = X_i / (n - i), the mean over the queries it
+ *            has received, as diffkv_prompt_significance gives it; it feeds the
+ *            `score` argument of diffkv_quantize_append.
+ *   lse      device fp32 [total_new][num_q_heads] as diffkv_chunk_attention
+ *            wrote it
+ *   score    device fp32 [total_new][num_kv_heads] out
+ *   ws       diffkv_workspace_size(DIFFKV_OP_CHUNK_SIGNIFICANCE, ...) bytes
+ * Tables of sequences without new tokens are left alone.  fp32 arithmetic.
+ * Other arguments, limits and errors as diffkv_chunk_attention.
+ */
+diffkv_status diffkv_chunk_significance(const diffkv_layout* layout, const diffkv_cache* cache,
+                                        int64_t total_new, int32_t max_new, const int32_t* new_len,
+                                        int32_t num_q_heads, const uint16_t* q, int64_t q_stride,
+                                        const uint16_t* k, int64_t k_stride, float sm_scale,
+                                        const diffkv_score_form* form, const float* lse, float* score,
+                                        void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Parallel free-list compaction (Sec. 5.2 recycling, Sec. 5.3): for the

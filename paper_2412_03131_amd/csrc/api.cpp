@@ -1,5 +1,6 @@
 // api.cpp -- the C ABI of include/diffkv.h: argument checks, workspace
 // carving and kernel dispatch.  No allocation, no synchronisation.
+#include <math.h>
 #include <string.h>
 
 #include "internal.hpp"
@@ -254,6 +255,67 @@ diffkv_status attention_call(const diffkv_layout* layout, const diffkv_cache* ca
     return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
 }
 
+// Chunk attention: the partial states of split rows.
+int64_t chunk_ws(int64_t B, int64_t Hq, int64_t Hkv, int64_t total_new, int64_t p_max)
+{
+    const int64_t splits = chunk_splits(B, Hq, Hkv, total_new, p_max);
+    return splits > 1 ? align256(total_new * Hq * splits * kChunkPart * 4) : 0;
+}
+
+// A row of `heads` heads every `stride` halfs, as the vector loads and stores need it.
+bool rows_valid(const void* p, int64_t stride, int64_t heads, int64_t rows)
+{
+    return p && (uintptr_t)p % 16 == 0 && stride % 8 == 0 && (stride >= heads * kD || rows <= 1) && stride >= 0;
+}
+
+// What both chunk entry points check, and the arguments they share.
+diffkv_status chunk_call(const diffkv_layout* layout, const diffkv_cache* cache, int64_t total_new, int32_t max_new,
+                         const int32_t* new_len, int32_t num_q_heads, const uint16_t* q, int64_t q_stride,
+                         const uint16_t* k, int64_t k_stride, float sm_scale, const diffkv_score_form* form, ChunkArgs& a,
+                         bool& mod)
+{
+    if (!layout_valid(layout) || !cache_valid(cache) || !cache->pool || !cache->seq_len) return DIFFKV_E_INVAL;
+    if (total_new < 0 || max_new < 0 || total_new > INT32_MAX / 4) return DIFFKV_E_INVAL;
+    if (num_q_heads <= 0 || num_q_heads % cache->num_kv_heads != 0) return DIFFKV_E_INVAL;
+    if (!(sm_scale > 0.0f) || sm_scale > 1e30f) return DIFFKV_E_INVAL;
+    if (form && (!(form->cap >= 0.0f) || form->cap > 1e30f || form->window < 0)) return DIFFKV_E_INVAL;
+    if (!layout_kernels_supported(layout)) return DIFFKV_E_UNSUPPORTED;
+    if (num_q_heads / cache->num_kv_heads > 8) return DIFFKV_E_UNSUPPORTED;
+    memset(&a, 0, sizeof(a));
+    if (cache->num_seqs == 0 || total_new == 0 || max_new == 0) return DIFFKV_OK;
+    if (!new_len || !rows_valid(q, q_stride, num_q_heads, total_new) ||
+        !rows_valid(k, k_stride, cache->num_kv_heads, total_new))
+        return DIFFKV_E_INVAL;
+    a.p_max = layout->p_max;
+    a.page_bytes = layout->page_bytes;
+    a.num_pages = cache->num_pages;
+    a.pool = cache->pool;
+    a.pool_rw = cache->pool;
+    a.page_table = cache->page_table;
+    a.len = cache->len;
+    a.seq_len = cache->seq_len;
+    a.B = cache->num_seqs;
+    a.Hkv = cache->num_kv_heads;
+    a.Hq = num_q_heads;
+    a.max_new = max_new < total_new ? max_new : (int32_t)total_new;  // no sequence has more rows than there are
+    a.total_new = total_new;
+    a.new_len = new_len;
+    a.q = q;
+    a.k = k;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    const float log2e = 1.4426950408889634f;
+    const float cap = form ? form->cap : 0.0f;
+    a.scale = cap > 0.0f ? sm_scale : sm_scale * log2e;
+    a.cap_in = cap > 0.0f ? 2.0f * log2e / cap : 0.0f;
+    a.cap_out = cap * log2e;
+    a.slopes = form ? form->slopes : nullptr;
+    a.window = form && form->window > 0 ? form->window : INT32_MAX;
+    a.layout = layout_index(layout);
+    mod = cap > 0.0f || a.slopes || a.window != INT32_MAX;
+    return DIFFKV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -295,6 +357,13 @@ diffkv_status diffkv_workspace_size(int32_t op, const diffkv_layout* layout, int
     case DIFFKV_OP_PROMPT_SIGNIFICANCE:
         if (num_q_heads <= 0 || total_new < 0) return DIFFKV_E_INVAL;
         *bytes = (size_t)prompt_ws(num_seqs, num_q_heads, total_new).total;
+        return DIFFKV_OK;
+    case DIFFKV_OP_CHUNK_ATTENTION:
+    case DIFFKV_OP_CHUNK_SIGNIFICANCE:
+        if (num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || total_new < 0) return DIFFKV_E_INVAL;
+        *bytes = op == DIFFKV_OP_CHUNK_ATTENTION
+                     ? (size_t)chunk_ws(num_seqs, num_q_heads, num_kv_heads, total_new, layout->p_max)
+                     : 0;
         return DIFFKV_OK;
     default:
         return DIFFKV_E_INVAL;
@@ -450,6 +519,117 @@ diffkv_status diffkv_prompt_significance(const diffkv_layout* layout, int32_t nu
     a.part = reinterpret_cast<float*>(base + w.part);
     a.lse2 = reinterpret_cast<float*>(base + w.lse2);
     hipError_t e = launch_prompt_significance(a, num_q_heads / num_kv_heads, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
+}
+
+diffkv_status diffkv_rotate(const diffkv_layout* layout, int64_t rows, const int32_t* pos, const float* inv_freq,
+                            int32_t rot_dim, int32_t style, float scale, int32_t num_q_heads, const uint16_t* q,
+                            int64_t q_stride, uint16_t* q_out, int64_t q_out_stride, int32_t num_kv_heads,
+                            const uint16_t* k, int64_t k_stride, uint16_t* k_out, int64_t k_out_stride, void* stream)
+{
+    if (!layout_valid(layout) || rows < 0 || num_q_heads <= 0 || num_kv_heads < 0) return DIFFKV_E_INVAL;
+    if (rot_dim <= 0 || rot_dim % 2 != 0 || rot_dim > layout->head_dim) return DIFFKV_E_INVAL;
+    if (style != DIFFKV_ROPE_HALF && style != DIFFKV_ROPE_INTERLEAVED) return DIFFKV_E_INVAL;
+    if (layout->head_dim != kD || rot_dim % 16 != 0) return DIFFKV_E_UNSUPPORTED;
+    if ((num_kv_heads > 0) != (k != nullptr) || (k != nullptr) != (k_out != nullptr)) return DIFFKV_E_INVAL;
+    if ((int64_t)num_q_heads + num_kv_heads > INT32_MAX / kD || rows > ((int64_t)1 << 40)) return DIFFKV_E_INVAL;
+    if (rows == 0) return DIFFKV_OK;
+    if (!pos || !inv_freq || (uintptr_t)inv_freq % 16 != 0) return DIFFKV_E_INVAL;
+    if (!rows_valid(q, q_stride, num_q_heads, rows) || !rows_valid(q_out, q_out_stride, num_q_heads, rows))
+        return DIFFKV_E_INVAL;
+    if (k && (!rows_valid(k, k_stride, num_kv_heads, rows) || !rows_valid(k_out, k_out_stride, num_kv_heads, rows)))
+        return DIFFKV_E_INVAL;
+    if ((q == q_out && q_stride != q_out_stride && rows > 1) || (k && k == k_out && k_stride != k_out_stride && rows > 1))
+        return DIFFKV_E_INVAL;
+    RotateArgs a;
+    memset(&a, 0, sizeof(a));
+    a.rows = rows;
+    a.pos = pos;
+    a.freq = inv_freq;
+    a.rot_dim = rot_dim;
+    a.style = style;
+    a.scale = scale;
+    a.in[0] = q;
+    a.in[1] = k;
+    a.out[0] = q_out;
+    a.out[1] = k_out;
+    a.in_stride[0] = q_stride;
+    a.in_stride[1] = k_stride;
+    a.out_stride[0] = q_out_stride;
+    a.out_stride[1] = k_out_stride;
+    a.heads[0] = num_q_heads;
+    a.heads[1] = num_kv_heads;
+    hipError_t e = launch_rotate(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
+}
+
+diffkv_status diffkv_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t trained_len,
+                                      double slow, double fast, float* inv_freq, float* scale)
+{
+    if (!inv_freq || !scale || rot_dim <= 0 || rot_dim % 2 != 0) return DIFFKV_E_INVAL;
+    if (!(base > 0.0) || !isfinite(base) || !(factor >= 1.0) || !isfinite(factor)) return DIFFKV_E_INVAL;
+    if (scaling < DIFFKV_ROPE_PLAIN || scaling > DIFFKV_ROPE_BY_PARTS) return DIFFKV_E_INVAL;
+    if (scaling == DIFFKV_ROPE_BASE) {
+        if (rot_dim <= 2) return DIFFKV_E_INVAL;
+        base *= pow(factor, (double)rot_dim / (rot_dim - 2));
+        if (!isfinite(base)) return DIFFKV_E_INVAL;
+    }
+    if (scaling == DIFFKV_ROPE_BY_PARTS && (trained_len <= 0 || !(slow >= 0.0) || !(fast > slow) || !isfinite(fast)))
+        return DIFFKV_E_INVAL;
+    for (int32_t i = 0; i < rot_dim / 2; ++i) {
+        double f = pow(base, -2.0 * i / rot_dim);
+        if (scaling == DIFFKV_ROPE_LINEAR) f /= factor;
+        if (scaling == DIFFKV_ROPE_BY_PARTS) {
+            const double turns = trained_len * f / 6.283185307179586477;
+            double g = (turns - slow) / (fast - slow);
+            g = g < 0.0 ? 0.0 : (g > 1.0 ? 1.0 : g);
+            f *= g + (1.0 - g) / factor;
+        }
+        inv_freq[i] = (float)f;
+    }
+    *scale = scaling == DIFFKV_ROPE_BY_PARTS ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+    return DIFFKV_OK;
+}
+
+diffkv_status diffkv_chunk_attention(const diffkv_layout* layout, const diffkv_cache* cache, int64_t total_new,
+                                     int32_t max_new, const int32_t* new_len, int32_t num_q_heads, const uint16_t* q,
+                                     int64_t q_stride, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                                     int64_t v_stride, float sm_scale, const diffkv_score_form* form, uint16_t* out,
+                                     float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    ChunkArgs a;
+    bool mod = false;
+    const diffkv_status s = chunk_call(layout, cache, total_new, max_new, new_len, num_q_heads, q, q_stride, k, k_stride,
+                                       sm_scale, form, a, mod);
+    if (s != DIFFKV_OK || a.total_new == 0) return s;
+    if (!rows_valid(v, v_stride, a.Hkv, total_new) || !out || (uintptr_t)out % 16 != 0) return DIFFKV_E_INVAL;
+    const int64_t need = chunk_ws(a.B, a.Hq, a.Hkv, total_new, a.p_max);
+    if (need > 0 && (!ws || (int64_t)ws_bytes < need)) return DIFFKV_E_WORKSPACE;
+    a.v = v;
+    a.v_stride = v_stride;
+    a.out = out;
+    a.lse = lse;
+    a.part = static_cast<float*>(ws);
+    a.splits = chunk_splits(a.B, a.Hq, a.Hkv, total_new, a.p_max);
+    hipError_t e = launch_chunk_attention(a, mod, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
+}
+
+diffkv_status diffkv_chunk_significance(const diffkv_layout* layout, const diffkv_cache* cache, int64_t total_new,
+                                        int32_t max_new, const int32_t* new_len, int32_t num_q_heads, const uint16_t* q,
+                                        int64_t q_stride, const uint16_t* k, int64_t k_stride, float sm_scale,
+                                        const diffkv_score_form* form, const float* lse, float* score, void* ws,
+                                        size_t ws_bytes, void* stream)
+{
+    ChunkArgs a;
+    bool mod = false;
+    const diffkv_status s = chunk_call(layout, cache, total_new, max_new, new_len, num_q_heads, q, q_stride, k, k_stride,
+                                       sm_scale, form, a, mod);
+    if (s != DIFFKV_OK || a.total_new == 0) return s;
+    if (!lse || !score) return DIFFKV_E_INVAL;
+    a.lse_in = lse;
+    a.score = score;
+    hipError_t e = launch_chunk_scores(a, mod, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
 }
 

@@ -1,0 +1,215 @@
+// chunk_common.hpp -- what the kernels on chunks of new tokens share: arguments,
+// the search for a workgroup's sequence, and the operands of their matrix products.
+//
+// A chunk's query heads of one KV head are its rows: row r of sequence b is query
+// head h*G + r % G of new token r / G (G query heads per KV head), at position
+// p = seq_len[b] + r / G.
+//
+// Scores q . k_hat with k_hat = s c + z per group of 32 dims, on
+// v_mfma_f32_16x16x32_f16, whose 32-element depth is one group.  The codes c enter as
+// fp16 denormals (value c 2^-24, the code's own bits), exactly; their group sums
+// are weighted by 2^15 s in fp32.  A row of q is scaled by the power of two 2^e that
+// brings its largest element to [2^13, 2^14), exactly, so that all terms have the unit
+// 2^(e-9):
+//   sum_g (2^15 s_g) (2^-24 sum_d c_d q_d 2^e) + sum_g z_g (2^(e-9) sum_d q_d)
+// The second sum is one more product of the same kind over the token's eight
+// metadata halfs as they lie in the page ({s, z} of four groups), against the row's
+// group sums as fp16 high and low parts (2^-22 relative).  So a logit's error is fp32's;
+// keys rounded to fp16 would move logits by 4e-4 (keys N(0, 1), four channels
+// times 10), and the normalizers with them.
+//
+// An operand register holds dims (d, d + 4) of an 8-dim block, the pairs that one
+// v_perm (8-bit codes) or one mask (4-bit codes) makes.
+#pragma once
+
+#include <utility>
+
+#include "internal.hpp"
+
+namespace dkv {
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+constexpr float kChunkLog2e = 1.4426950408889634f;
+constexpr float kChunkLn2 = 0.6931471805599453f;
+constexpr float kLowest = -1e30f;  // a running max before the first key (finite: no inf - inf)
+
+__device__ __forceinline__ f4 mfma_k32(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f4 mfma_k16(h4 a, h4 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0); }
+
+// fp16 results that overflow become the largest finite value (MODE.FP16_OVFL): the value
+// s c + z of a group's largest code can round past it.  True infinities stay.
+__device__ __forceinline__ void set_fp16_saturate() { __builtin_amdgcn_s_setreg(1 | (23 << 6) | (0 << 11), 1); }
+
+// ---- the sequence and row block of a workgroup --------------------------------
+struct SeqBlock {
+    int b, n;        // sequence, its new tokens (0: none of this launch's)
+    int blk;         // row block inside the sequence
+    long long row0;  // its first token row
+};
+
+// Number of row blocks that this launch takes of a sequence of n new tokens: those
+// whose rows lie in [lo, hi].
+__device__ __forceinline__ int chunk_blocks(int n, int G, int rows, int lo, int hi)
+{
+    const long long r = (long long)n * G;
+    return r < lo || r > hi ? 0 : (int)((r + rows - 1) / rows);
+}
+
+// Block number `want` in sequence order.  Every wave finds it by itself: 64 lengths at
+// a time, two prefix sums.  Lengths are clamped to [0, max_new] and to total_new rows.
+__device__ __forceinline__ SeqBlock find_block(const ChunkArgs& a, int want, int rows, int lo, int hi)
+{
+    SeqBlock s{-1, 0, 0, 0};
+    const int lane = lane_id();
+    const int G = a.Hq / a.Hkv;
+    if (a.max_new == 1 && a.total_new == a.B) {  // one token per sequence
+        if (want < a.B && G >= lo && G <= hi) s = SeqBlock{want, 1, 0, want};
+        return s;
+    }
+    long long row = 0;
+    int blocks = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        const int b = b0 + lane;
+        int n = b < a.B ? a.new_len[b] : 0;
+        n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
+        const long long before = row + (wave_incl_scan(n) - n);
+        const long long room = a.total_new - before;
+        if (n > room) n = room > 0 ? (int)room : 0;
+        const int nb = chunk_blocks(n, G, rows, lo, hi);
+        const int incl = wave_incl_scan(nb);
+        const unsigned long long past = __ballot(blocks + incl > want);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            s.b = b0 + l;
+            s.n = __builtin_amdgcn_readlane(n, l);
+            s.blk = want - blocks - __builtin_amdgcn_readlane(incl - nb, l);
+            s.row0 = read_lane<long long>(before, l);
+            return s;
+        }
+        blocks += __builtin_amdgcn_readlane(incl, kWave - 1);
+        row = read_lane<long long>(before + n, kWave - 1);
+    }
+    return s;
+}
+
+// ---- operands ---------------------------------------------------------------------
+// max over the four 16-lane rows, in every row
+__device__ __forceinline__ float rows_max(float v)
+{
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float rows_sum(float v)
+{
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// eight consecutive halfs -> the operand's pairs (0, 4), (1, 5), (2, 6), (3, 7)
+__device__ __forceinline__ h8 pair_order(u4 x)
+{
+    u4 r;
+    r[0] = __builtin_amdgcn_perm(x[2], x[0], 0x05040100u);
+    r[1] = __builtin_amdgcn_perm(x[2], x[0], 0x07060302u);
+    r[2] = __builtin_amdgcn_perm(x[3], x[1], 0x05040100u);
+    r[3] = __builtin_amdgcn_perm(x[3], x[1], 0x07060302u);
+    return __builtin_bit_cast(h8, r);
+}
+
+// eight key codes (8 bits: two dwords; 4 bits: one) -> fp16 denormals in pair order
+__device__ __forceinline__ h8 key_codes8(uint32_t lo, uint32_t hi)
+{
+    u4 r;
+    r[0] = __builtin_amdgcn_perm(hi, lo, 0x0C040C00u);
+    r[1] = __builtin_amdgcn_perm(hi, lo, 0x0C050C01u);
+    r[2] = __builtin_amdgcn_perm(hi, lo, 0x0C060C02u);
+    r[3] = __builtin_amdgcn_perm(hi, lo, 0x0C070C03u);
+    return __builtin_bit_cast(h8, r);
+}
+__device__ __forceinline__ h8 key_codes4(uint32_t w)
+{
+    u4 r;
+    r[0] = w & 0x000F000Fu;
+    r[1] = (w >> 4) & 0x000F000Fu;
+    r[2] = (w >> 8) & 0x000F000Fu;
+    r[3] = (w >> 12) & 0x000F000Fu;
+    return __builtin_bit_cast(h8, r);
+}
+
+// A row of q (this lane's eight dims of each group, lanes l, l + 16, l + 32, l + 48 hold the
+// row): its operands scaled by 2^e, the group sums' operand, and 2^(9-e).
+struct RowOperands {
+    h8 q[kNG];
+    h8 sums;      // row-quarter 0: {0, hi_g} pairs, quarter 1: {0, lo_g}, else 0
+    float unit;   // 2^(9-e)
+};
+__device__ __forceinline__ RowOperands row_operands(const u4 (&x)[kNG], int quarter)
+{
+    RowOperands o;
+    uint32_t top = 0;
+#pragma unroll
+    for (int g = 0; g < kNG; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t m = x[g][i] & 0x7fff7fffu;
+            const uint32_t a = m & 0xffffu, b = m >> 16;
+            top = top > a ? top : a;
+            top = top > b ? top : b;
+        }
+    {
+        uint32_t v = (uint32_t)__shfl_xor((int)top, 16);
+        top = top > v ? top : v;
+        v = (uint32_t)__shfl_xor((int)top, 32);
+        top = top > v ? top : v;
+    }
+    int e = 28 - (int)(top >> 10);
+    e = e > 15 ? 15 : e;  // (an infinite or NaN row: -3)
+    const _Float16 up = __builtin_bit_cast(_Float16, (unsigned short)((e + 15) << 10));
+    o.unit = __uint_as_float((uint32_t)(127 + 9 - e) << 23);
+    const h2 up2 = {up, up};
+    u4 sums = {0, 0, 0, 0};
+#pragma unroll
+    for (int g = 0; g < kNG; ++g) {
+        u4 y;
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const h2 v = __builtin_bit_cast(h2, (uint32_t)x[g][i]) * up2;
+            s += (float)v.x + (float)v.y;
+            y[i] = __builtin_bit_cast(uint32_t, v);
+        }
+        o.q[g] = pair_order(y);
+        s = rows_sum(s) * 0x1p-9f;
+        const _Float16 hi = (_Float16)s;
+        const _Float16 lo = (_Float16)(s - (float)hi);
+        const uint32_t bits = __builtin_bit_cast(unsigned short, quarter == 0 ? hi : lo);
+        sums[g] = quarter < 2 ? bits << 16 : 0u;
+    }
+    o.sums = __builtin_bit_cast(h8, sums);
+    return o;
+}
+
+// ---- the forms of a score --------------------------------------------------------
+// sm_scale q.k capped by cap tanh(x / cap), with slope (c - p) added; log2 units.
+struct ScoreForm {
+    float cap_in, cap_out;  // 2 log2(e) / cap, cap log2(e); cap_in 0: no cap
+    float slope;            // times log2(e); 0: none
+};
+// x: scaled score in natural units (with a cap) or log2 units (without)
+__device__ __forceinline__ float formed(float x, const ScoreForm& f, float away)
+{
+    if (f.cap_in != 0.0f) {
+        // tanh y = 1 - 2 / (1 + exp 2y): exact limits at both ends, 2^-23 absolute
+        const float ex = __builtin_amdgcn_exp2f(x * f.cap_in);
+        x = f.cap_out * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + ex));
+    }
+    return x - f.slope * away;
+}
+
+}  // namespace dkv

@@ -241,6 +241,61 @@ inline int prompt_segs(long long B, long long Hq, long long Hkv, long long total
 }
 hipError_t launch_prompt_significance(const PromptArgs& a, int g, hipStream_t st);
 
+// Attention and scores of chunks of new tokens (rows concatenated per sequence).
+struct ChunkArgs {
+    int p_max;
+    long long page_bytes;
+    long long num_pages;
+    const uint8_t* pool;
+    uint8_t* pool_rw;      // the same, for the scores
+    const int32_t* page_table;
+    const int32_t* len;
+    const int32_t* seq_len;
+    int B, Hkv, Hq, max_new;
+    long long total_new;
+    const int32_t* new_len;
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    long long q_stride, k_stride, v_stride;  // halfs from one token's row to the next
+    float scale;           // sm_scale, times log2(e) without a cap
+    float cap_in, cap_out; // 2 log2(e) / cap and cap log2(e); 0: no cap
+    const float* slopes;   // [Hq] or null
+    int window;            // INT32_MAX: none
+    uint16_t* out;         // [total_new][Hq][kD]
+    float* lse;            // [total_new][Hq] or null
+    const float* lse_in;   // scores: as attention wrote it
+    float* score;          // [total_new][Hkv]
+    float* part;           // partial states {acc[kD], max, sum} per (row, query head, split)
+    int splits;            // workgroups per row block
+    int rows_lo, rows_hi;  // the launch takes sequences with that many rows (new tokens x G)
+    int shares;            // scores: workgroups per table
+    int layout;
+};
+constexpr int kChunkPart = kD + 4;  // floats of a partial state (16-byte rows)
+int chunk_splits(long long B, long long Hq, long long Hkv, long long total_new, long long p_max);
+hipError_t launch_chunk_attention(const ChunkArgs& a, bool mod, hipStream_t st);
+hipError_t launch_chunk_scores(const ChunkArgs& a, bool mod, hipStream_t st);
+// Kernel entry points of layout n (k_chunk_l<n>.hip).
+const void* chunk_kernel_l0(int which, bool mod);
+const void* chunk_kernel_l1(int which, bool mod);
+const void* chunk_kernel_l2(int which, bool mod);
+const void* chunk_kernel_l3(int which, bool mod);
+
+// Rotary positions of queries and keys.
+struct RotateArgs {
+    long long rows;
+    const int32_t* pos;
+    const float* freq;     // [rot_dim / 2] radians per position
+    int rot_dim, style;
+    float scale;
+    const uint16_t* in[2];
+    uint16_t* out[2];
+    long long in_stride[2], out_stride[2];
+    int heads[2];
+};
+hipError_t launch_rotate(const RotateArgs& a, hipStream_t st);
+
 // Fixed device scratch of diffkv_decode_attention_noalloc, one per device.
 constexpr long long kNoAllocScratchBytes = 8ll << 20;
 hipError_t noalloc_scratch(void** ptr);

@@ -16,7 +16,10 @@ LIB_PATH = os.path.join(_HERE, "libdiffkv.so")
 OK, E_INVAL, E_UNSUPPORTED, E_WORKSPACE, E_LAUNCH, E_SCRATCH = 0, 1, 2, 3, 4, 5
 ST_OUT_OF_PAGES, ST_TABLE_OVERFLOW, ST_BAD_INPUT = 1, 2, 4
 OP_APPEND, OP_ATTENTION, OP_COMPACT, OP_ALLOC, OP_GENERATION, OP_PROMPT_SIGNIFICANCE = 0, 1, 2, 3, 4, 5
+OP_CHUNK_ATTENTION, OP_CHUNK_SIGNIFICANCE = 6, 7
 HIGH, LOW = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
 
 _lib = None
 
@@ -50,9 +53,14 @@ class CacheStruct(C.Structure):
     ]
 
 
+class ScoreForm(C.Structure):
+    _fields_ = [("cap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p)]
+
+
 EXPORTS = ("diffkv_layout_init", "diffkv_workspace_size", "diffkv_quantize_append",
            "diffkv_decode_attention", "diffkv_decode_attention_noalloc", "diffkv_update_significance",
-           "diffkv_prompt_significance", "diffkv_compact_free_list", "diffkv_alloc_pages",
+           "diffkv_prompt_significance", "diffkv_rotate", "diffkv_rope_frequencies", "diffkv_chunk_attention",
+           "diffkv_chunk_significance", "diffkv_compact_free_list", "diffkv_alloc_pages",
            "diffkv_generation_step", "diffkv_status_str")
 
 
@@ -75,6 +83,13 @@ def lib():
         L.diffkv_update_significance.argtypes = [PL, PC, i32, vp, f32, vp, vp]
         L.diffkv_prompt_significance.argtypes = [PL, i32, i64, i32, vp, i32, i32, vp, vp, f32, vp, vp,
                                                  vp, sz, vp]
+        PF = C.POINTER(ScoreForm)
+        L.diffkv_rotate.argtypes = [PL, i64, vp, vp, i32, i32, f32, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp]
+        L.diffkv_rope_frequencies.argtypes = [i32, C.c_double, i32, C.c_double, i32, C.c_double, C.c_double, vp, vp]
+        L.diffkv_chunk_attention.argtypes = [PL, PC, i64, i32, vp, i32, vp, i64, vp, i64, vp, i64, f32, PF, vp, vp,
+                                             vp, sz, vp]
+        L.diffkv_chunk_significance.argtypes = [PL, PC, i64, i32, vp, i32, vp, i64, vp, i64, f32, PF, vp, vp,
+                                                vp, sz, vp]
         L.diffkv_compact_free_list.argtypes = [PL, PC, i32, vp, vp, sz, vp]
         L.diffkv_alloc_pages.argtypes = [PL, PC, i32, vp, vp, sz, vp]
         L.diffkv_generation_step.argtypes = [PL, PC, f32, f32, i32, vp, sz, vp]
@@ -279,6 +294,107 @@ def prompt_significance(L, new_len, q, k, sm_scale, lse=None, score=None, max_ne
                                                _ptr(_bits16(q)), _ptr(_bits16(k)), float(sm_scale), _ptr(lse),
                                                _ptr(score), ws.data_ptr(), ws.nbytes, _stream(stream)),
               "diffkv_prompt_significance", *sizes)
+    return score
+
+
+def _rows(t, what):
+    """Address and row stride of [rows, heads, D] rows whose heads lie side by side (a slice of a
+    fused projection may be given)."""
+    if t.dim() != 3 or t.element_size() != 2 or t.stride(2) != 1 or (t.stride(1) != t.shape[2] and t.shape[1] > 1):
+        raise ValueError("%s: 16-bit [rows, heads, head_dim] with packed heads expected" % what)
+    return t.data_ptr(), t.stride(0)
+
+
+def _form(cap, window, slopes):
+    if cap == 0.0 and window == 0 and slopes is None:
+        return None
+    if slopes is not None and (slopes.dtype != torch.float32 or not slopes.is_contiguous()):
+        raise ValueError("slopes: contiguous fp32 [num_q_heads] expected")
+    return C.byref(ScoreForm(float(cap), int(window), _ptr(slopes)))
+
+
+def rope_frequencies(rot_dim, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, trained_len=0, slow=1.0, fast=32.0):
+    """diffkv_rope_frequencies: (fp32 [rot_dim / 2] on the host, the scale of cosines and sines)."""
+    freq = torch.empty(max(rot_dim // 2, 1), dtype=torch.float32)
+    scale = C.c_float(0.0)
+    _check(lib().diffkv_rope_frequencies(int(rot_dim), float(base), int(scaling), float(factor), int(trained_len),
+                                         float(slow), float(fast), freq.data_ptr(), C.addressof(scale)),
+           "diffkv_rope_frequencies")
+    return freq, scale.value
+
+
+def rotate(L, pos, inv_freq, q, k=None, style=ROPE_HALF, scale=1.0, q_out=None, k_out=None, stream=None):
+    """Rotary positions: q fp16 [rows, Hq, D], k fp16 [rows, Hkv, D] or None (rows may be strided), pos int32
+    [rows], inv_freq fp32 [rot_dim / 2] (device) -> (q_out, k_out), contiguous unless given; q_out=q turns in
+    place."""
+    rows, Hq = q.shape[0], q.shape[1]
+    if pos.dtype != torch.int32 or pos.shape != (rows,) or not pos.is_contiguous():
+        raise ValueError("pos: contiguous int32 [rows] expected")
+    if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq: contiguous fp32 expected")
+    if q_out is None:
+        q_out = torch.empty((rows, Hq, q.shape[2]), dtype=q.dtype, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    if q_out.shape != q.shape or (k is not None and (k_out.shape != k.shape or k.shape[0] != rows)):
+        raise ValueError("rotate: outputs shaped as their inputs expected")
+    kp, ks, Hkv = (None, 0, 0) if k is None else (*_rows(k, "k"), k.shape[1])
+    kop, kos = (None, 0) if k is None else _rows(k_out, "k_out")
+    qp, qs = _rows(q, "q")
+    qop, qos = _rows(q_out, "q_out")
+    _check(lib().diffkv_rotate(C.byref(L), rows, _ptr(pos), _ptr(inv_freq), 2 * inv_freq.shape[0], int(style),
+                               float(scale), Hq, qp, qs, qop, qos, Hkv, kp, ks, kop, kos, _stream(stream)),
+           "diffkv_rotate")
+    return q_out, k_out
+
+
+def _chunk(cache, new_len, max_new, what, q, *rows):
+    if max_new is None:
+        max_new = int(new_len.max().item()) if new_len.shape[0] else 0
+    for t in rows:
+        if t.shape[0] != q.shape[0] or t.shape[1] != cache.num_kv_heads:
+            raise ValueError("%s: [rows, num_kv_heads, head_dim] keys and values expected" % what)
+    return int(max_new)
+
+
+def chunk_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, slopes=None, out=None, lse=None,
+                    max_new=None, ws=None, stream=None, want_lse=True):
+    """diffkv_chunk_attention: q fp16 [rows, Hq, D], k, v fp16 [rows, Hkv, D] (device, rows concatenated per
+    sequence, may be strided), new_len int32 [B] (device) -> out fp16 [rows, Hq, D], lse fp32 [rows, Hq].
+    Call it before the rows are appended."""
+    rows, Hq, D = q.shape
+    max_new = _chunk(cache, new_len, max_new, "chunk_attention", q, k, v)
+    if out is None:
+        out = torch.empty((rows, Hq, D), dtype=torch.float16, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
+    sizes = (OP_CHUNK_ATTENTION, cache.L, cache.num_seqs, Hq, cache.num_kv_heads, rows)
+    if ws is None:
+        ws = _new_ws(workspace_size(*sizes), q.device)
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+    _check_ws(lib().diffkv_chunk_attention(
+        C.byref(cache.L), _cache_struct(cache), rows, max_new, _ptr(new_len), Hq, qp, qs, kp, ks, vp, vs,
+        float(sm_scale), _form(cap, window, slopes), _ptr(out), _ptr(lse), ws.data_ptr(), ws.nbytes, _stream(stream)),
+        "diffkv_chunk_attention", *sizes)
+    return out, lse
+
+
+def chunk_significance(cache, new_len, q, k, sm_scale, lse, cap=0.0, window=0, slopes=None, score=None,
+                       max_new=None, ws=None, stream=None):
+    """diffkv_chunk_significance: the chunk's probabilities (lse from chunk_attention with the same q, k and
+    form) enter the cached tokens' scores in place; returns the new tokens' scores, fp32 [rows, Hkv]."""
+    rows, Hq = q.shape[0], q.shape[1]
+    max_new = _chunk(cache, new_len, max_new, "chunk_significance", q, k)
+    if score is None:
+        score = torch.empty((rows, cache.num_kv_heads), dtype=torch.float32, device=q.device)
+    sizes = (OP_CHUNK_SIGNIFICANCE, cache.L, cache.num_seqs, Hq, cache.num_kv_heads, rows)
+    if ws is None:
+        ws = _new_ws(workspace_size(*sizes), q.device)
+    (qp, qs), (kp, ks) = _rows(q, "q"), _rows(k, "k")
+    _check_ws(lib().diffkv_chunk_significance(
+        C.byref(cache.L), _cache_struct(cache), rows, max_new, _ptr(new_len), Hq, qp, qs, kp, ks, float(sm_scale),
+        _form(cap, window, slopes), _ptr(lse), _ptr(score), ws.data_ptr(), ws.nbytes, _stream(stream)),
+        "diffkv_chunk_significance", *sizes)
     return score
 
 

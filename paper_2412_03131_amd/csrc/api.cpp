@@ -255,13 +255,6 @@ diffkv_status attention_call(const diffkv_layout* layout, const diffkv_cache* ca
     return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
 }
 
-// Chunk attention: the partial states of split rows.
-int64_t chunk_ws(int64_t B, int64_t Hq, int64_t Hkv, int64_t total_new, int64_t p_max)
-{
-    const int64_t splits = chunk_splits(B, Hq, Hkv, total_new, p_max);
-    return splits > 1 ? align256(total_new * Hq * splits * kChunkPart * 4) : 0;
-}
-
 // A row of `heads` heads every `stride` halfs, as the vector loads and stores need it.
 bool rows_valid(const void* p, int64_t stride, int64_t heads, int64_t rows)
 {
@@ -362,7 +355,7 @@ diffkv_status diffkv_workspace_size(int32_t op, const diffkv_layout* layout, int
     case DIFFKV_OP_CHUNK_SIGNIFICANCE:
         if (num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || total_new < 0) return DIFFKV_E_INVAL;
         *bytes = op == DIFFKV_OP_CHUNK_ATTENTION
-                     ? (size_t)chunk_ws(num_seqs, num_q_heads, num_kv_heads, total_new, layout->p_max)
+                     ? (size_t)chunk_plan(num_seqs, num_q_heads, num_kv_heads, total_new, layout->p_max).bytes
                      : 0;
         return DIFFKV_OK;
     default:
@@ -603,15 +596,14 @@ diffkv_status diffkv_chunk_attention(const diffkv_layout* layout, const diffkv_c
                                        sm_scale, form, a, mod);
     if (s != DIFFKV_OK || a.total_new == 0) return s;
     if (!rows_valid(v, v_stride, a.Hkv, total_new) || !out || (uintptr_t)out % 16 != 0) return DIFFKV_E_INVAL;
-    const int64_t need = chunk_ws(a.B, a.Hq, a.Hkv, total_new, a.p_max);
-    if (need > 0 && (!ws || (int64_t)ws_bytes < need)) return DIFFKV_E_WORKSPACE;
+    const ChunkPlan plan = chunk_plan(a.B, a.Hq, a.Hkv, total_new, a.p_max);
+    if (!ws || (int64_t)ws_bytes < plan.bytes) return DIFFKV_E_WORKSPACE;
     a.v = v;
     a.v_stride = v_stride;
     a.out = out;
     a.lse = lse;
-    a.part = static_cast<float*>(ws);
-    a.splits = chunk_splits(a.B, a.Hq, a.Hkv, total_new, a.p_max);
-    hipError_t e = launch_chunk_attention(a, mod, static_cast<hipStream_t>(stream));
+    a.arrive = static_cast<unsigned long long*>(ws);
+    hipError_t e = launch_chunk_attention(a, plan, mod, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
 }
 

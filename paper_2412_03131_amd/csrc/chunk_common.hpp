@@ -46,6 +46,30 @@ __device__ __forceinline__ f4 mfma_k16(h4 a, h4 b, f4 c) { return __builtin_amdg
 // s c + z of a group's largest code can round past it.  True infinities stay.
 __device__ __forceinline__ void set_fp16_saturate() { __builtin_amdgcn_s_setreg(1 | (23 << 6) | (0 << 11), 1); }
 
+// ---- loads -----------------------------------------------------------------------
+// Through a buffer resource: a uniform base and 32-bit offsets.  (With 64-bit addresses the
+// compiler keeps one per lane and piece of a page across the loops.)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t span(const void* base, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
+}
+// The lane number where the compiler cannot see that it is the same every time: what is worked out
+// from it is worked out there, not kept in registers across a loop that has none to spare.
+__device__ __forceinline__ int fresh(int lane)
+{
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+template <int BYTES>
+__device__ __forceinline__ auto fetch(__amdgpu_buffer_rsrc_t r, int lane_offset, int offset)
+{
+    if constexpr (BYTES == 16) return __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_offset, offset, 0));
+    else if constexpr (BYTES == 8) return __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(r, lane_offset, offset, 0));
+    else if constexpr (BYTES == 4) return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, lane_offset, offset, 0);
+    else if constexpr (BYTES == 2) return (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, lane_offset, offset, 0);
+    else return (uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, lane_offset, offset, 0);
+}
+
 // ---- the sequence and row block of a workgroup --------------------------------
 struct SeqBlock {
     int b, n;        // sequence, its new tokens (0: none of this launch's)
@@ -98,6 +122,31 @@ __device__ __forceinline__ SeqBlock find_block(const ChunkArgs& a, int want, int
     return s;
 }
 
+// ---- split rows, joined inside the launch -----------------------------------------
+// A row block whose steps are split over workgroups: each writes its rows' states {acc[kD], max,
+// sum} to its slot with agent-scope stores (through to memory: the workgroups may be on
+// different XCDs), and the one that arrives last reads them all back.
+__device__ __forceinline__ void put_pair(float* p, float x, float y)
+{
+    const unsigned long long v = ((unsigned long long)__float_as_uint(y) << 32) | __float_as_uint(x);
+    __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_pair(const float* p)
+{
+    const unsigned long long v = __hip_atomic_load(reinterpret_cast<unsigned long long*>(const_cast<float*>(p)),
+                                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+// After the workgroup's stores: whether it is the last of `splits` (uniform).
+__device__ __forceinline__ bool split_last(unsigned long long* word, int splits, int* lds_flag)
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) *lds_flag = arrive_count(word, call_tag()) == (unsigned long long)splits;
+    __syncthreads();
+    return *lds_flag != 0;
+}
+
 // ---- operands ---------------------------------------------------------------------
 // max over the four 16-lane rows, in every row
 __device__ __forceinline__ float rows_max(float v)
@@ -110,6 +159,8 @@ __device__ __forceinline__ float rows_sum(float v)
     v += __shfl_xor(v, 16);
     return v + __shfl_xor(v, 32);
 }
+
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
 // eight consecutive halfs -> the operand's pairs (0, 4), (1, 5), (2, 6), (3, 7)
 __device__ __forceinline__ h8 pair_order(u4 x)

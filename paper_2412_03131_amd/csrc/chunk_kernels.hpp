@@ -17,15 +17,71 @@ __device__ __forceinline__ int step_slot(int t, int m)
     return T == 16 ? m : 8 * (m >> 2) + 4 * t + (m & 3);
 }
 
-// What a lane (column c = lane % 16, quarter = lane / 16) holds of a step.
-template <int KB, int VB, int T>
-struct StepRaw {
+// ---- pages through LDS ------------------------------------------------------------
+// A wave stages a step's pages in a slot of its own with loads that have an LDS destination: the
+// page's bytes as they lie, 1 KB a load, no registers held while they are in flight.  The
+// buffer resource ends with the bytes that are needed (beyond, the loads fetch nothing).
+template <int KB, int VB, int T, bool MOD>
+struct Staged {
+    static constexpr SecOffsets O = sec_offsets(KvFmt{KB, VB, T});
+    static constexpr int need = MOD ? O.used : O.sc;
+    static constexpr int loads = (need + 1023) / 1024;
+    static constexpr int page = loads * 1024;
+    static constexpr int slot = (T == 16 ? 2 : 1) * page;
+};
+
+template <int NEED>
+__device__ __forceinline__ void stage_page(uint8_t* lds, const uint8_t* pg, int lane)
+{
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) void*)lds);
+    const unsigned long long base = (unsigned long long)pg;
+    const u4 rs = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)NEED, 0x00020000u};
+#pragma unroll
+    for (int i = 0; i < (NEED + 1023) / 1024; ++i)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at + 1024 * i),
+                     "v"(lane * 16), "s"(rs), "s"(1024 * i)
+                     : "memory");
+}
+// One KB of a page (piece i), by one wave.
+__device__ __forceinline__ void stage_piece(uint8_t* lds, const uint8_t* pg, int need, int i, int lane)
+{
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) void*)lds) + 1024 * i;
+    const unsigned long long base = (unsigned long long)pg;
+    const u4 rs = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)need, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(lane * 16), "s"(rs),
+                 "s"(1024 * i)
+                 : "memory");
+}
+// Four rows of 256 bytes, `stride` bytes apart from `base` on, rows beyond `last` read as the last.
+__device__ __forceinline__ void stage_rows(uint8_t* lds, const void* base, int stride, int row, int last, int lane)
+{
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) void*)lds);
+    const unsigned long long b = (unsigned long long)base;
+    const u4 rs = {(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at),
+                 "v"(min(row + (lane >> 4), last) * stride + (lane & 15) * 16), "s"(rs)
+                 : "memory");
+}
+// (the wave's only vector loads in flight are its slot's)
+__device__ __forceinline__ void staged_ready() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Keeps the reads of a slot where they are written: all of a step's at once need more registers than
+// four waves per SIMD have.
+__device__ __forceinline__ void keep_order() { asm volatile("" ::: "memory"); }
+__device__ __forceinline__ void staged_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// What a lane (column c = lane % 16, quarter = lane / 16) takes of a step.
+template <int KB>
+struct TileKeys {
+    uint32_t kc[kNG][KB / 4];  // key codes of token m = c, its quarter of each group
+    u4 km;                     // its {s, z} of four groups
+    int4 pos;                  // positions of the quarter's four tokens
+};
+// Of one group of its values (dims 32 g .. + 31: two 16-dim tiles).
+template <int VB, int T>
+struct GroupValues {
     static constexpr int kPieces = T == 16 ? 2 : 1;  // value code pieces per dim: one per page
-    uint32_t kc[2][kNG][KB / 4];  // key codes of token m = c, its quarter of each group
-    u4 km[2];                     // its {s, z} of four groups
-    uint32_t vc[kPieces][8];      // value codes of dims 16 dt + c, the quarter's tokens
-    u4 vm[2][kNG];                // {s, z} of the quarter's four tokens, per group
-    int4 pos[2];                  // their positions
+    uint32_t vc[kPieces][2];      // value codes of dims 32 g + 16 d + c, the quarter's tokens
+    u4 vm[2];                     // {s, z} of the quarter's four tokens
 };
 
 template <int VB, int T>
@@ -38,34 +94,39 @@ __device__ __forceinline__ uint32_t load_value_codes(const uint8_t* p)
 }
 
 template <int KB, int VB, int T, bool MOD>
-__device__ __forceinline__ void load_step(StepRaw<KB, VB, T>& r, const uint8_t* pg0, const uint8_t* pg1, int c, int quarter)
+__device__ __forceinline__ void load_keys(TileKeys<KB>& r, const uint8_t* slot_, int t, int c, int quarter)
 {
     constexpr SecOffsets O = sec_offsets(KvFmt{KB, VB, T});
+    const uint8_t* pg = slot_ + (T == 16 ? t * Staged<KB, VB, T, MOD>::page : 0);
+    const int slot = step_slot<T>(t, c);
+#pragma unroll
+    for (int g = 0; g < kNG; ++g) {
+        if constexpr (KB == 8) {
+            const u2 v = *reinterpret_cast<const u2*>(pg + O.kc + ((2 * g + (quarter >> 1)) * T + slot) * 16 + (quarter & 1) * 8);
+            r.kc[g][0] = v[0];
+            r.kc[g][1] = v[1];
+        } else {
+            r.kc[g][0] = *reinterpret_cast<const uint32_t*>(pg + O.kc + (g * T + slot) * 16 + quarter * 4);
+        }
+    }
+    r.km = *reinterpret_cast<const u4*>(pg + O.km + slot * 16);
+    if constexpr (MOD) r.pos = *reinterpret_cast<const int4*>(pg + O.pos + step_slot<T>(t, 4 * quarter) * 4);
+}
+
+template <int KB, int VB, int T, bool MOD>
+__device__ __forceinline__ void load_values(GroupValues<VB, T>& r, const uint8_t* slot_, int g, int c, int quarter)
+{
+    constexpr SecOffsets O = sec_offsets(KvFmt{KB, VB, T});
+    constexpr int row = T * VB / 8, piece = (T == 16 ? 4 : 8) * VB / 8;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const uint8_t* pg = T == 16 && t == 1 ? pg1 : pg0;
-        const int slot = step_slot<T>(t, c);
+        const uint8_t* pg = slot_ + (T == 16 ? t * Staged<KB, VB, T, MOD>::page : 0);
+        r.vm[t] = *reinterpret_cast<const u4*>(pg + O.vm + (g * T + step_slot<T>(t, 4 * quarter)) * 4);
+        if (t < GroupValues<VB, T>::kPieces) {
 #pragma unroll
-        for (int g = 0; g < kNG; ++g) {
-            if constexpr (KB == 8) {
-                const u2 v = *reinterpret_cast<const u2*>(pg + O.kc + ((2 * g + (quarter >> 1)) * T + slot) * 16 + (quarter & 1) * 8);
-                r.kc[t][g][0] = v[0];
-                r.kc[t][g][1] = v[1];
-            } else {
-                r.kc[t][g][0] = *reinterpret_cast<const uint32_t*>(pg + O.kc + (g * T + slot) * 16 + quarter * 4);
-            }
-        }
-        r.km[t] = *reinterpret_cast<const u4*>(pg + O.km + slot * 16);
-        const int first = step_slot<T>(t, 4 * quarter);
-#pragma unroll
-        for (int g = 0; g < kNG; ++g) r.vm[t][g] = *reinterpret_cast<const u4*>(pg + O.vm + (g * T + first) * 4);
-        if constexpr (MOD) r.pos[t] = *reinterpret_cast<const int4*>(pg + O.pos + first * 4);
-        if (t < StepRaw<KB, VB, T>::kPieces) {
-            constexpr int row = T * VB / 8, piece = (T == 16 ? 4 : 8) * VB / 8;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt)
-                r.vc[t < StepRaw<KB, VB, T>::kPieces ? t : 0][dt] =
-                    load_value_codes<VB, T>(pg + O.vc + (16 * dt + c) * row + quarter * piece);
+            for (int d = 0; d < 2; ++d)
+                r.vc[t < GroupValues<VB, T>::kPieces ? t : 0][d] =
+                    load_value_codes<VB, T>(pg + O.vc + (32 * g + 16 * d + c) * row + quarter * piece);
         }
     }
 }
@@ -95,10 +156,15 @@ __device__ __forceinline__ void value_pairs(uint32_t w, h2 s02, h2 z02, h2 s13, 
 }
 
 // The rows a wave works on: 16 RT of them, column c of tile rt is row 16 rt + c of its block.
+// Their queries' operands are read from LDS, where the workgroup's waves share them: five
+// registers of four a tile would not fit beside the rest.
+template <int RT>
+struct RowsLds {
+    h8 q[RT][kNG][kWave];
+    h8 sums[RT][kWave];
+};
 template <int RT>
 struct Rows {
-    h8 q[RT][kNG];
-    h8 sums[RT];
     float unit[RT];   // logit = unit * product sum (log2 units, or natural ones with a cap)
     int p[RT];        // position in the sequence
     ScoreForm form[RT];
@@ -106,65 +172,70 @@ struct Rows {
     f4 acc[RT][8];    // O^T: dims 16 dt + 4 quarter + r of row c
 };
 
-// One step's scores against the running softmax: logits x[rt][t][r] of tokens (t, 4 quarter + r)
-// -> weights 2^(x - m) as fp16 pairs (0, 2), (1, 3) of both tiles.  The running max is raised
-// only when a logit passes it by 8 (weights up to 2^8).
-template <int RT>
-__device__ __forceinline__ void softmax_step(Rows<RT>& R, float (&x)[RT][2][4], h8 (&P)[RT])
+// One step's scores against the running softmax: sums x[rt][t][r] of tokens (t, 4 quarter + r), a
+// logit being unit * x, -> weights 2^(logit - m).  The running max is raised only when a logit
+// passes it by 8 (weights up to 2^8).  before() is called where it is, before anything is scaled.
+template <int RT, typename F>
+__device__ __forceinline__ void raise_max(Rows<RT>& R, const float (&unit)[RT], const float (&x)[RT][2][4], F&& before)
 {
+    float top[RT];
     bool raise = false;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        float top = x[rt][0][0];
+        top[rt] = max3(max3(x[rt][0][0], x[rt][0][1], x[rt][0][2]), x[rt][0][3], max3(x[rt][1][0], x[rt][1][1], x[rt][1][2]));
+        top[rt] = max3(top[rt], x[rt][1][3], kLowest) * unit[rt];
+        raise |= top[rt] > R.m[rt] + 8.0f;
+    }
+    if (!__any(raise)) return;
+    before();
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        top[rt] = fmaxf(R.m[rt], rows_max(top[rt]));
+        const float f = __builtin_amdgcn_exp2f(R.m[rt] - top[rt]);
+        R.m[rt] = top[rt];
+        R.l[rt] *= f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] *= f;
+    }
+}
+__device__ __forceinline__ float weight(float x, float unit, float m)
+{
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(x, unit, -m));
+}
+// weights as fp16 pairs (0, 2), (1, 3) of both tiles
+__device__ __forceinline__ h8 pack_weights(const float (&w)[2][4])
+{
+    u4 bits;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const h2 a = {(_Float16)w[t][0], (_Float16)w[t][2]}, b = {(_Float16)w[t][1], (_Float16)w[t][3]};
+        bits[2 * t] = __builtin_bit_cast(uint32_t, a);
+        bits[2 * t + 1] = __builtin_bit_cast(uint32_t, b);
+    }
+    return __builtin_bit_cast(h8, bits);
+}
+template <int RT>
+__device__ __forceinline__ void softmax_step(Rows<RT>& R, const float (&unit)[RT], float (&x)[RT][2][4], h8 (&P)[RT])
+{
+    raise_max<RT>(R, unit, x, [] {});
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float sum = 0.0f;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, x[rt][t][r]);
-        raise |= top > R.m[rt] + 8.0f;
-    }
-    if (__any(raise)) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float top = x[rt][0][0];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) top = fmaxf(top, x[rt][t][r]);
-            top = fmaxf(R.m[rt], rows_max(top));
-            const float f = __builtin_amdgcn_exp2f(R.m[rt] - top);
-            R.m[rt] = top;
-            R.l[rt] *= f;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] *= f;
-        }
-    }
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        u4 bits;
-        float sum = 0.0f;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            float w[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                w[r] = __builtin_amdgcn_exp2f(x[rt][t][r] - R.m[rt]);
-                x[rt][t][r] = w[r];
-                sum += w[r];
-            }
-            const h2 a = {(_Float16)w[0], (_Float16)w[2]}, b = {(_Float16)w[1], (_Float16)w[3]};
-            bits[2 * t] = __builtin_bit_cast(uint32_t, a);
-            bits[2 * t + 1] = __builtin_bit_cast(uint32_t, b);
-        }
+            for (int r = 0; r < 4; ++r) sum += x[rt][t][r] = weight(x[rt][t][r], unit[rt], R.m[rt]);
         R.l[rt] += sum;
-        P[rt] = __builtin_bit_cast(h8, bits);
+        P[rt] = pack_weights(x[rt]);
     }
 }
 
-// A step of cached tokens; those with index >= left (in the step, by token) and those of tile t where
-// bit t of `bad` is set (a page ID outside the pool) do not exist.
-template <int KB, int VB, int T, int RT, bool MOD>
-__device__ __forceinline__ void cached_step(Rows<RT>& R, const StepRaw<KB, VB, T>& raw, int left, uint32_t bad,
-                                            const ChunkArgs& a, int quarter)
+// A step of cached tokens in the wave's slot; those with index >= left (in the step, by token) and
+// those of tile t where bit t of `bad` is set (a page ID outside the pool) do not exist.
+// next() is called once the slot has been read.
+template <int KB, int VB, int T, int RT, bool MOD, typename F>
+__device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, const uint8_t* slot, int left, uint32_t bad,
+                                            const ChunkArgs& a, int c, int quarter, F&& next)
 {
     float x[RT][2][4];
     const h4 pick0 = {(_Float16)(quarter == 0 ? 32768.0f : 0.0f), (_Float16)0.0f, (_Float16)0.0f, (_Float16)0.0f};
@@ -172,7 +243,10 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const StepRaw<KB, VB, T
     const f4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const h8 meta = __builtin_bit_cast(h8, raw.km[t]);
+        keep_order();
+        TileKeys<KB> raw;
+        load_keys<KB, VB, T, MOD>(raw, slot, t, c, quarter);
+        const h8 meta = __builtin_bit_cast(h8, raw.km);
         const h4 m01 = {meta[0], meta[1], meta[2], meta[3]}, m23 = {meta[4], meta[5], meta[6], meta[7]};
         // 2^15 s of the quarter's four tokens, per group: a product with a unit vector
         f4 s[kNG];
@@ -183,23 +257,23 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const StepRaw<KB, VB, T
         h8 k[kNG];
 #pragma unroll
         for (int g = 0; g < kNG; ++g) {
-            if constexpr (KB == 8) k[g] = key_codes8(raw.kc[t][g][0], raw.kc[t][g][1]);
-            else k[g] = key_codes4(raw.kc[t][g][0]);
+            if constexpr (KB == 8) k[g] = key_codes8(raw.kc[g][0], raw.kc[g][1]);
+            else k[g] = key_codes4(raw.kc[g][0]);
         }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            f4 sum = mfma_k32(meta, R.sums[rt], zero);
+            f4 sum = mfma_k32(meta, Q.sums[rt][16 * quarter + c], zero);
 #pragma unroll
             for (int g = 0; g < kNG; ++g) {
-                const f4 part = mfma_k32(k[g], R.q[rt][g], zero);
+                const f4 part = mfma_k32(k[g], Q.q[rt][g][16 * quarter + c], zero);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) sum[r] = __builtin_fmaf(s[g][r], part[r], sum[r]);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[rt][t][r] = sum[r] * R.unit[rt];
+            for (int r = 0; r < 4; ++r) x[rt][t][r] = MOD ? sum[r] * R.unit[rt] : sum[r];
         }
         if constexpr (MOD) {
-            const int pos[4] = {raw.pos[t].x, raw.pos[t].y, raw.pos[t].z, raw.pos[t].w};
+            const int pos[4] = {raw.pos.x, raw.pos.y, raw.pos.z, raw.pos.w};
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -226,13 +300,23 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const StepRaw<KB, VB, T
         }
     }
     h8 P[RT];
-    softmax_step<RT>(R, x, P);
+    float unit[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? 1.0f : R.unit[rt];
+    softmax_step<RT>(R, unit, x, P);
 #pragma unroll
     for (int g = 0; g < kNG; ++g) {
+        keep_order();
+        GroupValues<VB, T> val;
+        load_values<KB, VB, T, MOD>(val, slot, g, c, quarter);
+        if (g == kNG - 1) {
+            staged_read();
+            next();
+        }
         h2 s02[2], z02[2], s13[2], z13[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            u4 m = raw.vm[t][g];
+            u4 m = val.vm[t];
             if (!whole) {  // nothing behind a section's end reaches the sums
 #pragma unroll
                 for (int r = 0; r < 4; ++r) m[r] = (keep[t] >> r) & 1 ? m[r] : 0u;
@@ -247,10 +331,10 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const StepRaw<KB, VB, T
             const int dt = 2 * g + d;
             u4 v;
             uint32_t p, q;
-            value_pairs<VB>(raw.vc[0][dt], s02[0], z02[0], s13[0], z13[0], p, q);
+            value_pairs<VB>(val.vc[0][d], s02[0], z02[0], s13[0], z13[0], p, q);
             v[0] = p;
             v[1] = q;
-            value_pairs<VB>(T == 16 ? raw.vc[StepRaw<KB, VB, T>::kPieces - 1][dt] : raw.vc[0][dt] >> (4 * VB), s02[1], z02[1],
+            value_pairs<VB>(T == 16 ? val.vc[GroupValues<VB, T>::kPieces - 1][d] : val.vc[0][d] >> (4 * VB), s02[1], z02[1],
                             s13[1], z13[1], p, q);
             v[2] = p;
             v[3] = q;
@@ -261,10 +345,42 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const StepRaw<KB, VB, T
     }
 }
 
+// An infinite or NaN own value must not reach the rows that do not see its token (0 * inf in a matrix
+// product): it enters the product as 0 and is added here to those that do.  x: the step's weights.
+template <int RT>
+__device__ __forceinline__ void odd_values(Rows<RT>& R, const float (&x)[RT][2][4], const uint16_t* v, int i0, int n, int first,
+                                           const ChunkArgs& a, int c, int quarter)
+{
+#pragma unroll 1
+    for (int token = 0; token < 32 && i0 + token < n; ++token) {
+        float p[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            p[rt] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float pi = __shfl(x[rt][i >> 2][i & 3], c + 16 * (token >> 3));
+                p[rt] = (token & 7) == i ? pi : p[rt];
+            }
+        }
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t w = v[(long long)(i0 + token) * a.v_stride + 16 * dt + 4 * quarter + r];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const int away = R.p[rt] - first - (i0 + token);
+                    if ((w & 0x7c00u) == 0x7c00u && away >= 0 && away < a.window) R.acc[rt][dt][r] += p[rt] * h2f(w);
+                }
+            }
+    }
+}
+
 // A step of the chunk's own tokens i0 .. i0 + 31 of n, keys at k, values at v (strides in halfs).
 // first: position of token 0.
 template <int RT, bool MOD>
-__device__ __forceinline__ void own_step(Rows<RT>& R, const uint16_t* k, const uint16_t* v, int i0, int n, int first,
+__device__ __forceinline__ void own_step(Rows<RT>& R, const RowsLds<RT>& Q, const uint16_t* k, const uint16_t* v, int i0, int n, int first,
                                          const ChunkArgs& a, int c, int quarter)
 {
     float x[RT][2][4];
@@ -283,7 +399,7 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const uint16_t* k, const u
         for (int g = 0; g < kNG; ++g) {
             const h8 kk = pair_order(raw[g]);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) sum[rt] = mfma_k32(kk, R.q[rt][g], sum[rt]);
+            for (int rt = 0; rt < RT; ++rt) sum[rt] = mfma_k32(kk, Q.q[rt][g][16 * quarter + c], sum[rt]);
         }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -291,13 +407,16 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const uint16_t* k, const u
             for (int r = 0; r < 4; ++r) {
                 const int token = i0 + step_slot<32>(t, 4 * quarter + r);
                 const int away = R.p[rt] - first - token;
-                float y = sum[rt][r] * (R.unit[rt] * 0x1p-9f);
-                if constexpr (MOD) y = formed(y, R.form[rt], (float)away);
+                float y = sum[rt][r] * 0x1p-9f;
+                if constexpr (MOD) y = formed(y * R.unit[rt], R.form[rt], (float)away);
                 x[rt][t][r] = away >= 0 && away < a.window ? y : -INFINITY;
             }
     }
     h8 P[RT];
-    softmax_step<RT>(R, x, P);
+    float unit[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? 1.0f : R.unit[rt];
+    softmax_step<RT>(R, unit, x, P);
     // values: the quarter's eight tokens of dims 16 dt + c
     bool odd = false;
 #pragma unroll
@@ -317,28 +436,7 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const uint16_t* k, const u
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, P[rt], R.acc[rt][dt]);
     }
-    // An infinite or NaN value must not reach the rows that do not see its token (0 * inf in a matrix
-    // product): it entered as 0 above and is added here to those that do.
-    if (__any(odd)) {
-        for (int token = 0; token < 32 && i0 + token < n; ++token)
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t w = v[(long long)(i0 + token) * a.v_stride + 16 * dt + 4 * quarter + r];
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        float p = 0.0f;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float pi = __shfl(x[rt][i >> 2][i & 3], c + 16 * (token >> 3));
-                            p = (token & 7) == i ? pi : p;
-                        }
-                        const int away = R.p[rt] - first - (i0 + token);
-                        if ((w & 0x7c00u) == 0x7c00u && away >= 0 && away < a.window) R.acc[rt][dt][r] += p * h2f(w);
-                    }
-                }
-    }
+    if (__any(odd)) odd_values<RT>(R, x, v, i0, n, first, a, c, quarter);
 }
 
 // ---- attention: few rows, tokens split over waves and workgroups ------------------------
@@ -347,24 +445,37 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const uint16_t* k, const u
 // (high pages, low pages, the chunk's own tokens), its four waves every fourth step each.  A
 // wave holds its rows' queries as matrix operands and the transposed result O^T, so the
 // scores of a step come out with a lane's values in one row and go into the second product as
-// they lie: no exchange between lanes but the rare raise of the running max.  Pages go from memory
-// to registers; a step's loads are in flight while the one before is computed.
+// they lie: no exchange between lanes but the rare raise of the running max.  A wave's next step is
+// staged in LDS as soon as the one before has been read from there; with four waves per
+// SIMD the others' work covers the rest of its way.
 constexpr int kChunkWaves = 4;
 
 template <int LI, int RT, bool MOD>
-__global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? 2 : 1) void chunk_rows(ChunkArgs a)
+__global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : (RT == 2 ? 2 : 1)) void chunk_rows(ChunkArgs a)
 {
     constexpr KvFmt hi = kLayoutFmts[LI].hi, lo = kLayoutFmts[LI].lo;
     constexpr int kRows = 16 * RT;
-    __shared__ float lds_acc[kChunkWaves][16][kD + 4];
-    __shared__ float lds_ml[kChunkWaves][2][16];
+    constexpr int kSlot = Staged<hi.kb, hi.vb, hi.T, MOD>::slot > Staged<lo.kb, lo.vb, lo.T, MOD>::slot
+                              ? Staged<hi.kb, hi.vb, hi.T, MOD>::slot
+                              : Staged<lo.kb, lo.vb, lo.T, MOD>::slot;
+    union Shared {
+        uint8_t slot[kChunkWaves][kSlot];
+        struct {
+            float acc[kChunkWaves][16][kD + 4];
+            float ml[kChunkWaves][2][16];
+            int last;
+        } merge;
+    };
+    __shared__ __align__(1024) Shared lds;
+    __shared__ RowsLds<RT> Q;
     set_fp16_saturate();
     const int lane = lane_id(), wave = wave_index();
     const int c = lane & 15, quarter = lane >> 4;
     const int G = a.Hq / a.Hkv;
-    const int item = (int)blockIdx.x / a.splits, split = (int)blockIdx.x - item * a.splits;
-    const int h = item % a.Hkv;
-    const SeqBlock sb = find_block(a, item / a.Hkv, kRows, a.rows_lo, a.rows_hi);
+    // KV heads fastest: with eight of them a table's workgroups share an XCD's L2
+    const int item = (int)blockIdx.x / a.Hkv, h = (int)blockIdx.x - item * a.Hkv;
+    const int block = item / a.splits, split = item - block * a.splits;
+    const SeqBlock sb = find_block(a, block, kRows, a.rows_lo, a.rows_hi);
     if (sb.b < 0) return;
     const int first = a.seq_len[sb.b];
     const int rows = sb.n * G, r0 = sb.blk * kRows;
@@ -378,9 +489,363 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? 2 : 1) void chunk_ro
 #pragma unroll
         for (int g = 0; g < kNG; ++g) x[g] = *reinterpret_cast<const u4*>(q + g * kG);
         const RowOperands o = row_operands(x, quarter);
+        if (wave == 0) {
 #pragma unroll
-        for (int g = 0; g < kNG; ++g) R.q[rt][g] = o.q[g];
-        R.sums[rt] = o.sums;
+            for (int g = 0; g < kNG; ++g) Q.q[rt][g][lane] = o.q[g];
+            Q.sums[rt][lane] = o.sums;
+        }
+        R.unit[rt] = o.unit * a.scale;
+        R.p[rt] = first + j;
+        R.form[rt] = ScoreForm{a.cap_in, a.cap_out, MOD && a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f};
+        R.m[rt] = kLowest;
+        R.l[rt] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    __syncthreads();
+    const int t = sb.b * a.Hkv + h;
+    const int len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
+    const int last = min(r0 + kRows, rows) - 1;
+    const int own = last / G + 1;  // tokens of the chunk that some row sees
+    const int s_hi = (len_hi + 31) >> 5, s_lo = (len_lo + 31) >> 5, s_own = (own + 31) >> 5;
+    const int steps = s_hi + s_lo + s_own;
+    // no more workgroups than give every wave a step
+    const int splits = min(a.splits, (steps + kChunkWaves - 1) / kChunkWaves);
+    if (split >= splits) return;
+    const int begin = (int)((long long)steps * split / splits), end = (int)((long long)steps * (split + 1) / splits);
+    const int32_t* table = a.page_table + (long long)t * a.p_max;
+
+    // a step's page, IDs outside the pool read as page 0 (and count no token)
+    auto page_id = [&](int u, int part) {
+        const bool high = u < s_hi;
+        const int T = high ? hi.T : lo.T, len = high ? len_hi : len_lo;
+        const int i = min(T == 16 ? 2 * (high ? u : u - s_hi) + part : (high ? u : u - s_hi), (len + T - 1) / T - 1);
+        return __builtin_amdgcn_readfirstlane(table[high ? i : a.p_max - 1 - i]);
+    };
+    auto outside = [&](int id) { return (unsigned long long)(unsigned)id >= (unsigned long long)a.num_pages; };
+    using Hi = Staged<hi.kb, hi.vb, hi.T, MOD>;
+    using Lo = Staged<lo.kb, lo.vb, lo.T, MOD>;
+    uint8_t* slot = lds.slot[wave];
+    uint32_t bad = 0;  // of the staged step
+    auto stage = [&](int u, int id0, int id1) {
+        const bool o0 = outside(id0), o1 = outside(id1);
+        const uint8_t* p0 = a.pool + (long long)(o0 ? 0 : id0) * a.page_bytes;
+        const uint8_t* p1 = a.pool + (long long)(o1 ? 0 : id1) * a.page_bytes;
+        if (u < s_hi) {
+            stage_page<Hi::need>(slot, p0, lane);
+            if (hi.T == 16) stage_page<Hi::need>(slot + Hi::page, p1, lane);
+        } else {
+            stage_page<Lo::need>(slot, p0, lane);
+            if (lo.T == 16) stage_page<Lo::need>(slot + Lo::page, p1, lane);
+        }
+        const bool two = u < s_hi ? hi.T == 16 : lo.T == 16;
+        bad = two ? (o0 ? 1u : 0u) | (o1 ? 2u : 0u) : (o0 ? 3u : 0u);
+    };
+    const int cached = min(end, s_hi + s_lo);
+    int u = begin + wave;
+    if (u < cached) {
+        stage(u, page_id(u, 0), page_id(u, 1));
+        int n0 = 0, n1 = 0;
+        while (u < cached) {
+            const int next = u + kChunkWaves;
+            if (next < cached) {
+                n0 = page_id(next, 0);
+                n1 = page_id(next, 1);
+            }
+            const uint32_t b = bad;
+            auto ahead = [&]() {
+                if (next < cached) stage(next, n0, n1);
+            };
+            staged_ready();
+            if (u < s_hi) cached_step<hi.kb, hi.vb, hi.T, RT, MOD>(R, Q, slot, len_hi - 32 * u, b, a, c, quarter, ahead);
+            else cached_step<lo.kb, lo.vb, lo.T, RT, MOD>(R, Q, slot, len_lo - 32 * (u - s_hi), b, a, c, quarter, ahead);
+            u = next;
+        }
+    }
+    {
+        const uint16_t* k = a.k + sb.row0 * a.k_stride + h * kD;
+        const uint16_t* v = a.v + sb.row0 * a.v_stride + h * kD;
+        for (int s = max(begin - s_hi - s_lo, 0) + wave; s < end - s_hi - s_lo; s += kChunkWaves)
+            own_step<RT, MOD>(R, Q, k, v, 32 * s, own, first, a, c, quarter);
+    }
+
+    // the waves' states, 16 rows at a time: 16 threads a row, eight dims each
+    const int row = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8;
+    const long long slot_no = (long long)block * a.Hkv + h;
+    float* part = a.part + (slot_no * a.splits + split) * kRows * kChunkPart;
+    auto write = [&](int at, const float (&o)[8], float m, float sum) {
+        if (at >= rows) return;
+        const int j = at / G, hq = h * G + at - j * G;
+        const long long row_q = (sb.row0 + j) * a.Hq + hq;
+        const float inv = 1.0f / sum;
+        h8 r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = (_Float16)(o[i] * inv);
+        *reinterpret_cast<h8*>(a.out + row_q * kD + d) = r;
+        if (a.lse && d == 0) a.lse[row_q] = kChunkLn2 * (m + __builtin_amdgcn_logf(sum));
+    };
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        __syncthreads();
+        const float l = rows_sum(R.l[rt]);
+        if (quarter == 0) {
+            lds.merge.ml[wave][0][c] = R.m[rt];
+            lds.merge.ml[wave][1][c] = l;
+        }
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f4*>(&lds.merge.acc[wave][c][16 * dt + 4 * quarter]) = R.acc[rt][dt];
+        __syncthreads();
+        float m = kLowest, sum = 0.0f, o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kChunkWaves; ++w) m = fmaxf(m, lds.merge.ml[w][0][row]);
+#pragma unroll
+        for (int w = 0; w < kChunkWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(lds.merge.ml[w][0][row] - m);
+            sum += f * lds.merge.ml[w][1][row];
+            const f4 x = *reinterpret_cast<const f4*>(&lds.merge.acc[w][row][d]);
+            const f4 y = *reinterpret_cast<const f4*>(&lds.merge.acc[w][row][d + 4]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                o[i] += f * x[i];
+                o[i + 4] += f * y[i];
+            }
+        }
+        if (splits == 1) {
+            write(r0 + 16 * rt + row, o, m, sum);
+        } else {
+            float* to = part + (16 * rt + row) * kChunkPart;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) put_pair(to + d + i, o[i], o[i + 1]);
+            if (d == 0) put_pair(to + kD, m, sum);
+        }
+    }
+    if (splits == 1 || !split_last(a.arrive + slot_no, splits, &lds.merge.last)) return;
+    // the last of the block's workgroups joins their states, in order
+    const float* first_part = a.part + slot_no * a.splits * kRows * kChunkPart;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const float* from = first_part + (16 * rt + row) * kChunkPart;
+        float m = kLowest, sum = 0.0f, o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int k = 0; k < splits; ++k, from += kRows * kChunkPart) {
+            const float2 ml = get_pair(from + kD);
+            float2 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = get_pair(from + d + 2 * i);
+            const float top = fmaxf(m, ml.x);
+            const float f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(ml.x - top);
+            m = top;
+            sum = sum * f + ml.y * g;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                o[2 * i] = o[2 * i] * f + x[i].x * g;
+                o[2 * i + 1] = o[2 * i + 1] * f + x[i].y * g;
+            }
+        }
+        write(r0 + 16 * rt + row, o, m, sum);
+    }
+}
+
+// ---- attention: many rows, pages dequantized once for a workgroup -----------------------------
+//
+// A workgroup takes 256 rows of one (sequence, KV head), 32 per wave, and goes over the table's
+// steps together: each step's 32 tokens are turned into matrix operands once, by all eight
+// waves (one key and one value operand of a lane each), and read from LDS by all of them: keys
+// as exact codes with their scales in 32 bits beside them, values dequantized to fp16.  Two
+// buffers: while a step is computed from one, the next one's pages are on their way to
+// registers, from where they go into the other.
+constexpr int kTileWaves = 8;
+constexpr int kTileRows = kTileWaves * 32;
+static_assert(kTileRows == kChunkRows, "row blocks of the plan");
+
+struct TileBuf {
+    h8 k[2][kNG][kWave];     // [tile][group][lane]
+    h8 v[8][kWave];          // [16-dim tile][lane]
+    h8 meta[2][16];          // [tile][token] {s, z} of four groups
+    float s[2][kNG][16];     // 2^15 s (own tokens: 2^-9, their products are sums of halfs)
+    int pos[2][16];
+    uint32_t odd[kTileWaves];  // own values that are not finite, by the wave that met them
+};
+
+// The staged pages of a step (slot) into operands: wave w makes the key operand of tile w / 4, group
+// w % 4, and the value operand of dims 16 w ..; wave 0 the metadata.  Tokens with index >= left and
+// those of tile t where bit t of `bad` is set do not exist.
+template <int KB, int VB, int T, bool MOD>
+__device__ __forceinline__ void tile_put(TileBuf& b, const uint8_t* slot_, int left, uint32_t bad, int wave, int lane)
+{
+    constexpr SecOffsets O = sec_offsets(KvFmt{KB, VB, T});
+    constexpr int page = T == 16 ? Staged<KB, VB, T, MOD>::page : 0;  // from one tile's page to the other's
+    const int c = lane & 15, quarter = lane >> 4;
+    {
+        const int t = wave >> 2, g = wave & 3;
+        const uint8_t* pg = slot_ + t * page;
+        const int slot = step_slot<T>(t, c);
+        if constexpr (KB == 8) {
+            const u2 v = *reinterpret_cast<const u2*>(pg + O.kc + ((2 * g + (quarter >> 1)) * T + slot) * 16 + (quarter & 1) * 8);
+            b.k[t][g][lane] = key_codes8(v[0], v[1]);
+        } else {
+            b.k[t][g][lane] = key_codes4(*reinterpret_cast<const uint32_t*>(pg + O.kc + (g * T + slot) * 16 + quarter * 4));
+        }
+    }
+    constexpr int row = T * VB / 8, piece = (T == 16 ? 4 : 8) * VB / 8;
+    const int at = O.vc + (16 * wave + c) * row + quarter * piece;
+    uint32_t codes[2];
+    codes[0] = load_value_codes<VB, T>(slot_ + at);
+    codes[1] = T == 16 ? load_value_codes<VB, T>(slot_ + page + at) : codes[0] >> (4 * VB);
+    u4 v;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        u4 m = *reinterpret_cast<const u4*>(slot_ + t * page + O.vm + ((wave >> 1) * T + step_slot<T>(t, 4 * quarter)) * 4);
+        if (left < 32 || bad) {  // nothing behind a section's end reaches the sums
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                m[i] = (T == 16 ? 16 * t : 0) + step_slot<T>(t, 4 * quarter + i) < left && !((bad >> t) & 1) ? m[i] : 0u;
+        }
+        uint32_t p, q;
+        value_pairs<VB>(codes[t], __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x05040100u)),
+                        __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x07060302u)),
+                        __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[3], m[1], 0x05040100u)),
+                        __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[3], m[1], 0x07060302u)), p, q);
+        v[2 * t] = p;
+        v[2 * t + 1] = q;
+    }
+    b.v[wave][lane] = __builtin_bit_cast(h8, v);
+    if (wave == 0 && lane < 32) {
+        const uint8_t* pg = slot_ + quarter * page;
+        const int slot = step_slot<T>(quarter, c);
+        const h8 m = *reinterpret_cast<const h8*>(pg + O.km + slot * 16);
+        b.meta[quarter][c] = m;
+#pragma unroll
+        for (int g = 0; g < kNG; ++g) b.s[quarter][g][c] = 32768.0f * (float)m[2 * g];
+        if constexpr (MOD) b.pos[quarter][c] = *reinterpret_cast<const int32_t*>(pg + O.pos + slot * 4);
+    }
+}
+
+// The same of own tokens, staged as 32 rows of keys, then 32 of values; the first `left` exist, the
+// first is at position pos0.
+constexpr int kOwnSlot = 2 * 32 * kD * 2;
+__device__ __forceinline__ void tile_put_own(TileBuf& b, const uint8_t* slot, int left, int pos0, int wave, int lane)
+{
+    const int c = lane & 15, quarter = lane >> 4;
+    b.k[wave >> 2][wave & 3][lane] =
+        pair_order(*reinterpret_cast<const u4*>(slot + step_slot<32>(wave >> 2, c) * 256 + (wave & 3) * 64 + quarter * 16));
+    const uint16_t* values = reinterpret_cast<const uint16_t*>(slot + kOwnSlot / 2) + 16 * wave + c;
+    uint32_t w[8];
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int token = 8 * quarter + e;
+        w[e] = values[token * kD];
+        const bool none = token >= left, bad = (w[e] & 0x7c00u) == 0x7c00u;
+        odd |= bad && !none;
+        w[e] = bad || none ? 0u : w[e];
+    }
+    b.v[wave][lane] = __builtin_bit_cast(h8, u4{w[0] | w[2] << 16, w[1] | w[3] << 16, w[4] | w[6] << 16, w[5] | w[7] << 16});
+    const unsigned long long any = __ballot(odd);
+    if (lane == 0) b.odd[wave] = any != 0;
+    if (wave == 0 && lane < 32) {
+        b.meta[quarter][c] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
+#pragma unroll
+        for (int g = 0; g < kNG; ++g) b.s[quarter][g][c] = 0x1p-9f;
+        b.pos[quarter][c] = pos0 + step_slot<32>(quarter, c);
+    }
+}
+
+// Nothing is scheduled across.  The step is written in the order it is to be issued: left to itself the
+// compiler, short of registers, puts every product right before its use and waits for it.
+__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
+// x is computed before the next phase.
+__device__ __forceinline__ void by_now(float& x) { asm volatile("" : "+v"(x)); }
+
+// The sums x[rt][t][r] of a staged step: token (t, 4 quarter + r) against rows 16 rt + c.  Units of a
+// tile's group: while one's products are issued, the additions of the one before run beside
+// them and the operands of the one after the next are read.
+template <int RT>
+__device__ __forceinline__ void tile_sums(const TileBuf& b, const h8 (&q)[RT][kNG], const h8 (&sums)[RT], float (&x)[RT][2][4],
+                                          int lane)
+{
+    const int c = lane & 15, quarter = lane >> 4;
+    const f4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int kUnits = 2 * kNG;
+    h8 k[kUnits], meta[2];
+    f4 s[kUnits], sum[2][RT], part[kUnits][RT];
+    auto read = [&](int i) {
+        k[i] = b.k[i / kNG][i % kNG][lane];
+        s[i] = *reinterpret_cast<const f4*>(&b.s[i / kNG][i % kNG][4 * quarter]);
+    };
+    meta[0] = b.meta[0][c];
+    read(0);
+    read(1);
+    phase();
+#pragma unroll
+    for (int i = 0; i <= kUnits; ++i) {
+        const int t = i / kNG;
+        if (i % kNG == 0 && i < kUnits) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) sum[t][rt] = mfma_k32(meta[t], sums[rt], zero);
+        }
+        if (i < kUnits) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) part[i][rt] = mfma_k32(k[i], q[rt][i % kNG], zero);
+        }
+        if (i + 2 < kUnits) read(i + 2);
+        if (i + 2 == kNG) meta[1] = b.meta[1][c];
+        if (i > 0) {
+            const int e = i - 1;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                {
+                    float y = __builtin_fmaf(s[e][r], part[e][rt][r], sum[e / kNG][rt][r]);
+                    by_now(y);
+                    sum[e / kNG][rt][r] = y;
+                }
+        }
+        phase();
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[rt][t][r] = sum[t][rt][r];
+}
+
+template <int LI, bool MOD>
+__global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a)
+{
+    constexpr KvFmt hi = kLayoutFmts[LI].hi, lo = kLayoutFmts[LI].lo;
+    constexpr int RT = 2;
+    using Hi = Staged<hi.kb, hi.vb, hi.T, MOD>;
+    using Lo = Staged<lo.kb, lo.vb, lo.T, MOD>;
+    constexpr int kPages = Hi::slot > Lo::slot ? Hi::slot : Lo::slot, kSlot = kPages > kOwnSlot ? kPages : kOwnSlot;
+    __shared__ __align__(1024) uint8_t slots[2][kSlot];
+    __shared__ __align__(16) TileBuf bufs[3];
+    __shared__ int last_flag;
+    set_fp16_saturate();
+    const int lane = lane_id(), wave = wave_index();
+    const int c = lane & 15, quarter = lane >> 4;
+    const int G = a.Hq / a.Hkv;
+    const int item = (int)blockIdx.x / a.Hkv, h = (int)blockIdx.x - item * a.Hkv;
+    const int block = item / a.splits, split = item - block * a.splits;
+    const SeqBlock sb = find_block(a, block, kTileRows, a.rows_lo, a.rows_hi);
+    if (sb.b < 0) return;
+    const int first = a.seq_len[sb.b];
+    const int rows = sb.n * G, r0 = sb.blk * kTileRows + wave * 32;  // the wave's first row
+    h8 q[RT][kNG], sums[RT];
+    Rows<RT> R;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = min(r0 + 16 * rt + c, rows - 1);
+        const int j = row / G, hq = h * G + row - j * G;
+        const uint16_t* p = a.q + (sb.row0 + j) * a.q_stride + hq * kD + quarter * 8;
+        u4 x[kNG];
+#pragma unroll
+        for (int g = 0; g < kNG; ++g) x[g] = *reinterpret_cast<const u4*>(p + g * kG);
+        const RowOperands o = row_operands(x, quarter);
+#pragma unroll
+        for (int g = 0; g < kNG; ++g) q[rt][g] = o.q[g];
+        sums[rt] = o.sums;
         R.unit[rt] = o.unit * a.scale;
         R.p[rt] = first + j;
         R.form[rt] = ScoreForm{a.cap_in, a.cap_out, MOD && a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f};
@@ -391,96 +856,245 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? 2 : 1) void chunk_ro
     }
     const int t = sb.b * a.Hkv + h;
     const int len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
-    const int last = min(r0 + kRows, rows) - 1;
-    const int own = last / G + 1;  // tokens of the chunk that some row sees
+    const int own = (min((sb.blk + 1) * kTileRows, rows) - 1) / G + 1;  // own tokens that some row sees
+    const bool idle = r0 >= rows;                                        // a wave without rows only helps
+    const int j_first = min(r0, rows - 1) / G;  // the wave's first position
     const int s_hi = (len_hi + 31) >> 5, s_lo = (len_lo + 31) >> 5, s_own = (own + 31) >> 5;
-    const int steps = s_hi + s_lo + s_own;
-    const int begin = (int)((long long)steps * split / a.splits), end = (int)((long long)steps * (split + 1) / a.splits);
+    const int steps = s_hi + s_lo + s_own, splits = min(a.splits, steps);
+    if (split >= splits) return;
+    const int begin = (int)((long long)steps * split / splits), end = (int)((long long)steps * (split + 1) / splits);
     const int32_t* table = a.page_table + (long long)t * a.p_max;
+    const uint16_t* ok = a.k + sb.row0 * a.k_stride + h * kD;
+    const uint16_t* ov = a.v + sb.row0 * a.v_stride + h * kD;
 
-    auto section = [&](auto kb, auto vb, auto tt, int sec, int from, int to, int len) {
-        constexpr int KB = decltype(kb)::value, VB = decltype(vb)::value, T = decltype(tt)::value;
-        const int pages = (len + T - 1) / T;
-        // a step's page IDs; one outside the pool reads page 0 and counts no token
-        auto page = [&](int k, bool& ok) {
-            const int i = min(k, pages - 1);
-            const int id = table[sec == 0 ? i : a.p_max - 1 - i];
-            ok = (unsigned long long)(unsigned)id < (unsigned long long)a.num_pages;
-            return a.pool + (long long)(ok ? id : 0) * a.page_bytes;
-        };
-        StepRaw<KB, VB, T> raw;
-        for (int s = from + wave; s < to; s += kChunkWaves) {
-            bool ok0, ok1 = true;
-            const uint8_t* p0 = page(T == 16 ? 2 * s : s, ok0);
-            const uint8_t* p1 = T == 16 ? page(2 * s + 1, ok1) : p0;
-            load_step<KB, VB, T, MOD>(raw, p0, p1, c, quarter);
-            const uint32_t bad = T == 16 ? (ok0 ? 0u : 1u) | (ok1 ? 0u : 2u) : (ok0 ? 0u : 3u);
-            cached_step<KB, VB, T, RT, MOD>(R, raw, len - 32 * s, bad, a, quarter);
+    // lane l: the pages of step id_step + l (-1: outside the pool, reads as page 0 and counts no token)
+    int id_step = begin, ids0 = 0, ids1 = 0;
+    auto fetch_ids = [&](int from) {
+        id_step = from;
+        const int u = min(from + lane, s_hi + s_lo - 1);
+        const bool high = u < s_hi;
+        const int T = high ? hi.T : lo.T, len = high ? len_hi : len_lo, k = high ? u : u - s_hi;
+        const int last = (len + T - 1) / T - 1, i0 = T == 16 ? 2 * k : k, i1 = T == 16 ? min(i0 + 1, last) : i0;
+        ids0 = table[high ? i0 : a.p_max - 1 - i0];
+        ids1 = table[high ? i1 : a.p_max - 1 - i1];
+        ids0 = (unsigned long long)(unsigned)ids0 < (unsigned long long)a.num_pages ? ids0 : -1;
+        ids1 = (unsigned long long)(unsigned)ids1 < (unsigned long long)a.num_pages ? ids1 : -1;
+    };
+    if (begin < s_hi + s_lo) fetch_ids(begin);
+    // step u's pages (or own rows) on their way into a slot, 1 KB pieces over the waves; which of its
+    // tiles lie outside the pool
+    auto load = [&](int u, uint8_t* slot) -> uint32_t {
+        if (u >= s_hi + s_lo) {
+            const int i0 = 32 * (u - s_hi - s_lo);
+            stage_rows(slot + wave * 1024, ok + (long long)i0 * a.k_stride, 2 * (int)a.k_stride, 4 * wave, own - 1 - i0, fresh(lane));
+            stage_rows(slot + kOwnSlot / 2 + wave * 1024, ov + (long long)i0 * a.v_stride, 2 * (int)a.v_stride, 4 * wave,
+                       own - 1 - i0, fresh(lane));
+            return 0;
+        }
+        if (u >= id_step + kWave) fetch_ids(u);
+        const int id0 = __builtin_amdgcn_readlane(ids0, u - id_step), id1 = __builtin_amdgcn_readlane(ids1, u - id_step);
+        const bool high = u < s_hi, two = high ? hi.T == 16 : lo.T == 16;
+        const int loads = high ? Hi::loads : Lo::loads, need = high ? Hi::need : Lo::need;
+        for (int i = wave; i < (two ? 2 : 1) * loads; i += kTileWaves) {
+            const int part = i >= loads ? 1 : 0, id = part ? id1 : id0;
+            stage_piece(slot + part * loads * 1024, a.pool + (long long)(id < 0 ? 0 : id) * a.page_bytes, need, i - part * loads,
+                        fresh(lane));
+        }
+        return two ? (id0 < 0 ? 1u : 0u) | (id1 < 0 ? 2u : 0u) : (id0 < 0 ? 3u : 0u);
+    };
+    auto put = [&](int u, TileBuf& b, const uint8_t* slot, uint32_t bad) {
+        if (u < s_hi) tile_put<hi.kb, hi.vb, hi.T, MOD>(b, slot, len_hi - 32 * u, bad, wave, fresh(lane));
+        else if (u < s_hi + s_lo) tile_put<lo.kb, lo.vb, lo.T, MOD>(b, slot, len_lo - 32 * (u - s_hi), bad, wave, fresh(lane));
+        else tile_put_own(b, slot, own - 32 * (u - s_hi - s_lo), first + 32 * (u - s_hi - s_lo), wave, fresh(lane));
+    };
+    // steps begin, begin + 1 on their way; `bad` of the step that is computed, the next and the one after
+    uint32_t now_bad = load(begin, slots[0]), next_bad = begin + 1 < end ? load(begin + 1, slots[1]) : 0, last_bad = 0;
+    staged_ready();
+    __syncthreads();
+    put(begin, bufs[0], slots[0], now_bad);
+    bufs[2].v[wave][lane] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});  // "before" the first step
+    h8 P[RT];  // the weights of the step before, whose values are still to be added
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) P[rt] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
+    auto add_values = [&](const TileBuf& b) {
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+            const h8 V = b.v[dt][lane];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, P[rt], R.acc[rt][dt]);
         }
     };
-    using std::integral_constant;
-    if (begin < s_hi)
-        section(integral_constant<int, hi.kb>{}, integral_constant<int, hi.vb>{}, integral_constant<int, hi.T>{}, 0, begin,
-                min(end, s_hi), len_hi);
-    if (end > s_hi && begin < s_hi + s_lo)
-        section(integral_constant<int, lo.kb>{}, integral_constant<int, lo.vb>{}, integral_constant<int, lo.T>{}, 1,
-                max(begin - s_hi, 0), min(end - s_hi, s_lo), len_lo);
-    {
-        const uint16_t* k = a.k + sb.row0 * a.k_stride + h * kD;
-        const uint16_t* v = a.v + sb.row0 * a.v_stride + h * kD;
-        for (int s = max(begin - s_hi - s_lo, 0) + wave; s < end - s_hi - s_lo; s += kChunkWaves)
-            own_step<RT, MOD>(R, k, v, 32 * s, own, first, a, c, quarter);
-    }
-
-    // the waves' states, 16 rows at a time
+    int at = 0;  // buffer of the step
+    __syncthreads();
+    // a step, of cached tokens or (own) of the chunk's
+    auto step = [&](int u, auto own_) {
+        constexpr bool mine = decltype(own_)::value;
+        const TileBuf& b = bufs[at];
+        const TileBuf& before = bufs[at == 0 ? 2 : at - 1];
+        TileBuf& after = bufs[at == 2 ? 0 : at + 1];
+        const int i0 = 32 * (u - s_hi - s_lo);
+        // the slot of the step after the next is free: its step (this one) has been put
+        if (u + 2 < end) last_bad = load(u + 2, slots[(u - begin) & 1]);
+        if (!idle) {
+            const int T = u < s_hi ? hi.T : lo.T;
+            const int left = mine ? 32 : (u < s_hi ? len_hi - 32 * u : len_lo - 32 * (u - s_hi));
+            // logits with a score form, -inf where a row does not see a token
+            auto hide = [&](float (&x)[RT][2][4]) {
+                if (MOD || (mine && i0 + 31 > j_first)) {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const float l = rows_sum(R.l[rt]);
-        if (quarter == 0) {
-            lds_ml[wave][0][c] = R.m[rt];
-            lds_ml[wave][1][c] = l;
-        }
+                    for (int tt = 0; tt < 2; ++tt) {
+                        const int4 ps = *reinterpret_cast<const int4*>(&b.pos[tt][4 * quarter]);
+                        const int pos[4] = {ps.x, ps.y, ps.z, ps.w};
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f4*>(&lds_acc[wave][c][16 * dt + 4 * quarter]) = R.acc[rt][dt];
-        __syncthreads();
-        // 16 threads a row, eight dims each
-        const int row = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8;
-        const int at = r0 + 16 * rt + row;
-        float m = kLowest, sum = 0.0f, o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int w = 0; w < kChunkWaves; ++w) m = fmaxf(m, lds_ml[w][0][row]);
+                            for (int r = 0; r < 4; ++r) {
+                                const int away = R.p[rt] - pos[r];
+                                const float y = MOD ? formed(x[rt][tt][r] * R.unit[rt], R.form[rt], (float)away) : x[rt][tt][r];
+                                x[rt][tt][r] = (away >= 0 || !mine) && away < a.window ? y : -INFINITY;
+                            }
+                    }
+                }
+                if (!mine && (left < 32 || now_bad)) {
 #pragma unroll
-        for (int w = 0; w < kChunkWaves; ++w) {
-            const float f = __builtin_amdgcn_exp2f(lds_ml[w][0][row] - m);
-            sum += f * lds_ml[w][1][row];
-            const f4 x = *reinterpret_cast<const f4*>(&lds_acc[w][row][d]), y = *reinterpret_cast<const f4*>(&lds_acc[w][row][d + 4]);
+                    for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                o[i] += f * x[i];
-                o[i + 4] += f * y[i];
+                        for (int r = 0; r < 4; ++r) {
+                            const int token = T == 16 ? 16 * tt + 4 * quarter + r : step_slot<32>(tt, 4 * quarter + r);
+                            const bool there = token < left && !((now_bad >> tt) & 1);
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt) x[rt][tt][r] = there ? x[rt][tt][r] : -INFINITY;
+                        }
+                }
+            };
+            float unit[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? 1.0f : R.unit[rt];
+            {
+                // the values of the step before beside this step's exponentials
+                float x[RT][2][4];
+                tile_sums<RT>(b, q, sums, x, lane);
+                h8 V[8];
+                V[0] = before.v[0][lane];
+                V[1] = before.v[1][lane];
+                phase();
+                hide(x);
+                raise_max<RT>(R, unit, x, [&] {  // (the step before still has the old max)
+                    add_values(before);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) P[rt] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
+                });
+                phase();
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V[dt], P[rt], R.acc[rt][dt]);
+                    if (dt + 2 < 8) V[dt + 2] = before.v[dt + 2][lane];
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {  // a score of each row tile
+                        float& w = x[rt][dt >> 2][dt & 3];
+                        w = weight(w, unit[rt], R.m[rt]);
+                        R.l[rt] += w;
+                        by_now(w);
+                        by_now(R.l[rt]);
+                    }
+                    phase();
+                }
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) P[rt] = pack_weights(x[rt]);
             }
-        }
-        if (at < rows) {
-            const int j = at / G, hq = h * G + at - j * G;
-            const long long row_q = (sb.row0 + j) * a.Hq + hq;
-            if (a.splits == 1) {
-                const float inv = 1.0f / sum;
-                h8 r;
+            if constexpr (mine) {
+                uint32_t odd = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r[i] = (_Float16)(o[i] * inv);
-                *reinterpret_cast<h8*>(a.out + row_q * kD + d) = r;
-                if (a.lse && (threadIdx.x & 15) == 0) a.lse[row_q] = kChunkLn2 * (m + __builtin_amdgcn_logf(sum));
-            } else {
-                float* part = a.part + (row_q * a.splits + split) * kChunkPart;
-                *reinterpret_cast<f4*>(part + d) = f4{o[0], o[1], o[2], o[3]};
-                *reinterpret_cast<f4*>(part + d + 4) = f4{o[4], o[5], o[6], o[7]};
-                if ((threadIdx.x & 15) == 0) {
-                    part[kD] = m;
-                    part[kD + 1] = sum;
+                for (int w = 0; w < kTileWaves; ++w) odd |= b.odd[w];
+                if (odd) {  // (the weights once more: kept until here they cost registers in every step)
+                    float x[RT][2][4];
+                    tile_sums<RT>(b, q, sums, x, lane);
+                    hide(x);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                x[rt][tt][r] = weight(x[rt][tt][r], unit[rt], R.m[rt]);
+                    odd_values<RT>(R, x, ov, i0, own, first, a, c, quarter);
                 }
             }
         }
+        if (u + 1 < end) put(u + 1, after, slots[(u + 1 - begin) & 1], next_bad);
+        at = at == 2 ? 0 : at + 1;
+        now_bad = next_bad;
+        next_bad = last_bad;
+        staged_ready();
         __syncthreads();
+    };
+    for (int u = begin; u < min(end, s_hi + s_lo); ++u) step(u, std::false_type{});
+    for (int u = max(begin, s_hi + s_lo); u < end; ++u) step(u, std::true_type{});
+    if (!idle) add_values(bufs[at == 0 ? 2 : at - 1]);
+
+    float l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) l[rt] = rows_sum(R.l[rt]);
+    const long long slot_no = (long long)block * a.Hkv + h;
+    auto write = [&](int rt) {
+        const int at = r0 + 16 * rt + c;
+        if (at >= rows) return;
+        const int j = at / G, hq = h * G + at - j * G;
+        const long long row_q = (sb.row0 + j) * a.Hq + hq;
+        const float inv = 1.0f / l[rt];
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+            h4 r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = (_Float16)(R.acc[rt][dt][i] * inv);
+            *reinterpret_cast<h4*>(a.out + row_q * kD + 16 * dt + 4 * quarter) = r;
+        }
+        if (a.lse && quarter == 0) a.lse[row_q] = kChunkLn2 * (R.m[rt] + __builtin_amdgcn_logf(l[rt]));
+    };
+    if (splits == 1) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) write(rt);
+        return;
+    }
+    float* part = a.part + slot_no * a.splits * kTileRows * kChunkPart;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float* to = part + ((long long)split * kTileRows + wave * 32 + 16 * rt + c) * kChunkPart;
+        if (r0 + 16 * rt + c >= rows) continue;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+            put_pair(to + 16 * dt + 4 * quarter, R.acc[rt][dt][0], R.acc[rt][dt][1]);
+            put_pair(to + 16 * dt + 4 * quarter + 2, R.acc[rt][dt][2], R.acc[rt][dt][3]);
+        }
+        if (quarter == 0) put_pair(to + kD, R.m[rt], l[rt]);
+    }
+    if (!split_last(a.arrive + slot_no, splits, &last_flag)) return;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        if (r0 + 16 * rt + c >= rows) continue;
+        const float* from = part + (wave * 32 + 16 * rt + c) * kChunkPart;
+        float m = kLowest, sum = 0.0f;
+        f4 o[8];
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) o[dt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < splits; ++k, from += kTileRows * kChunkPart) {
+            const float2 ml = get_pair(from + kD);
+            const float top = fmaxf(m, ml.x);
+            const float f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(ml.x - top);
+            m = top;
+            sum = sum * f + ml.y * g;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) {
+                const float2 x = get_pair(from + 16 * dt + 4 * quarter), y = get_pair(from + 16 * dt + 4 * quarter + 2);
+                o[dt] = o[dt] * f + f4{x.x, x.y, y.x, y.y} * g;
+            }
+        }
+        R.m[rt] = m;
+        l[rt] = sum;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] = o[dt];
+        write(rt);
     }
 }
 
@@ -671,7 +1285,8 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs
 
 }  // namespace dkv
 
-// Kernel entry points of layout n: which = 0 scores, 1 / 2 / 4 attention with that many row tiles.
+// Kernel entry points of layout n: which = 0 scores, 1 / 2 attention of few rows with that many row
+// tiles, 3 of many.
 #define DKV_CHUNK_KERNELS(LI)                                                                                  \
     const void* chunk_kernel_l##LI(int which, bool mod)                                                        \
     {                                                                                                          \
@@ -679,7 +1294,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs
         case 0: return mod ? (const void*)chunk_scores<LI, true> : (const void*)chunk_scores<LI, false>;       \
         case 1: return mod ? (const void*)chunk_rows<LI, 1, true> : (const void*)chunk_rows<LI, 1, false>;     \
         case 2: return mod ? (const void*)chunk_rows<LI, 2, true> : (const void*)chunk_rows<LI, 2, false>;     \
-        case 4: return mod ? (const void*)chunk_rows<LI, 4, true> : (const void*)chunk_rows<LI, 4, false>;     \
+        case 3: return mod ? (const void*)chunk_tiles<LI, true> : (const void*)chunk_tiles<LI, false>;         \
         default: return nullptr;                                                                               \
         }                                                                                                      \
     }

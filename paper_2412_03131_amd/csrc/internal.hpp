@@ -266,15 +266,30 @@ struct ChunkArgs {
     float* lse;            // [total_new][Hq] or null
     const float* lse_in;   // scores: as attention wrote it
     float* score;          // [total_new][Hkv]
-    float* part;           // partial states {acc[kD], max, sum} per (row, query head, split)
+    unsigned long long* arrive;  // arrival word per row block (split ones)
+    float* part;           // [row block][split][row] partial states {acc[kD], max, sum}
     int splits;            // workgroups per row block
+    int blocks;            // row blocks of a KV head that the launch may have
     int rows_lo, rows_hi;  // the launch takes sequences with that many rows (new tokens x G)
     int shares;            // scores: workgroups per table
     int layout;
 };
 constexpr int kChunkPart = kD + 4;  // floats of a partial state (16-byte rows)
-int chunk_splits(long long B, long long Hq, long long Hkv, long long total_new, long long p_max);
-hipError_t launch_chunk_attention(const ChunkArgs& a, bool mod, hipStream_t st);
+
+// How a chunk attention call splits: sequences of at most kChunkFewRows rows in blocks of 16 (or 32)
+// rows, longer ones in blocks of kChunkRows, each with so many workgroups per block; the row blocks
+// there can be (all KV heads) and the workspace.  A function of what the workspace size is told.
+constexpr int kChunkFewRows = 64;
+constexpr int kChunkRows = 256;
+constexpr int kTileThreads = 512;  // of a workgroup on kChunkRows rows
+struct ChunkPlan {
+    int few_splits, many_splits;
+    long long few_blocks, many_blocks;
+    long long few_part, many_part;  // floats of partial states
+    long long bytes;
+};
+ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_new, long long p_max);
+hipError_t launch_chunk_attention(const ChunkArgs& a, const ChunkPlan& plan, bool mod, hipStream_t st);
 hipError_t launch_chunk_scores(const ChunkArgs& a, bool mod, hipStream_t st);
 // Kernel entry points of layout n (k_chunk_l<n>.hip).
 const void* chunk_kernel_l0(int which, bool mod);

@@ -4,28 +4,6 @@
 
 namespace dkv {
 
-// Joins the partial states of a row's splits: one wave per (token, query head), two dims a lane.
-__global__ __launch_bounds__(256) void chunk_join(ChunkArgs a)
-{
-    set_fp16_saturate();
-    const long long row = (long long)blockIdx.x * 4 + wave_index();
-    if (row >= a.total_new * a.Hq) return;
-    const int lane = lane_id();
-    const float* part = a.part + row * a.splits * kChunkPart;
-    float m = kLowest, sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, part[s * kChunkPart + kD]);
-    for (int s = 0; s < a.splits; ++s) {
-        const float f = __builtin_amdgcn_exp2f(part[s * kChunkPart + kD] - m);
-        sum += f * part[s * kChunkPart + kD + 1];
-        o0 += f * part[s * kChunkPart + 2 * lane];
-        o1 += f * part[s * kChunkPart + 2 * lane + 1];
-    }
-    const float inv = 1.0f / sum;
-    const h2 r = {(_Float16)(o0 * inv), (_Float16)(o1 * inv)};
-    *reinterpret_cast<h2*>(a.out + row * kD + 2 * lane) = r;
-    if (a.lse && lane == 0) a.lse[row] = kChunkLn2 * (m + __builtin_amdgcn_logf(sum));
-}
-
 static const void* chunk_kernel(int li, int which, bool mod)
 {
     switch (li) {
@@ -37,41 +15,65 @@ static const void* chunk_kernel(int li, int which, bool mod)
     }
 }
 
-// Workgroups per row block: about 1024 in all, no more than the longest table there can be has
-// steps of 32 tokens for their waves, at most 64.
-int chunk_splits(long long B, long long Hq, long long Hkv, long long total_new, long long p_max)
+static long long align256(long long x) { return (x + 255) & ~255ll; }
+
+ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_new, long long p_max)
 {
-    const long long G = Hq / Hkv;
+    ChunkPlan p{};
+    const long long G = Hq / Hkv, rows = total_new * G;
     const long long seqs = B < total_new ? B : total_new;
-    const long long items = Hkv * (seqs + total_new * G / 64);
-    const long long most = p_max / 8 + 1;
-    long long s = items > 0 ? 1024 / items : 1;
-    if (s > most) s = most;
-    if (s > 64) s = 64;
-    return (int)(s < 1 ? 1 : s);
+    const long long steps = p_max / 2 + total_new / 32 + 2;  // 32-token steps of the longest table there can be
+    auto clamp = [](long long x, long long lo, long long hi) { return x < lo ? lo : (x > hi ? hi : x); };
+    // few rows: about 2048 workgroups, a step for each of their waves
+    p.few_splits = seqs ? (int)clamp(2048 / (Hkv * seqs), 1, clamp(steps / 4, 1, 64)) : 1;
+    p.few_blocks = Hkv * clamp(rows / 16 + 2 * seqs, 0, seqs * (kChunkFewRows / 16));  // (in blocks of 32: two each)
+    p.few_part = p.few_splits > 1 ? p.few_blocks * p.few_splits * 16 * kChunkPart : 0;
+    // many rows: about 512 workgroups of eight waves
+    const long long longs = clamp(rows / (kChunkFewRows + 1), 0, seqs);
+    p.many_blocks = longs ? Hkv * (rows / kChunkRows + longs) : 0;
+    const long long whole = Hkv * clamp(rows / kChunkRows, 1, rows + 1);
+    p.many_splits = (int)clamp(512 / whole, 1, clamp(steps / 8, 1, 16));
+    p.many_part = p.many_splits > 1 ? p.many_blocks * p.many_splits * kChunkRows * kChunkPart : 0;
+    p.bytes = align256((p.few_blocks + p.many_blocks) * 8) + align256(p.few_part * 4) + align256(p.many_part * 4);
+    return p;
 }
 
-hipError_t launch_chunk_attention(const ChunkArgs& args, bool mod, hipStream_t st)
+hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, bool mod, hipStream_t st)
 {
+    const long long G = args.Hq / args.Hkv, rows = args.max_new * G;
+    const long long seqs = args.B < args.total_new ? args.B : args.total_new;
+    unsigned long long* arrive = args.arrive;
+    float* part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(arrive) + align256((plan.few_blocks + plan.many_blocks) * 8));
+    auto launch = [&](ChunkArgs& a, int which, long long blocks, int threads) {
+        const void* kern = chunk_kernel(a.layout, which, mod);
+        const long long grid = blocks * a.Hkv * a.splits;
+        if (!kern || grid > INT32_MAX) return hipErrorInvalidValue;
+        if (grid < 1) return hipSuccess;
+        void* kargs[] = {&a};
+        return hipLaunchKernel(kern, dim3((unsigned)grid), dim3((unsigned)threads), kargs, 0, st);
+    };
+    if (rows > kChunkFewRows) {
+        ChunkArgs a = args;
+        a.rows_lo = kChunkFewRows + 1;
+        a.rows_hi = INT32_MAX;
+        a.splits = plan.many_splits;
+        a.arrive = arrive + plan.few_blocks;
+        a.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(part) + align256(plan.few_part * 4));
+        const hipError_t e = launch(a, 3, plan.many_blocks / a.Hkv, kTileThreads);
+        if (e != hipSuccess) return e;
+        // (all sequences have the one length then)
+        if (args.total_new == (long long)args.B * args.max_new) return hipSuccess;
+    }
     ChunkArgs a = args;
-    const long long G = a.Hq / a.Hkv;
-    const long long rows = a.max_new * G;
-    const int rt = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
-    const void* kern = chunk_kernel(a.layout, rt, mod);
-    if (!kern) return hipErrorInvalidValue;
     a.rows_lo = 1;
-    a.rows_hi = INT32_MAX;
-    // row blocks: at most one more than whole ones per sequence, and as many as the longest has
-    const long long per = 16 * rt, seqs = a.B < a.total_new ? a.B : a.total_new;
-    long long blocks = a.total_new * G / per + seqs;
-    const long long other = seqs * ((rows + per - 1) / per);
-    if (other < blocks) blocks = other;
-    const long long grid = blocks * a.Hkv * a.splits;
-    if (grid < 1 || grid > INT32_MAX) return hipErrorInvalidValue;
-    void* kargs[] = {&a};
-    hipError_t e = hipLaunchKernel(kern, dim3((unsigned)grid), dim3(4 * kWave), kargs, 0, st);
-    if (e != hipSuccess || a.splits == 1) return e;
-    return launch1(chunk_join, (unsigned)((a.total_new * a.Hq + 3) / 4), 256, st, a);
+    a.rows_hi = kChunkFewRows;
+    a.splits = plan.few_splits;
+    a.part = part;
+    // blocks of 32 rows where the longest of the few have more than 16
+    const int rt = rows > 16 && rows <= kChunkFewRows ? 2 : 1;
+    const long long per = 16 * rt, most = rows < kChunkFewRows ? rows : kChunkFewRows;
+    const long long whole = args.total_new * G / per + seqs, each = seqs * ((most + per - 1) / per);
+    return launch(a, rt, whole < each ? whole : each, 4 * kWave);
 }
 
 hipError_t launch_chunk_scores(const ChunkArgs& args, bool mod, hipStream_t st)

@@ -122,6 +122,30 @@ __device__ __forceinline__ SeqBlock find_block(const ChunkArgs& a, int want, int
     return s;
 }
 
+// First row and length of sequence s.b (clamped as there); every wave by itself.
+__device__ __forceinline__ void sequence_rows(const ChunkArgs& a, SeqBlock& s)
+{
+    if (a.max_new == 1 && a.total_new == a.B) {
+        s.n = 1;
+        s.row0 = s.b;
+        return;
+    }
+    const int lane = lane_id();
+    long long row = 0;
+    int n = 0;
+    for (int b0 = 0; b0 <= s.b; b0 += kWave) {
+        const int i = b0 + lane;
+        int x = i <= s.b ? a.new_len[i] : 0;
+        x = x < 0 ? 0 : (x > a.max_new ? a.max_new : x);
+        const int incl = wave_incl_scan(x), l = min(s.b - b0, kWave - 1);
+        n = __builtin_amdgcn_readlane(x, l);
+        row += __builtin_amdgcn_readlane(incl, l);
+    }
+    s.row0 = row - n;
+    const long long room = a.total_new - s.row0;
+    s.n = n <= room ? n : (room > 0 ? (int)room : 0);
+}
+
 // ---- split rows, joined inside the launch -----------------------------------------
 // A row block whose steps are split over workgroups: each writes its rows' states {acc[kD], max,
 // sum} to its slot with agent-scope stores (through to memory: the workgroups may be on
@@ -136,6 +160,15 @@ __device__ __forceinline__ float2 get_pair(const float* p)
     const unsigned long long v = __hip_atomic_load(reinterpret_cast<unsigned long long*>(const_cast<float*>(p)),
                                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+// Sixteen bytes of a state with agent scope (cache policy bit 4 is sc1: past the XCD's L2).
+__device__ __forceinline__ void put_quad(__amdgpu_buffer_rsrc_t r, int lane_offset, int offset, f4 x)
+{
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x), r, lane_offset, offset, 16);
+}
+__device__ __forceinline__ f4 get_quad(__amdgpu_buffer_rsrc_t r, int lane_offset, int offset)
+{
+    return __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_offset, offset, 16));
 }
 // After the workgroup's stores: whether it is the last of `splits` (uniform).
 __device__ __forceinline__ bool split_last(unsigned long long* word, int splits, int* lds_flag)

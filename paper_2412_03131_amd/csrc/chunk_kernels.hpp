@@ -657,6 +657,8 @@ constexpr int kTileWaves = 8;
 constexpr int kTileRows = kTileWaves * 32;
 static_assert(kTileRows == kChunkRows, "row blocks of the plan");
 
+constexpr int kStepUnits = 64;  // work units of a step
+
 struct TileBuf {
     h8 k[2][kNG][kWave];     // [tile][group][lane]
     h8 v[8][kWave];          // [16-dim tile][lane]
@@ -819,19 +821,53 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
     using Hi = Staged<hi.kb, hi.vb, hi.T, MOD>;
     using Lo = Staged<lo.kb, lo.vb, lo.T, MOD>;
     constexpr int kPages = Hi::slot > Lo::slot ? Hi::slot : Lo::slot, kSlot = kPages > kOwnSlot ? kPages : kOwnSlot;
-    __shared__ __align__(1024) uint8_t slots[2][kSlot];
-    __shared__ __align__(16) TileBuf bufs[3];
-    __shared__ int last_flag;
+    struct Shared {
+        uint8_t slots[2][kSlot];  // (first: the loads that write there take 16-bit addresses)
+        TileBuf bufs[3];
+        long long scan[kTileWaves];
+        long long found_at;
+        int found, last;
+    };
+    __shared__ __align__(1024) Shared sh;
+    auto& slots = sh.slots;
+    auto& bufs = sh.bufs;
     set_fp16_saturate();
     const int lane = lane_id(), wave = wave_index();
     const int c = lane & 15, quarter = lane >> 4;
     const int G = a.Hq / a.Hkv;
-    const int item = (int)blockIdx.x / a.Hkv, h = (int)blockIdx.x - item * a.Hkv;
-    const int block = item / a.splits, split = item - block * a.splits;
-    const SeqBlock sb = find_block(a, block, kTileRows, a.rows_lo, a.rows_hi);
-    if (sb.b < 0) return;
+
+    // The work of all tables end to end, cut into equal shares
+    const int own_units = 2 * kTileRows / G;  // of one block's own tokens more than the block before has
+    const int tables = a.B * a.Hkv, chunk = (tables + kTileWaves * kWave - 1) / (kTileWaves * kWave);
+    const int t0 = min((int)threadIdx.x * chunk, tables), t1 = min(t0 + chunk, tables);
+    auto blocks_units = [&](int t, int& nb) -> long long {  // units of a block's cached steps; blocks
+        int n = a.new_len[t / a.Hkv];
+        n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
+        nb = chunk_blocks(n, G, kTileRows, a.rows_lo, a.rows_hi);
+        return nb ? (long long)(((a.len[2 * t] + 31) >> 5) + ((a.len[2 * t + 1] + 31) >> 5)) * kStepUnits : 0;
+    };
+    auto units_to = [&](long long cached, int nb) { return nb * cached + (long long)own_units * nb * (nb + 1) / 2; };
+    long long mine = 0;
+    for (int t = t0; t < t1; ++t) {
+        int nb;
+        const long long cached = blocks_units(t, nb);
+        mine += units_to(cached, nb);
+    }
+    long long total;
+    const long long mine_from = block_excl_scan_wide(mine, sh.scan, &total);
+    // a share has at least eight steps (its fixed cost is about as much)
+    const long long quantum = max((total + gridDim.x - 1) / gridDim.x, 8ll * kStepUnits);
+    // consecutive shares on one XCD (workgroups go round over the eight): they read the same tables
+    const int per_xcd = ((int)gridDim.x + 7) >> 3;
+    const int share = gridDim.x % 8 == 0 ? ((int)blockIdx.x & 7) * per_xcd + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
+    const long long start = share * quantum, stop = min(total, start + quantum);
+    if (start >= total) return;
+    int piece = 0;
+    // One piece: units cur .. piece_end of the row block of head h that has from .. to
+    auto tile_piece = [&](const SeqBlock& sb, int h, long long from, long long to, long long cur, long long piece_end) {
     const int first = a.seq_len[sb.b];
     const int rows = sb.n * G, r0 = sb.blk * kTileRows + wave * 32;  // the wave's first row
+    if (sb.blk * kTileRows >= rows) return;
     h8 q[RT][kNG], sums[RT];
     Rows<RT> R;
 #pragma unroll
@@ -860,9 +896,14 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
     const bool idle = r0 >= rows;                                        // a wave without rows only helps
     const int j_first = min(r0, rows - 1) / G;  // the wave's first position
     const int s_hi = (len_hi + 31) >> 5, s_lo = (len_lo + 31) >> 5, s_own = (own + 31) >> 5;
-    const int steps = s_hi + s_lo + s_own, splits = min(a.splits, steps);
-    if (split >= splits) return;
-    const int begin = (int)((long long)steps * split / splits), end = (int)((long long)steps * (split + 1) / splits);
+    // units -> steps: the own steps share the block's units behind the cached ones'
+    auto step_of = [&](long long x) -> int {
+        const long long before_own = (long long)(s_hi + s_lo) * kStepUnits;
+        if (x < before_own) return (int)(x / kStepUnits);
+        return s_hi + s_lo + (int)((x - before_own) * s_own / (to - from - before_own));
+    };
+    const int begin = step_of(cur - from), end = step_of(piece_end - from);
+    const bool whole = cur == from && piece_end == to;
     const int32_t* table = a.page_table + (long long)t * a.p_max;
     const uint16_t* ok = a.k + sb.row0 * a.k_stride + h * kD;
     const uint16_t* ov = a.v + sb.row0 * a.v_stride + h * kD;
@@ -880,7 +921,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
         ids0 = (unsigned long long)(unsigned)ids0 < (unsigned long long)a.num_pages ? ids0 : -1;
         ids1 = (unsigned long long)(unsigned)ids1 < (unsigned long long)a.num_pages ? ids1 : -1;
     };
-    if (begin < s_hi + s_lo) fetch_ids(begin);
+    if (begin < min(end, s_hi + s_lo)) fetch_ids(begin);
     // step u's pages (or own rows) on their way into a slot, 1 KB pieces over the waves; which of its
     // tiles lie outside the pool
     auto load = [&](int u, uint8_t* slot) -> uint32_t {
@@ -908,10 +949,11 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
         else tile_put_own(b, slot, own - 32 * (u - s_hi - s_lo), first + 32 * (u - s_hi - s_lo), wave, fresh(lane));
     };
     // steps begin, begin + 1 on their way; `bad` of the step that is computed, the next and the one after
-    uint32_t now_bad = load(begin, slots[0]), next_bad = begin + 1 < end ? load(begin + 1, slots[1]) : 0, last_bad = 0;
+    uint32_t now_bad = begin < end ? load(begin, slots[0]) : 0, next_bad = begin + 1 < end ? load(begin + 1, slots[1]) : 0;
+    uint32_t last_bad = 0;
     staged_ready();
     __syncthreads();
-    put(begin, bufs[0], slots[0], now_bad);
+    if (begin < end) put(begin, bufs[0], slots[0], now_bad);
     bufs[2].v[wave][lane] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});  // "before" the first step
     h8 P[RT];  // the weights of the step before, whose values are still to be added
 #pragma unroll
@@ -1036,7 +1078,6 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
     float l[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) l[rt] = rows_sum(R.l[rt]);
-    const long long slot_no = (long long)block * a.Hkv + h;
     auto write = [&](int rt) {
         const int at = r0 + 16 * rt + c;
         if (at >= rows) return;
@@ -1052,49 +1093,104 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
         }
         if (a.lse && quarter == 0) a.lse[row_q] = kChunkLn2 * (R.m[rt] + __builtin_amdgcn_logf(l[rt]));
     };
-    if (splits == 1) {
+    if (whole) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) write(rt);
         return;
     }
-    float* part = a.part + slot_no * a.splits * kTileRows * kChunkPart;
+    // Cut by a share's end: the pieces' states are joined by the last of them, in order.  A share has at most
+    // two pieces of cut blocks, its first (slot 0) and its last (slot 1, if it is not also the first);
+    // the block's word is that of the share where it begins.
+    // A wave's part of a state: its accumulators lane by lane (1 KB each), then max and sum of its rows.
+    constexpr int kWavePart = RT * 8 * 1024 + RT * 128;
+    static_assert(kTileWaves * kWavePart <= kTileRows * kChunkPart * 4, "a piece's room in the workspace");
+    auto part_of = [&](int k, bool first_piece) {
+        return span(reinterpret_cast<uint8_t*>(a.part + (2ll * k + (first_piece ? 0 : 1)) * kTileRows * kChunkPart) +
+                        wave * kWavePart,
+                    kWavePart);
+    };
+    const int k0 = (int)(from / quantum), k1 = (int)((to - 1) / quantum);
+    {
+        const __amdgpu_buffer_rsrc_t out = part_of(share, piece == 0);
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        float* to = part + ((long long)split * kTileRows + wave * 32 + 16 * rt + c) * kChunkPart;
-        if (r0 + 16 * rt + c >= rows) continue;
+        for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) {
-            put_pair(to + 16 * dt + 4 * quarter, R.acc[rt][dt][0], R.acc[rt][dt][1]);
-            put_pair(to + 16 * dt + 4 * quarter + 2, R.acc[rt][dt][2], R.acc[rt][dt][3]);
+            for (int dt = 0; dt < 8; ++dt) put_quad(out, lane * 16, (rt * 8 + dt) * 1024, R.acc[rt][dt]);
+            if (quarter == 0)
+                __builtin_amdgcn_raw_buffer_store_b64(u2{__float_as_uint(R.m[rt]), __float_as_uint(l[rt])}, out, c * 8,
+                                                      RT * 8 * 1024 + rt * 128, 16);
         }
-        if (quarter == 0) put_pair(to + kD, R.m[rt], l[rt]);
     }
-    if (!split_last(a.arrive + slot_no, splits, &last_flag)) return;
+    if (!split_last(a.arrive + k0, k1 - k0 + 1, &sh.last)) return;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        if (r0 + 16 * rt + c >= rows) continue;
-        const float* from = part + (wave * 32 + 16 * rt + c) * kChunkPart;
-        float m = kLowest, sum = 0.0f;
-        f4 o[8];
+        R.m[rt] = kLowest;
+        l[rt] = 0.0f;
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) o[dt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int k = 0; k < splits; ++k, from += kTileRows * kChunkPart) {
-            const float2 ml = get_pair(from + kD);
-            const float top = fmaxf(m, ml.x);
-            const float f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(ml.x - top);
-            m = top;
-            sum = sum * f + ml.y * g;
+        for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    for (int k = k0; k <= k1; ++k) {
+        const __amdgpu_buffer_rsrc_t in = part_of(k, k > k0 || from == k0 * quantum);
+        f4 o[RT][8];
+        u2 ml[RT];
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt) {
-                const float2 x = get_pair(from + 16 * dt + 4 * quarter), y = get_pair(from + 16 * dt + 4 * quarter + 2);
-                o[dt] = o[dt] * f + f4{x.x, x.y, y.x, y.y} * g;
+        for (int rt = 0; rt < RT; ++rt) {
+            ml[rt] = __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(in, c * 8, RT * 8 * 1024 + rt * 128, 16));
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) o[rt][dt] = get_quad(in, lane * 16, (rt * 8 + dt) * 1024);
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const float m = __uint_as_float(ml[rt][0]), top = fmaxf(R.m[rt], m);
+            const float f = __builtin_amdgcn_exp2f(R.m[rt] - top), g = __builtin_amdgcn_exp2f(m - top);
+            R.m[rt] = top;
+            l[rt] = l[rt] * f + __uint_as_float(ml[rt][1]) * g;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] = R.acc[rt][dt] * f + o[rt][dt] * g;
+        }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) write(rt);
+    };
+    for (long long cur = start; cur < stop; ++piece) {
+        // the table that has unit `cur`
+        __syncthreads();
+        if (cur >= mine_from && cur < mine_from + mine) {
+            long long at = mine_from;
+            for (int t = t0; t < t1; ++t) {
+                int nb;
+                const long long cached = blocks_units(t, nb);
+                const long long next = at + units_to(cached, nb);
+                if (cur < next) {
+                    sh.found = t;
+                    sh.found_at = at;
+                    break;
+                }
+                at = next;
             }
         }
-        R.m[rt] = m;
-        l[rt] = sum;
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] = o[dt];
-        write(rt);
+        __syncthreads();
+        const int t = __builtin_amdgcn_readfirstlane(sh.found);
+        const long long table_at = read_lane<long long>(sh.found_at, 0);
+        int nb;
+        const long long cached = blocks_units(t, nb);
+        int blk = 0;
+        {
+            int above = nb - 1;  // the last block that starts at or before cur
+            while (blk < above) {
+                const int mid = (blk + above + 1) >> 1;
+                if (table_at + units_to(cached, mid) <= cur) blk = mid;
+                else above = mid - 1;
+            }
+        }
+        const long long from = table_at + units_to(cached, blk), to = table_at + units_to(cached, blk + 1);
+        const long long piece_end = min(stop, to);
+        SeqBlock sb;
+        sb.b = t / a.Hkv;
+        sb.blk = blk;
+        sequence_rows(a, sb);
+        tile_piece(sb, t - sb.b * a.Hkv, from, to, cur, piece_end);
+        cur = piece_end;
     }
 }
 

@@ -276,16 +276,19 @@ struct ChunkArgs {
 };
 constexpr int kChunkPart = kD + 4;  // floats of a partial state (16-byte rows)
 
-// How a chunk attention call splits: sequences of at most kChunkFewRows rows in blocks of 16 (or 32)
-// rows, longer ones in blocks of kChunkRows, each with so many workgroups per block; the row blocks
-// there can be (all KV heads) and the workspace.  A function of what the workspace size is told.
+// How a chunk attention call is laid out: sequences of at most kChunkFewRows rows (new tokens x query heads
+// of a KV head) in blocks of 16 or 32 rows, each with few_splits workgroups; longer ones in blocks of
+// kChunkRows, all of them cut into kTileShares equal shares.  A function of what the workspace size is
+// told.
 constexpr int kChunkFewRows = 64;
 constexpr int kChunkRows = 256;
 constexpr int kTileThreads = 512;  // of a workgroup on kChunkRows rows
+constexpr int kTileShares = 256;   // one for each CU
 struct ChunkPlan {
-    int few_splits, many_splits;
-    long long few_blocks, many_blocks;
-    long long few_part, many_part;  // floats of partial states
+    int few_splits;
+    long long few_blocks;  // of all KV heads
+    long long few_part;    // floats of partial states
+    bool many;             // there can be longer sequences
     long long bytes;
 };
 ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_new, long long p_max);

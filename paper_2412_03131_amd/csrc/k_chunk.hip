@@ -28,13 +28,9 @@ ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_n
     p.few_splits = seqs ? (int)clamp(2048 / (Hkv * seqs), 1, clamp(steps / 4, 1, 64)) : 1;
     p.few_blocks = Hkv * clamp(rows / 16 + 2 * seqs, 0, seqs * (kChunkFewRows / 16));  // (in blocks of 32: two each)
     p.few_part = p.few_splits > 1 ? p.few_blocks * p.few_splits * 16 * kChunkPart : 0;
-    // many rows: about 512 workgroups of eight waves
-    const long long longs = clamp(rows / (kChunkFewRows + 1), 0, seqs);
-    p.many_blocks = longs ? Hkv * (rows / kChunkRows + longs) : 0;
-    const long long whole = Hkv * clamp(rows / kChunkRows, 1, rows + 1);
-    p.many_splits = (int)clamp(512 / whole, 1, clamp(steps / 8, 1, 16));
-    p.many_part = p.many_splits > 1 ? p.many_blocks * p.many_splits * kChunkRows * kChunkPart : 0;
-    p.bytes = align256((p.few_blocks + p.many_blocks) * 8) + align256(p.few_part * 4) + align256(p.many_part * 4);
+    p.many = rows > kChunkFewRows;
+    p.bytes = align256((p.few_blocks + kTileShares) * 8) + align256(p.few_part * 4) +
+              (p.many ? 2ll * kTileShares * kChunkRows * kChunkPart * 4 : 0);
     return p;
 }
 
@@ -43,37 +39,34 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     const long long G = args.Hq / args.Hkv, rows = args.max_new * G;
     const long long seqs = args.B < args.total_new ? args.B : args.total_new;
     unsigned long long* arrive = args.arrive;
-    float* part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(arrive) + align256((plan.few_blocks + plan.many_blocks) * 8));
-    auto launch = [&](ChunkArgs& a, int which, long long blocks, int threads) {
+    float* part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(arrive) + align256((plan.few_blocks + kTileShares) * 8));
+    auto launch = [&](ChunkArgs& a, int which, long long grid, int threads) {
         const void* kern = chunk_kernel(a.layout, which, mod);
-        const long long grid = blocks * a.Hkv * a.splits;
-        if (!kern || grid > INT32_MAX) return hipErrorInvalidValue;
-        if (grid < 1) return hipSuccess;
+        if (!kern || grid < 1 || grid > INT32_MAX) return hipErrorInvalidValue;
         void* kargs[] = {&a};
         return hipLaunchKernel(kern, dim3((unsigned)grid), dim3((unsigned)threads), kargs, 0, st);
     };
     if (rows > kChunkFewRows) {
         ChunkArgs a = args;
-        a.rows_lo = kChunkFewRows + 1;
+        a.rows_lo = 17;
         a.rows_hi = INT32_MAX;
-        a.splits = plan.many_splits;
         a.arrive = arrive + plan.few_blocks;
         a.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(part) + align256(plan.few_part * 4));
-        const hipError_t e = launch(a, 3, plan.many_blocks / a.Hkv, kTileThreads);
+        const hipError_t e = launch(a, 3, kTileShares, kTileThreads);
         if (e != hipSuccess) return e;
         // (all sequences have the one length then)
         if (args.total_new == (long long)args.B * args.max_new) return hipSuccess;
     }
+    // Few rows: all sequences if none is longer, else those of one block of 16 rows
     ChunkArgs a = args;
     a.rows_lo = 1;
-    a.rows_hi = kChunkFewRows;
+    a.rows_hi = rows > kChunkFewRows ? 16 : kChunkFewRows;
     a.splits = plan.few_splits;
     a.part = part;
-    // blocks of 32 rows where the longest of the few have more than 16
     const int rt = rows > 16 && rows <= kChunkFewRows ? 2 : 1;
-    const long long per = 16 * rt, most = rows < kChunkFewRows ? rows : kChunkFewRows;
+    const long long per = 16 * rt, most = rows < a.rows_hi ? rows : a.rows_hi;
     const long long whole = args.total_new * G / per + seqs, each = seqs * ((most + per - 1) / per);
-    return launch(a, rt, whole < each ? whole : each, 4 * kWave);
+    return launch(a, rt, (whole < each ? whole : each) * a.Hkv * a.splits, 4 * kWave);
 }
 
 hipError_t launch_chunk_scores(const ChunkArgs& args, bool mod, hipStream_t st)

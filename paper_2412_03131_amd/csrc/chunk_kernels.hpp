@@ -696,12 +696,7 @@ __device__ __forceinline__ void tile_put(TileBuf& b, const uint8_t* slot_, int l
     u4 v;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        u4 m = *reinterpret_cast<const u4*>(slot_ + t * page + O.vm + ((wave >> 1) * T + step_slot<T>(t, 4 * quarter)) * 4);
-        if (left < 32 || bad) {  // nothing behind a section's end reaches the sums
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                m[i] = (T == 16 ? 16 * t : 0) + step_slot<T>(t, 4 * quarter + i) < left && !((bad >> t) & 1) ? m[i] : 0u;
-        }
+        const u4 m = *reinterpret_cast<const u4*>(slot_ + t * page + O.vm + ((wave >> 1) * T + step_slot<T>(t, 4 * quarter)) * 4);
         uint32_t p, q;
         value_pairs<VB>(codes[t], __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x05040100u)),
                         __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x07060302u)),
@@ -709,6 +704,16 @@ __device__ __forceinline__ void tile_put(TileBuf& b, const uint8_t* slot_, int l
                         __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[3], m[1], 0x07060302u)), p, q);
         v[2 * t] = p;
         v[2 * t + 1] = q;
+    }
+    if (left < 32 || bad) {  // nothing behind a section's end reaches the sums
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            auto none = [&](int i) {
+                return (T == 16 ? 16 * t : 0) + step_slot<T>(t, 4 * quarter + i) >= left || ((bad >> t) & 1);
+            };
+            v[2 * t] &= (none(0) ? 0u : 0xffffu) | (none(2) ? 0u : 0xffff0000u);
+            v[2 * t + 1] &= (none(1) ? 0u : 0xffffu) | (none(3) ? 0u : 0xffff0000u);
+        }
     }
     b.v[wave][lane] = __builtin_bit_cast(h8, v);
     if (wave == 0 && lane < 32) {
@@ -1197,183 +1202,258 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
 // ---- scores ---------------------------------------------------------------------------------
 //
 // A wave takes 64 tokens of a table (or of the chunk's own), their keys in registers as matrix
-// operands, and goes over all rows of the sequence: tiles of 16 positions, one query head after
-// another, so that the maximum over the heads is between registers of one lane and one exp2
-// serves all heads of a position.  A tile's queries pass through LDS for the workgroup's four waves.
-// Position i of a tile is its row 4 (i % 4) + i / 4: a chunk of up to four positions needs
-// only the first of a lane's four results.
+// operands, and goes over all rows of the sequence in sets of 16, whose queries pass through LDS for
+// the workgroup's four waves.  A set is either 16 positions of one query head (the maximum over the
+// heads is taken between one set's results and the next's, in a lane) or 4 positions of four heads
+// (between a lane's four results): the second for chunks of up to four tokens and where four divides
+// the heads well.  One exp2 serves all heads of a position.  A chunk of at most kScoreSets sets is
+// staged once and stays for all of a workgroup's tokens; a longer one passes four sets at a time,
+// each made by one wave while the four before are used.
+//
+// Queries stay unscaled here: a token's scales are in registers, in fp32, and take the 2^24 of
+// the codes themselves; the unit of the sums is 2^-5, so that a group's sum of 32 halfs fits one.
 constexpr int kScoreTokens = 64;                             // per wave
 constexpr int kScoreBlock = kScoreTokens * kChunkWaves;      // per workgroup pass
+constexpr int kScoreSets = 8;                                // in LDS
 
-template <int LI, bool MOD>
+struct ScoreSet {
+    h8 q[kNG][kWave];
+    h8 sums[kWave];
+    float lse[16];    // log2 units; +inf: no such row
+    float slope[16];  // log2 units
+};
+
+// One set's operands, by one wave: row m = c is new token j (of n), head hq (of [h0, h0 + G)).
+__device__ __forceinline__ void score_stage(ScoreSet& s, const ChunkArgs& a, long long row0, int j, int n, int hq, bool head, int c,
+                                            int quarter, int lane)
+{
+    const bool there = j < n && head;
+    const long long row = row0 + (there ? j : 0);
+    if (!there) hq = 0;
+    const uint16_t* q = a.q + row * a.q_stride + hq * kD + quarter * 8;
+    u4 sums;
+    const h2 one = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+    for (int g = 0; g < kNG; ++g) {
+        const u4 x = *reinterpret_cast<const u4*>(q + g * kG);
+        float t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, (uint32_t)x[i]), one, t, false);
+        s.q[g][lane] = pair_order(x);
+        t = rows_sum(t) * 0x1p-5f;
+        const _Float16 hi = (_Float16)t;
+        const _Float16 lo = (_Float16)(t - (float)hi);
+        const uint32_t bits = __builtin_bit_cast(unsigned short, quarter == 0 ? hi : lo);
+        sums[g] = quarter < 2 ? bits << 16 : 0u;
+    }
+    s.sums[lane] = __builtin_bit_cast(h8, sums);
+    if (quarter == 0) {
+        s.lse[c] = there ? a.lse_in[row * a.Hq + hq] * kChunkLog2e : INFINITY;
+        s.slope[c] = a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f;
+    }
+}
+
+template <int LI, bool FOUR, bool MOD>
 __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs a)
 {
     constexpr KvFmt hi = kLayoutFmts[LI].hi, lo = kLayoutFmts[LI].lo;
-    __shared__ __align__(16) h8 lds_q[2][kNG][kWave];   // one head's operands: [group][lane]
-    __shared__ __align__(16) h8 lds_sum[2][kWave];
-    __shared__ __align__(16) float lds_unit[2][16], lds_lse[2][16];
+    __shared__ ScoreSet sets[kScoreSets];
     const int lane = lane_id(), wave = wave_index();
     const int c = lane & 15, quarter = lane >> 4;
     const int G = a.Hq / a.Hkv;
-    const int t = (int)blockIdx.x / a.shares, share = (int)blockIdx.x - t * a.shares;
-    const int b = t / a.Hkv, h = t - b * a.Hkv;
-    int n = 0;
-    long long row0 = 0;
-    if (a.max_new == 1 && a.total_new == a.B) {
-        n = 1;
-        row0 = b;
-    } else {
-        for (int b0 = 0; b0 <= b; b0 += kWave) {
-            const int i = b0 + lane;
-            int x = i <= b ? a.new_len[i] : 0;
-            x = x < 0 ? 0 : (x > a.max_new ? a.max_new : x);
-            const int incl = wave_incl_scan(x);
-            const int lb = min(b - b0, kWave - 1);
-            n = __builtin_amdgcn_readlane(x, lb);
-            row0 += __builtin_amdgcn_readlane(incl, lb) - (b0 + kWave > b ? n : 0);
-        }
-        const long long room = a.total_new - row0;
-        if (n > room) n = room > 0 ? (int)room : 0;
-    }
+    // KV heads fastest: with eight of them a table's workgroups share an XCD's L2
+    const int seq_share = (int)blockIdx.x / a.Hkv, h = (int)blockIdx.x - seq_share * a.Hkv;
+    const int b = seq_share / a.shares, share = seq_share - b * a.shares;
+    const int t = b * a.Hkv + h;
+    SeqBlock sb;
+    sb.b = b;
+    sequence_rows(a, sb);
+    const int n = sb.n;
     if (n == 0) return;
     const int first = a.seq_len[b];
     const int len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
     const int b_hi = (len_hi + kScoreBlock - 1) / kScoreBlock, b_lo = (len_lo + kScoreBlock - 1) / kScoreBlock;
     const int blocks = b_hi + b_lo + (n + kScoreBlock - 1) / kScoreBlock;
+    if (share >= blocks) return;
     const int32_t* table = a.page_table + (long long)t * a.p_max;
     const f4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int kPos = FOUR ? 4 : 16;
+    const int HS = FOUR ? (G + 3) >> 2 : G;             // sets of a position tile
+    const int all = (n + kPos - 1) / kPos * HS;
+    auto stage = [&](int i, int into) {
+        const int pt = i / HS, hs = i - pt * HS;
+        const int j = FOUR ? 4 * pt + (c >> 2) : 16 * pt + 4 * (c & 3) + (c >> 2), g = FOUR ? 4 * hs + (c & 3) : hs;
+        score_stage(sets[into], a, sb.row0, j, n, h * G + g, g < G, c, quarter, lane);
+    };
+    const bool once = all <= kScoreSets;
+    if (once) {
+        for (int i = wave; i < all; i += kChunkWaves) stage(i, i);
+        __syncthreads();
+    }
 
     for (int blk = share; blk < blocks; blk += a.shares) {
         const int sec = blk < b_hi ? 0 : (blk < b_hi + b_lo ? 1 : 2);
         const int len = sec == 0 ? len_hi : (sec == 1 ? len_lo : n);
         const int tok0 = (blk - (sec == 0 ? 0 : (sec == 1 ? b_hi : b_hi + b_lo))) * kScoreBlock + wave * kScoreTokens;
-        h8 K[4][kNG];
+        const bool idle = tok0 >= len;
+        h8 K[4][kNG], meta[4];
         float s[4][kNG];
-        h8 meta[4];
         int pos[4];
-        float* where[4];
+        float* where = nullptr;  // the score of token (tile = quarter, c), which this lane finishes
+        int where_pos = 0;
+        float old = 0.0f;
+        const int token = tok0 + lane;
+        if (!idle && sec == 2) {
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-            const int token = tok0 + 16 * kt + c;
-            where[kt] = nullptr;
-            if (sec == 2) {
-                const uint16_t* row = a.k + (row0 + min(token, n - 1)) * a.k_stride + h * kD + quarter * 8;
+            for (int kt = 0; kt < 4; ++kt) {
+                const uint16_t* row = a.k + (sb.row0 + min(tok0 + 16 * kt + c, n - 1)) * a.k_stride + h * kD + quarter * 8;
 #pragma unroll
                 for (int g = 0; g < kNG; ++g) {
                     K[kt][g] = pair_order(*reinterpret_cast<const u4*>(row + g * kG));
-                    s[kt][g] = 0x1p-9f;
+                    s[kt][g] = 0x1p-5f;
                 }
                 meta[kt] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
-                pos[kt] = first + token;
-                if (token < n && quarter == 0) where[kt] = a.score + (row0 + token) * a.Hkv + h;
-                continue;
+                pos[kt] = first + tok0 + 16 * kt + c;
             }
+            if (token < n) where = a.score + (sb.row0 + token) * a.Hkv + h;
+            where_pos = first + token;
+        } else if (!idle) {
             auto take = [&](auto kb, auto vb, auto tt) {
                 constexpr int KB = decltype(kb)::value, VB = decltype(vb)::value, T = decltype(tt)::value;
                 constexpr SecOffsets O = sec_offsets(KvFmt{KB, VB, T});
-                const int tk = min(token, len - 1), page = tk / T, slot = tk - page * T;
-                const int id = table[sec == 0 ? page : a.p_max - 1 - page];
-                const bool ok = (unsigned long long)(unsigned)id < (unsigned long long)a.num_pages;
-                uint8_t* pg = a.pool_rw + (long long)(ok ? id : 0) * a.page_bytes;
+                constexpr int kPer = T / 16;  // tiles of a page
+                int id[4 / kPer];
 #pragma unroll
-                for (int g = 0; g < kNG; ++g) {
-                    if constexpr (KB == 8) {
-                        const u2 v = *reinterpret_cast<const u2*>(pg + O.kc + ((2 * g + (quarter >> 1)) * T + slot) * 16 + (quarter & 1) * 8);
-                        K[kt][g] = key_codes8(v[0], v[1]);
-                    } else {
-                        K[kt][g] = key_codes4(*reinterpret_cast<const uint32_t*>(pg + O.kc + (g * T + slot) * 16 + quarter * 4));
-                    }
+                for (int i = 0; i < 4 / kPer; ++i) {
+                    const int page = min(tok0 / T + i, (len - 1) / T);
+                    id[i] = __builtin_amdgcn_readfirstlane(table[sec == 0 ? page : a.p_max - 1 - page]);
                 }
-                meta[kt] = *reinterpret_cast<const h8*>(pg + O.km + slot * 16);
+                int mine = id[0];
 #pragma unroll
-                for (int g = 0; g < kNG; ++g) s[kt][g] = 32768.0f * (float)meta[kt][2 * g];
-                pos[kt] = *reinterpret_cast<const int32_t*>(pg + O.pos + slot * 4);
-                if (token < len && quarter == 0 && ok) where[kt] = reinterpret_cast<float*>(pg + O.sc + slot * 4);
+                for (int i = 1; i < 4 / kPer; ++i) mine = quarter / kPer == i ? id[i] : mine;
+                {
+                    // (an ID outside the pool reads page 0; its tokens' scores are not written)
+                    const bool ok = (unsigned long long)(unsigned)mine < (unsigned long long)a.num_pages;
+                    uint8_t* pg = a.pool_rw + (long long)(ok ? mine : 0) * a.page_bytes;
+                    const int slot = 16 * (quarter % kPer) + c;
+                    where_pos = *reinterpret_cast<const int32_t*>(pg + O.pos + slot * 4);
+                    old = *reinterpret_cast<const float*>(pg + O.sc + slot * 4);
+                    if (token < len && ok) where = reinterpret_cast<float*>(pg + O.sc + slot * 4);
+                }
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt) {
+                    const int i = id[kt / kPer];
+                    const bool ok = (unsigned long long)(unsigned)i < (unsigned long long)a.num_pages;
+                    const __amdgpu_buffer_rsrc_t r = span(a.pool + (long long)(ok ? i : 0) * a.page_bytes, O.used);
+                    const int slot = 16 * (kt % kPer) + c;
+#pragma unroll
+                    for (int g = 0; g < kNG; ++g) {
+                        if constexpr (KB == 8) {
+                            const u2 v = fetch<8>(r, ((quarter >> 1) * T + slot) * 16 + (quarter & 1) * 8, O.kc + 2 * g * T * 16);
+                            K[kt][g] = key_codes8(v[0], v[1]);
+                        } else {
+                            K[kt][g] = key_codes4(fetch<4>(r, slot * 16 + quarter * 4, O.kc + g * T * 16));
+                        }
+                    }
+                    meta[kt] = __builtin_bit_cast(h8, fetch<16>(r, slot * 16, O.km));
+                    if constexpr (MOD) pos[kt] = (int)fetch<4>(r, slot * 4, O.pos);
+                }
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int g = 0; g < kNG; ++g) s[kt][g] = 0x1p19f * (float)meta[kt][2 * g];
             };
             using std::integral_constant;
             if (sec == 0) take(integral_constant<int, hi.kb>{}, integral_constant<int, hi.vb>{}, integral_constant<int, hi.T>{});
             else take(integral_constant<int, lo.kb>{}, integral_constant<int, lo.vb>{}, integral_constant<int, lo.T>{});
         }
         float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        // the chunk's own tokens are seen from their own positions on
-        const int p_begin = sec == 2 ? (tok0 - wave * kScoreTokens) / 16 : 0;
-        const int p_tiles = (n + 15) / 16;
-        for (int pt = p_begin; pt < p_tiles; ++pt) {
-            float top[4][4];
+        constexpr int kTops = FOUR ? 1 : 4;
+        float top[4][kTops];
+        // set i (in LDS at `from`): its position tile, and whether it is its tile's last
+        auto use = [&](int i, const ScoreSet& S) {
+            const int pt = i / HS, hs = i - pt * HS;
+            if (hs == 0) {
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
+                for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) top[kt][r] = -INFINITY;
-            for (int g0 = 0; g0 < G; ++g0) {
-                const int buf = g0 & 1;
-                const int hq = h * G + g0;
-                __syncthreads();
-                if (wave == 0) {
-                    // row m = c of the tile is position 16 pt + 4 (c % 4) + c / 4
-                    const int j = 16 * pt + 4 * (c & 3) + (c >> 2);
-                    const uint16_t* q = a.q + (row0 + min(j, n - 1)) * a.q_stride + hq * kD + quarter * 8;
-                    u4 x[kNG];
+                    for (int r = 0; r < kTops; ++r) top[kt][r] = -INFINITY;
+            }
+            const f4 lse = *reinterpret_cast<const f4*>(&S.lse[4 * quarter]);
+            f4 slope = zero;
+            if constexpr (MOD) slope = *reinterpret_cast<const f4*>(&S.slope[4 * quarter]);
+            h8 q[kNG];
 #pragma unroll
-                    for (int g = 0; g < kNG; ++g) x[g] = *reinterpret_cast<const u4*>(q + g * kG);
-                    const RowOperands o = row_operands(x, quarter);
+            for (int g = 0; g < kNG; ++g) q[g] = S.q[g][lane];
+            const h8 qs = S.sums[lane];
+            const float unit = a.scale * 32.0f;
+            const int j = FOUR ? 4 * pt + quarter : 16 * pt + quarter;  // + 4 r
+            f4 sum[4];
 #pragma unroll
-                    for (int g = 0; g < kNG; ++g) lds_q[buf][g][lane] = o.q[g];
-                    lds_sum[buf][lane] = o.sums;
-                    if (quarter == 0) {
-                        lds_unit[buf][c] = o.unit * a.scale;
-                        lds_lse[buf][c] = j < n ? a.lse_in[(row0 + j) * a.Hq + hq] * kChunkLog2e : INFINITY;
-                    }
-                }
-                __syncthreads();
-                const f4 unit = *reinterpret_cast<const f4*>(&lds_unit[buf][4 * quarter]);
-                const f4 lse = *reinterpret_cast<const f4*>(&lds_lse[buf][4 * quarter]);
-                const ScoreForm form{a.cap_in, a.cap_out, MOD && a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f};
-                h8 q[kNG];
+            for (int kt = 0; kt < 4; ++kt) sum[kt] = mfma_k32(qs, meta[kt], zero);
 #pragma unroll
-                for (int g = 0; g < kNG; ++g) q[g] = lds_q[buf][g][lane];
-                const h8 qs = lds_sum[buf][lane];
+            for (int g = 0; g < kNG; ++g) {
+                f4 part[4];
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt) {
-                    f4 sum = mfma_k32(qs, meta[kt], zero);
+                for (int kt = 0; kt < 4; ++kt) part[kt] = mfma_k32(q[g], K[kt][g], zero);
 #pragma unroll
-                    for (int g = 0; g < kNG; ++g) {
-                        const f4 part = mfma_k32(q[g], K[kt][g], zero);
+                for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) sum[r] = __builtin_fmaf(s[kt][g], part[r], sum[r]);
-                    }
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float x;
-                        if constexpr (MOD) {
-                            const int away = first + 16 * pt + 4 * r + quarter - pos[kt];
-                            x = formed(sum[r] * unit[r], form, (float)away) - lse[r];
-                            x = away < a.window ? x : -INFINITY;
-                        } else {
-                            x = __builtin_fmaf(sum[r], unit[r], -lse[r]);
-                        }
-                        top[kt][r] = fmaxf(top[kt][r], x);
-                    }
-                }
+                    for (int r = 0; r < 4; ++r) sum[kt][r] = __builtin_fmaf(s[kt][g], part[kt][r], sum[kt][r]);
             }
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
+            for (int kt = 0; kt < 4; ++kt) {
+                float x[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int away = first + 16 * pt + 4 * r + quarter - pos[kt];
-                    total[kt] += away >= 0 || sec != 2 ? __builtin_amdgcn_exp2f(top[kt][r]) : 0.0f;
+                    if constexpr (MOD) {
+                        const int away = first + j + (FOUR ? 0 : 4 * r) - pos[kt];
+                        const float y = formed(sum[kt][r] * unit, ScoreForm{a.cap_in, a.cap_out, slope[r]}, (float)away) - lse[r];
+                        x[r] = away < a.window ? y : -INFINITY;
+                    } else {
+                        x[r] = __builtin_fmaf(sum[kt][r], unit, -lse[r]);
+                    }
                 }
-        }
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-            const float x = rows_sum(total[kt]);
-            if (where[kt]) {
-                if (sec == 2) {
-                    *where[kt] = x / (float)(first + n - pos[kt]);
+                if constexpr (FOUR) {
+                    top[kt][0] = max3(max3(top[kt][0], x[0], x[1]), x[2], x[3]);
                 } else {
-                    const float old = *where[kt];
-                    const int received = max(first + n - pos[kt], 1);
-                    *where[kt] = old + (x - (float)n * old) / (float)received;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) top[kt][r] = fmaxf(top[kt][r], x[r]);
                 }
+            }
+            if (hs == HS - 1) {
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int r = 0; r < kTops; ++r) {
+                        const float p = __builtin_amdgcn_exp2f(top[kt][r]);
+                        // the chunk's own tokens are seen from their own positions on
+                        total[kt] += sec != 2 || j + 4 * r >= tok0 + 16 * kt + c ? p : 0.0f;
+                    }
+            }
+        };
+        if (once) {
+            if (!idle)
+                for (int i = 0; i < all; ++i) use(i, sets[i]);
+        } else {
+            // (own tokens: from the first tile that sees one of the workgroup's)
+            const int begin = sec == 2 ? (tok0 - wave * kScoreTokens) / kPos * HS : 0;
+            __syncthreads();
+            if (begin + wave < all) stage(begin + wave, wave);
+            __syncthreads();
+            int half = 0;
+            for (int i0 = begin; i0 < all; i0 += kChunkWaves, half ^= 1) {
+                if (i0 + kChunkWaves + wave < all) stage(i0 + kChunkWaves + wave, (half ^ 1) * kChunkWaves + wave);
+                if (!idle)
+                    for (int i = i0; i < min(i0 + kChunkWaves, all); ++i) use(i, sets[half * kChunkWaves + i - i0]);
+                __syncthreads();
+            }
+        }
+        if (!idle) {
+            const float x = xsum4(total[0], total[1], total[2], total[3]);  // quarter r: tile r's
+            if (where) {
+                const int received = max(first + n - where_pos, 1);
+                *where = sec == 2 ? x / (float)received : old + (x - (float)n * old) / (float)received;
             }
         }
     }
@@ -1381,13 +1461,14 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs
 
 }  // namespace dkv
 
-// Kernel entry points of layout n: which = 0 scores, 1 / 2 attention of few rows with that many row
-// tiles, 3 of many.
+// Kernel entry points of layout n: which = 0 scores (sets of 16 positions), 4 (of 4 positions and
+// heads), 1 / 2 attention of few rows with that many row tiles, 3 of many.
 #define DKV_CHUNK_KERNELS(LI)                                                                                  \
     const void* chunk_kernel_l##LI(int which, bool mod)                                                        \
     {                                                                                                          \
         switch (which) {                                                                                       \
-        case 0: return mod ? (const void*)chunk_scores<LI, true> : (const void*)chunk_scores<LI, false>;       \
+        case 0: return mod ? (const void*)chunk_scores<LI, false, true> : (const void*)chunk_scores<LI, false, false>; \
+        case 4: return mod ? (const void*)chunk_scores<LI, true, true> : (const void*)chunk_scores<LI, true, false>; \
         case 1: return mod ? (const void*)chunk_rows<LI, 1, true> : (const void*)chunk_rows<LI, 1, false>;     \
         case 2: return mod ? (const void*)chunk_rows<LI, 2, true> : (const void*)chunk_rows<LI, 2, false>;     \
         case 3: return mod ? (const void*)chunk_tiles<LI, true> : (const void*)chunk_tiles<LI, false>;         \

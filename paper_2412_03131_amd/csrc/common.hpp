@@ -282,6 +282,19 @@ __device__ __forceinline__ void arrive_claim_once(unsigned long long* w, unsigne
                                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// ---- sums over the four 16-lane rows of a wave ------------------------------
+// Sum over the four rows with a transpose: row r of the result holds the sum of
+// argument r (heads a, b, c, d -> rows 0, 1, 2, 3).
+__device__ __forceinline__ float xsum4(float a, float b, float c, float d)
+{
+    auto ab = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    auto cd = __builtin_amdgcn_permlane16_swap(__float_as_uint(c), __float_as_uint(d), false, false);
+    const float u = __uint_as_float(ab[0]) + __uint_as_float(ab[1]);
+    const float w = __uint_as_float(cd[0]) + __uint_as_float(cd[1]);
+    auto uw = __builtin_amdgcn_permlane32_swap(__float_as_uint(u), __float_as_uint(w), false, false);
+    return __uint_as_float(uw[0]) + __uint_as_float(uw[1]);
+}
+
 // ---- fp16 helpers ----------------------------------------------------------
 __device__ __forceinline__ float h2f(uint32_t bits16)
 {

@@ -72,11 +72,13 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
 hipError_t launch_chunk_scores(const ChunkArgs& args, bool mod, hipStream_t st)
 {
     ChunkArgs a = args;
-    const void* kern = chunk_kernel(a.layout, 0, mod);
+    const int G = a.Hq / a.Hkv;
+    // four heads a set where they are used (3, 4, 7 and 8 query heads) or the chunk is short
+    const void* kern = chunk_kernel(a.layout, a.max_new <= 4 || (G + 3) / 4 * 4 <= G + 1 ? 4 : 0, mod);
     if (!kern) return hipErrorInvalidValue;
     const long long T = (long long)a.B * a.Hkv;
     const long long most = (long long)a.p_max * 16 / 256 + 3 + (a.max_new + 255) / 256;
-    long long shares = (4096 + T - 1) / T;
+    long long shares = a.max_new <= 16 ? (2048 + T - 1) / T : most;
     if (shares > most) shares = most;
     a.shares = (int)shares;
     const long long grid = T * shares;

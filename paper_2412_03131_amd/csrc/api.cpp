@@ -356,7 +356,7 @@ diffkv_status diffkv_workspace_size(int32_t op, const diffkv_layout* layout, int
         if (num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || total_new < 0) return DIFFKV_E_INVAL;
         *bytes = op == DIFFKV_OP_CHUNK_ATTENTION
                      ? (size_t)chunk_plan(num_seqs, num_q_heads, num_kv_heads, total_new, layout->p_max).bytes
-                     : 0;
+                     : (size_t)kScoreBytes;
         return DIFFKV_OK;
     default:
         return DIFFKV_E_INVAL;
@@ -619,6 +619,9 @@ diffkv_status diffkv_chunk_significance(const diffkv_layout* layout, const diffk
                                        sm_scale, form, a, mod);
     if (s != DIFFKV_OK || a.total_new == 0) return s;
     if (!lse || !score) return DIFFKV_E_INVAL;
+    if (!ws || (int64_t)ws_bytes < kScoreBytes) return DIFFKV_E_WORKSPACE;
+    a.arrive = static_cast<unsigned long long*>(ws);
+    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kScoreShares * 8);
     a.lse_in = lse;
     a.score = score;
     hipError_t e = launch_chunk_scores(a, mod, static_cast<hipStream_t>(stream));

@@ -17,9 +17,6 @@
 // group sums as fp16 high and low parts (2^-22 relative).  So a logit's error is fp32's;
 // keys rounded to fp16 would move logits by 4e-4 (keys N(0, 1), four channels
 // times 10), and the normalizers with them.
-//
-// An operand register holds dims (d, d + 4) of an 8-dim block, the pairs that one
-// v_perm (8-bit codes) or one mask (4-bit codes) makes.
 #pragma once
 
 #include <utility>
@@ -181,48 +178,41 @@ __device__ __forceinline__ bool split_last(unsigned long long* word, int splits,
 }
 
 // ---- operands ---------------------------------------------------------------------
-// max over the four 16-lane rows, in every row
+// max and sum over the four 16-lane rows, in every row
 __device__ __forceinline__ float rows_max(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
 }
 __device__ __forceinline__ float rows_sum(float v)
 {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(x[0]) + __uint_as_float(x[1]);
 }
-
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
-// eight consecutive halfs -> the operand's pairs (0, 4), (1, 5), (2, 6), (3, 7)
-__device__ __forceinline__ h8 pair_order(u4 x)
-{
-    u4 r;
-    r[0] = __builtin_amdgcn_perm(x[2], x[0], 0x05040100u);
-    r[1] = __builtin_amdgcn_perm(x[2], x[0], 0x07060302u);
-    r[2] = __builtin_amdgcn_perm(x[3], x[1], 0x05040100u);
-    r[3] = __builtin_amdgcn_perm(x[3], x[1], 0x07060302u);
-    return __builtin_bit_cast(h8, r);
-}
-
-// eight key codes (8 bits: two dwords; 4 bits: one) -> fp16 denormals in pair order
+// eight key codes (8 bits: two dwords; 4 bits: one) -> fp16 denormals in order
 __device__ __forceinline__ h8 key_codes8(uint32_t lo, uint32_t hi)
 {
     u4 r;
-    r[0] = __builtin_amdgcn_perm(hi, lo, 0x0C040C00u);
-    r[1] = __builtin_amdgcn_perm(hi, lo, 0x0C050C01u);
-    r[2] = __builtin_amdgcn_perm(hi, lo, 0x0C060C02u);
-    r[3] = __builtin_amdgcn_perm(hi, lo, 0x0C070C03u);
+    r[0] = __builtin_amdgcn_perm(0u, lo, 0x0C010C00u);
+    r[1] = __builtin_amdgcn_perm(0u, lo, 0x0C030C02u);
+    r[2] = __builtin_amdgcn_perm(0u, hi, 0x0C010C00u);
+    r[3] = __builtin_amdgcn_perm(0u, hi, 0x0C030C02u);
     return __builtin_bit_cast(h8, r);
 }
 __device__ __forceinline__ h8 key_codes4(uint32_t w)
 {
+    const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
     u4 r;
-    r[0] = w & 0x000F000Fu;
-    r[1] = (w >> 4) & 0x000F000Fu;
-    r[2] = (w >> 8) & 0x000F000Fu;
-    r[3] = (w >> 12) & 0x000F000Fu;
+    r[0] = __builtin_amdgcn_perm(odd, even, 0x0C040C00u);
+    r[1] = __builtin_amdgcn_perm(odd, even, 0x0C050C01u);
+    r[2] = __builtin_amdgcn_perm(odd, even, 0x0C060C02u);
+    r[3] = __builtin_amdgcn_perm(odd, even, 0x0C070C03u);
     return __builtin_bit_cast(h8, r);
 }
 
@@ -268,7 +258,7 @@ __device__ __forceinline__ RowOperands row_operands(const u4 (&x)[kNG], int quar
             s += (float)v.x + (float)v.y;
             y[i] = __builtin_bit_cast(uint32_t, v);
         }
-        o.q[g] = pair_order(y);
+        o.q[g] = __builtin_bit_cast(h8, y);
         s = rows_sum(s) * 0x1p-9f;
         const _Float16 hi = (_Float16)s;
         const _Float16 lo = (_Float16)(s - (float)hi);

@@ -397,7 +397,7 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const RowsLds<RT>& Q, cons
         for (int rt = 0; rt < RT; ++rt) sum[rt] = zero;
 #pragma unroll
         for (int g = 0; g < kNG; ++g) {
-            const h8 kk = pair_order(raw[g]);
+            const h8 kk = __builtin_bit_cast(h8, raw[g]);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) sum[rt] = mfma_k32(kk, Q.q[rt][g][16 * quarter + c], sum[rt]);
         }
@@ -734,7 +734,7 @@ __device__ __forceinline__ void tile_put_own(TileBuf& b, const uint8_t* slot, in
 {
     const int c = lane & 15, quarter = lane >> 4;
     b.k[wave >> 2][wave & 3][lane] =
-        pair_order(*reinterpret_cast<const u4*>(slot + step_slot<32>(wave >> 2, c) * 256 + (wave & 3) * 64 + quarter * 16));
+        *reinterpret_cast<const h8*>(slot + step_slot<32>(wave >> 2, c) * 256 + (wave & 3) * 64 + quarter * 16);
     const uint16_t* values = reinterpret_cast<const uint16_t*>(slot + kOwnSlot / 2) + 16 * wave + c;
     uint32_t w[8];
     bool odd = false;
@@ -1201,20 +1201,21 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
 
 // ---- scores ---------------------------------------------------------------------------------
 //
-// A wave takes 64 tokens of a table (or of the chunk's own), their keys in registers as matrix
+// A wave takes 32 tokens of a table (or of the chunk's own), their keys in registers as matrix
 // operands, and goes over all rows of the sequence in sets of 16, whose queries pass through LDS for
-// the workgroup's four waves.  A set is either 16 positions of one query head (the maximum over the
+// the workgroup's eight waves.  A set is either 16 positions of one query head (the maximum over the
 // heads is taken between one set's results and the next's, in a lane) or 4 positions of four heads
 // (between a lane's four results): the second for chunks of up to four tokens and where four divides
 // the heads well.  One exp2 serves all heads of a position.  A chunk of at most kScoreSets sets is
-// staged once and stays for all of a workgroup's tokens; a longer one passes four sets at a time,
-// each made by one wave while the four before are used.
+// staged once and stays for all of a workgroup's tokens; a longer one passes four sets at a time.
 //
 // Queries stay unscaled here: a token's scales are in registers, in fp32, and take the 2^24 of
 // the codes themselves; the unit of the sums is 2^-5, so that a group's sum of 32 halfs fits one.
-constexpr int kScoreTokens = 64;                             // per wave
-constexpr int kScoreBlock = kScoreTokens * kChunkWaves;      // per workgroup pass
-constexpr int kScoreSets = 8;                                // in LDS
+constexpr int kScoreWaves = 8, kScoreTiles = 2;
+constexpr int kScoreTokens = 16 * kScoreTiles;               // per wave
+constexpr int kScoreBlock = kScoreTokens * kScoreWaves;      // per workgroup pass
+constexpr int kScorePass = 4;                                // sets per pass of a long chunk
+constexpr int kScoreSets = 3 * kScorePass;                   // in LDS
 
 struct ScoreSet {
     h8 q[kNG][kWave];
@@ -1223,23 +1224,30 @@ struct ScoreSet {
     float slope[16];  // log2 units
 };
 
-// One set's operands, by one wave: row m = c is new token j (of n), head hq (of [h0, h0 + G)).
-__device__ __forceinline__ void score_stage(ScoreSet& s, const ChunkArgs& a, long long row0, int j, int n, int hq, bool head, int c,
-                                            int quarter, int lane)
+// One set on its way, by one wave: row m = c is at `offset` bytes from `base`; its queries go straight to
+// where the products read them (a load with an LDS destination puts lane l's 16 bytes at l).
+__device__ __forceinline__ void score_load(ScoreSet& s, const void* base, int offset, int quarter)
 {
-    const bool there = j < n && head;
-    const long long row = row0 + (there ? j : 0);
-    if (!there) hq = 0;
-    const uint16_t* q = a.q + row * a.q_stride + hq * kD + quarter * 8;
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) void*)&s.q[0][0]);
+    const unsigned long long p = (unsigned long long)base;
+    const u4 rs = {(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
+#pragma unroll
+    for (int g = 0; g < kNG; ++g)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at + g * 1024),
+                     "v"(offset + quarter * 16), "s"(rs), "s"(g * 2 * kG)
+                     : "memory");
+}
+// ... and arrived: the group sums beside them, by the same wave.
+__device__ __forceinline__ void score_sums(ScoreSet& s, float lse, float slope, int c, int quarter, int lane)
+{
     u4 sums;
     const h2 one = {(_Float16)1.0f, (_Float16)1.0f};
 #pragma unroll
     for (int g = 0; g < kNG; ++g) {
-        const u4 x = *reinterpret_cast<const u4*>(q + g * kG);
+        const u4 x = __builtin_bit_cast(u4, s.q[g][lane]);
         float t = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) t = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, (uint32_t)x[i]), one, t, false);
-        s.q[g][lane] = pair_order(x);
         t = rows_sum(t) * 0x1p-5f;
         const _Float16 hi = (_Float16)t;
         const _Float16 lo = (_Float16)(t - (float)hi);
@@ -1248,89 +1256,163 @@ __device__ __forceinline__ void score_stage(ScoreSet& s, const ChunkArgs& a, lon
     }
     s.sums[lane] = __builtin_bit_cast(h8, sums);
     if (quarter == 0) {
-        s.lse[c] = there ? a.lse_in[row * a.Hq + hq] * kChunkLog2e : INFINITY;
-        s.slope[c] = a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f;
+        s.lse[c] = lse;
+        s.slope[c] = slope;
     }
 }
 
 template <int LI, bool FOUR, bool MOD>
-__global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs a)
+__global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs a)
 {
     constexpr KvFmt hi = kLayoutFmts[LI].hi, lo = kLayoutFmts[LI].lo;
     __shared__ ScoreSet sets[kScoreSets];
+    __shared__ long long scan[kScoreWaves], found_at;
+    __shared__ int found, last;
     const int lane = lane_id(), wave = wave_index();
     const int c = lane & 15, quarter = lane >> 4;
     const int G = a.Hq / a.Hkv;
-    // KV heads fastest: with eight of them a table's workgroups share an XCD's L2
-    const int seq_share = (int)blockIdx.x / a.Hkv, h = (int)blockIdx.x - seq_share * a.Hkv;
-    const int b = seq_share / a.shares, share = seq_share - b * a.shares;
-    const int t = b * a.Hkv + h;
-    SeqBlock sb;
-    sb.b = b;
-    sequence_rows(a, sb);
-    const int n = sb.n;
-    if (n == 0) return;
-    const int first = a.seq_len[b];
-    const int len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
-    const int b_hi = (len_hi + kScoreBlock - 1) / kScoreBlock, b_lo = (len_lo + kScoreBlock - 1) / kScoreBlock;
-    const int blocks = b_hi + b_lo + (n + kScoreBlock - 1) / kScoreBlock;
-    if (share >= blocks) return;
-    const int32_t* table = a.page_table + (long long)t * a.p_max;
-    const f4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
     constexpr int kPos = FOUR ? 4 : 16;
     const int HS = FOUR ? (G + 3) >> 2 : G;             // sets of a position tile
-    const int all = (n + kPos - 1) / kPos * HS;
-    auto stage = [&](int i, int into) {
-        const int pt = i / HS, hs = i - pt * HS;
-        const int j = FOUR ? 4 * pt + (c >> 2) : 16 * pt + 4 * (c & 3) + (c >> 2), g = FOUR ? 4 * hs + (c & 3) : hs;
-        score_stage(sets[into], a, sb.row0, j, n, h * G + g, g < G, c, quarter, lane);
+
+    // The work of all tables end to end, cut into equal shares.  A block of 256 tokens costs its sets and
+    // as much as kBlockUnits more for its keys; the own tokens' block i begins at its first position's set.
+    constexpr int kBlockUnits = 8;
+    const int own_step = kScoreBlock / kPos * HS;
+    struct Table {
+        int n, all, b_hi, b_lo, own;  // new tokens, sets, blocks
     };
-    const bool once = all <= kScoreSets;
+    auto table_of = [&](int t) {
+        int n = a.new_len[t / a.Hkv];
+        n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
+        Table x{n, (n + kPos - 1) / kPos * HS, 0, 0, 0};
+        if (n > 0) {
+            x.b_hi = (a.len[2 * t] + kScoreBlock - 1) / kScoreBlock;
+            x.b_lo = (a.len[2 * t + 1] + kScoreBlock - 1) / kScoreBlock;
+            x.own = (n + kScoreBlock - 1) / kScoreBlock;
+        }
+        return x;
+    };
+    auto units_to = [&](const Table& x, int blocks) -> long long {
+        const long long cached = min(blocks, x.b_hi + x.b_lo), own = blocks - cached;
+        return (cached + own) * (x.all + kBlockUnits) - own * (own - 1) / 2 * own_step;
+    };
+    const int tables = a.B * a.Hkv, chunk = (tables + kScoreWaves * kWave - 1) / (kScoreWaves * kWave);
+    const int t0 = min((int)threadIdx.x * chunk, tables), t1 = min(t0 + chunk, tables);
+    long long mine = 0;
+    for (int t = t0; t < t1; ++t) {
+        const Table x = table_of(t);
+        mine += units_to(x, x.b_hi + x.b_lo + x.own);
+    }
+    long long total_units;
+    const long long mine_from = block_excl_scan_wide(mine, scan, &total_units);
+    const long long quantum = max((total_units + gridDim.x - 1) / gridDim.x, 2ll * kBlockUnits);
+    // consecutive shares on one XCD: they read the same tables
+    const int share = gridDim.x % 8 == 0 ? ((int)blockIdx.x & 7) * ((int)gridDim.x >> 3) + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
+    const long long start = share * quantum, stop = min(total_units, start + quantum);
+    const f4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    int piece = 0;
+    for (long long cur = start; cur < stop;) {
+    // the table that has unit `cur`
+    __syncthreads();
+    if (cur >= mine_from && cur < mine_from + mine) {
+        long long at = mine_from;
+        for (int t = t0; t < t1; ++t) {
+            const Table x = table_of(t);
+            const long long next = at + units_to(x, x.b_hi + x.b_lo + x.own);
+            if (cur < next) {
+                found = t;
+                found_at = at;
+                break;
+            }
+            at = next;
+        }
+    }
+    __syncthreads();
+    const int t = __builtin_amdgcn_readfirstlane(found);
+    const long long table_at = read_lane<long long>(found_at, 0);
+    const Table tb = table_of(t);
+    const int blocks = tb.b_hi + tb.b_lo + tb.own;
+    int blk = 0;
+    for (int above = blocks - 1; blk < above;) {  // the last block that starts at or before cur
+        const int mid = (blk + above + 1) >> 1;
+        if (table_at + units_to(tb, mid) <= cur) blk = mid;
+        else above = mid - 1;
+    }
+    const bool once = tb.all <= kScoreSets;
+    SeqBlock sb;
+    sb.b = t / a.Hkv;
+    sequence_rows(a, sb);
+    const int n = sb.n, h = t - sb.b * a.Hkv;
+    const int first = a.seq_len[sb.b];
+    const int len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
+    const int b_hi = tb.b_hi, b_lo = tb.b_lo;
+    const int all = (n + kPos - 1) / kPos * HS;
+    const int32_t* table = a.page_table + (long long)t * a.p_max;
+    // set i on its way into LDS; its rows' normalizers and slopes (row c's)
+    float row_lse = 0.0f, row_slope = 0.0f;
+    auto load_set = [&](int i, ScoreSet& S) {
+        const int ln = fresh(lane), c = ln & 15;
+        const int pt = i / HS, hs = i - pt * HS, j0 = kPos * pt;
+        const int j = j0 + (FOUR ? c >> 2 : 4 * (c & 3) + (c >> 2)), g = FOUR ? 4 * hs + (c & 3) : hs;
+        const bool there = j < n && g < G;
+        const int jj = there ? j : j0, hq = h * G + (there ? g : 0);
+        score_load(S, a.q + (sb.row0 + j0) * a.q_stride, 2 * ((jj - j0) * (int)a.q_stride + hq * kD), ln >> 4);
+        row_lse = there ? a.lse_in[(sb.row0 + jj) * a.Hq + hq] * kChunkLog2e : INFINITY;
+        if constexpr (MOD) row_slope = a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f;
+    };
     if (once) {
-        for (int i = wave; i < all; i += kChunkWaves) stage(i, i);
+        for (int i = wave; i < all; i += kScoreWaves) {
+            load_set(i, sets[i]);
+            staged_ready();
+            score_sums(sets[i], row_lse, row_slope, c, quarter, lane);
+        }
         __syncthreads();
     }
-
-    for (int blk = share; blk < blocks; blk += a.shares) {
+    for (; blk < blocks && cur < stop; ++blk, ++piece) {
+        const long long from = table_at + units_to(tb, blk), to = table_at + units_to(tb, blk + 1);
+        const long long piece_from = cur, piece_end = min(stop, to);
+        cur = piece_end;
+        if (n == 0 || (once && piece_from != from)) continue;  // (a block of these is its first unit's share's)
         const int sec = blk < b_hi ? 0 : (blk < b_hi + b_lo ? 1 : 2);
         const int len = sec == 0 ? len_hi : (sec == 1 ? len_lo : n);
         const int tok0 = (blk - (sec == 0 ? 0 : (sec == 1 ? b_hi : b_hi + b_lo))) * kScoreBlock + wave * kScoreTokens;
         const bool idle = tok0 >= len;
-        h8 K[4][kNG], meta[4];
-        float s[4][kNG];
-        int pos[4];
-        float* where = nullptr;  // the score of token (tile = quarter, c), which this lane finishes
+        h8 K[kScoreTiles][kNG], meta[kScoreTiles];
+        float s[kScoreTiles][kNG];
+        int pos[kScoreTiles];
+        float* where = nullptr;  // the score of token (tile = quarter, c), which lanes of quarters 0 and 1 finish
         int where_pos = 0;
         float old = 0.0f;
         const int token = tok0 + lane;
         if (!idle && sec == 2) {
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
+            for (int kt = 0; kt < kScoreTiles; ++kt) {
                 const uint16_t* row = a.k + (sb.row0 + min(tok0 + 16 * kt + c, n - 1)) * a.k_stride + h * kD + quarter * 8;
 #pragma unroll
                 for (int g = 0; g < kNG; ++g) {
-                    K[kt][g] = pair_order(*reinterpret_cast<const u4*>(row + g * kG));
+                    K[kt][g] = *reinterpret_cast<const h8*>(row + g * kG);
                     s[kt][g] = 0x1p-5f;
                 }
                 meta[kt] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
                 pos[kt] = first + tok0 + 16 * kt + c;
             }
-            if (token < n) where = a.score + (sb.row0 + token) * a.Hkv + h;
+            if (token < n && quarter < kScoreTiles) where = a.score + (sb.row0 + token) * a.Hkv + h;
             where_pos = first + token;
         } else if (!idle) {
             auto take = [&](auto kb, auto vb, auto tt) {
                 constexpr int KB = decltype(kb)::value, VB = decltype(vb)::value, T = decltype(tt)::value;
                 constexpr SecOffsets O = sec_offsets(KvFmt{KB, VB, T});
                 constexpr int kPer = T / 16;  // tiles of a page
-                int id[4 / kPer];
+                constexpr int kIds = kScoreTiles / kPer;
+                int id[kIds];
 #pragma unroll
-                for (int i = 0; i < 4 / kPer; ++i) {
+                for (int i = 0; i < kIds; ++i) {
                     const int page = min(tok0 / T + i, (len - 1) / T);
                     id[i] = __builtin_amdgcn_readfirstlane(table[sec == 0 ? page : a.p_max - 1 - page]);
                 }
                 int mine = id[0];
 #pragma unroll
-                for (int i = 1; i < 4 / kPer; ++i) mine = quarter / kPer == i ? id[i] : mine;
+                for (int i = 1; i < kIds; ++i) mine = quarter / kPer == i ? id[i] : mine;
                 {
                     // (an ID outside the pool reads page 0; its tokens' scores are not written)
                     const bool ok = (unsigned long long)(unsigned)mine < (unsigned long long)a.num_pages;
@@ -1338,10 +1420,10 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs
                     const int slot = 16 * (quarter % kPer) + c;
                     where_pos = *reinterpret_cast<const int32_t*>(pg + O.pos + slot * 4);
                     old = *reinterpret_cast<const float*>(pg + O.sc + slot * 4);
-                    if (token < len && ok) where = reinterpret_cast<float*>(pg + O.sc + slot * 4);
+                    if (token < len && ok && quarter < kScoreTiles) where = reinterpret_cast<float*>(pg + O.sc + slot * 4);
                 }
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt) {
+                for (int kt = 0; kt < kScoreTiles; ++kt) {
                     const int i = id[kt / kPer];
                     const bool ok = (unsigned long long)(unsigned)i < (unsigned long long)a.num_pages;
                     const __amdgpu_buffer_rsrc_t r = span(a.pool + (long long)(ok ? i : 0) * a.page_bytes, O.used);
@@ -1359,7 +1441,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs
                     if constexpr (MOD) pos[kt] = (int)fetch<4>(r, slot * 4, O.pos);
                 }
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
+                for (int kt = 0; kt < kScoreTiles; ++kt)
 #pragma unroll
                     for (int g = 0; g < kNG; ++g) s[kt][g] = 0x1p19f * (float)meta[kt][2 * g];
             };
@@ -1367,15 +1449,15 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs
             if (sec == 0) take(integral_constant<int, hi.kb>{}, integral_constant<int, hi.vb>{}, integral_constant<int, hi.T>{});
             else take(integral_constant<int, lo.kb>{}, integral_constant<int, lo.vb>{}, integral_constant<int, lo.T>{});
         }
-        float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        float total[kScoreTiles] = {0.0f, 0.0f};
         constexpr int kTops = FOUR ? 1 : 4;
-        float top[4][kTops];
+        float top[kScoreTiles][kTops];
         // set i (in LDS at `from`): its position tile, and whether it is its tile's last
         auto use = [&](int i, const ScoreSet& S) {
             const int pt = i / HS, hs = i - pt * HS;
             if (hs == 0) {
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
+                for (int kt = 0; kt < kScoreTiles; ++kt)
 #pragma unroll
                     for (int r = 0; r < kTops; ++r) top[kt][r] = -INFINITY;
             }
@@ -1388,21 +1470,31 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs
             const h8 qs = S.sums[lane];
             const float unit = a.scale * 32.0f;
             const int j = FOUR ? 4 * pt + quarter : 16 * pt + quarter;  // + 4 r
-            f4 sum[4];
+            // a group's products beside the additions of the one before
+            f4 sum[kScoreTiles], part[kNG][kScoreTiles];
+            phase();
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) sum[kt] = mfma_k32(qs, meta[kt], zero);
+            for (int kt = 0; kt < kScoreTiles; ++kt) sum[kt] = mfma_k32(qs, meta[kt], zero);
 #pragma unroll
-            for (int g = 0; g < kNG; ++g) {
-                f4 part[4];
+            for (int g = 0; g <= kNG; ++g) {
+                if (g < kNG) {
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt) part[kt] = mfma_k32(q[g], K[kt][g], zero);
+                    for (int kt = 0; kt < kScoreTiles; ++kt) part[g][kt] = mfma_k32(q[g], K[kt][g], zero);
+                }
+                if (g > 0) {
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
+                    for (int kt = 0; kt < kScoreTiles; ++kt)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sum[kt][r] = __builtin_fmaf(s[kt][g], part[kt][r], sum[kt][r]);
+                        for (int r = 0; r < 4; ++r) {
+                            float y = __builtin_fmaf(s[kt][g - 1], part[g - 1][kt][r], sum[kt][r]);
+                            by_now(y);
+                            sum[kt][r] = y;
+                        }
+                }
+                phase();
             }
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
+            for (int kt = 0; kt < kScoreTiles; ++kt) {
                 float x[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -1423,7 +1515,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs
             }
             if (hs == HS - 1) {
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
+                for (int kt = 0; kt < kScoreTiles; ++kt)
 #pragma unroll
                     for (int r = 0; r < kTops; ++r) {
                         const float p = __builtin_amdgcn_exp2f(top[kt][r]);
@@ -1437,25 +1529,57 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_scores(ChunkArgs
                 for (int i = 0; i < all; ++i) use(i, sets[i]);
         } else {
             // (own tokens: from the first tile that sees one of the workgroup's)
-            const int begin = sec == 2 ? (tok0 - wave * kScoreTokens) / kPos * HS : 0;
+            const int low = sec == 2 ? (tok0 - wave * kScoreTokens) / kPos * HS : 0;
+            // (cuts lie between position tiles: the maximum over the heads is not divided)
+            auto cut = [&](long long units) { return low + (int)(max(units - kBlockUnits, 0ll) / HS) * HS; };
+            const int begin = cut(piece_from - from), end = piece_end == to ? all : cut(piece_end - from);
+            // passes of kScorePass sets through three thirds of LDS: one is used, the next one's sums are
+            // made, the one after is on its way (each set by one wave)
+            const bool makes = wave < kScorePass;
             __syncthreads();
-            if (begin + wave < all) stage(begin + wave, wave);
+            if (makes && begin + wave < end) {
+                load_set(begin + wave, sets[wave]);
+                staged_ready();
+                score_sums(sets[wave], row_lse, row_slope, c, quarter, lane);
+            }
+            if (makes && begin + kScorePass + wave < end) load_set(begin + kScorePass + wave, sets[kScorePass + wave]);
+            staged_ready();
             __syncthreads();
-            int half = 0;
-            for (int i0 = begin; i0 < all; i0 += kChunkWaves, half ^= 1) {
-                if (i0 + kChunkWaves + wave < all) stage(i0 + kChunkWaves + wave, (half ^ 1) * kChunkWaves + wave);
+            int third = 0;
+            for (int i0 = begin; i0 < end; i0 += kScorePass) {
+                const int second = third == 2 ? 0 : third + 1, next = second == 2 ? 0 : second + 1;
+                if (makes && i0 + kScorePass + wave < end)
+                    score_sums(sets[second * kScorePass + wave], row_lse, row_slope, c, quarter, lane);
+                if (makes && i0 + 2 * kScorePass + wave < end)
+                    load_set(i0 + 2 * kScorePass + wave, sets[next * kScorePass + wave]);
                 if (!idle)
-                    for (int i = i0; i < min(i0 + kChunkWaves, all); ++i) use(i, sets[half * kChunkWaves + i - i0]);
+                    for (int i = i0; i < min(i0 + kScorePass, end); ++i) use(i, sets[third * kScorePass + i - i0]);
+                third = second;
+                staged_ready();
                 __syncthreads();
             }
         }
-        if (!idle) {
-            const float x = xsum4(total[0], total[1], total[2], total[3]);  // quarter r: tile r's
-            if (where) {
-                const int received = max(first + n - where_pos, 1);
-                *where = sec == 2 ? x / (float)received : old + (x - (float)n * old) / (float)received;
+        float x = xsum4(total[0], total[1], 0.0f, 0.0f);  // quarter r: tile r's
+        if (piece_from != from || piece_end != to) {
+            if (!once) {
+                // cut by a share's end: the pieces' sums are added by the last of them, in order (slots and
+                // words as in chunk_tiles)
+                auto part_of = [&](int k, bool first_piece) {
+                    return a.part + (2ll * k + (first_piece ? 0 : 1)) * kScoreBlock + wave * kScoreTokens + (lane & 31);  // (lane: the token it finishes)
+                };
+                const int k0 = (int)(from / quantum), k1 = (int)((to - 1) / quantum);
+                if (lane < kScoreTokens) __hip_atomic_store(part_of(share, piece == 0), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (!split_last(a.arrive + k0, k1 - k0 + 1, &last)) continue;
+                x = 0.0f;
+                for (int k = k0; k <= k1; ++k)
+                    x += __hip_atomic_load(part_of(k, k > k0 || from == k0 * quantum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
         }
+        if (where) {
+            const int received = max(first + n - where_pos, 1);
+            *where = sec == 2 ? x / (float)received : old + (x - (float)n * old) / (float)received;
+        }
+    }
     }
 }
 

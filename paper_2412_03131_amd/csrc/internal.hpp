@@ -271,7 +271,6 @@ struct ChunkArgs {
     int splits;            // workgroups per row block
     int blocks;            // row blocks of a KV head that the launch may have
     int rows_lo, rows_hi;  // the launch takes sequences with that many rows (new tokens x G)
-    int shares;            // scores: workgroups per table
     int layout;
 };
 constexpr int kChunkPart = kD + 4;  // floats of a partial state (16-byte rows)
@@ -293,6 +292,10 @@ struct ChunkPlan {
 };
 ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_new, long long p_max);
 hipError_t launch_chunk_attention(const ChunkArgs& a, const ChunkPlan& plan, bool mod, hipStream_t st);
+// Shares of a chunk scores call (two workgroups for each CU), and the workspace: an arrival word and two
+// slots of 256 sums each.
+constexpr int kScoreShares = 512;
+constexpr long long kScoreBytes = kScoreShares * (8ll + 2 * 256 * 4);
 hipError_t launch_chunk_scores(const ChunkArgs& a, bool mod, hipStream_t st);
 // Kernel entry points of layout n (k_chunk_l<n>.hip).
 const void* chunk_kernel_l0(int which, bool mod);

@@ -76,15 +76,9 @@ hipError_t launch_chunk_scores(const ChunkArgs& args, bool mod, hipStream_t st)
     // four heads a set where they are used (3, 4, 7 and 8 query heads) or the chunk is short
     const void* kern = chunk_kernel(a.layout, a.max_new <= 4 || (G + 3) / 4 * 4 <= G + 1 ? 4 : 0, mod);
     if (!kern) return hipErrorInvalidValue;
-    const long long T = (long long)a.B * a.Hkv;
-    const long long most = (long long)a.p_max * 16 / 256 + 3 + (a.max_new + 255) / 256;
-    long long shares = a.max_new <= 16 ? (2048 + T - 1) / T : most;
-    if (shares > most) shares = most;
-    a.shares = (int)shares;
-    const long long grid = T * shares;
-    if (grid < 1 || grid > INT32_MAX) return hipErrorInvalidValue;
+    const long long grid = kScoreShares;
     void* kargs[] = {&a};
-    return hipLaunchKernel(kern, dim3((unsigned)grid), dim3(4 * kWave), kargs, 0, st);
+    return hipLaunchKernel(kern, dim3((unsigned)grid), dim3(8 * kWave), kargs, 0, st);
 }
 
 }  // namespace dkv

@@ -1206,8 +1206,8 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
 // the workgroup's eight waves.  A set is either 16 positions of one query head (the maximum over the
 // heads is taken between one set's results and the next's, in a lane) or 4 positions of four heads
 // (between a lane's four results): the second for chunks of up to four tokens and where four divides
-// the heads well.  One exp2 serves all heads of a position.  A chunk of at most kScoreSets sets is
-// staged once and stays for all of a workgroup's tokens; a longer one passes four sets at a time.
+// the heads well.  One exp2 serves all heads of a position.  Short chunks have a
+// kernel of their own (chunk_scores_short); the sets of a longer one pass four at a time.
 //
 // Queries stay unscaled here: a token's scales are in registers, in fp32, and take the 2^24 of
 // the codes themselves; the unit of the sums is 2^-5, so that a group's sum of 32 halfs fits one.
@@ -1216,6 +1216,8 @@ constexpr int kScoreTokens = 16 * kScoreTiles;               // per wave
 constexpr int kScoreBlock = kScoreTokens * kScoreWaves;      // per workgroup pass
 constexpr int kScorePass = 4;                                // sets per pass of a long chunk
 constexpr int kScoreSets = 3 * kScorePass;                   // in LDS
+constexpr int kShortSets = 4;                                // of a short chunk, of four positions and heads
+__device__ __forceinline__ bool score_short(int n, int G) { return (n + 3) / 4 * ((G + 3) >> 2) <= kShortSets; }
 
 struct ScoreSet {
     h8 q[kNG][kWave];
@@ -1261,6 +1263,68 @@ __device__ __forceinline__ void score_sums(ScoreSet& s, float lse, float slope, 
     }
 }
 
+// One set against a wave's tokens: the running maxima over the heads, of position p (+ 4 r) and tokens
+// 16 kt + c, in log2 units.
+template <bool FOUR, bool MOD>
+__device__ __forceinline__ void score_use(const ScoreSet& S, const ChunkArgs& a, const h8 (&K)[kScoreTiles][kNG],
+                                          const h8 (&meta)[kScoreTiles], const float (&s)[kScoreTiles][kNG],
+                                          const int (&pos)[kScoreTiles], int p, float (&top)[kScoreTiles][FOUR ? 1 : 4], int quarter,
+                                          int lane)
+{
+    const f4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    const f4 lse = *reinterpret_cast<const f4*>(&S.lse[4 * quarter]);
+    f4 slope = zero;
+    if constexpr (MOD) slope = *reinterpret_cast<const f4*>(&S.slope[4 * quarter]);
+    h8 q[kNG];
+#pragma unroll
+    for (int g = 0; g < kNG; ++g) q[g] = S.q[g][lane];
+    const h8 qs = S.sums[lane];
+    const float unit = a.scale * 32.0f;
+    // a group's products beside the additions of the one before
+    f4 sum[kScoreTiles], part[kNG][kScoreTiles];
+    phase();
+#pragma unroll
+    for (int kt = 0; kt < kScoreTiles; ++kt) sum[kt] = mfma_k32(qs, meta[kt], zero);
+#pragma unroll
+    for (int g = 0; g <= kNG; ++g) {
+        if (g < kNG) {
+#pragma unroll
+            for (int kt = 0; kt < kScoreTiles; ++kt) part[g][kt] = mfma_k32(q[g], K[kt][g], zero);
+        }
+        if (g > 0) {
+#pragma unroll
+            for (int kt = 0; kt < kScoreTiles; ++kt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float y = __builtin_fmaf(s[kt][g - 1], part[g - 1][kt][r], sum[kt][r]);
+                    by_now(y);
+                    sum[kt][r] = y;
+                }
+        }
+        phase();
+    }
+#pragma unroll
+    for (int kt = 0; kt < kScoreTiles; ++kt) {
+        float x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if constexpr (MOD) {
+                const int away = p + (FOUR ? 0 : 4 * r) - pos[kt];
+                const float y = formed(sum[kt][r] * unit, ScoreForm{a.cap_in, a.cap_out, slope[r]}, (float)away) - lse[r];
+                x[r] = away < a.window ? y : -INFINITY;
+            } else {
+                x[r] = __builtin_fmaf(sum[kt][r], unit, -lse[r]);
+            }
+        }
+        if constexpr (FOUR) {
+            top[kt][0] = max3(max3(top[kt][0], x[0], x[1]), x[2], x[3]);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top[kt][r] = fmaxf(top[kt][r], x[r]);
+        }
+    }
+}
+
 template <int LI, bool FOUR, bool MOD>
 __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs a)
 {
@@ -1285,7 +1349,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
         int n = a.new_len[t / a.Hkv];
         n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
         Table x{n, (n + kPos - 1) / kPos * HS, 0, 0, 0};
-        if (n > 0) {
+        if (!score_short(n, G)) {
             x.b_hi = (a.len[2 * t] + kScoreBlock - 1) / kScoreBlock;
             x.b_lo = (a.len[2 * t + 1] + kScoreBlock - 1) / kScoreBlock;
             x.own = (n + kScoreBlock - 1) / kScoreBlock;
@@ -1338,7 +1402,6 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
         if (table_at + units_to(tb, mid) <= cur) blk = mid;
         else above = mid - 1;
     }
-    const bool once = tb.all <= kScoreSets;
     SeqBlock sb;
     sb.b = t / a.Hkv;
     sequence_rows(a, sb);
@@ -1360,19 +1423,11 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
         row_lse = there ? a.lse_in[(sb.row0 + jj) * a.Hq + hq] * kChunkLog2e : INFINITY;
         if constexpr (MOD) row_slope = a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f;
     };
-    if (once) {
-        for (int i = wave; i < all; i += kScoreWaves) {
-            load_set(i, sets[i]);
-            staged_ready();
-            score_sums(sets[i], row_lse, row_slope, c, quarter, lane);
-        }
-        __syncthreads();
-    }
     for (; blk < blocks && cur < stop; ++blk, ++piece) {
         const long long from = table_at + units_to(tb, blk), to = table_at + units_to(tb, blk + 1);
         const long long piece_from = cur, piece_end = min(stop, to);
         cur = piece_end;
-        if (n == 0 || (once && piece_from != from)) continue;  // (a block of these is its first unit's share's)
+        if (n == 0) continue;
         const int sec = blk < b_hi ? 0 : (blk < b_hi + b_lo ? 1 : 2);
         const int len = sec == 0 ? len_hi : (sec == 1 ? len_lo : n);
         const int tok0 = (blk - (sec == 0 ? 0 : (sec == 1 ? b_hi : b_hi + b_lo))) * kScoreBlock + wave * kScoreTokens;
@@ -1452,7 +1507,6 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
         float total[kScoreTiles] = {0.0f, 0.0f};
         constexpr int kTops = FOUR ? 1 : 4;
         float top[kScoreTiles][kTops];
-        // set i (in LDS at `from`): its position tile, and whether it is its tile's last
         auto use = [&](int i, const ScoreSet& S) {
             const int pt = i / HS, hs = i - pt * HS;
             if (hs == 0) {
@@ -1461,58 +1515,8 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
 #pragma unroll
                     for (int r = 0; r < kTops; ++r) top[kt][r] = -INFINITY;
             }
-            const f4 lse = *reinterpret_cast<const f4*>(&S.lse[4 * quarter]);
-            f4 slope = zero;
-            if constexpr (MOD) slope = *reinterpret_cast<const f4*>(&S.slope[4 * quarter]);
-            h8 q[kNG];
-#pragma unroll
-            for (int g = 0; g < kNG; ++g) q[g] = S.q[g][lane];
-            const h8 qs = S.sums[lane];
-            const float unit = a.scale * 32.0f;
-            const int j = FOUR ? 4 * pt + quarter : 16 * pt + quarter;  // + 4 r
-            // a group's products beside the additions of the one before
-            f4 sum[kScoreTiles], part[kNG][kScoreTiles];
-            phase();
-#pragma unroll
-            for (int kt = 0; kt < kScoreTiles; ++kt) sum[kt] = mfma_k32(qs, meta[kt], zero);
-#pragma unroll
-            for (int g = 0; g <= kNG; ++g) {
-                if (g < kNG) {
-#pragma unroll
-                    for (int kt = 0; kt < kScoreTiles; ++kt) part[g][kt] = mfma_k32(q[g], K[kt][g], zero);
-                }
-                if (g > 0) {
-#pragma unroll
-                    for (int kt = 0; kt < kScoreTiles; ++kt)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            float y = __builtin_fmaf(s[kt][g - 1], part[g - 1][kt][r], sum[kt][r]);
-                            by_now(y);
-                            sum[kt][r] = y;
-                        }
-                }
-                phase();
-            }
-#pragma unroll
-            for (int kt = 0; kt < kScoreTiles; ++kt) {
-                float x[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if constexpr (MOD) {
-                        const int away = first + j + (FOUR ? 0 : 4 * r) - pos[kt];
-                        const float y = formed(sum[kt][r] * unit, ScoreForm{a.cap_in, a.cap_out, slope[r]}, (float)away) - lse[r];
-                        x[r] = away < a.window ? y : -INFINITY;
-                    } else {
-                        x[r] = __builtin_fmaf(sum[kt][r], unit, -lse[r]);
-                    }
-                }
-                if constexpr (FOUR) {
-                    top[kt][0] = max3(max3(top[kt][0], x[0], x[1]), x[2], x[3]);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) top[kt][r] = fmaxf(top[kt][r], x[r]);
-                }
-            }
+            const int j = kPos * pt + quarter;  // (+ 4 r with sixteen positions)
+            score_use<FOUR, MOD>(S, a, K, meta, s, pos, first + j, top, quarter, lane);
             if (hs == HS - 1) {
 #pragma unroll
                 for (int kt = 0; kt < kScoreTiles; ++kt)
@@ -1524,10 +1528,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
                     }
             }
         };
-        if (once) {
-            if (!idle)
-                for (int i = 0; i < all; ++i) use(i, sets[i]);
-        } else {
+        {
             // (own tokens: from the first tile that sees one of the workgroup's)
             const int low = sec == 2 ? (tok0 - wave * kScoreTokens) / kPos * HS : 0;
             // (cuts lie between position tiles: the maximum over the heads is not divided)
@@ -1561,7 +1562,6 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
         }
         float x = xsum4(total[0], total[1], 0.0f, 0.0f);  // quarter r: tile r's
         if (piece_from != from || piece_end != to) {
-            if (!once) {
                 // cut by a share's end: the pieces' sums are added by the last of them, in order (slots and
                 // words as in chunk_tiles)
                 auto part_of = [&](int k, bool first_piece) {
@@ -1573,7 +1573,6 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
                 x = 0.0f;
                 for (int k = k0; k <= k1; ++k)
                     x += __hip_atomic_load(part_of(k, k > k0 || from == k0 * quantum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
         }
         if (where) {
             const int received = max(first + n - where_pos, 1);
@@ -1583,16 +1582,191 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
     }
 }
 
+// The short chunks: at most kShortSets sets of four positions and heads, staged once for a workgroup's share
+// of its table.  Each wave takes every eighth step of 32 tokens, the keys' half of its pages by way of LDS as
+// in chunk_rows, the next step's on its way while one is computed.  Bound by memory.
+template <int LI, bool MOD>
+__global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores_short(ChunkArgs a)
+{
+    constexpr KvFmt hi = kLayoutFmts[LI].hi, lo = kLayoutFmts[LI].lo;
+    constexpr SecOffsets Oh = sec_offsets(hi), Ol = sec_offsets(lo);
+    constexpr int kHi = (Oh.vc + 1023) / 1024 * 1024, kLo = (Ol.vc + 1023) / 1024 * 1024;  // a page's room
+    constexpr int kSlot = (hi.T == 16 ? 2 : 1) * kHi > (lo.T == 16 ? 2 : 1) * kLo ? (hi.T == 16 ? 2 : 1) * kHi
+                                                                                 : (lo.T == 16 ? 2 : 1) * kLo;
+    struct Shared {
+        uint8_t slot[kScoreWaves][kSlot];
+        ScoreSet sets[kShortSets];
+    };
+    __shared__ __align__(1024) Shared sh;
+    const int lane = lane_id(), wave = wave_index();
+    const int c = lane & 15, quarter = lane >> 4;
+    const int G = a.Hq / a.Hkv, HS = (G + 3) >> 2;
+    const int item = (int)blockIdx.x / a.Hkv, h = (int)blockIdx.x - item * a.Hkv;
+    SeqBlock sb;
+    sb.b = item / a.splits;
+    const int share = item - sb.b * a.splits;
+    sequence_rows(a, sb);
+    const int n = sb.n;
+    if (n == 0 || !score_short(n, G)) return;
+    const int t = sb.b * a.Hkv + h;
+    const int first = a.seq_len[sb.b], len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
+    const int s_hi = (len_hi + 31) >> 5, s_lo = (len_lo + 31) >> 5, steps = s_hi + s_lo + 1;  // (the last: own tokens)
+    const int shares = min(a.splits, (steps + kScoreWaves - 1) / kScoreWaves);
+    if (share >= shares) return;
+    const int begin = (int)((long long)steps * share / shares), end = (int)((long long)steps * (share + 1) / shares);
+    const int32_t* table = a.page_table + (long long)t * a.p_max;
+    uint8_t* slot = sh.slot[wave];
+
+    auto page_id = [&](int u, int part) {
+        const bool high = u < s_hi;
+        const int T = high ? hi.T : lo.T, len = high ? len_hi : len_lo, k = high ? u : u - s_hi;
+        const int i = min(T == 16 ? 2 * k + part : k, (len + T - 1) / T - 1);
+        const int id = __builtin_amdgcn_readfirstlane(table[high ? i : a.p_max - 1 - i]);
+        return (unsigned long long)(unsigned)id < (unsigned long long)a.num_pages ? id : -1;  // (outside: reads page 0)
+    };
+    // the staged step: this lane's token (tile = quarter, c; quarters 0 and 1), its score and position
+    float* where = nullptr;
+    float old = 0.0f;
+    int where_pos = 0;
+    int pos[kScoreTiles] = {0, 0};
+    auto stage = [&](int u, int id0, int id1) {
+        const bool high = u < s_hi;
+        const uint8_t* p0 = a.pool + (long long)(id0 < 0 ? 0 : id0) * a.page_bytes;
+        const uint8_t* p1 = a.pool + (long long)(id1 < 0 ? 0 : id1) * a.page_bytes;
+        if (high) {
+            stage_page<Oh.vc>(slot, p0, lane);
+            if (hi.T == 16) stage_page<Oh.vc>(slot + kHi, p1, lane);
+        } else {
+            stage_page<Ol.vc>(slot, p0, lane);
+            if (lo.T == 16) stage_page<Ol.vc>(slot + kLo, p1, lane);
+        }
+        const bool two = high ? hi.T == 16 : lo.T == 16;
+        const int tile = quarter & 1, id = two && tile ? id1 : id0;
+        uint8_t* pg = a.pool_rw + (long long)(id < 0 ? 0 : id) * a.page_bytes;
+        const int sl = two ? c : 16 * tile + c;
+        where_pos = *reinterpret_cast<const int32_t*>(pg + (high ? Oh.pos : Ol.pos) + 4 * sl);
+        float* at = reinterpret_cast<float*>(pg + (high ? Oh.sc : Ol.sc) + 4 * sl);
+        old = *at;
+        const int left = high ? len_hi - 32 * u : len_lo - 32 * (u - s_hi);
+        where = quarter < 2 && id >= 0 && 16 * tile + c < left ? at : nullptr;
+    };
+    const int cached = min(end, s_hi + s_lo);
+    int u = begin + wave;
+    if (u < cached) stage(u, page_id(u, 0), page_id(u, 1));
+
+    const int all = (n + 3) / 4 * HS;
+    if (wave < all) {
+        const int pt = wave / HS, hs = wave - pt * HS, j = 4 * pt + (c >> 2), g = 4 * hs + (c & 3);
+        const bool there = j < n && g < G;
+        const int jj = there ? j : 4 * pt, hq = h * G + (there ? g : 0);
+        const long long row = sb.row0 + jj;
+        const uint16_t* q = a.q + row * a.q_stride + hq * kD + quarter * 8;
+        u4 x[kNG];
+#pragma unroll
+        for (int g4 = 0; g4 < kNG; ++g4) x[g4] = *reinterpret_cast<const u4*>(q + g4 * kG);
+        const float lse = there ? a.lse_in[row * a.Hq + hq] * kChunkLog2e : INFINITY;
+        const float slope = MOD && a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f;
+        ScoreSet& S = sh.sets[wave];
+#pragma unroll
+        for (int g4 = 0; g4 < kNG; ++g4) S.q[g4][lane] = __builtin_bit_cast(h8, x[g4]);
+        score_sums(S, lse, slope, c, quarter, lane);
+    }
+    __syncthreads();
+
+    // a step's sums over all queries: quarter 0's for tile 0, quarter 1's for tile 1
+    auto received = [&](const h8 (&K)[kScoreTiles][kNG], const h8 (&meta)[kScoreTiles], const float (&s)[kScoreTiles][kNG], int own) {
+        float total[kScoreTiles] = {0.0f, 0.0f}, top[kScoreTiles][1];
+        for (int i = 0; i < all; ++i) {
+            const int pt = i / HS, hs = i - pt * HS, j = 4 * pt + quarter;
+            if (hs == 0) top[0][0] = top[1][0] = -INFINITY;
+            score_use<true, MOD>(sh.sets[i], a, K, meta, s, pos, first + j, top, quarter, lane);
+            if (hs == HS - 1) {
+#pragma unroll
+                for (int kt = 0; kt < kScoreTiles; ++kt) {
+                    const float p = __builtin_amdgcn_exp2f(top[kt][0]);
+                    total[kt] += own < 0 || j >= own + 16 * kt + c ? p : 0.0f;
+                }
+            }
+        }
+        return xsum4(total[0], total[1], 0.0f, 0.0f);
+    };
+    int n0 = 0, n1 = 0;
+    while (u < cached) {
+        const int next = u + kScoreWaves;
+        if (next < cached) {
+            n0 = page_id(next, 0);
+            n1 = page_id(next, 1);
+        }
+        staged_ready();
+        h8 K[kScoreTiles][kNG], meta[kScoreTiles];
+        float s[kScoreTiles][kNG];
+        auto take = [&](auto kb, auto vb, auto tt, int page) {
+            constexpr int KB = decltype(kb)::value, VB = decltype(vb)::value, T = decltype(tt)::value;
+            constexpr SecOffsets O = sec_offsets(KvFmt{KB, VB, T});
+#pragma unroll
+            for (int kt = 0; kt < kScoreTiles; ++kt) {
+                const uint8_t* pg = slot + (T == 16 ? kt * page : 0);
+                const int sl = T == 16 ? c : 16 * kt + c;
+#pragma unroll
+                for (int g = 0; g < kNG; ++g) {
+                    if constexpr (KB == 8) {
+                        const u2 v = *reinterpret_cast<const u2*>(pg + O.kc + ((2 * g + (quarter >> 1)) * T + sl) * 16 + (quarter & 1) * 8);
+                        K[kt][g] = key_codes8(v[0], v[1]);
+                    } else {
+                        K[kt][g] = key_codes4(*reinterpret_cast<const uint32_t*>(pg + O.kc + (g * T + sl) * 16 + quarter * 4));
+                    }
+                }
+                meta[kt] = *reinterpret_cast<const h8*>(pg + O.km + sl * 16);
+#pragma unroll
+                for (int g = 0; g < kNG; ++g) s[kt][g] = 0x1p19f * (float)meta[kt][2 * g];
+            }
+        };
+        using std::integral_constant;
+        if (u < s_hi) take(integral_constant<int, hi.kb>{}, integral_constant<int, hi.vb>{}, integral_constant<int, hi.T>{}, kHi);
+        else take(integral_constant<int, lo.kb>{}, integral_constant<int, lo.vb>{}, integral_constant<int, lo.T>{}, kLo);
+        float* at = where;
+        const float before = old;
+        const int at_pos = where_pos;
+        if constexpr (MOD) {  // every quarter's lane c needs the positions of its two tokens
+            pos[0] = __shfl(at_pos, c);
+            pos[1] = __shfl(at_pos, 16 + c);
+        }
+        staged_read();
+        if (next < cached) stage(next, n0, n1);
+        const float x = received(K, meta, s, -1);
+        if (at) *at = before + (x - (float)n * before) / (float)max(first + n - at_pos, 1);
+        u = next;
+    }
+    if (u == s_hi + s_lo && u < end) {  // (one wave of one share) the chunk's own tokens, at most 16
+        h8 K[kScoreTiles][kNG], meta[kScoreTiles];
+        float s[kScoreTiles][kNG];
+#pragma unroll
+        for (int kt = 0; kt < kScoreTiles; ++kt) {
+            const uint16_t* row = a.k + (sb.row0 + min(16 * kt + c, n - 1)) * a.k_stride + h * kD + quarter * 8;
+#pragma unroll
+            for (int g = 0; g < kNG; ++g) {
+                K[kt][g] = *reinterpret_cast<const h8*>(row + g * kG);
+                s[kt][g] = 0x1p-5f;
+            }
+            meta[kt] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
+            pos[kt] = first + 16 * kt + c;
+        }
+        const float x = received(K, meta, s, 0);
+        if (lane < n) a.score[(sb.row0 + lane) * a.Hkv + h] = x / (float)(n - lane);
+    }
+}
+
 }  // namespace dkv
 
 // Kernel entry points of layout n: which = 0 scores (sets of 16 positions), 4 (of 4 positions and
-// heads), 1 / 2 attention of few rows with that many row tiles, 3 of many.
+// heads), 5 (of short chunks), 1 / 2 attention of few rows with that many row tiles, 3 of many.
 #define DKV_CHUNK_KERNELS(LI)                                                                                  \
     const void* chunk_kernel_l##LI(int which, bool mod)                                                        \
     {                                                                                                          \
         switch (which) {                                                                                       \
         case 0: return mod ? (const void*)chunk_scores<LI, false, true> : (const void*)chunk_scores<LI, false, false>; \
         case 4: return mod ? (const void*)chunk_scores<LI, true, true> : (const void*)chunk_scores<LI, true, false>; \
+        case 5: return mod ? (const void*)chunk_scores_short<LI, true> : (const void*)chunk_scores_short<LI, false>; \
         case 1: return mod ? (const void*)chunk_rows<LI, 1, true> : (const void*)chunk_rows<LI, 1, false>;     \
         case 2: return mod ? (const void*)chunk_rows<LI, 2, true> : (const void*)chunk_rows<LI, 2, false>;     \
         case 3: return mod ? (const void*)chunk_tiles<LI, true> : (const void*)chunk_tiles<LI, false>;         \

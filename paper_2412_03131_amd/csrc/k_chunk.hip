@@ -72,11 +72,26 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
 hipError_t launch_chunk_scores(const ChunkArgs& args, bool mod, hipStream_t st)
 {
     ChunkArgs a = args;
-    const int G = a.Hq / a.Hkv;
-    // four heads a set where they are used (3, 4, 7 and 8 query heads) or the chunk is short
-    const void* kern = chunk_kernel(a.layout, a.max_new <= 4 || (G + 3) / 4 * 4 <= G + 1 ? 4 : 0, mod);
+    const long long G = a.Hq / a.Hkv, T = (long long)a.B * a.Hkv;
+    const bool longs = ((long long)a.max_new + 3) / 4 * ((G + 3) / 4) > 4;
+    if (longs) {
+        // four heads a set where they are used (3, 4, 7 and 8 query heads)
+        const void* kern = chunk_kernel(a.layout, (G + 3) / 4 * 4 <= G + 1 ? 4 : 0, mod);
+        if (!kern) return hipErrorInvalidValue;
+        void* kargs[] = {&a};
+        const hipError_t e = hipLaunchKernel(kern, dim3(kScoreShares), dim3(8 * kWave), kargs, 0, st);
+        // (all sequences have the one length then)
+        if (e != hipSuccess || a.total_new == (long long)a.B * a.max_new) return e;
+    }
+    const void* kern = chunk_kernel(a.layout, 5, mod);
     if (!kern) return hipErrorInvalidValue;
-    const long long grid = kScoreShares;
+    // about 1024 workgroups, a step for each of their waves
+    const long long most = (a.p_max / 2 + 2 + 7) / 8;
+    long long shares = (1024 + T - 1) / T;
+    if (shares > most) shares = most;
+    a.splits = (int)(shares < 1 ? 1 : shares);
+    const long long grid = T * a.splits;
+    if (grid > INT32_MAX) return hipErrorInvalidValue;
     void* kargs[] = {&a};
     return hipLaunchKernel(kern, dim3((unsigned)grid), dim3(8 * kWave), kargs, 0, st);
 }

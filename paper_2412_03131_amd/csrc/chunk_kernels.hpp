@@ -572,7 +572,9 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
     // the waves' states, 16 rows at a time: 16 threads a row, eight dims each
     const int row = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8;
     const long long slot_no = (long long)block * a.Hkv + h;
-    float* part = a.part + (slot_no * a.splits + split) * kRows * kChunkPart;
+    auto part_of = [&](int k) {
+        return span(a.part + (slot_no * a.splits + k) * kRows * kChunkPart, kRows * kChunkPart * 4);
+    };
     auto write = [&](int at, const float (&o)[8], float m, float sum) {
         if (at >= rows) return;
         const int j = at / G, hq = h * G + at - j * G;
@@ -612,35 +614,44 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
         }
         if (splits == 1) {
             write(r0 + 16 * rt + row, o, m, sum);
-        } else {
-            float* to = part + (16 * rt + row) * kChunkPart;
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) put_pair(to + d + i, o[i], o[i + 1]);
-            if (d == 0) put_pair(to + kD, m, sum);
+        } else if (r0 + 16 * rt + row < rows) {
+            const __amdgpu_buffer_rsrc_t to = part_of(split);
+            const int at = (16 * rt + row) * kChunkPart * 4;
+            put_quad(to, at + d * 4, 0, f4{o[0], o[1], o[2], o[3]});
+            put_quad(to, at + d * 4, 16, f4{o[4], o[5], o[6], o[7]});
+            if (d == 0) put_quad(to, at, kD * 4, f4{m, sum, 0.0f, 0.0f});
         }
     }
     if (splits == 1 || !split_last(a.arrive + slot_no, splits, &lds.merge.last)) return;
     // the last of the block's workgroups joins their states, in order
-    const float* first_part = a.part + slot_no * a.splits * kRows * kChunkPart;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const float* from = first_part + (16 * rt + row) * kChunkPart;
-        float m = kLowest, sum = 0.0f, o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (int k = 0; k < splits; ++k, from += kRows * kChunkPart) {
-            const float2 ml = get_pair(from + kD);
-            float2 x[4];
+        if (r0 + 16 * rt + row >= rows) continue;
+        float m = kLowest, sum = 0.0f;
+        f4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
+        constexpr int kAhead = 4;  // states whose loads are in flight together
+        for (int k = 0; k < splits; k += kAhead) {
+            f4 ml[kAhead], px[kAhead], py[kAhead];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = get_pair(from + d + 2 * i);
-            const float top = fmaxf(m, ml.x);
-            const float f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(ml.x - top);
-            m = top;
-            sum = sum * f + ml.y * g;
+            for (int i = 0; i < kAhead; ++i) {
+                const __amdgpu_buffer_rsrc_t from = part_of(min(k + i, splits - 1));
+                const int at = (16 * rt + row) * kChunkPart * 4;
+                ml[i] = get_quad(from, at, kD * 4);
+                px[i] = get_quad(from, at + d * 4, 0);
+                py[i] = get_quad(from, at + d * 4, 16);
+            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                o[2 * i] = o[2 * i] * f + x[i].x * g;
-                o[2 * i + 1] = o[2 * i + 1] * f + x[i].y * g;
+            for (int i = 0; i < kAhead; ++i) {
+                if (k + i >= splits) continue;
+                const float top = fmaxf(m, ml[i][0]);
+                const float f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(ml[i][0] - top);
+                m = top;
+                sum = sum * f + ml[i][1] * g;
+                x = x * f + px[i] * g;
+                y = y * f + py[i] * g;
             }
         }
+        const float o[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
         write(r0 + 16 * rt + row, o, m, sum);
     }
 }

@@ -24,8 +24,8 @@ ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_n
     const long long seqs = B < total_new ? B : total_new;
     const long long steps = p_max / 2 + total_new / 32 + 2;  // 32-token steps of the longest table there can be
     auto clamp = [](long long x, long long lo, long long hi) { return x < lo ? lo : (x > hi ? hi : x); };
-    // few rows: about 2048 workgroups, a step for each of their waves
-    p.few_splits = seqs ? (int)clamp(2048 / (Hkv * seqs), 1, clamp(steps / 4, 1, 64)) : 1;
+    // few rows: about 1024 workgroups, a step for each of their waves
+    p.few_splits = seqs ? (int)clamp(1024 / (Hkv * seqs), 1, clamp(steps / 4, 1, 64)) : 1;
     p.few_blocks = Hkv * clamp(rows / 16 + 2 * seqs, 0, seqs * (kChunkFewRows / 16));  // (in blocks of 32: two each)
     p.few_part = p.few_splits > 1 ? p.few_blocks * p.few_splits * 16 * kChunkPart : 0;
     p.many = rows > kChunkFewRows;
@@ -61,9 +61,10 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     ChunkArgs a = args;
     a.rows_lo = 1;
     a.rows_hi = rows > kChunkFewRows ? 16 : kChunkFewRows;
-    a.splits = plan.few_splits;
     a.part = part;
     const int rt = rows > 16 && rows <= kChunkFewRows ? 2 : 1;
+    // (half as many with two row tiles, of which a CU holds half as many)
+    a.splits = rt == 2 && plan.few_splits > 1 ? plan.few_splits / 2 : plan.few_splits;
     const long long per = 16 * rt, most = rows < a.rows_hi ? rows : a.rows_hi;
     const long long whole = args.total_new * G / per + seqs, each = seqs * ((most + per - 1) / per);
     return launch(a, rt, (whole < each ? whole : each) * a.Hkv * a.splits, 4 * kWave);

@@ -235,8 +235,9 @@ __device__ __forceinline__ void softmax_step(Rows<RT>& R, const float (&unit)[RT
 // next() is called once the slot has been read.
 template <int KB, int VB, int T, int RT, bool MOD, typename F>
 __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, const uint8_t* slot, int left, uint32_t bad,
-                                            const ChunkArgs& a, int c, int quarter, F&& next)
+                                            const ChunkArgs& a, int lane, F&& next)
 {
+    const int c = lane & 15, quarter = lane >> 4;
     float x[RT][2][4];
     const h4 pick0 = {(_Float16)(quarter == 0 ? 32768.0f : 0.0f), (_Float16)0.0f, (_Float16)0.0f, (_Float16)0.0f};
     const h4 pick1 = {(_Float16)0.0f, (_Float16)0.0f, (_Float16)(quarter == 0 ? 32768.0f : 0.0f), (_Float16)0.0f};
@@ -316,11 +317,7 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
         h2 s02[2], z02[2], s13[2], z13[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            u4 m = val.vm[t];
-            if (!whole) {  // nothing behind a section's end reaches the sums
-#pragma unroll
-                for (int r = 0; r < 4; ++r) m[r] = (keep[t] >> r) & 1 ? m[r] : 0u;
-            }
+            const u4 m = val.vm[t];
             s02[t] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x05040100u));
             z02[t] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x07060302u));
             s13[t] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[3], m[1], 0x05040100u));
@@ -338,6 +335,13 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
                             s13[1], z13[1], p, q);
             v[2] = p;
             v[3] = q;
+            if (!whole) {  // nothing behind a section's end reaches the sums
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    v[2 * t] &= (keep[t] & 1 ? 0xffffu : 0u) | (keep[t] & 4 ? 0xffff0000u : 0u);
+                    v[2 * t + 1] &= (keep[t] & 2 ? 0xffffu : 0u) | (keep[t] & 8 ? 0xffff0000u : 0u);
+                }
+            }
             const h8 V = __builtin_bit_cast(h8, v);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, P[rt], R.acc[rt][dt]);
@@ -479,30 +483,16 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
     if (sb.b < 0) return;
     const int first = a.seq_len[sb.b];
     const int rows = sb.n * G, r0 = sb.blk * kRows;
-    Rows<RT> R;
+    // the queries' loads first, then the table's lengths and first pages, whose loads follow each other
+    u4 x[RT][kNG];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int row = min(r0 + 16 * rt + c, rows - 1);
         const int j = row / G, hq = h * G + row - j * G;
         const uint16_t* q = a.q + (sb.row0 + j) * a.q_stride + hq * kD + quarter * 8;
-        u4 x[kNG];
 #pragma unroll
-        for (int g = 0; g < kNG; ++g) x[g] = *reinterpret_cast<const u4*>(q + g * kG);
-        const RowOperands o = row_operands(x, quarter);
-        if (wave == 0) {
-#pragma unroll
-            for (int g = 0; g < kNG; ++g) Q.q[rt][g][lane] = o.q[g];
-            Q.sums[rt][lane] = o.sums;
-        }
-        R.unit[rt] = o.unit * a.scale;
-        R.p[rt] = first + j;
-        R.form[rt] = ScoreForm{a.cap_in, a.cap_out, MOD && a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f};
-        R.m[rt] = kLowest;
-        R.l[rt] = 0.0f;
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int g = 0; g < kNG; ++g) x[rt][g] = *reinterpret_cast<const u4*>(q + g * kG);
     }
-    __syncthreads();
     const int t = sb.b * a.Hkv + h;
     const int len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
     const int last = min(r0 + kRows, rows) - 1;
@@ -543,9 +533,33 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
     };
     const int cached = min(end, s_hi + s_lo);
     int u = begin + wave;
+    int n0 = 0, n1 = 0;
     if (u < cached) {
-        stage(u, page_id(u, 0), page_id(u, 1));
-        int n0 = 0, n1 = 0;
+        n0 = page_id(u, 0);
+        n1 = page_id(u, 1);
+    }
+    Rows<RT> R;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = min(r0 + 16 * rt + c, rows - 1);
+        const int j = row / G, hq = h * G + row - j * G;
+        const RowOperands o = row_operands(x[rt], quarter);
+        if (wave == 0) {
+#pragma unroll
+            for (int g = 0; g < kNG; ++g) Q.q[rt][g][lane] = o.q[g];
+            Q.sums[rt][lane] = o.sums;
+        }
+        R.unit[rt] = o.unit * a.scale;
+        R.p[rt] = first + j;
+        R.form[rt] = ScoreForm{a.cap_in, a.cap_out, MOD && a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f};
+        R.m[rt] = kLowest;
+        R.l[rt] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    __syncthreads();
+    if (u < cached) stage(u, n0, n1);
+    {
         while (u < cached) {
             const int next = u + kChunkWaves;
             if (next < cached) {
@@ -557,8 +571,8 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
                 if (next < cached) stage(next, n0, n1);
             };
             staged_ready();
-            if (u < s_hi) cached_step<hi.kb, hi.vb, hi.T, RT, MOD>(R, Q, slot, len_hi - 32 * u, b, a, c, quarter, ahead);
-            else cached_step<lo.kb, lo.vb, lo.T, RT, MOD>(R, Q, slot, len_lo - 32 * (u - s_hi), b, a, c, quarter, ahead);
+            if (u < s_hi) cached_step<hi.kb, hi.vb, hi.T, RT, MOD>(R, Q, slot, len_hi - 32 * u, b, a, fresh(lane), ahead);
+            else cached_step<lo.kb, lo.vb, lo.T, RT, MOD>(R, Q, slot, len_lo - 32 * (u - s_hi), b, a, fresh(lane), ahead);
             u = next;
         }
     }

@@ -454,6 +454,63 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const RowsLds<RT>& Q, cons
 // SIMD the others' work covers the rest of its way.
 constexpr int kChunkWaves = 4;
 
+// The piece of workgroup blockIdx.x: tables in order, a table's row blocks, a block's pieces.  All blocks
+// of a table have about one piece per `quantum` steps, the quantum such that all pieces together (a
+// table's last is half a quantum on average) are kRowPieces, and at least a step for each wave.
+constexpr int kRowTables = 1024;  // (more are not split)
+struct RowPiece {
+    int table, blk, split, splits, block;
+};
+__device__ __forceinline__ RowPiece row_piece(const ChunkArgs& a, int rows, int* lds)
+{
+    const int tables = a.B * a.Hkv, G = a.Hq / a.Hkv;
+    constexpr int kPer = kRowTables / (kChunkWaves * kWave);
+    int steps[kPer], nb[kPer], sum = 0, count = 0;
+    const int t0 = (int)threadIdx.x * kPer;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int t = t0 + i;
+        steps[i] = nb[i] = 0;
+        if (t < tables) {
+            int n = a.new_len[t / a.Hkv];
+            n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
+            nb[i] = chunk_blocks(n, G, rows, a.rows_lo, a.rows_hi);
+            steps[i] = nb[i] ? ((a.len[2 * t] + 31) >> 5) + ((a.len[2 * t + 1] + 31) >> 5) + ((n + 31) >> 5) : 0;
+        }
+        sum += nb[i] * steps[i];
+        count += nb[i];
+    }
+    int total, blocks;
+    block_excl_scan<int>(sum, lds, &total);
+    int block = block_excl_scan<int>(count, lds, &blocks);
+    const int quantum = max((total + a.pieces - 1) / max(a.pieces - blocks / 2, a.pieces / 4), kChunkWaves);
+    int pieces = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) pieces += nb[i] * ((steps[i] + quantum - 1) / quantum);
+    int all, at = block_excl_scan<int>(pieces, lds, &all);
+    if ((int)blockIdx.x >= all) return RowPiece{-1, 0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int each = (steps[i] + quantum - 1) / quantum, next = at + nb[i] * each;
+        if ((int)blockIdx.x >= at && (int)blockIdx.x < next) {
+            const int k = (int)blockIdx.x - at, blk = k / each;
+            lds[0] = t0 + i;
+            lds[1] = blk;
+            lds[2] = k - blk * each;
+            lds[3] = each;
+            lds[4] = block + blk;
+        }
+        at = next;
+        block += nb[i];
+    }
+    __syncthreads();
+    const RowPiece p{__builtin_amdgcn_readfirstlane(lds[0]), __builtin_amdgcn_readfirstlane(lds[1]),
+                     __builtin_amdgcn_readfirstlane(lds[2]), __builtin_amdgcn_readfirstlane(lds[3]),
+                     __builtin_amdgcn_readfirstlane(lds[4])};
+    __syncthreads();
+    return p;
+}
+
 template <int LI, int RT, bool MOD>
 __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : (RT == 2 ? 2 : 1)) void chunk_rows(ChunkArgs a)
 {
@@ -469,6 +526,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
             float ml[kChunkWaves][2][16];
             int last;
         } merge;
+        int find[8];
     };
     __shared__ __align__(1024) Shared lds;
     __shared__ RowsLds<RT> Q;
@@ -476,11 +534,32 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
     const int lane = lane_id(), wave = wave_index();
     const int c = lane & 15, quarter = lane >> 4;
     const int G = a.Hq / a.Hkv;
-    // KV heads fastest: with eight of them a table's workgroups share an XCD's L2
-    const int item = (int)blockIdx.x / a.Hkv, h = (int)blockIdx.x - item * a.Hkv;
-    const int block = item / a.splits, split = item - block * a.splits;
-    const SeqBlock sb = find_block(a, block, kRows, a.rows_lo, a.rows_hi);
-    if (sb.b < 0) return;
+    // Which piece of which row block: every block has as many pieces as its table's steps want.
+    SeqBlock sb;
+    int h, split, splits;
+    long long slot_no;   // the block's number (its arrival word)
+    long long part_no;   // its first piece's state
+    if (a.splits == 1) {  // none is split
+        const int item = (int)blockIdx.x / a.Hkv;
+        h = (int)blockIdx.x - item * a.Hkv;
+        sb = find_block(a, item, kRows, a.rows_lo, a.rows_hi);
+        if (sb.b < 0) return;
+        split = 0;
+        splits = 1;
+        slot_no = part_no = 0;
+    } else {
+        const RowPiece p = row_piece(a, kRows, lds.find);
+        if (p.table < 0) return;
+        sb.b = p.table / a.Hkv;
+        h = p.table - sb.b * a.Hkv;
+        sb.blk = p.blk;
+        split = p.split;
+        splits = p.splits;
+        slot_no = p.block;
+        part_no = (int)blockIdx.x - split;
+        sequence_rows(a, sb);
+        if (sb.blk * kRows >= sb.n * G) return;  // (lengths that do not sum to total_new)
+    }
     const int first = a.seq_len[sb.b];
     const int rows = sb.n * G, r0 = sb.blk * kRows;
     // the queries' loads first, then the table's lengths and first pages, whose loads follow each other
@@ -499,9 +578,6 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
     const int own = last / G + 1;  // tokens of the chunk that some row sees
     const int s_hi = (len_hi + 31) >> 5, s_lo = (len_lo + 31) >> 5, s_own = (own + 31) >> 5;
     const int steps = s_hi + s_lo + s_own;
-    // no more workgroups than give every wave a step
-    const int splits = min(a.splits, (steps + kChunkWaves - 1) / kChunkWaves);
-    if (split >= splits) return;
     const int begin = (int)((long long)steps * split / splits), end = (int)((long long)steps * (split + 1) / splits);
     const int32_t* table = a.page_table + (long long)t * a.p_max;
 
@@ -585,9 +661,8 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
 
     // the waves' states, 16 rows at a time: 16 threads a row, eight dims each
     const int row = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8;
-    const long long slot_no = (long long)block * a.Hkv + h;
     auto part_of = [&](int k) {
-        return span(a.part + (slot_no * a.splits + k) * kRows * kChunkPart, kRows * kChunkPart * 4);
+        return span(a.part + (part_no + k) * kRows * kChunkPart, kRows * kChunkPart * 4);
     };
     auto write = [&](int at, const float (&o)[8], float m, float sum) {
         if (at >= rows) return;

@@ -268,24 +268,25 @@ struct ChunkArgs {
     float* score;          // [total_new][Hkv]
     unsigned long long* arrive;  // arrival word per row block (split ones)
     float* part;           // [row block][split][row] partial states {acc[kD], max, sum}
-    int splits;            // workgroups per row block
-    int blocks;            // row blocks of a KV head that the launch may have
+    int splits;            // few rows: 1 if none is split; short scores: workgroups per table
+    int pieces;            // few rows: the pieces that all row blocks are cut into, about
     int rows_lo, rows_hi;  // the launch takes sequences with that many rows (new tokens x G)
     int layout;
 };
 constexpr int kChunkPart = kD + 4;  // floats of a partial state (16-byte rows)
 
 // How a chunk attention call is laid out: sequences of at most kChunkFewRows rows (new tokens x query heads
-// of a KV head) in blocks of 16 or 32 rows, each with few_splits workgroups; longer ones in blocks of
+// of a KV head) in blocks of 16 or 32 rows, which up to kRowPieces workgroups share; longer ones in blocks of
 // kChunkRows, all of them cut into kTileShares equal shares.  A function of what the workspace size is
 // told.
 constexpr int kChunkFewRows = 64;
 constexpr int kChunkRows = 256;
 constexpr int kTileThreads = 512;  // of a workgroup on kChunkRows rows
 constexpr int kTileShares = 256;   // one for each CU
+constexpr int kRowPieces = 1024;   // four for each CU
 struct ChunkPlan {
-    int few_splits;
-    long long few_blocks;  // of all KV heads
+    bool few_split;        // few rows: there are so few blocks that they are split
+    long long few_blocks;  // row blocks of 16 there can be, of all KV heads
     long long few_part;    // floats of partial states
     bool many;             // there can be longer sequences
     long long bytes;

@@ -22,12 +22,11 @@ ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_n
     ChunkPlan p{};
     const long long G = Hq / Hkv, rows = total_new * G;
     const long long seqs = B < total_new ? B : total_new;
-    const long long steps = p_max / 2 + total_new / 32 + 2;  // 32-token steps of the longest table there can be
     auto clamp = [](long long x, long long lo, long long hi) { return x < lo ? lo : (x > hi ? hi : x); };
-    // few rows: about 1024 workgroups, a step for each of their waves
-    p.few_splits = seqs ? (int)clamp(1024 / (Hkv * seqs), 1, clamp(steps / 4, 1, 64)) : 1;
     p.few_blocks = Hkv * clamp(rows / 16 + 2 * seqs, 0, seqs * (kChunkFewRows / 16));  // (in blocks of 32: two each)
-    p.few_part = p.few_splits > 1 ? p.few_blocks * p.few_splits * 16 * kChunkPart : 0;
+    p.few_split = B * Hkv <= kRowPieces && Hkv * seqs < kRowPieces;
+    // (row_piece makes at most kRowPieces and one per block of them, of 16 rows; of 32 half as many)
+    p.few_part = p.few_split ? (kRowPieces + p.few_blocks) * 16 * kChunkPart : 0;
     p.many = rows > kChunkFewRows;
     p.bytes = align256((p.few_blocks + kTileShares) * 8) + align256(p.few_part * 4) +
               (p.many ? 2ll * kTileShares * kChunkRows * kChunkPart * 4 : 0);
@@ -63,11 +62,15 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     a.rows_hi = rows > kChunkFewRows ? 16 : kChunkFewRows;
     a.part = part;
     const int rt = rows > 16 && rows <= kChunkFewRows ? 2 : 1;
-    // (half as many with two row tiles, of which a CU holds half as many)
-    a.splits = rt == 2 && plan.few_splits > 1 ? plan.few_splits / 2 : plan.few_splits;
+    a.splits = plan.few_split ? 0 : 1;
+    a.pieces = kRowPieces / rt;  // (a CU holds half as many workgroups with two row tiles)
     const long long per = 16 * rt, most = rows < a.rows_hi ? rows : a.rows_hi;
     const long long whole = args.total_new * G / per + seqs, each = seqs * ((most + per - 1) / per);
-    return launch(a, rt, (whole < each ? whole : each) * a.Hkv * a.splits, 4 * kWave);
+    const long long blocks = (whole < each ? whole : each) * a.Hkv;
+    if (!plan.few_split) return launch(a, rt, blocks, 4 * kWave);
+    // a piece has at least a step for each of its four waves, a table at most a step per page and two of its own
+    const long long pieces = blocks * ((a.p_max + 4 + 3) / 4), cap = a.pieces + blocks;
+    return launch(a, rt, pieces < cap ? pieces : cap, 4 * kWave);
 }
 
 hipError_t launch_chunk_scores(const ChunkArgs& args, bool mod, hipStream_t st)

@@ -260,6 +260,7 @@ bool rows_valid(const void* p, int64_t stride, int64_t heads, int64_t rows)
 {
     return p && (uintptr_t)p % 16 == 0 && stride % 8 == 0 && (stride >= heads * kD || rows <= 1) && stride >= 0;
 }
+constexpr int64_t kMaxStride = 1 << 24;  // chunk kernels: 32 rows stay within 31-bit offsets
 
 // What both chunk entry points check, and the arguments they share.
 diffkv_status chunk_call(const diffkv_layout* layout, const diffkv_cache* cache, int64_t total_new, int32_t max_new,
@@ -279,6 +280,7 @@ diffkv_status chunk_call(const diffkv_layout* layout, const diffkv_cache* cache,
     if (!new_len || !rows_valid(q, q_stride, num_q_heads, total_new) ||
         !rows_valid(k, k_stride, cache->num_kv_heads, total_new))
         return DIFFKV_E_INVAL;
+    if (q_stride > kMaxStride || k_stride > kMaxStride) return DIFFKV_E_UNSUPPORTED;
     a.p_max = layout->p_max;
     a.page_bytes = layout->page_bytes;
     a.num_pages = cache->num_pages;
@@ -299,13 +301,13 @@ diffkv_status chunk_call(const diffkv_layout* layout, const diffkv_cache* cache,
     a.k_stride = k_stride;
     const float log2e = 1.4426950408889634f;
     const float cap = form ? form->cap : 0.0f;
-    a.scale = cap > 0.0f ? sm_scale : sm_scale * log2e;
     a.cap_in = cap > 0.0f ? 2.0f * log2e / cap : 0.0f;
-    a.cap_out = cap * log2e;
+    a.cap = cap;
     a.slopes = form ? form->slopes : nullptr;
     a.window = form && form->window > 0 ? form->window : INT32_MAX;
     a.layout = layout_index(layout);
     mod = cap > 0.0f || a.slopes || a.window != INT32_MAX;
+    a.scale = mod ? sm_scale : sm_scale * log2e;
     return DIFFKV_OK;
 }
 
@@ -596,6 +598,7 @@ diffkv_status diffkv_chunk_attention(const diffkv_layout* layout, const diffkv_c
                                        sm_scale, form, a, mod);
     if (s != DIFFKV_OK || a.total_new == 0) return s;
     if (!rows_valid(v, v_stride, a.Hkv, total_new) || !out || (uintptr_t)out % 16 != 0) return DIFFKV_E_INVAL;
+    if (v_stride > kMaxStride) return DIFFKV_E_UNSUPPORTED;
     const ChunkPlan plan = chunk_plan(a.B, a.Hq, a.Hkv, total_new, a.p_max);
     if (!ws || (int64_t)ws_bytes < plan.bytes) return DIFFKV_E_WORKSPACE;
     a.v = v;

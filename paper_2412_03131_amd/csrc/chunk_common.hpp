@@ -270,20 +270,21 @@ __device__ __forceinline__ RowOperands row_operands(const u4 (&x)[kNG], int quar
 }
 
 // ---- the forms of a score --------------------------------------------------------
-// sm_scale q.k capped by cap tanh(x / cap), with slope (c - p) added; log2 units.
+// sm_scale q.k capped by cap tanh(x / cap), with slope (c - p) added, in natural units (a slope or
+// a normalizer times log2(e) would be rounded where a score is still far from its row's
+// largest: 2^-24 of biases of 40 and more).
 struct ScoreForm {
-    float cap_in, cap_out;  // 2 log2(e) / cap, cap log2(e); cap_in 0: no cap
-    float slope;            // times log2(e); 0: none
+    float cap_in, cap;  // 2 log2(e) / cap; 0: no cap
+    float slope;        // 0: none
 };
-// x: scaled score in natural units (with a cap) or log2 units (without)
 __device__ __forceinline__ float formed(float x, const ScoreForm& f, float away)
 {
     if (f.cap_in != 0.0f) {
         // tanh y = 1 - 2 / (1 + exp 2y): exact limits at both ends, 2^-23 absolute
         const float ex = __builtin_amdgcn_exp2f(x * f.cap_in);
-        x = f.cap_out * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + ex));
+        x = f.cap * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + ex));
     }
-    return x - f.slope * away;
+    return __builtin_fmaf(-f.slope, away, x);
 }
 
 }  // namespace dkv

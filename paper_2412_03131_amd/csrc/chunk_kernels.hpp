@@ -165,7 +165,7 @@ struct RowsLds {
 };
 template <int RT>
 struct Rows {
-    float unit[RT];   // logit = unit * product sum (log2 units, or natural ones with a cap)
+    float unit[RT];   // logit = unit * product sum (log2 units, natural ones with a score form)
     int p[RT];        // position in the sequence
     ScoreForm form[RT];
     float m[RT], l[RT];
@@ -213,6 +213,19 @@ __device__ __forceinline__ h8 pack_weights(const float (&w)[2][4])
         bits[2 * t + 1] = __builtin_bit_cast(uint32_t, b);
     }
     return __builtin_bit_cast(h8, bits);
+}
+// What the rounding left of them (two 11-bit parts hold 22 bits).  With one row tile, where the
+// matrix cores have time to spare, the weights enter whole: the results' error against 64 bits is then the
+// values' and their own rounding alone (1.4 times a 32-bit computation's rounded once; 1.5 to 1.7 with
+// rounded weights).
+__device__ __forceinline__ h8 pack_rest(const float (&w)[2][4], h8 P)
+{
+    float rest[2][4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) rest[t][r] = w[t][r] - (float)P[4 * t + 2 * (r & 1) + (r >> 1)];
+    return pack_weights(rest);
 }
 template <int RT>
 __device__ __forceinline__ void softmax_step(Rows<RT>& R, const float (&unit)[RT], float (&x)[RT][2][4], h8 (&P)[RT])
@@ -303,8 +316,10 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
     h8 P[RT];
     float unit[RT];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? 1.0f : R.unit[rt];
+    for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? kChunkLog2e : R.unit[rt];
     softmax_step<RT>(R, unit, x, P);
+    h8 rest;
+    if constexpr (RT == 1) rest = pack_rest(x[0], P[0]);
 #pragma unroll
     for (int g = 0; g < kNG; ++g) {
         keep_order();
@@ -345,6 +360,7 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
             const h8 V = __builtin_bit_cast(h8, v);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, P[rt], R.acc[rt][dt]);
+            if constexpr (RT == 1) R.acc[0][dt] = mfma_k32(V, rest, R.acc[0][dt]);
         }
     }
 }
@@ -419,8 +435,10 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const RowsLds<RT>& Q, cons
     h8 P[RT];
     float unit[RT];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? 1.0f : R.unit[rt];
+    for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? kChunkLog2e : R.unit[rt];
     softmax_step<RT>(R, unit, x, P);
+    h8 rest;
+    if constexpr (RT == 1) rest = pack_rest(x[0], P[0]);
     // values: the quarter's eight tokens of dims 16 dt + c
     bool odd = false;
 #pragma unroll
@@ -439,6 +457,7 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const RowsLds<RT>& Q, cons
         const h8 V = __builtin_bit_cast(h8, w);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, P[rt], R.acc[rt][dt]);
+        if constexpr (RT == 1) R.acc[0][dt] = mfma_k32(V, rest, R.acc[0][dt]);
     }
     if (__any(odd)) odd_values<RT>(R, x, v, i0, n, first, a, c, quarter);
 }
@@ -627,7 +646,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
         }
         R.unit[rt] = o.unit * a.scale;
         R.p[rt] = first + j;
-        R.form[rt] = ScoreForm{a.cap_in, a.cap_out, MOD && a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f};
+        R.form[rt] = ScoreForm{a.cap_in, a.cap, MOD && a.slopes ? a.slopes[hq] : 0.0f};
         R.m[rt] = kLowest;
         R.l[rt] = 0.0f;
 #pragma unroll
@@ -989,7 +1008,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
         sums[rt] = o.sums;
         R.unit[rt] = o.unit * a.scale;
         R.p[rt] = first + j;
-        R.form[rt] = ScoreForm{a.cap_in, a.cap_out, MOD && a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f};
+        R.form[rt] = ScoreForm{a.cap_in, a.cap, MOD && a.slopes ? a.slopes[hq] : 0.0f};
         R.m[rt] = kLowest;
         R.l[rt] = 0.0f;
 #pragma unroll
@@ -1116,7 +1135,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
             };
             float unit[RT];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? 1.0f : R.unit[rt];
+            for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? kChunkLog2e : R.unit[rt];
             {
                 // the values of the step before beside this step's exponentials
                 float x[RT][2][4];
@@ -1322,8 +1341,8 @@ __device__ __forceinline__ bool score_short(int n, int G) { return (n + 3) / 4 *
 struct ScoreSet {
     h8 q[kNG][kWave];
     h8 sums[kWave];
-    float lse[16];    // log2 units; +inf: no such row
-    float slope[16];  // log2 units
+    float lse[16];    // log2 units (natural ones with a score form); +inf: no such row
+    float slope[16];
 };
 
 // One set on its way, by one wave: row m = c is at `offset` bytes from `base`; its queries go straight to
@@ -1410,8 +1429,8 @@ __device__ __forceinline__ void score_use(const ScoreSet& S, const ChunkArgs& a,
         for (int r = 0; r < 4; ++r) {
             if constexpr (MOD) {
                 const int away = p + (FOUR ? 0 : 4 * r) - pos[kt];
-                const float y = formed(sum[kt][r] * unit, ScoreForm{a.cap_in, a.cap_out, slope[r]}, (float)away) - lse[r];
-                x[r] = away < a.window ? y : -INFINITY;
+                const float y = formed(sum[kt][r] * unit, ScoreForm{a.cap_in, a.cap, slope[r]}, (float)away) - lse[r];
+                x[r] = away < a.window ? y * kChunkLog2e : -INFINITY;
             } else {
                 x[r] = __builtin_fmaf(sum[kt][r], unit, -lse[r]);
             }
@@ -1520,8 +1539,8 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
         const bool there = j < n && g < G;
         const int jj = there ? j : j0, hq = h * G + (there ? g : 0);
         score_load(S, a.q + (sb.row0 + j0) * a.q_stride, 2 * ((jj - j0) * (int)a.q_stride + hq * kD), ln >> 4);
-        row_lse = there ? a.lse_in[(sb.row0 + jj) * a.Hq + hq] * kChunkLog2e : INFINITY;
-        if constexpr (MOD) row_slope = a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f;
+        row_lse = there ? a.lse_in[(sb.row0 + jj) * a.Hq + hq] * (MOD ? 1.0f : kChunkLog2e) : INFINITY;
+        if constexpr (MOD) row_slope = a.slopes ? a.slopes[hq] : 0.0f;
     };
     for (; blk < blocks && cur < stop; ++blk, ++piece) {
         const long long from = table_at + units_to(tb, blk), to = table_at + units_to(tb, blk + 1);
@@ -1764,8 +1783,8 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores_short(Chu
         u4 x[kNG];
 #pragma unroll
         for (int g4 = 0; g4 < kNG; ++g4) x[g4] = *reinterpret_cast<const u4*>(q + g4 * kG);
-        const float lse = there ? a.lse_in[row * a.Hq + hq] * kChunkLog2e : INFINITY;
-        const float slope = MOD && a.slopes ? a.slopes[hq] * kChunkLog2e : 0.0f;
+        const float lse = there ? a.lse_in[row * a.Hq + hq] * (MOD ? 1.0f : kChunkLog2e) : INFINITY;
+        const float slope = MOD && a.slopes ? a.slopes[hq] : 0.0f;
         ScoreSet& S = sh.sets[wave];
 #pragma unroll
         for (int g4 = 0; g4 < kNG; ++g4) S.q[g4][lane] = __builtin_bit_cast(h8, x[g4]);

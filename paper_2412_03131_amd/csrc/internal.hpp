@@ -258,8 +258,8 @@ struct ChunkArgs {
     const uint16_t* k;
     const uint16_t* v;
     long long q_stride, k_stride, v_stride;  // halfs from one token's row to the next
-    float scale;           // sm_scale, times log2(e) without a cap
-    float cap_in, cap_out; // 2 log2(e) / cap and cap log2(e); 0: no cap
+    float scale;           // sm_scale, times log2(e) without a score form
+    float cap_in, cap;     // 2 log2(e) / cap and cap; 0: no cap
     const float* slopes;   // [Hq] or null
     int window;            // INT32_MAX: none
     uint16_t* out;         // [total_new][Hq][kD]

@@ -39,9 +39,13 @@ constexpr float kLowest = -1e30f;  // a running max before the first key (finite
 __device__ __forceinline__ f4 mfma_k32(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f4 mfma_k16(h4 a, h4 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0); }
 
-// fp16 results that overflow become the largest finite value (MODE.FP16_OVFL): the value
-// s c + z of a group's largest code can round past it.  True infinities stay.
-__device__ __forceinline__ void set_fp16_saturate() { __builtin_amdgcn_s_setreg(1 | (23 << 6) | (0 << 11), 1); }
+// s c + z of a group's largest code can round past the largest finite fp16 (s >= 0, z finite): it
+// becomes that.  (The mode bit for it, MODE.FP16_OVFL, also loses NaN operands of matrix products.)
+__device__ __forceinline__ uint32_t finite_pair(h2 x)
+{
+    const h2 top = {(_Float16)65504.0f, (_Float16)65504.0f};
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(x, top));
+}
 
 // ---- loads -----------------------------------------------------------------------
 // Through a buffer resource: a uniform base and 32-bit offsets.  (With 64-bit addresses the

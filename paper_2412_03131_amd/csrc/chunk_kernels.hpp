@@ -151,8 +151,8 @@ __device__ __forceinline__ void value_pairs(uint32_t w, h2 s02, h2 z02, h2 s13, 
         y02 = __builtin_bit_cast(h2, (x & m) | 0x64006400u) + m1024;
         y13 = __builtin_elementwise_fma(__builtin_bit_cast(h2, (x & (m << VB)) | 0x64006400u), inv, off);
     }
-    p02 = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(s02, y02, z02));
-    p13 = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(s13, y13, z13));
+    p02 = finite_pair(__builtin_elementwise_fma(s02, y02, z02));
+    p13 = finite_pair(__builtin_elementwise_fma(s13, y13, z13));
 }
 
 // The rows a wave works on: 16 RT of them, column c of tile rt is row 16 rt + c of its block.
@@ -480,52 +480,75 @@ constexpr int kRowTables = 1024;  // (more are not split)
 struct RowPiece {
     int table, blk, split, splits, block;
 };
-__device__ __forceinline__ RowPiece row_piece(const ChunkArgs& a, int rows, int* lds)
+__device__ __forceinline__ int piece_quantum(const ChunkArgs& a, int total, int blocks)
 {
-    const int tables = a.B * a.Hkv, G = a.Hq / a.Hkv;
+    return max((total + a.pieces - 1) / max(a.pieces - blocks / 2, a.pieces / 4), kChunkWaves);
+}
+// A table's row blocks and the steps of each.
+__device__ __forceinline__ void row_steps(const ChunkArgs& a, int rows, int t, int& steps, int& nb)
+{
+    int n = a.max_new == 1 && a.total_new == a.B ? 1 : a.new_len[t / a.Hkv];
+    n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
+    nb = chunk_blocks(n, a.Hq / a.Hkv, rows, a.rows_lo, a.rows_hi);
+    // (at most 2^18, so that the sums of 4096 blocks stay below 2^31: a longer table's pieces are longer)
+    steps = nb ? min(((a.len[2 * t] + 31) >> 5) + ((a.len[2 * t + 1] + 31) >> 5) + ((n + 31) >> 5), 1 << 18) : 0;
+}
+__device__ __forceinline__ RowPiece row_piece(const ChunkArgs& a, int rows, long long* lds)
+{
+    const int tables = a.B * a.Hkv, me = (int)blockIdx.x;
+    if (tables <= kWave) {  // a lane per table, every wave by itself
+        const int lane = lane_id();
+        int steps = 0, nb = 0;
+        if (lane < tables) row_steps(a, rows, lane, steps, nb);
+        const int total = __builtin_amdgcn_readlane(wave_incl_scan(nb * steps), kWave - 1);
+        const int blocks = wave_incl_scan(nb);
+        const int quantum = piece_quantum(a, total, __builtin_amdgcn_readlane(blocks, kWave - 1));
+        const int each = (steps + quantum - 1) / quantum;
+        const int end = wave_incl_scan(nb * each);
+        const unsigned long long past = __ballot(end > me);
+        if (!past) return RowPiece{-1, 0, 0, 0, 0};
+        const int l = __builtin_ctzll(past);
+        const int e = __builtin_amdgcn_readlane(each, l), k = me - __builtin_amdgcn_readlane(end - nb * each, l), blk = k / e;
+        return RowPiece{l, blk, k - blk * e, e, __builtin_amdgcn_readlane(blocks - nb, l) + blk};
+    }
     constexpr int kPer = kRowTables / (kChunkWaves * kWave);
     int steps[kPer], nb[kPer], sum = 0, count = 0;
     const int t0 = (int)threadIdx.x * kPer;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const int t = t0 + i;
         steps[i] = nb[i] = 0;
-        if (t < tables) {
-            int n = a.new_len[t / a.Hkv];
-            n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
-            nb[i] = chunk_blocks(n, G, rows, a.rows_lo, a.rows_hi);
-            steps[i] = nb[i] ? ((a.len[2 * t] + 31) >> 5) + ((a.len[2 * t + 1] + 31) >> 5) + ((n + 31) >> 5) : 0;
-        }
+        if (t0 + i < tables) row_steps(a, rows, t0 + i, steps[i], nb[i]);
         sum += nb[i] * steps[i];
         count += nb[i];
     }
-    int total, blocks;
-    block_excl_scan<int>(sum, lds, &total);
-    int block = block_excl_scan<int>(count, lds, &blocks);
-    const int quantum = max((total + a.pieces - 1) / max(a.pieces - blocks / 2, a.pieces / 4), kChunkWaves);
-    int pieces = 0;
+    long long both;
+    const long long before = block_excl_scan<long long>(((long long)count << 32) | sum, lds, &both);
+    const int quantum = piece_quantum(a, (int)(both & 0xffffffff), (int)(both >> 32));
+    int pieces = 0, block = (int)(before >> 32);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) pieces += nb[i] * ((steps[i] + quantum - 1) / quantum);
-    int all, at = block_excl_scan<int>(pieces, lds, &all);
-    if ((int)blockIdx.x >= all) return RowPiece{-1, 0, 0, 0, 0};
+    long long all, at = block_excl_scan<long long>(pieces, lds, &all);
+    if (me >= all) return RowPiece{-1, 0, 0, 0, 0};
+    int* found = reinterpret_cast<int*>(lds);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const int each = (steps[i] + quantum - 1) / quantum, next = at + nb[i] * each;
-        if ((int)blockIdx.x >= at && (int)blockIdx.x < next) {
-            const int k = (int)blockIdx.x - at, blk = k / each;
-            lds[0] = t0 + i;
-            lds[1] = blk;
-            lds[2] = k - blk * each;
-            lds[3] = each;
-            lds[4] = block + blk;
+        const int each = (steps[i] + quantum - 1) / quantum;
+        const long long next = at + nb[i] * each;
+        if (me >= at && me < next) {
+            const int k = me - (int)at, blk = k / each;
+            found[0] = t0 + i;
+            found[1] = blk;
+            found[2] = k - blk * each;
+            found[3] = each;
+            found[4] = block + blk;
         }
         at = next;
         block += nb[i];
     }
     __syncthreads();
-    const RowPiece p{__builtin_amdgcn_readfirstlane(lds[0]), __builtin_amdgcn_readfirstlane(lds[1]),
-                     __builtin_amdgcn_readfirstlane(lds[2]), __builtin_amdgcn_readfirstlane(lds[3]),
-                     __builtin_amdgcn_readfirstlane(lds[4])};
+    const RowPiece p{__builtin_amdgcn_readfirstlane(found[0]), __builtin_amdgcn_readfirstlane(found[1]),
+                     __builtin_amdgcn_readfirstlane(found[2]), __builtin_amdgcn_readfirstlane(found[3]),
+                     __builtin_amdgcn_readfirstlane(found[4])};
     __syncthreads();
     return p;
 }
@@ -545,11 +568,10 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
             float ml[kChunkWaves][2][16];
             int last;
         } merge;
-        int find[8];
+        long long find[kChunkWaves];
     };
     __shared__ __align__(1024) Shared lds;
     __shared__ RowsLds<RT> Q;
-    set_fp16_saturate();
     const int lane = lane_id(), wave = wave_index();
     const int c = lane & 15, quarter = lane >> 4;
     const int G = a.Hq / a.Hkv;
@@ -955,7 +977,6 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
     __shared__ __align__(1024) Shared sh;
     auto& slots = sh.slots;
     auto& bufs = sh.bufs;
-    set_fp16_saturate();
     const int lane = lane_id(), wave = wave_index();
     const int c = lane & 15, quarter = lane >> 4;
     const int G = a.Hq / a.Hkv;

@@ -16,8 +16,10 @@ def kept_tokens(cache):
     """Per table: keys [n, D] and values [n, D] in 64 bits, positions, scores, and where they are
     (page, section, slot), the high section first."""
     L = cache.L
-    pool, table = cache.pool.cpu().numpy(), cache.page_table.cpu().numpy()
+    table = cache.page_table.cpu().numpy()
     lens = cache.len.cpu().numpy()
+    used = np.unique(table[(table >= 0) & (table < cache.num_pages)])
+    pool = dict(zip(used.tolist(), cache.pool[torch.from_numpy(used).long().to(cache.pool.device)].cpu().numpy()))
     out = []
     for t in range(cache.num_tables):
         ks, vs, pos, score, where = [], [], [], [], []
@@ -27,6 +29,8 @@ def kept_tokens(cache):
                 n = min(T, int(lens[t, sec]) - u0)
                 i = u0 // T
                 page = int(table[t, i if sec == 0 else L.p_max - 1 - i])
+                if page not in pool:  # an ID outside the pool counts no token
+                    continue
                 b = pool[page]
 
                 def seg(off, size):
@@ -49,9 +53,10 @@ def kept_tokens(cache):
 
 def score_at(cache, where):
     """Scores now in the pages at `where`."""
-    pool = cache.pool.cpu().numpy()
     L = cache.L
-    return np.array([pool[p, L.off_score[s] + 4 * i:L.off_score[s] + 4 * i + 4].view(np.float32)[0] for p, s, i in where],
+    used = np.unique([p for p, _, _ in where]).astype(np.int64)
+    pool = dict(zip(used.tolist(), cache.pool[torch.from_numpy(used).to(cache.pool.device)].cpu().numpy()))
+    return np.array([pool[p][L.off_score[s] + 4 * i:L.off_score[s] + 4 * i + 4].view(np.float32)[0] for p, s, i in where],
                     np.float64)
 
 
@@ -105,13 +110,15 @@ def rotated(x, pos, freq, style, scale):
     return y
 
 
-def filled(dk, layout, B, Hkv, lens, seed, max_len=None, prune=0.3, high=0.4, device="cuda", kscale=1.0):
+def filled(dk, layout, B, Hkv, lens, seed, max_len=None, prune=0.3, high=0.4, device="cuda", kscale=1.0, before=0):
     """A cache that saw lens[b] tokens of each sequence, high / low / pruned by quota."""
     rng = np.random.default_rng(seed)
     lens = np.asarray(lens, np.int32)
     L = dk.layout(max_seq_len=max_len or int(lens.max(initial=1)) + 512, **layout)
     pages = int(sum(Hkv * (2 * (int(n) // 16 + 2)) for n in lens)) + 8
-    cache = dk.Cache(L, pages, B, Hkv, device=device, ring=torch.from_numpy(rng.permutation(pages).astype(np.int32)))
+    # (`before` pages that nothing uses come first in the pool)
+    ring = np.concatenate([before + rng.permutation(pages), np.arange(before)]).astype(np.int32)
+    cache = dk.Cache(L, before + pages, B, Hkv, device=device, ring=torch.from_numpy(ring))
     rows = int(lens.sum())
     if rows:
         k = rng.standard_normal((rows, Hkv, D)) * kscale

@@ -390,7 +390,7 @@ diffkv_status diffkv_rope_frequencies(int32_t rot_dim, double base, int32_t scal
  *   cap > 0:         x <- cap * tanh(x / cap);
  *   slopes != NULL:  x <- x - slopes[hq] * (p - c)  (device fp32 [num_q_heads]);
  *   window > 0:      the key is seen only if p - c < window.
- * cap finite and >= 0, window >= 0, else DIFFKV_E_INVAL.
+ * cap 0 or from 1e-30 to 1e30, window >= 0, else DIFFKV_E_INVAL.
  */
 typedef struct diffkv_score_form {
     float cap;
@@ -413,19 +413,22 @@ typedef struct diffkv_score_form {
  *            written, and rows that no sequence owns are left as they were.
  *   q, k, v  device fp16: row r, head h at q + r*q_stride + h*head_dim (slices
  *            of a fused projection can be passed), 16-byte aligned, strides in
- *            elements, multiples of 8, at least heads*head_dim
+ *            elements, multiples of 8, at least heads*head_dim (any value with
+ *            one row) and at most 2^24 (DIFFKV_E_UNSUPPORTED above)
  *   out      device fp16 [total_new][num_q_heads][head_dim], 16-byte aligned
  *   lse      device fp32 [total_new][num_q_heads] (natural log of the softmax
  *            denominator) or NULL
  *   ws       diffkv_workspace_size(DIFFKV_OP_CHUNK_ATTENTION, ...) bytes, no
- *            clearing needed; calls that may overlap need one each
+ *            clearing needed, 16-byte aligned; calls that may overlap need one
+ *            each
  * The cache is read only.  A page ID outside the pool counts no tokens.
- * sm_scale positive and finite (DIFFKV_E_INVAL otherwise).  The layouts of
+ * sm_scale above 0 and at most 1e30 (DIFFKV_E_INVAL otherwise).  The layouts of
  * diffkv_layout_init's list, up to 8 query heads per KV head.
  * Precision: q . k_hat exact up to fp32 summation, fp32 softmax statistics;
- * weights and v_hat are rounded to fp16 (2^-11 each), products summed in fp32,
- * and out is rounded once.  A non-finite own value reaches only the rows that
- * see its token.
+ * v_hat is rounded to fp16 (2^-11), the weights too where a sequence has more
+ * than 16 rows (new tokens times query heads per KV head), products are summed
+ * in fp32, and out is rounded once.  A NaN or infinite own key or value reaches
+ * only the rows that see its token.
  */
 diffkv_status diffkv_chunk_attention(const diffkv_layout* layout, const diffkv_cache* cache,
                                      int64_t total_new, int32_t max_new, const int32_t* new_len,

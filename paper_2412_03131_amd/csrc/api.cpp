@@ -272,7 +272,7 @@ diffkv_status chunk_call(const diffkv_layout* layout, const diffkv_cache* cache,
     if (total_new < 0 || max_new < 0 || total_new > INT32_MAX / 4) return DIFFKV_E_INVAL;
     if (num_q_heads <= 0 || num_q_heads % cache->num_kv_heads != 0) return DIFFKV_E_INVAL;
     if (!(sm_scale > 0.0f) || sm_scale > 1e30f) return DIFFKV_E_INVAL;
-    if (form && (!(form->cap >= 0.0f) || form->cap > 1e30f || form->window < 0)) return DIFFKV_E_INVAL;
+    if (form && (!(form->cap >= 0.0f) || form->cap > 1e30f || (form->cap > 0.0f && form->cap < 1e-30f) || form->window < 0)) return DIFFKV_E_INVAL;
     if (!layout_kernels_supported(layout)) return DIFFKV_E_UNSUPPORTED;
     if (num_q_heads / cache->num_kv_heads > 8) return DIFFKV_E_UNSUPPORTED;
     memset(&a, 0, sizeof(a));
@@ -357,7 +357,7 @@ diffkv_status diffkv_workspace_size(int32_t op, const diffkv_layout* layout, int
     case DIFFKV_OP_CHUNK_SIGNIFICANCE:
         if (num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || total_new < 0) return DIFFKV_E_INVAL;
         *bytes = op == DIFFKV_OP_CHUNK_ATTENTION
-                     ? (size_t)chunk_plan(num_seqs, num_q_heads, num_kv_heads, total_new, layout->p_max).bytes
+                     ? (size_t)chunk_plan(num_seqs, num_q_heads, num_kv_heads, total_new).bytes
                      : (size_t)kScoreBytes;
         return DIFFKV_OK;
     default:
@@ -599,8 +599,9 @@ diffkv_status diffkv_chunk_attention(const diffkv_layout* layout, const diffkv_c
     if (s != DIFFKV_OK || a.total_new == 0) return s;
     if (!rows_valid(v, v_stride, a.Hkv, total_new) || !out || (uintptr_t)out % 16 != 0) return DIFFKV_E_INVAL;
     if (v_stride > kMaxStride) return DIFFKV_E_UNSUPPORTED;
-    const ChunkPlan plan = chunk_plan(a.B, a.Hq, a.Hkv, total_new, a.p_max);
+    const ChunkPlan plan = chunk_plan(a.B, a.Hq, a.Hkv, total_new);
     if (!ws || (int64_t)ws_bytes < plan.bytes) return DIFFKV_E_WORKSPACE;
+    if ((uintptr_t)ws % 16 != 0) return DIFFKV_E_INVAL;
     a.v = v;
     a.v_stride = v_stride;
     a.out = out;
@@ -623,6 +624,7 @@ diffkv_status diffkv_chunk_significance(const diffkv_layout* layout, const diffk
     if (s != DIFFKV_OK || a.total_new == 0) return s;
     if (!lse || !score) return DIFFKV_E_INVAL;
     if (!ws || (int64_t)ws_bytes < kScoreBytes) return DIFFKV_E_WORKSPACE;
+    if ((uintptr_t)ws % 16 != 0) return DIFFKV_E_INVAL;
     a.arrive = static_cast<unsigned long long*>(ws);
     a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kScoreShares * 8);
     a.lse_in = lse;

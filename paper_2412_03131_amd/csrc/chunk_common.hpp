@@ -151,17 +151,6 @@ __device__ __forceinline__ void sequence_rows(const ChunkArgs& a, SeqBlock& s)
 // A row block whose steps are split over workgroups: each writes its rows' states {acc[kD], max,
 // sum} to its slot with agent-scope stores (through to memory: the workgroups may be on
 // different XCDs), and the one that arrives last reads them all back.
-__device__ __forceinline__ void put_pair(float* p, float x, float y)
-{
-    const unsigned long long v = ((unsigned long long)__float_as_uint(y) << 32) | __float_as_uint(x);
-    __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 get_pair(const float* p)
-{
-    const unsigned long long v = __hip_atomic_load(reinterpret_cast<unsigned long long*>(const_cast<float*>(p)),
-                                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-}
 // Sixteen bytes of a state with agent scope (cache policy bit 4 is sc1: past the XCD's L2).
 __device__ __forceinline__ void put_quad(__amdgpu_buffer_rsrc_t r, int lane_offset, int offset, f4 x)
 {

@@ -554,7 +554,7 @@ __device__ __forceinline__ RowPiece row_piece(const ChunkArgs& a, int rows, long
 }
 
 template <int LI, int RT, bool MOD>
-__global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : (RT == 2 ? 2 : 1)) void chunk_rows(ChunkArgs a)
+__global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 2) void chunk_rows(ChunkArgs a)
 {
     constexpr KvFmt hi = kLayoutFmts[LI].hi, lo = kLayoutFmts[LI].lo;
     constexpr int kRows = 16 * RT;
@@ -590,7 +590,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
         slot_no = part_no = 0;
     } else {
         const RowPiece p = row_piece(a, kRows, lds.find);
-        if (p.table < 0) return;
+        if (p.table < 0 || p.block >= a.blocks) return;  // (the second: lengths that do not sum to total_new)
         sb.b = p.table / a.Hkv;
         h = p.table - sb.b * a.Hkv;
         sb.blk = p.blk;
@@ -1513,7 +1513,6 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
     // consecutive shares on one XCD: they read the same tables
     const int share = gridDim.x % 8 == 0 ? ((int)blockIdx.x & 7) * ((int)gridDim.x >> 3) + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
     const long long start = share * quantum, stop = min(total_units, start + quantum);
-    const f4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
     int piece = 0;
     for (long long cur = start; cur < stop;) {
     // the table that has unit `cur`
@@ -1567,7 +1566,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
         const long long from = table_at + units_to(tb, blk), to = table_at + units_to(tb, blk + 1);
         const long long piece_from = cur, piece_end = min(stop, to);
         cur = piece_end;
-        if (n == 0) continue;
+        if (n == 0 || score_short(n, G)) continue;  // (lengths that do not sum to total_new)
         const int sec = blk < b_hi ? 0 : (blk < b_hi + b_lo ? 1 : 2);
         const int len = sec == 0 ? len_hi : (sec == 1 ? len_lo : n);
         const int tok0 = (blk - (sec == 0 ? 0 : (sec == 1 ? b_hi : b_hi + b_lo))) * kScoreBlock + wave * kScoreTokens;
@@ -1673,7 +1672,8 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
             const int low = sec == 2 ? (tok0 - wave * kScoreTokens) / kPos * HS : 0;
             // (cuts lie between position tiles: the maximum over the heads is not divided)
             auto cut = [&](long long units) { return low + (int)(max(units - kBlockUnits, 0ll) / HS) * HS; };
-            const int begin = cut(piece_from - from), end = piece_end == to ? all : cut(piece_end - from);
+            // (never past the rows that are there, also where lengths do not sum to total_new)
+            const int begin = cut(piece_from - from), end = piece_end == to ? all : min(cut(piece_end - from), all);
             // passes of kScorePass sets through three thirds of LDS: one is used, the next one's sums are
             // made, the one after is on its way (each set by one wave)
             const bool makes = wave < kScorePass;
@@ -1705,7 +1705,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
                 // cut by a share's end: the pieces' sums are added by the last of them, in order (slots and
                 // words as in chunk_tiles)
                 auto part_of = [&](int k, bool first_piece) {
-                    return a.part + (2ll * k + (first_piece ? 0 : 1)) * kScoreBlock + wave * kScoreTokens + (lane & 31);  // (lane: the token it finishes)
+                    return a.part + (2ll * k + (first_piece ? 0 : 1)) * kScoreBlock + wave * kScoreTokens + (lane & 31);
                 };
                 const int k0 = (int)(from / quantum), k1 = (int)((to - 1) / quantum);
                 if (lane < kScoreTokens) __hip_atomic_store(part_of(share, piece == 0), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

@@ -270,6 +270,7 @@ struct ChunkArgs {
     float* part;           // [row block][split][row] partial states {acc[kD], max, sum}
     int splits;            // few rows: 1 if none is split; short scores: workgroups per table
     int pieces;            // few rows: the pieces that all row blocks are cut into, about
+    int blocks;            // few rows: arrival words of row blocks
     int rows_lo, rows_hi;  // the launch takes sequences with that many rows (new tokens x G)
     int layout;
 };
@@ -288,10 +289,9 @@ struct ChunkPlan {
     bool few_split;        // few rows: there are so few blocks that they are split
     long long few_blocks;  // row blocks of 16 there can be, of all KV heads
     long long few_part;    // floats of partial states
-    bool many;             // there can be longer sequences
     long long bytes;
 };
-ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_new, long long p_max);
+ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_new);
 hipError_t launch_chunk_attention(const ChunkArgs& a, const ChunkPlan& plan, bool mod, hipStream_t st);
 // Shares of a chunk scores call (two workgroups for each CU), and the workspace: an arrival word and two
 // slots of 256 sums each.

@@ -17,7 +17,7 @@ static const void* chunk_kernel(int li, int which, bool mod)
 
 static long long align256(long long x) { return (x + 255) & ~255ll; }
 
-ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_new, long long p_max)
+ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_new)
 {
     ChunkPlan p{};
     const long long G = Hq / Hkv, rows = total_new * G;
@@ -27,9 +27,8 @@ ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_n
     p.few_split = B * Hkv <= kRowPieces && Hkv * seqs < kRowPieces;
     // (row_piece makes at most kRowPieces and one per block of them, of 16 rows; of 32 half as many)
     p.few_part = p.few_split ? (kRowPieces + p.few_blocks) * 16 * kChunkPart : 0;
-    p.many = rows > kChunkFewRows;
     p.bytes = align256((p.few_blocks + kTileShares) * 8) + align256(p.few_part * 4) +
-              (p.many ? 2ll * kTileShares * kChunkRows * kChunkPart * 4 : 0);
+              (rows > kChunkFewRows ? 2ll * kTileShares * kChunkRows * kChunkPart * 4 : 0);
     return p;
 }
 
@@ -63,6 +62,7 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     a.part = part;
     const int rt = rows > 16 && rows <= kChunkFewRows ? 2 : 1;
     a.splits = plan.few_split ? 0 : 1;
+    a.blocks = (int)(plan.few_blocks < INT32_MAX ? plan.few_blocks : INT32_MAX);
     a.pieces = kRowPieces / rt;  // (a CU holds half as many workgroups with two row tiles)
     const long long per = 16 * rt, most = rows < a.rows_hi ? rows : a.rows_hi;
     const long long whole = args.total_new * G / per + seqs, each = seqs * ((most + per - 1) / per);

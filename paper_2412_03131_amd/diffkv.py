@@ -297,19 +297,18 @@ def prompt_significance(L, new_len, q, k, sm_scale, lse=None, score=None, max_ne
     return score
 
 
-def _rows(t, what):
+def _rows(t, what, head_dim):
     """Address and row stride of [rows, heads, D] rows whose heads lie side by side (a slice of a
     fused projection may be given)."""
-    if t.dim() != 3 or t.element_size() != 2 or t.stride(2) != 1 or (t.stride(1) != t.shape[2] and t.shape[1] > 1):
-        raise ValueError("%s: 16-bit [rows, heads, head_dim] with packed heads expected" % what)
+    if t.dim() != 3 or t.dtype != torch.float16 or t.shape[2] != head_dim or t.stride(2) != 1 or (
+            t.stride(1) != head_dim and t.shape[1] > 1):
+        raise ValueError("%s: fp16 [rows, heads, %d] with packed heads expected" % (what, head_dim))
     return t.data_ptr(), t.stride(0)
 
 
 def _form(cap, window, slopes):
     if cap == 0.0 and window == 0 and slopes is None:
         return None
-    if slopes is not None and (slopes.dtype != torch.float32 or not slopes.is_contiguous()):
-        raise ValueError("slopes: contiguous fp32 [num_q_heads] expected")
     return C.byref(ScoreForm(float(cap), int(window), _ptr(slopes)))
 
 
@@ -338,10 +337,10 @@ def rotate(L, pos, inv_freq, q, k=None, style=ROPE_HALF, scale=1.0, q_out=None, 
         k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
     if q_out.shape != q.shape or (k is not None and (k_out.shape != k.shape or k.shape[0] != rows)):
         raise ValueError("rotate: outputs shaped as their inputs expected")
-    kp, ks, Hkv = (None, 0, 0) if k is None else (*_rows(k, "k"), k.shape[1])
-    kop, kos = (None, 0) if k is None else _rows(k_out, "k_out")
-    qp, qs = _rows(q, "q")
-    qop, qos = _rows(q_out, "q_out")
+    kp, ks, Hkv = (None, 0, 0) if k is None else (*_rows(k, "k", L.head_dim), k.shape[1])
+    kop, kos = (None, 0) if k is None else _rows(k_out, "k_out", L.head_dim)
+    qp, qs = _rows(q, "q", L.head_dim)
+    qop, qos = _rows(q_out, "q_out", L.head_dim)
     _check(lib().diffkv_rotate(C.byref(L), rows, _ptr(pos), _ptr(inv_freq), 2 * inv_freq.shape[0], int(style),
                                float(scale), Hq, qp, qs, qop, qos, Hkv, kp, ks, kop, kos, _stream(stream)),
            "diffkv_rotate")
@@ -349,12 +348,19 @@ def rotate(L, pos, inv_freq, q, k=None, style=ROPE_HALF, scale=1.0, q_out=None, 
 
 
 def _chunk(cache, new_len, max_new, what, q, *rows):
+    if new_len.dtype != torch.int32 or new_len.shape != (cache.num_seqs,) or not new_len.is_contiguous():
+        raise ValueError("%s: new_len: contiguous int32 [num_seqs] expected" % what)
     if max_new is None:
         max_new = int(new_len.max().item()) if new_len.shape[0] else 0
     for t in rows:
         if t.shape[0] != q.shape[0] or t.shape[1] != cache.num_kv_heads:
             raise ValueError("%s: [rows, num_kv_heads, head_dim] keys and values expected" % what)
     return int(max_new)
+
+
+def _dense(t, what, dtype, *shape):
+    if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous()):
+        raise ValueError("%s: contiguous %s %s expected" % (what, dtype, list(shape)))
 
 
 def chunk_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, slopes=None, out=None, lse=None,
@@ -368,10 +374,13 @@ def chunk_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, slopes
         out = torch.empty((rows, Hq, D), dtype=torch.float16, device=q.device)
     if lse is None and want_lse:
         lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
+    _dense(out, "out", torch.float16, rows, Hq, D)
+    _dense(lse, "lse", torch.float32, rows, Hq)
+    _dense(slopes, "slopes", torch.float32, Hq)
     sizes = (OP_CHUNK_ATTENTION, cache.L, cache.num_seqs, Hq, cache.num_kv_heads, rows)
     if ws is None:
         ws = _new_ws(workspace_size(*sizes), q.device)
-    (qp, qs), (kp, ks), (vp, vs) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+    (qp, qs), (kp, ks), (vp, vs) = (_rows(t, w, cache.L.head_dim) for t, w in ((q, "q"), (k, "k"), (v, "v")))
     _check_ws(lib().diffkv_chunk_attention(
         C.byref(cache.L), _cache_struct(cache), rows, max_new, _ptr(new_len), Hq, qp, qs, kp, ks, vp, vs,
         float(sm_scale), _form(cap, window, slopes), _ptr(out), _ptr(lse), ws.data_ptr(), ws.nbytes, _stream(stream)),
@@ -387,10 +396,13 @@ def chunk_significance(cache, new_len, q, k, sm_scale, lse, cap=0.0, window=0, s
     max_new = _chunk(cache, new_len, max_new, "chunk_significance", q, k)
     if score is None:
         score = torch.empty((rows, cache.num_kv_heads), dtype=torch.float32, device=q.device)
+    _dense(lse, "lse", torch.float32, rows, Hq)
+    _dense(score, "score", torch.float32, rows, cache.num_kv_heads)
+    _dense(slopes, "slopes", torch.float32, Hq)
     sizes = (OP_CHUNK_SIGNIFICANCE, cache.L, cache.num_seqs, Hq, cache.num_kv_heads, rows)
     if ws is None:
         ws = _new_ws(workspace_size(*sizes), q.device)
-    (qp, qs), (kp, ks) = _rows(q, "q"), _rows(k, "k")
+    (qp, qs), (kp, ks) = (_rows(t, w, cache.L.head_dim) for t, w in ((q, "q"), (k, "k")))
     _check_ws(lib().diffkv_chunk_significance(
         C.byref(cache.L), _cache_struct(cache), rows, max_new, _ptr(new_len), Hq, qp, qs, kp, ks, float(sm_scale),
         _form(cap, window, slopes), _ptr(lse), _ptr(score), ws.data_ptr(), ws.nbytes, _stream(stream)),

@@ -55,7 +55,7 @@ def test_refused_arguments(dk, bad):
     assert significance(dk, **bad) == dk.E_INVAL
 
 
-@pytest.mark.parametrize("form", [(-1.0, 0), (math.nan, 0), (math.inf, 0), (0.0, -1)], ids=str)
+@pytest.mark.parametrize("form", [(-1.0, 0), (math.nan, 0), (math.inf, 0), (0.0, -1), (1e-35, 0)], ids=str)
 def test_refused_forms(dk, form):
     f = C.byref(dk.ScoreForm(form[0], form[1], None))
     assert attention(dk, form=f) == dk.E_INVAL
@@ -166,3 +166,31 @@ def test_binding_refuses_rows_that_are_not_packed(dk):
         dk.rotate(dk.layout(), torch.zeros(3, dtype=torch.int64), torch.zeros(32), x)
     with pytest.raises(ValueError):
         dk.rotate(dk.layout(), torch.zeros(2, dtype=torch.int32), torch.zeros(32), x)
+
+
+def test_binding_refuses_types_and_shapes(dk):
+    class Nothing:
+        num_kv_heads, num_seqs, L = 2, 1, dk.layout()
+    q = torch.zeros((3, 8, 128), dtype=torch.float16)
+    kv = torch.zeros((3, 2, 128), dtype=torch.float16)
+    nl = torch.tensor([3], dtype=torch.int32)
+    lse = torch.zeros((3, 8))
+    good = dict(q=q, k=kv, v=kv, new_len=nl, out=q.clone(), lse=lse, slopes=None)
+    for bad in (dict(q=q.bfloat16()), dict(k=kv.bfloat16()), dict(v=kv[..., :64].contiguous()), dict(new_len=nl.long()),
+                dict(new_len=torch.zeros(2, dtype=torch.int32)), dict(out=q.float()), dict(out=q[:2]), dict(lse=lse.double()),
+                dict(lse=lse[:, :7]), dict(slopes=torch.zeros(7)), dict(slopes=torch.zeros(8, dtype=torch.float64)),
+                dict(q=q[..., :64].contiguous(), out=q[..., :64].contiguous())):
+        a = dict(good, **bad)
+        with pytest.raises(ValueError):
+            dk.chunk_attention(Nothing, a["new_len"], a["q"], a["k"], a["v"], 0.1, slopes=a["slopes"], out=a["out"],
+                               lse=a["lse"], max_new=3, ws=q)
+    for bad in (dict(lse=lse.half()), dict(score=torch.zeros((3, 3))), dict(k=kv.float())):
+        a = dict(good, score=torch.zeros((3, 2)), **bad) if "score" not in bad else dict(good, **bad)
+        with pytest.raises(ValueError):
+            dk.chunk_significance(Nothing, nl, a["q"], a["k"], 0.1, a["lse"], score=a["score"], max_new=3, ws=q)
+
+
+def test_misaligned_workspaces(dk):
+    L = dk.layout(max_seq_len=256)
+    need = dk.workspace_size(dk.OP_CHUNK_ATTENTION, L, 2, 8, 2, 10)
+    assert attention(dk, ws=FAKE + 8, ws_bytes=need) == dk.E_INVAL

@@ -442,3 +442,35 @@ def test_values_at_the_ends_of_fp16(n):
     dk.quantize_append(cache, one, k, v, torch.rand((96, 1), device=DEV), quota=quota, total_new=96, max_new=96)
     q, k, v = fused(rng, n, 4, 1)
     both(cache, [n], q, k, v, "large values, n %d" % n)
+
+
+@pytest.mark.parametrize("new_len,want", [([5, 9, 200], [5, 9, 6]), ([1, 1, 4], [1, 1, 0]), ([40, 300, 300], [40, 300, 10])],
+                         ids=str)
+def test_lengths_past_the_rows_are_clamped(new_len, want):
+    """Lengths that sum to more rows than there are: the rows that are there are those of the clamped
+    lengths; nothing behind them, or behind the workspace, is written."""
+    rng = np.random.default_rng(sum(new_len))
+    cache = filled(dk, {}, 3, 2, [300, 40, 700], seed=2)
+    rows = sum(want)
+    q, k, v = fused(rng, rows, 8, 2)
+    nl = torch.tensor(new_len, dtype=torch.int32, device=DEV)
+    before = kept_tokens(cache)
+    out = torch.full((rows + 5, 8, D), 7.0, dtype=torch.float16, device=DEV)
+    lse = torch.full((rows + 5, 8), 7.0, device=DEV)
+    score = torch.full((rows + 5, 2), 7.0, device=DEV)
+    ws = []
+    for op in (dk.OP_CHUNK_ATTENTION, dk.OP_CHUNK_SIGNIFICANCE):
+        need = dk.workspace_size(op, cache.L, 3, 8, 2, rows)
+        ws.append((torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device=DEV), need))
+    print("case: lengths %s for %d rows" % (new_len, rows), flush=True)
+    dk.chunk_attention(cache, nl, q, k, v, SCALE, out=out[:rows], lse=lse[:rows], max_new=max(new_len), ws=ws[0][0][:ws[0][1]])
+    torch.cuda.synchronize()
+    check_attention(cache, want, q, k, v, out[:rows], lse[:rows], "clamped")
+    dk.chunk_significance(cache, nl, q, k, SCALE, lse[:rows], score=score[:rows], max_new=max(new_len),
+                          ws=ws[1][0][:ws[1][1]])
+    torch.cuda.synchronize()
+    check_scores(cache, before, want, q, k, lse[:rows], score[:rows], "clamped")
+    for t in (out, lse, score):
+        assert bool((t[rows:] == 7.0).all())
+    for w, need in ws:
+        assert bool((w[need:] == 0x5A).all())

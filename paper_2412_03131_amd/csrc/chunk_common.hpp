@@ -36,8 +36,20 @@ constexpr float kChunkLog2e = 1.4426950408889634f;
 constexpr float kChunkLn2 = 0.6931471805599453f;
 constexpr float kLowest = -1e30f;  // a running max before the first key (finite: no inf - inf)
 
-__device__ __forceinline__ f4 mfma_k32(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f4 mfma_k16(h4 a, h4 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0); }
+// The operands are named once more after the product: the compiler would otherwise place a result over an
+// operand that ends there, and what the hardware does then is not relied on.
+__device__ __forceinline__ f4 mfma_k32(h8 a, h8 b, f4 c)
+{
+    f4 d = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    asm("" : "+v"(d) : "v"(a), "v"(b));
+    return d;
+}
+__device__ __forceinline__ f4 mfma_k16(h4 a, h4 b, f4 c)
+{
+    f4 d = __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0);
+    asm("" : "+v"(d) : "v"(a), "v"(b));
+    return d;
+}
 
 // s c + z of a group's largest code can round past the largest finite fp16 (s >= 0, z finite): it
 // becomes that.  (The mode bit for it, MODE.FP16_OVFL, also loses NaN operands of matrix products.)

@@ -285,9 +285,20 @@ struct ScoreForm {
 __device__ __forceinline__ float formed(float x, const ScoreForm& f, float away)
 {
     if (f.cap_in != 0.0f) {
-        // tanh y = 1 - 2 / (1 + exp 2y): exact limits at both ends, 2^-23 absolute
-        const float ex = __builtin_amdgcn_exp2f(x * f.cap_in);
-        x = f.cap * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + ex));
+        // With t = 2 log2(e) x / cap: below |x| = 5/8 cap x + x t^2 Q(t^2), Q a Chebyshev fit of degree 4
+        // (2^-23 of the result: 1 - 2 / (1 + exp) alone would leave 2^-23 of the cap, 10^-6 of a score's
+        // probability at caps of 30); above it, where a wave has any, 1 - 2 e / (1 + e), e = 2^-|t|.
+        const float t = x * f.cap_in, u = t * t;
+        float y = __builtin_fmaf(u, -1.5262884e-7f, 4.3717801e-6f);
+        y = __builtin_fmaf(y, u, -9.3320843e-5f);
+        y = __builtin_fmaf(y, u, 1.9235463e-3f);
+        y = __builtin_fmaf(y, u, -4.0037747e-2f);
+        y = __builtin_fmaf(x, u * y, x);
+        if (!(fabsf(t) < 1.8f)) {
+            const float e = __builtin_amdgcn_exp2f(-fabsf(t));
+            y = __builtin_copysignf(__builtin_fmaf(-f.cap, 2.0f * e * __builtin_amdgcn_rcpf(1.0f + e), f.cap), x);
+        }
+        x = y;
     }
     return __builtin_fmaf(-f.slope, away, x);
 }

@@ -7,8 +7,8 @@
 //
 // Scores q . k_hat with k_hat = s c + z per group of 32 dims, on
 // v_mfma_f32_16x16x32_f16, whose 32-element depth is one group.  The codes c enter as
-// fp16 denormals (value c 2^-24, the code's own bits), exactly; their group sums
-// are weighted by 2^15 s in fp32.  A row of q is scaled by the power of two 2^e that
+// fp16 denormals (value c 2^-24, the code's own bits; see key_unit), exactly; their
+// group sums are weighted by 2^15 s in fp32.  A row of q is scaled by the power of two 2^e that
 // brings its largest element to [2^13, 2^14), exactly, so that all terms have the unit
 // 2^(e-9):
 //   sum_g (2^15 s_g) (2^-24 sum_d c_d q_d 2^e) + sum_g z_g (2^(e-9) sum_d q_d)
@@ -33,6 +33,7 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr float kChunkLog2e = 1.4426950408889634f;
+constexpr float kChunkLog2eRest = 1.925963034e-08f;  // log2(e) less that
 constexpr float kChunkLn2 = 0.6931471805599453f;
 constexpr float kLowest = -1e30f;  // a running max before the first key (finite: no inf - inf)
 
@@ -200,7 +201,11 @@ __device__ __forceinline__ float rows_sum(float v)
 }
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
-// eight key codes (8 bits: two dwords; 4 bits: one) -> fp16 denormals in order
+// eight key codes (8 bits: two dwords; 4 bits: one) -> fp16 denormals in order.  Codes of 4 bits stand four
+// bits higher, 2^-20 c: a matrix product aligns its terms by their exponents alone and cuts them off 2^-24
+// below, so small denormals would lose what their leading zeros take (4e-5 of a probability, measured).
+template <int KB>
+constexpr float key_unit() { return KB == 4 ? 1.0f / 16 : 1.0f; }
 __device__ __forceinline__ h8 key_codes8(uint32_t lo, uint32_t hi)
 {
     u4 r;
@@ -212,7 +217,7 @@ __device__ __forceinline__ h8 key_codes8(uint32_t lo, uint32_t hi)
 }
 __device__ __forceinline__ h8 key_codes4(uint32_t w)
 {
-    const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
+    const uint32_t even = (w << 4) & 0xF0F0F0F0u, odd = w & 0xF0F0F0F0u;
     u4 r;
     r[0] = __builtin_amdgcn_perm(odd, even, 0x0C040C00u);
     r[1] = __builtin_amdgcn_perm(odd, even, 0x0C050C01u);

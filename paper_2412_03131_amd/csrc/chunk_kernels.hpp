@@ -252,8 +252,8 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
 {
     const int c = lane & 15, quarter = lane >> 4;
     float x[RT][2][4];
-    const h4 pick0 = {(_Float16)(quarter == 0 ? 32768.0f : 0.0f), (_Float16)0.0f, (_Float16)0.0f, (_Float16)0.0f};
-    const h4 pick1 = {(_Float16)0.0f, (_Float16)0.0f, (_Float16)(quarter == 0 ? 32768.0f : 0.0f), (_Float16)0.0f};
+    const h4 pick0 = {(_Float16)(quarter == 0 ? 0x1p15f * key_unit<KB>() : 0.0f), (_Float16)0.0f, (_Float16)0.0f, (_Float16)0.0f};
+    const h4 pick1 = {(_Float16)0.0f, (_Float16)0.0f, (_Float16)(quarter == 0 ? 0x1p15f * key_unit<KB>() : 0.0f), (_Float16)0.0f};
     const f4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -262,7 +262,7 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
         load_keys<KB, VB, T, MOD>(raw, slot, t, c, quarter);
         const h8 meta = __builtin_bit_cast(h8, raw.km);
         const h4 m01 = {meta[0], meta[1], meta[2], meta[3]}, m23 = {meta[4], meta[5], meta[6], meta[7]};
-        // 2^15 s of the quarter's four tokens, per group: a product with a unit vector
+        // 2^15 s (times the codes' unit) of the quarter's four tokens, per group: a product with a unit vector
         f4 s[kNG];
         s[0] = mfma_k16(m01, pick0, zero);
         s[1] = mfma_k16(m01, pick1, zero);
@@ -804,7 +804,7 @@ struct TileBuf {
     h8 k[2][kNG][kWave];     // [tile][group][lane]
     h8 v[8][kWave];          // [16-dim tile][lane]
     h8 meta[2][16];          // [tile][token] {s, z} of four groups
-    float s[2][kNG][16];     // 2^15 s (own tokens: 2^-9, their products are sums of halfs)
+    float s[2][kNG][16];     // 2^15 s times the codes' unit (own tokens: 2^-9, their products are sums of halfs)
     int pos[2][16];
     uint32_t odd[kTileWaves];  // own values that are not finite, by the wave that met them
 };
@@ -863,7 +863,7 @@ __device__ __forceinline__ void tile_put(TileBuf& b, const uint8_t* slot_, int l
         const h8 m = *reinterpret_cast<const h8*>(pg + O.km + slot * 16);
         b.meta[quarter][c] = m;
 #pragma unroll
-        for (int g = 0; g < kNG; ++g) b.s[quarter][g][c] = 32768.0f * (float)m[2 * g];
+        for (int g = 0; g < kNG; ++g) b.s[quarter][g][c] = 0x1p15f * key_unit<KB>() * (float)m[2 * g];
         if constexpr (MOD) b.pos[quarter][c] = *reinterpret_cast<const int32_t*>(pg + O.pos + slot * 4);
     }
 }
@@ -1403,8 +1403,20 @@ __device__ __forceinline__ void score_sums(ScoreSet& s, float lse, float slope, 
     }
 }
 
+// A score's probability.  In natural units the whole powers of two are split off before the product with
+// log2(e) is rounded: 2^-24 of it alone would be 10^-6 of a probability of e^-20.
+template <bool MOD>
+__device__ __forceinline__ float probability(float x)
+{
+    if constexpr (!MOD) return __builtin_amdgcn_exp2f(x);
+    x = fmaxf(x, -150.0f);
+    const float whole = __builtin_rintf(x * kChunkLog2e);
+    const float rest = __builtin_fmaf(x, kChunkLog2eRest, __builtin_fmaf(x, kChunkLog2e, -whole));
+    return __builtin_ldexpf(__builtin_amdgcn_exp2f(rest), (int)whole);
+}
+
 // One set against a wave's tokens: the running maxima over the heads, of position p (+ 4 r) and tokens
-// 16 kt + c, in log2 units.
+// 16 kt + c, in log2 units (natural ones with a score form).
 template <bool FOUR, bool MOD>
 __device__ __forceinline__ void score_use(const ScoreSet& S, const ChunkArgs& a, const h8 (&K)[kScoreTiles][kNG],
                                           const h8 (&meta)[kScoreTiles], const float (&s)[kScoreTiles][kNG],
@@ -1451,7 +1463,7 @@ __device__ __forceinline__ void score_use(const ScoreSet& S, const ChunkArgs& a,
             if constexpr (MOD) {
                 const int away = p + (FOUR ? 0 : 4 * r) - pos[kt];
                 const float y = formed(sum[kt][r] * unit, ScoreForm{a.cap_in, a.cap, slope[r]}, (float)away) - lse[r];
-                x[r] = away < a.window ? y * kChunkLog2e : -INFINITY;
+                x[r] = away < a.window ? y : -INFINITY;
             } else {
                 x[r] = __builtin_fmaf(sum[kt][r], unit, -lse[r]);
             }
@@ -1637,7 +1649,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
 #pragma unroll
                 for (int kt = 0; kt < kScoreTiles; ++kt)
 #pragma unroll
-                    for (int g = 0; g < kNG; ++g) s[kt][g] = 0x1p19f * (float)meta[kt][2 * g];
+                    for (int g = 0; g < kNG; ++g) s[kt][g] = 0x1p19f * key_unit<KB>() * (float)meta[kt][2 * g];
             };
             using std::integral_constant;
             if (sec == 0) take(integral_constant<int, hi.kb>{}, integral_constant<int, hi.vb>{}, integral_constant<int, hi.T>{});
@@ -1661,7 +1673,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
                 for (int kt = 0; kt < kScoreTiles; ++kt)
 #pragma unroll
                     for (int r = 0; r < kTops; ++r) {
-                        const float p = __builtin_amdgcn_exp2f(top[kt][r]);
+                        const float p = probability<MOD>(top[kt][r]);
                         // the chunk's own tokens are seen from their own positions on
                         total[kt] += sec != 2 || j + 4 * r >= tok0 + 16 * kt + c ? p : 0.0f;
                     }
@@ -1823,7 +1835,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores_short(Chu
             if (hs == HS - 1) {
 #pragma unroll
                 for (int kt = 0; kt < kScoreTiles; ++kt) {
-                    const float p = __builtin_amdgcn_exp2f(top[kt][0]);
+                    const float p = probability<MOD>(top[kt][0]);
                     total[kt] += own < 0 || j >= own + 16 * kt + c ? p : 0.0f;
                 }
             }
@@ -1858,7 +1870,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores_short(Chu
                 }
                 meta[kt] = *reinterpret_cast<const h8*>(pg + O.km + sl * 16);
 #pragma unroll
-                for (int g = 0; g < kNG; ++g) s[kt][g] = 0x1p19f * (float)meta[kt][2 * g];
+                for (int g = 0; g < kNG; ++g) s[kt][g] = 0x1p19f * key_unit<KB>() * (float)meta[kt][2 * g];
             }
         };
         using std::integral_constant;

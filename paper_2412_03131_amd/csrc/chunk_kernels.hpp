@@ -466,16 +466,19 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const RowsLds<RT>& Q, cons
 //
 // A workgroup takes 16 RT rows of one (sequence, KV head) and its share of the table's steps
 // (high pages, low pages, the chunk's own tokens), its four waves every fourth step each.  A
-// wave holds its rows' queries as matrix operands and the transposed result O^T, so the
-// scores of a step come out with a lane's values in one row and go into the second product as
-// they lie: no exchange between lanes but the rare raise of the running max.  A wave's next step is
-// staged in LDS as soon as the one before has been read from there; with four waves per
-// SIMD the others' work covers the rest of its way.
+// wave has the transposed result O^T, so the scores of a step come out with a lane's values in
+// one row and go into the second product as they lie: no exchange between lanes but the rare raise of
+// the running max.  A wave's next step is staged in LDS as soon as the one before has been read from
+// there; with four waves per SIMD (two with two row tiles) the others' work covers the rest of its way.
+// Bound: 64 sequences' single tokens over 1k-4k (8 KV heads, K8V4 / K4V2, 144 MB of pages) take 46 us, 3.2 TB/s
+// against 4.9 of a copy, one token of 16 sequences over 32k with a cap and slopes 109 us at 3.6 TB/s: VALU issue
+// (dequantization) and the longest tables' pieces; calls of few tables the chain lengths - page IDs -
+// pages - states (12 us over 600 tokens).
 constexpr int kChunkWaves = 4;
 
 // The piece of workgroup blockIdx.x: tables in order, a table's row blocks, a block's pieces.  All blocks
 // of a table have about one piece per `quantum` steps, the quantum such that all pieces together (a
-// table's last is half a quantum on average) are kRowPieces, and at least a step for each wave.
+// table's last is half a quantum on average) are kRowPieces at most, and at least a step for each wave.
 constexpr int kRowTables = 1024;  // (more are not split)
 struct RowPiece {
     int table, blk, split, splits, block;
@@ -483,6 +486,14 @@ struct RowPiece {
 __device__ __forceinline__ int piece_quantum(const ChunkArgs& a, int total, int blocks)
 {
     return max((total + a.pieces - 1) / max(a.pieces - blocks / 2, a.pieces / 4), kChunkWaves);
+}
+// No block has more than half the root of its steps: the pieces' states are read by one workgroup, which
+// takes about as long for four of them as a wave for a step.  (One sequence, 8 KV heads, one token over 8192:
+// 96 us with as many pieces as there can be, 26 with the root of the steps, 23 with half of it; over 32768 302,
+// 56, 38; eight tokens for each of four over 8192: 47, 34, 30.)
+__device__ __forceinline__ int block_pieces(int steps, int quantum)
+{
+    return min((steps + quantum - 1) / quantum, (int)(0.5f * __builtin_sqrtf((float)steps)) + 1);
 }
 // A table's row blocks and the steps of each.
 __device__ __forceinline__ void row_steps(const ChunkArgs& a, int rows, int t, int& steps, int& nb)
@@ -503,7 +514,7 @@ __device__ __forceinline__ RowPiece row_piece(const ChunkArgs& a, int rows, long
         const int total = __builtin_amdgcn_readlane(wave_incl_scan(nb * steps), kWave - 1);
         const int blocks = wave_incl_scan(nb);
         const int quantum = piece_quantum(a, total, __builtin_amdgcn_readlane(blocks, kWave - 1));
-        const int each = (steps + quantum - 1) / quantum;
+        const int each = block_pieces(steps, quantum);
         const int end = wave_incl_scan(nb * each);
         const unsigned long long past = __ballot(end > me);
         if (!past) return RowPiece{-1, 0, 0, 0, 0};
@@ -526,13 +537,13 @@ __device__ __forceinline__ RowPiece row_piece(const ChunkArgs& a, int rows, long
     const int quantum = piece_quantum(a, (int)(both & 0xffffffff), (int)(both >> 32));
     int pieces = 0, block = (int)(before >> 32);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) pieces += nb[i] * ((steps[i] + quantum - 1) / quantum);
+    for (int i = 0; i < kPer; ++i) pieces += nb[i] * block_pieces(steps[i], quantum);
     long long all, at = block_excl_scan<long long>(pieces, lds, &all);
     if (me >= all) return RowPiece{-1, 0, 0, 0, 0};
     int* found = reinterpret_cast<int*>(lds);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const int each = (steps[i] + quantum - 1) / quantum;
+        const int each = block_pieces(steps[i], quantum);
         const long long next = at + nb[i] * each;
         if (me >= at && me < next) {
             const int k = me - (int)at, blk = k / each;
@@ -1737,6 +1748,8 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
 // The short chunks: at most kShortSets sets of four positions and heads, staged once for a workgroup's share
 // of its table.  Each wave takes every eighth step of 32 tokens, the keys' half of its pages by way of LDS as
 // in chunk_rows, the next step's on its way while one is computed.  Bound by memory.
+// (4 query heads per KV head, 64 sequences over 2048 tokens, here / in passes of a longer chunk: 4 tokens 23 / 23 us,
+// 8 26 / 60, 16 32 / 66.  Room for eight sets leaves one workgroup a CU less: 16 tokens 43, 32 tokens 60 / 88.)
 template <int LI, bool MOD>
 __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores_short(ChunkArgs a)
 {

@@ -279,8 +279,11 @@ constexpr int kChunkPart = kD + 4;  // floats of a partial state (16-byte rows)
 // How a chunk attention call is laid out: sequences of at most kChunkFewRows rows (new tokens x query heads
 // of a KV head) in blocks of 16 or 32 rows, which up to kRowPieces workgroups share; longer ones in blocks of
 // kChunkRows, all of them cut into kTileShares equal shares.  A function of what the workspace size is
-// told.
-constexpr int kChunkFewRows = 64;
+// told.  The border (8 KV heads, 4 query heads each, blocks of 32 / shares of 256 rows): 64 rows for each of
+// 64 sequences over 2048 tokens 91 / 148 us; 128 rows 168 / 155, but for 16 sequences 52 / 58 and for 4 over
+// 8192 49 / 63; 256 rows for 16 sequences 93 / 70.  Beside longer sequences only those of one block of 16 rows
+// stay (a second launch: the blocks of the others would take a CU each from the shares).
+constexpr int kChunkFewRows = 128;
 constexpr int kChunkRows = 256;
 constexpr int kTileThreads = 512;  // of a workgroup on kChunkRows rows
 constexpr int kTileShares = 256;   // one for each CU

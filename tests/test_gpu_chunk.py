@@ -474,3 +474,13 @@ def test_lengths_past_the_rows_are_clamped(new_len, want):
         assert bool((t[rows:] == 7.0).all())
     for w, need in ws:
         assert bool((w[need:] == 0x5A).all())
+
+
+@pytest.mark.parametrize("G,n", [(4, 4), (4, 5), (4, 16), (4, 20), (4, 32), (4, 33), (8, 2), (8, 3), (8, 16), (8, 17),
+                                 (1, 16), (1, 17), (1, 128), (1, 129)])
+def test_both_sides_of_the_row_borders(G, n):
+    """16, 17, 128 and 129 rows of a sequence and those around: every kernel and its number of row tiles."""
+    rng = np.random.default_rng(10 * G + n)
+    cache = filled(dk, {}, 3, 1, [333, 0, 90], seed=n)
+    q, k, v = fused(rng, 2 * n + 1, G, 1)
+    both(cache, [n, 1, n], q, k, v, "G %d, n %d" % (G, n))

@@ -802,9 +802,17 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
 // A workgroup takes 256 rows of one (sequence, KV head), 32 per wave, and goes over the table's
 // steps together: each step's 32 tokens are turned into matrix operands once, by all eight
 // waves (one key and one value operand of a lane each), and read from LDS by all of them: keys
-// as exact codes with their scales in 32 bits beside them, values dequantized to fp16.  Two
-// buffers: while a step is computed from one, the next one's pages are on their way to
-// registers, from where they go into the other.
+// as exact codes with their scales in 32 bits beside them, values dequantized to fp16.  Raw pages
+// arrive in one of two slots by loads with an LDS destination, asked for two steps ahead; operands lie
+// in one of three buffers: a step's scores are computed from one while the step before's weights meet
+// their values from another and the next one is made.
+// The blocks of all tables end to end are cut into equal shares, one per CU: with a workgroup per block the
+// longest ones set the time (257-512 tokens for each of 8 sequences over 0-8192: 546 us, with shares 377).
+// Bound by issue: that case takes 366 us at 160 GFLOP, 2048 tokens over 8192 at 64 / 8 heads 788 us, 577
+// TFLOP/s (an 8192^3 fp16 library product 1137); VALU 62 % busy, 34 % of the waves' time waits on LDS
+// operands, barriers and products.
+// The weights enter as fp16 once (pack_rest's second product per tile would cost half as many matrix
+// instructions again here): the outputs' error against 64 bits is 1.5 times a 32-bit computation's.
 constexpr int kTileWaves = 8;
 constexpr int kTileRows = kTileWaves * 32;
 static_assert(kTileRows == kChunkRows, "row blocks of the plan");
@@ -1356,9 +1364,12 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
 // operands, and goes over all rows of the sequence in sets of 16, whose queries pass through LDS for
 // the workgroup's eight waves.  A set is either 16 positions of one query head (the maximum over the
 // heads is taken between one set's results and the next's, in a lane) or 4 positions of four heads
-// (between a lane's four results): the second for chunks of up to four tokens and where four divides
-// the heads well.  One exp2 serves all heads of a position.  Short chunks have a
-// kernel of their own (chunk_scores_short); the sets of a longer one pass four at a time.
+// (between a lane's four results): the second where four divides the heads.  One exp2 serves all
+// heads of a position.  Short chunks have a kernel of their own (chunk_scores_short); the sets of a longer one
+// pass four at a time, the blocks of all tables cut into equal shares, two per CU (364 us without shares, 190
+// with them, 155 with queries loaded straight to where the products read them: 257-512 tokens for each of 8
+// sequences over 0-8192, 77 GFLOP, 498 TFLOP/s).  Bound by issue: two products, eight additions in fp32 and a
+// maximum for 64 scores of a group.
 //
 // Queries stay unscaled here: a token's scales are in registers, in fp32, and take the 2^24 of
 // the codes themselves; the unit of the sums is 2^-5, so that a group's sum of 32 halfs fits one.

@@ -283,12 +283,17 @@ constexpr int kChunkPart = kD + 4;  // floats of a partial state (16-byte rows)
 // 64 sequences over 2048 tokens 91 / 148 us; 128 rows 168 / 155, but for 16 sequences 52 / 58 and for 4 over
 // 8192 49 / 63; 256 rows for 16 sequences 93 / 70.  Beside longer sequences only those of one block of 16 rows
 // stay (a second launch: the blocks of the others would take a CU each from the shares).
+// Calls of few rows altogether (kChunkFewTotal, of all query heads) stay with the few-row kernel: one sequence's
+// 64 tokens (32 / 8 heads) over 8192 37 us, in shares 73; over 32768 80 / 106; its 128 over 8192 51 / 74, but over
+// 32768 187 / 121; 512 tokens over 8192 of 4 heads on one KV head 35 / 66.
 constexpr int kChunkFewRows = 128;
+constexpr int kChunkFewTotal = 2048;
 constexpr int kChunkRows = 256;
 constexpr int kTileThreads = 512;  // of a workgroup on kChunkRows rows
 constexpr int kTileShares = 256;   // one for each CU
 constexpr int kRowPieces = 1024;   // four for each CU
 struct ChunkPlan {
+    long long few_rows;    // a sequence's rows up to which it is one of few
     bool few_split;        // few rows: there are so few blocks that they are split
     long long few_blocks;  // row blocks of 16 there can be, of all KV heads
     long long few_part;    // floats of partial states

@@ -23,12 +23,13 @@ ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_n
     const long long G = Hq / Hkv, rows = total_new * G;
     const long long seqs = B < total_new ? B : total_new;
     auto clamp = [](long long x, long long lo, long long hi) { return x < lo ? lo : (x > hi ? hi : x); };
-    p.few_blocks = Hkv * clamp(rows / 16 + 2 * seqs, 0, seqs * (kChunkFewRows / 16));  // (in blocks of 32: two each)
+    p.few_rows = total_new * Hq <= kChunkFewTotal && rows > kChunkFewRows ? rows : kChunkFewRows;
+    p.few_blocks = Hkv * clamp(rows / 16 + 2 * seqs, 0, seqs * ((p.few_rows + 31) / 32 * 2));  // (in blocks of 32: two each)
     p.few_split = B * Hkv <= kRowPieces && Hkv * seqs < kRowPieces;
     // (row_piece makes at most kRowPieces and one per block of them, of 16 rows; of 32 half as many)
     p.few_part = p.few_split ? (kRowPieces + p.few_blocks) * 16 * kChunkPart : 0;
     p.bytes = align256((p.few_blocks + kTileShares) * 8) + align256(p.few_part * 4) +
-              (rows > kChunkFewRows ? 2ll * kTileShares * kChunkRows * kChunkPart * 4 : 0);
+              (rows > p.few_rows ? 2ll * kTileShares * kChunkRows * kChunkPart * 4 : 0);
     return p;
 }
 
@@ -44,7 +45,7 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
         void* kargs[] = {&a};
         return hipLaunchKernel(kern, dim3((unsigned)grid), dim3((unsigned)threads), kargs, 0, st);
     };
-    if (rows > kChunkFewRows) {
+    if (rows > plan.few_rows) {
         ChunkArgs a = args;
         a.rows_lo = 17;
         a.rows_hi = INT32_MAX;
@@ -58,11 +59,11 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     // Few rows: all sequences if none is longer, else those of one block of 16 rows
     ChunkArgs a = args;
     a.rows_lo = 1;
-    a.rows_hi = rows > kChunkFewRows ? 16 : kChunkFewRows;
+    a.rows_hi = rows > plan.few_rows ? 16 : (int)plan.few_rows;
     a.part = part;
     // Two row tiles share a step's dequantization (20 rows for each of 64 sequences over 2048 tokens 52 us, with
     // one tile 67; 64 rows 91 and 117; 32 rows for 4 over 8192 30 and 40)
-    const int rt = rows > 16 && rows <= kChunkFewRows ? 2 : 1;
+    const int rt = rows > 16 && rows <= plan.few_rows ? 2 : 1;
     a.splits = plan.few_split ? 0 : 1;
     a.blocks = (int)(plan.few_blocks < INT32_MAX ? plan.few_blocks : INT32_MAX);
     a.pieces = kRowPieces / rt;  // (a CU holds half as many workgroups with two row tiles)
@@ -70,8 +71,8 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     const long long whole = args.total_new * G / per + seqs, each = seqs * ((most + per - 1) / per);
     const long long blocks = (whole < each ? whole : each) * a.Hkv;
     if (!plan.few_split) return launch(a, rt, blocks, 4 * kWave);
-    // a piece has at least a step for each of its four waves, a table at most a step per page and two of its own
-    const long long pieces = blocks * ((a.p_max + 4 + 3) / 4), cap = a.pieces + blocks;
+    // a piece has at least a step for each of its four waves, a table at most a step per page and its own
+    const long long pieces = blocks * ((a.p_max + 2 + (a.max_new + 31) / 32 + 3) / 4), cap = a.pieces + blocks;
     return launch(a, rt, pieces < cap ? pieces : cap, 4 * kWave);
 }
 

@@ -484,3 +484,83 @@ def test_both_sides_of_the_row_borders(G, n):
     cache = filled(dk, {}, 3, 1, [333, 0, 90], seed=n)
     q, k, v = fused(rng, 2 * n + 1, G, 1)
     both(cache, [n, 1, n], q, k, v, "G %d, n %d" % (G, n))
+
+
+@pytest.mark.parametrize("layout", range(4))
+@pytest.mark.parametrize("G", [1, 3, 4, 8])
+def test_calls_of_many_rows(layout, G):
+    """More rows than the few-row kernel takes altogether: tiles and shares, beside short chunks."""
+    rng = np.random.default_rng(200 * layout + G)
+    lens, new_len = [0, 333, 130, 64, 17], [1100 if G == 1 else 330, 1, 0, 140, 17]
+    assert sum(new_len) * 2 * G > 2048
+    cache = filled(dk, LAYOUTS[layout], 5, 2, lens, seed=layout)
+    q, k, v = fused(rng, sum(new_len), 2 * G, 2)
+    both(cache, new_len, q, k, v, "many rows, layout %d, G %d" % (layout, G))
+
+
+@pytest.mark.parametrize("form", [dict(cap=20.0), dict(window=45), dict(slopes=True), dict(cap=5.0, window=130, slopes=True)],
+                         ids=str)
+def test_score_forms_of_many_rows(form):
+    rng = np.random.default_rng(5)
+    form = dict(form)
+    if form.get("slopes"):
+        form["slopes"] = (2.0 ** -np.arange(1, 7)).astype(np.float32)
+    cache = filled(dk, {}, 3, 2, [700, 0, 90], seed=9)
+    q, k, v = fused(rng, 401, 6, 2, kscale=2.0)
+    both(cache, [200, 1, 200], q, k, v, "many rows, form %s" % form, **form)
+
+
+@pytest.mark.parametrize("rows", [256, 257])
+def test_both_sides_of_the_border_of_all_rows(rows):
+    rng = np.random.default_rng(rows)
+    cache = filled(dk, {}, 1, 1, [900], seed=rows)
+    q, k, v = fused(rng, rows, 8, 1)
+    both(cache, [rows], q, k, v, "%d tokens" % rows)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_lost_pages_and_non_finite_values_of_many_rows(bad):
+    rng = np.random.default_rng(3)
+    n, at = 300, 77
+    cache = filled(dk, {}, 2, 1, [400, 50], seed=8)
+    cache.page_table[0, 1] = -1
+    cache.page_table[0, cache.L.p_max - 2] = 2 ** 31 - 1
+    q, k, v = (x.contiguous() for x in fused(rng, 2 * n, 4, 1))
+    nl = torch.tensor([n, n], dtype=torch.int32, device=DEV)
+    want, want_lse = dk.chunk_attention(cache, nl, q, k, v, SCALE, max_new=n)
+    torch.cuda.synchronize()
+    check_attention(cache, [n, n], q, k, v, want, want_lse, "lost pages")
+    v[at, 0, 77] = bad
+    k[n + at, 0, 5] = float("nan")
+    out, lse = dk.chunk_attention(cache, nl, q, k, v, SCALE, max_new=n)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:at], want[:at]) and torch.equal(lse[:n], want_lse[:n])
+    assert not torch.isfinite(out[at:n, :, 77]).any()
+    others = torch.arange(D, device=DEV) != 77
+    assert torch.equal(out[at:n][..., others], want[at:n][..., others])
+    assert torch.equal(out[n:n + at], want[n:n + at]) and torch.isnan(out[n + at:]).all()
+    assert torch.isnan(lse[n + at:]).all()
+
+
+def test_many_rows_captured_and_repeated():
+    """Tiles in equal shares, replayed: bit-equal every time."""
+    rng = np.random.default_rng(61)
+    new_len = [300, 1, 25]
+    cache = filled(dk, {}, 3, 2, [900, 40, 333], seed=5)
+    q, k, v = fused(rng, sum(new_len), 8, 2)
+    nl = torch.tensor(new_len, dtype=torch.int32, device=DEV)
+    out = torch.empty((sum(new_len), 8, D), dtype=torch.float16, device=DEV)
+    lse = torch.empty((sum(new_len), 8), device=DEV)
+    ws = torch.empty(dk.workspace_size(dk.OP_CHUNK_ATTENTION, cache.L, 3, 8, 2, sum(new_len)), dtype=torch.uint8, device=DEV)
+    call = lambda: dk.chunk_attention(cache, nl, q, k, v, SCALE, out=out, lse=lse, max_new=300, ws=ws)
+    call()
+    torch.cuda.synchronize()
+    want = out.clone(), lse.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for _ in range(4):
+        for f in (g.replay, call):
+            out.fill_(0.0)
+            f()
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])

@@ -214,10 +214,11 @@ __device__ __forceinline__ h8 pack_weights(const float (&w)[2][4])
     }
     return __builtin_bit_cast(h8, bits);
 }
-// What the rounding left of them (two 11-bit parts hold 22 bits).  With one row tile, where the
-// matrix cores have time to spare, the weights enter whole: the results' error against 64 bits is then the
-// values' and their own rounding alone (1.4 times a 32-bit computation's rounded once; 1.5 to 1.7 with
-// rounded weights).
+// What the rounding left of them (two 11-bit parts hold 22 bits).  With one row tile the weights enter whole
+// (64 single tokens over 1k-4k: 44 -> 46 us): the results' error against 64 bits is then the values' and
+// their own rounding alone, 1.25 times a 32-bit computation's rounded once.  With two row tiles and in
+// chunk_tiles they are rounded once, 1.5 times it: the second products would take 2 to 13 % there (eight tokens
+// for each of 64 sequences over 2048 50 -> 56 us).
 __device__ __forceinline__ h8 pack_rest(const float (&w)[2][4], h8 P)
 {
     float rest[2][4];

@@ -25,7 +25,7 @@ ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_n
     auto clamp = [](long long x, long long lo, long long hi) { return x < lo ? lo : (x > hi ? hi : x); };
     p.few_rows = total_new * Hq <= kChunkFewTotal && rows > kChunkFewRows ? rows : kChunkFewRows;
     p.few_blocks = Hkv * clamp(rows / 16 + 2 * seqs, 0, seqs * ((p.few_rows + 31) / 32 * 2));  // (in blocks of 32: two each)
-    p.few_split = B * Hkv <= kRowPieces && Hkv * seqs < kRowPieces;
+    p.few_split = B * Hkv < kRowPieces;  // (not by the rows: a workspace for many serves calls of fewer)
     // (row_piece makes at most kRowPieces and one per block of them, of 16 rows; of 32 half as many)
     p.few_part = p.few_split ? (kRowPieces + p.few_blocks) * 16 * kChunkPart : 0;
     p.bytes = align256((p.few_blocks + kTileShares) * 8) + align256(p.few_part * 4) +

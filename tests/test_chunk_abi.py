@@ -194,3 +194,12 @@ def test_misaligned_workspaces(dk):
     L = dk.layout(max_seq_len=256)
     need = dk.workspace_size(dk.OP_CHUNK_ATTENTION, L, 2, 8, 2, 10)
     assert attention(dk, ws=FAKE + 8, ws_bytes=need) == dk.E_INVAL
+
+
+@pytest.mark.parametrize("seqs,Hq,Hkv", [(1, 32, 8), (1, 8, 1), (128, 32, 8), (127, 32, 8), (1024, 4, 1), (3, 5, 5),
+                                         (16, 64, 8), (2000, 8, 8)])
+def test_a_workspace_for_more_rows_serves_fewer(dk, seqs, Hq, Hkv):
+    L = dk.layout(max_seq_len=4096)
+    rows = sorted(set(list(range(1, 700)) + [seqs - 1, seqs, seqs + 1, 1023, 1024, 1025, 5000, 70000]) - {0})
+    need = [dk.workspace_size(dk.OP_CHUNK_ATTENTION, L, seqs, Hq, Hkv, r) for r in rows]
+    assert need == sorted(need)

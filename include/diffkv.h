@@ -421,7 +421,9 @@ typedef struct diffkv_score_form {
  *   ws       diffkv_workspace_size(DIFFKV_OP_CHUNK_ATTENTION, ...) bytes, no
  *            clearing needed, 16-byte aligned; calls that may overlap need one
  *            each
- * The cache is read only.  A page ID outside the pool counts no tokens.
+ * The cache is read only.  A page ID outside the pool counts no tokens, and no
+ * section length leads out of the table's row: the high section ends with the
+ * row, the low one where the high one begins.
  * sm_scale above 0 and at most 1e30 (DIFFKV_E_INVAL otherwise).  The layouts of
  * diffkv_layout_init's list, up to 8 query heads per KV head.
  * Precision: q . k_hat exact up to fp32 summation, fp32 softmax statistics;

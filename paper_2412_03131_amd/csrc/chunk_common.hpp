@@ -84,6 +84,22 @@ __device__ __forceinline__ auto fetch(__amdgpu_buffer_rsrc_t r, int lane_offset,
     else return (uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, lane_offset, offset, 0);
 }
 
+// ---- a table's sections ------------------------------------------------------------
+// Section lengths as the kernels use them: no length leads out of the table's row.  The high section's
+// pages are at most its slots, the low section's at most those that the high one leaves.
+struct SecLens {
+    int hi, lo;
+};
+template <int LI>
+__device__ __forceinline__ SecLens section_lens(const ChunkArgs& a, int t)
+{
+    constexpr unsigned Th = kLayoutFmts[LI].hi.T, Tl = kLayoutFmts[LI].lo.T;
+    const unsigned P = (unsigned)a.p_max;
+    const unsigned hi = (unsigned)max(a.len[2 * t], 0), lo = (unsigned)max(a.len[2 * t + 1], 0);
+    const unsigned ph = min((hi + Th - 1) / Th, P), pl = min((lo + Tl - 1) / Tl, P - ph);
+    return SecLens{(int)min(hi, ph * Th), (int)min(lo, pl * Tl)};
+}
+
 // ---- the sequence and row block of a workgroup --------------------------------
 struct SeqBlock {
     int b, n;        // sequence, its new tokens (0: none of this launch's)

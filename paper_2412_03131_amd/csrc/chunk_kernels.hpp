@@ -497,21 +497,24 @@ __device__ __forceinline__ int block_pieces(int steps, int quantum)
     return min((steps + quantum - 1) / quantum, (int)(0.5f * __builtin_sqrtf((float)steps)) + 1);
 }
 // A table's row blocks and the steps of each.
+template <int LI>
 __device__ __forceinline__ void row_steps(const ChunkArgs& a, int rows, int t, int& steps, int& nb)
 {
     int n = a.max_new == 1 && a.total_new == a.B ? 1 : a.new_len[t / a.Hkv];
     n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
     nb = chunk_blocks(n, a.Hq / a.Hkv, rows, a.rows_lo, a.rows_hi);
     // (at most 2^18, so that the sums of 4096 blocks stay below 2^31: a longer table's pieces are longer)
-    steps = nb ? min(((a.len[2 * t] + 31) >> 5) + ((a.len[2 * t + 1] + 31) >> 5) + ((n + 31) >> 5), 1 << 18) : 0;
+    const SecLens len = section_lens<LI>(a, t);
+    steps = nb ? min(((len.hi + 31) >> 5) + ((len.lo + 31) >> 5) + ((n + 31) >> 5), 1 << 18) : 0;
 }
+template <int LI>
 __device__ __forceinline__ RowPiece row_piece(const ChunkArgs& a, int rows, long long* lds)
 {
     const int tables = a.B * a.Hkv, me = (int)blockIdx.x;
     if (tables <= kWave) {  // a lane per table, every wave by itself
         const int lane = lane_id();
         int steps = 0, nb = 0;
-        if (lane < tables) row_steps(a, rows, lane, steps, nb);
+        if (lane < tables) row_steps<LI>(a, rows, lane, steps, nb);
         const int total = __builtin_amdgcn_readlane(wave_incl_scan(nb * steps), kWave - 1);
         const int blocks = wave_incl_scan(nb);
         const int quantum = piece_quantum(a, total, __builtin_amdgcn_readlane(blocks, kWave - 1));
@@ -529,7 +532,7 @@ __device__ __forceinline__ RowPiece row_piece(const ChunkArgs& a, int rows, long
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         steps[i] = nb[i] = 0;
-        if (t0 + i < tables) row_steps(a, rows, t0 + i, steps[i], nb[i]);
+        if (t0 + i < tables) row_steps<LI>(a, rows, t0 + i, steps[i], nb[i]);
         sum += nb[i] * steps[i];
         count += nb[i];
     }
@@ -601,7 +604,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
         splits = 1;
         slot_no = part_no = 0;
     } else {
-        const RowPiece p = row_piece(a, kRows, lds.find);
+        const RowPiece p = row_piece<LI>(a, kRows, lds.find);
         if (p.table < 0 || p.block >= a.blocks) return;  // (the second: lengths that do not sum to total_new)
         sb.b = p.table / a.Hkv;
         h = p.table - sb.b * a.Hkv;
@@ -626,7 +629,8 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
         for (int g = 0; g < kNG; ++g) x[rt][g] = *reinterpret_cast<const u4*>(q + g * kG);
     }
     const int t = sb.b * a.Hkv + h;
-    const int len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
+    const SecLens len = section_lens<LI>(a, t);
+    const int len_hi = len.hi, len_lo = len.lo;
     const int last = min(r0 + kRows, rows) - 1;
     const int own = last / G + 1;  // tokens of the chunk that some row sees
     const int s_hi = (len_hi + 31) >> 5, s_lo = (len_lo + 31) >> 5, s_own = (own + 31) >> 5;
@@ -1009,7 +1013,8 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
         int n = a.new_len[t / a.Hkv];
         n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
         nb = chunk_blocks(n, G, kTileRows, a.rows_lo, a.rows_hi);
-        return nb ? (long long)(((a.len[2 * t] + 31) >> 5) + ((a.len[2 * t + 1] + 31) >> 5)) * kStepUnits : 0;
+        const SecLens len = section_lens<LI>(a, t);
+        return nb ? (long long)(((len.hi + 31) >> 5) + ((len.lo + 31) >> 5)) * kStepUnits : 0;
     };
     auto units_to = [&](long long cached, int nb) { return nb * cached + (long long)own_units * nb * (nb + 1) / 2; };
     long long mine = 0;
@@ -1056,7 +1061,8 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
         for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     const int t = sb.b * a.Hkv + h;
-    const int len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
+    const SecLens len = section_lens<LI>(a, t);
+    const int len_hi = len.hi, len_lo = len.lo;
     const int own = (min((sb.blk + 1) * kTileRows, rows) - 1) / G + 1;  // own tokens that some row sees
     const bool idle = r0 >= rows;                                        // a wave without rows only helps
     const int j_first = min(r0, rows - 1) / G;  // the wave's first position
@@ -1525,8 +1531,9 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
         n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
         Table x{n, (n + kPos - 1) / kPos * HS, 0, 0, 0};
         if (!score_short(n, G)) {
-            x.b_hi = (a.len[2 * t] + kScoreBlock - 1) / kScoreBlock;
-            x.b_lo = (a.len[2 * t + 1] + kScoreBlock - 1) / kScoreBlock;
+            const SecLens len = section_lens<LI>(a, t);
+            x.b_hi = (len.hi + kScoreBlock - 1) / kScoreBlock;
+            x.b_lo = (len.lo + kScoreBlock - 1) / kScoreBlock;
             x.own = (n + kScoreBlock - 1) / kScoreBlock;
         }
         return x;
@@ -1581,7 +1588,8 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
     sequence_rows(a, sb);
     const int n = sb.n, h = t - sb.b * a.Hkv;
     const int first = a.seq_len[sb.b];
-    const int len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
+    const SecLens lens = section_lens<LI>(a, t);
+    const int len_hi = lens.hi, len_lo = lens.lo;
     const int b_hi = tb.b_hi, b_lo = tb.b_lo;
     const int all = (n + kPos - 1) / kPos * HS;
     const int32_t* table = a.page_table + (long long)t * a.p_max;
@@ -1786,7 +1794,8 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores_short(Chu
     const int n = sb.n;
     if (n == 0 || !score_short(n, G)) return;
     const int t = sb.b * a.Hkv + h;
-    const int first = a.seq_len[sb.b], len_hi = a.len[2 * t], len_lo = a.len[2 * t + 1];
+    const SecLens len = section_lens<LI>(a, t);
+    const int first = a.seq_len[sb.b], len_hi = len.hi, len_lo = len.lo;
     const int s_hi = (len_hi + 31) >> 5, s_lo = (len_lo + 31) >> 5, steps = s_hi + s_lo + 1;  // (the last: own tokens)
     const int shares = min(a.splits, (steps + kScoreWaves - 1) / kScoreWaves);
     if (share >= shares) return;

@@ -1,0 +1,62 @@
+"""Chunk operators where a cache, a batch or its values are out of the ordinary: lengths past a table's row,
+padded batches, values that are not finite, scores far apart.  Definitions and tolerances are those of
+test_gpu_chunk.py unless a test derives its own."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():  # pragma: no cover
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+from chunk_ref import D, filled  # noqa: E402
+from paper_2412_03131_amd import diffkv as dk  # noqa: E402
+from test_gpu_chunk import DEV, LAYOUTS, SCALE, fused  # noqa: E402
+
+# Chunks that reach every kernel with eight query heads on two KV heads: single tokens (blocks of one row tile,
+# short scores), a few (two row tiles), tens (scores of long chunks), and more rows than the few-row kernel takes
+CHUNKS = [[1, 1, 1], [6, 1, 4], [30, 2, 9], [300, 2, 40]]
+
+
+def run(cache, new_len, q, k, v, rows=None, max_new=None, **form):
+    """Attention, then scores; rows beyond the lengths' sum hold 7."""
+    rows = q.shape[0] if rows is None else rows
+    max_new = max(new_len) if max_new is None else max_new
+    nl = torch.tensor(new_len, dtype=torch.int32, device=DEV)
+    out = torch.full((rows, q.shape[1], D), 7.0, dtype=torch.float16, device=DEV)
+    lse = torch.full((rows, q.shape[1]), 7.0, device=DEV)
+    score = torch.full((rows, k.shape[1]), 7.0, device=DEV)
+    dk.chunk_attention(cache, nl, q, k, v, SCALE, out=out, lse=lse, max_new=max_new, **form)
+    torch.cuda.synchronize()
+    dk.chunk_significance(cache, nl, q, k, SCALE, lse, score=score, max_new=max_new, **form)
+    torch.cuda.synchronize()
+    return out, lse, score
+
+
+def same(a, b):
+    return all(torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8)) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("layout", [0, 3])
+@pytest.mark.parametrize("new_len", CHUNKS, ids=str)
+def test_lengths_past_the_table_stay_in_its_row(layout, new_len):
+    """Section lengths of more pages than the row has slots, or below zero: the high section ends with the row,
+    the low one where the high one begins.  Everything is as with those lengths, byte for byte; the
+    neighbouring tables' page IDs are neither read nor their scores moved a second time."""
+    rng = np.random.default_rng(layout)
+    cache = filled(dk, LAYOUTS[layout], 3, 2, [300, 70, 200], seed=layout)
+    P, Tl = cache.L.p_max, cache.L.tokens_per_page[1]
+    assert Tl == (16 if layout == 3 else 32)
+    q, k, v = fused(rng, sum(new_len), 8, 2)
+    lens, pool = cache.len.clone(), cache.pool.clone()
+    for t, hi, lo in ((2, 16 * 5000, 0), (1, 0, 2 ** 31 - 1), (3, 50, 40000), (4, 2 ** 31 - 1, 2 ** 31 - 1), (0, -5, -70)):
+        bounded = (min(max(hi, 0), P * 16), min(max(lo, 0), max(P - -(-max(hi, 0) // 16), 0) * Tl))
+        print("case: layout %d, %s, table %d of lengths %d, %d" % (layout, new_len, t, hi, lo), flush=True)
+        got = []
+        for pair in (bounded, (hi, lo)):
+            cache.len.copy_(lens)
+            cache.len[t] = torch.tensor(pair, dtype=torch.int32, device=DEV)
+            cache.pool.copy_(pool)
+            got.append(run(cache, new_len, q, k, v) + (cache.pool.clone(),))
+        assert same(*got)

@@ -500,12 +500,12 @@ __device__ __forceinline__ int block_pieces(int steps, int quantum)
 template <int LI>
 __device__ __forceinline__ void row_steps(const ChunkArgs& a, int rows, int t, int& steps, int& nb)
 {
-    int n = a.max_new == 1 && a.total_new == a.B ? 1 : a.new_len[t / a.Hkv];
-    n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
+    const SecLens len = section_lens<LI>(a, t);
+    const int n = new_tokens(a, t / a.Hkv);
     nb = chunk_blocks(n, a.Hq / a.Hkv, rows, a.rows_lo, a.rows_hi);
     // (at most 2^18, so that the sums of 4096 blocks stay below 2^31: a longer table's pieces are longer)
-    const SecLens len = section_lens<LI>(a, t);
-    steps = nb ? min(((len.hi + 31) >> 5) + ((len.lo + 31) >> 5) + ((n + 31) >> 5), 1 << 18) : 0;
+    steps = min(((len.hi + 31) >> 5) + ((len.lo + 31) >> 5) + ((n + 31) >> 5), 1 << 18);
+    steps &= -(int)(nb > 0);  // (a mask: the lengths' loads do not wait for the new tokens')
 }
 template <int LI>
 __device__ __forceinline__ RowPiece row_piece(const ChunkArgs& a, int rows, long long* lds)
@@ -595,11 +595,19 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
     int h, split, splits;
     long long slot_no;   // the block's number (its arrival word)
     long long part_no;   // its first piece's state
+    const int first_n = first_tokens(a);
     if (a.splits == 1) {  // none is split
         const int item = (int)blockIdx.x / a.Hkv;
         h = (int)blockIdx.x - item * a.Hkv;
-        sb = find_block(a, item, kRows, a.rows_lo, a.rows_hi);
-        if (sb.b < 0) return;
+        if (a.one_block) {
+            sb.b = item;
+            sb.blk = 0;
+            sequence_rows(a, sb, first_n);
+            if (chunk_blocks(sb.n, G, kRows, a.rows_lo, a.rows_hi) == 0) return;
+        } else {
+            sb = find_block(a, item, kRows, a.rows_lo, a.rows_hi);
+            if (sb.b < 0) return;
+        }
         split = 0;
         splits = 1;
         slot_no = part_no = 0;
@@ -613,7 +621,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
         splits = p.splits;
         slot_no = p.block;
         part_no = (int)blockIdx.x - split;
-        sequence_rows(a, sb);
+        sequence_rows(a, sb, first_n);
         if (sb.blk * kRows >= sb.n * G) return;  // (lengths that do not sum to total_new)
     }
     const int first = a.seq_len[sb.b];
@@ -1010,8 +1018,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
     const int tables = a.B * a.Hkv, chunk = (tables + kTileWaves * kWave - 1) / (kTileWaves * kWave);
     const int t0 = min((int)threadIdx.x * chunk, tables), t1 = min(t0 + chunk, tables);
     auto blocks_units = [&](int t, int& nb) -> long long {  // units of a block's cached steps; blocks
-        int n = a.new_len[t / a.Hkv];
-        n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
+        const int n = new_tokens(a, t / a.Hkv);
         nb = chunk_blocks(n, G, kTileRows, a.rows_lo, a.rows_hi);
         const SecLens len = section_lens<LI>(a, t);
         return nb ? (long long)(((len.hi + 31) >> 5) + ((len.lo + 31) >> 5)) * kStepUnits : 0;
@@ -1032,6 +1039,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
     const int share = gridDim.x % 8 == 0 ? ((int)blockIdx.x & 7) * per_xcd + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
     const long long start = share * quantum, stop = min(total, start + quantum);
     if (start >= total) return;
+    const int first_n = first_tokens(a);
     int piece = 0;
     // One piece: units cur .. piece_end of the row block of head h that has from .. to
     auto tile_piece = [&](const SeqBlock& sb, int h, long long from, long long to, long long cur, long long piece_end) {
@@ -1359,7 +1367,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
         SeqBlock sb;
         sb.b = t / a.Hkv;
         sb.blk = blk;
-        sequence_rows(a, sb);
+        sequence_rows(a, sb, first_n);
         tile_piece(sb, t - sb.b * a.Hkv, from, to, cur, piece_end);
         cur = piece_end;
     }
@@ -1527,8 +1535,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
         int n, all, b_hi, b_lo, own;  // new tokens, sets, blocks
     };
     auto table_of = [&](int t) {
-        int n = a.new_len[t / a.Hkv];
-        n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
+        const int n = new_tokens(a, t / a.Hkv);
         Table x{n, (n + kPos - 1) / kPos * HS, 0, 0, 0};
         if (!score_short(n, G)) {
             const SecLens len = section_lens<LI>(a, t);
@@ -1555,6 +1562,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
     // consecutive shares on one XCD: they read the same tables
     const int share = gridDim.x % 8 == 0 ? ((int)blockIdx.x & 7) * ((int)gridDim.x >> 3) + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
     const long long start = share * quantum, stop = min(total_units, start + quantum);
+    const int first_n = first_tokens(a);
     int piece = 0;
     for (long long cur = start; cur < stop;) {
     // the table that has unit `cur`
@@ -1585,7 +1593,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
     }
     SeqBlock sb;
     sb.b = t / a.Hkv;
-    sequence_rows(a, sb);
+    sequence_rows(a, sb, first_n);
     const int n = sb.n, h = t - sb.b * a.Hkv;
     const int first = a.seq_len[sb.b];
     const SecLens lens = section_lens<LI>(a, t);
@@ -1790,12 +1798,12 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores_short(Chu
     SeqBlock sb;
     sb.b = item / a.splits;
     const int share = item - sb.b * a.splits;
-    sequence_rows(a, sb);
-    const int n = sb.n;
-    if (n == 0 || !score_short(n, G)) return;
     const int t = sb.b * a.Hkv + h;
     const SecLens len = section_lens<LI>(a, t);
     const int first = a.seq_len[sb.b], len_hi = len.hi, len_lo = len.lo;
+    sequence_rows(a, sb, first_tokens(a));
+    const int n = sb.n;
+    if (n == 0 || !score_short(n, G)) return;
     const int s_hi = (len_hi + 31) >> 5, s_lo = (len_lo + 31) >> 5, steps = s_hi + s_lo + 1;  // (the last: own tokens)
     const int shares = min(a.splits, (steps + kScoreWaves - 1) / kScoreWaves);
     if (share >= shares) return;

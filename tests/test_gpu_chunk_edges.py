@@ -10,9 +10,9 @@ torch = pytest.importorskip("torch")
 if not torch.cuda.is_available():  # pragma: no cover
     pytest.skip("needs a GPU", allow_module_level=True)
 
-from chunk_ref import D, filled  # noqa: E402
+from chunk_ref import D, filled, kept_tokens  # noqa: E402
 from paper_2412_03131_amd import diffkv as dk  # noqa: E402
-from test_gpu_chunk import DEV, LAYOUTS, SCALE, fused  # noqa: E402
+from test_gpu_chunk import DEV, LAYOUTS, SCALE, check_attention, check_scores, fused  # noqa: E402
 
 # Chunks that reach every kernel with eight query heads on two KV heads: single tokens (blocks of one row tile,
 # short scores), a few (two row tiles), tens (scores of long chunks), and more rows than the few-row kernel takes
@@ -60,3 +60,22 @@ def test_lengths_past_the_table_stay_in_its_row(layout, new_len):
             cache.pool.copy_(pool)
             got.append(run(cache, new_len, q, k, v) + (cache.pool.clone(),))
         assert same(*got)
+
+
+@pytest.mark.parametrize("new_len", [[1, 0, 1], [0, 1, 0], [0] * 40 + [1] * 60 + [0, 1] * 20, [0, 1, 1] * 500], ids=len)
+def test_single_tokens_of_a_padded_batch(new_len):
+    """As many rows as sequences, one token at most each, but some sequences have none: every token goes with its
+    own sequence's cache, rows that no sequence owns stay as they were, and so do the scores of sequences without
+    new tokens.  (few tables, tables found by a workgroup's scan, tables that are not split)"""
+    rng = np.random.default_rng(len(new_len))
+    B, n = len(new_len), sum(new_len)
+    lens = rng.integers(0, 120, B)
+    cache = filled(dk, {}, B, 1, lens, seed=B, max_len=256)
+    q, k, v = fused(rng, B, 4, 1)
+    print("case: a padded batch of %d" % B, flush=True)
+    before = kept_tokens(cache)
+    out, lse, score = run(cache, new_len, q, k, v)
+    check_attention(cache, new_len, q[:n], k[:n], v[:n], out[:n], lse[:n], "padded")
+    check_scores(cache, before, new_len, q[:n], k[:n], lse[:n], score[:n], "padded")
+    for x in (out, lse, score):
+        assert bool((x[n:] == 7.0).all())

@@ -1534,10 +1534,11 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
     struct Table {
         int n, all, b_hi, b_lo, own;  // new tokens, sets, blocks
     };
+    auto takes = [&](int n) { return n > 0 && (a.all_lengths || !score_short(n, G)); };
     auto table_of = [&](int t) {
         const int n = new_tokens(a, t / a.Hkv);
         Table x{n, (n + kPos - 1) / kPos * HS, 0, 0, 0};
-        if (!score_short(n, G)) {
+        if (takes(n)) {
             const SecLens len = section_lens<LI>(a, t);
             x.b_hi = (len.hi + kScoreBlock - 1) / kScoreBlock;
             x.b_lo = (len.lo + kScoreBlock - 1) / kScoreBlock;
@@ -1617,7 +1618,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, 4) void chunk_scores(ChunkArgs
         const long long from = table_at + units_to(tb, blk), to = table_at + units_to(tb, blk + 1);
         const long long piece_from = cur, piece_end = min(stop, to);
         cur = piece_end;
-        if (n == 0 || score_short(n, G)) continue;  // (lengths that do not sum to total_new)
+        if (!takes(n)) continue;  // (lengths that do not sum to total_new)
         const int sec = blk < b_hi ? 0 : (blk < b_hi + b_lo ? 1 : 2);
         const int len = sec == 0 ? len_hi : (sec == 1 ? len_lo : n);
         const int tok0 = (blk - (sec == 0 ? 0 : (sec == 1 ? b_hi : b_hi + b_lo))) * kScoreBlock + wave * kScoreTokens;

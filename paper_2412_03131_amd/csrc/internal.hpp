@@ -269,6 +269,7 @@ struct ChunkArgs {
     unsigned long long* arrive;  // arrival word per row block (split ones)
     float* part;           // [row block][split][row] partial states {acc[kD], max, sum}
     int splits;            // few rows: 1 if none is split; short scores: workgroups per table
+    bool all_lengths;      // scores of long chunks: also of the short ones
     bool one_block;        // few rows, none split: a sequence has one row block at most, block i is sequence i's
     int pieces;            // few rows: the pieces that all row blocks are cut into, about
     int blocks;            // few rows: arrival words of row blocks

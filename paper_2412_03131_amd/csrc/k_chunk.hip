@@ -47,14 +47,15 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     };
     if (rows > plan.few_rows) {
         ChunkArgs a = args;
-        a.rows_lo = 17;
+        // With room for the longest chunk in every sequence all lengths are that one, or the rows are padded:
+        // these take all sequences then, and no second launch (4-5 us) looks for shorter ones.
+        const bool all = args.total_new == (long long)args.B * args.max_new;
+        a.rows_lo = all ? 1 : 17;
         a.rows_hi = INT32_MAX;
         a.arrive = arrive + plan.few_blocks;
         a.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(part) + align256(plan.few_part * 4));
         const hipError_t e = launch(a, 3, kTileShares, kTileThreads);
-        if (e != hipSuccess) return e;
-        // (all sequences have the one length then)
-        if (args.total_new == (long long)args.B * args.max_new) return hipSuccess;
+        if (e != hipSuccess || all) return e;
     }
     // Few rows: all sequences if none is longer, else those of one block of 16 rows
     ChunkArgs a = args;
@@ -90,10 +91,11 @@ hipError_t launch_chunk_scores(const ChunkArgs& args, bool mod, hipStream_t st)
         // of sixteen positions: 4 query heads per KV head 100 / 109 us, 3 100 / 95, 5 160 / 128, 6 159 / 144, 7 165 / 164)
         const void* kern = chunk_kernel(a.layout, G % 4 == 0 ? 4 : 0, mod);
         if (!kern) return hipErrorInvalidValue;
+        // (as for attention: one length, or padded rows)
+        a.all_lengths = a.total_new == (long long)a.B * a.max_new;
         void* kargs[] = {&a};
         const hipError_t e = hipLaunchKernel(kern, dim3(kScoreShares), dim3(8 * kWave), kargs, 0, st);
-        // (all sequences have the one length then)
-        if (e != hipSuccess || a.total_new == (long long)a.B * a.max_new) return e;
+        if (e != hipSuccess || a.all_lengths) return e;
     }
     const void* kern = chunk_kernel(a.layout, 5, mod);
     if (!kern) return hipErrorInvalidValue;

@@ -79,3 +79,21 @@ def test_single_tokens_of_a_padded_batch(new_len):
     check_scores(cache, before, new_len, q[:n], k[:n], lse[:n], score[:n], "padded")
     for x in (out, lse, score):
         assert bool((x[n:] == 7.0).all())
+
+
+@pytest.mark.parametrize("max_new,new_len", [(100, [100, 1]), (300, [300, 1]), (300, [2, 16, 0, 300, 17]), (300, [0, 3]),
+                                             (300, [3]), (300, [90]), (16, [16, 3, 0])], ids=str)
+def test_rows_padded_to_the_longest_chunk(max_new, new_len):
+    """As many rows as sequences times the longest chunk, with shorter and empty chunks among them: the short
+    ones' outputs and scores are there, rows that no sequence owns stay as they were."""
+    rng = np.random.default_rng(len(new_len))
+    B, n = len(new_len), sum(new_len)
+    cache = filled(dk, {}, B, 2, [300, 70, 0, 150, 40][:B], seed=B)
+    q, k, v = fused(rng, B * max_new, 16, 2)
+    print("case: %s padded to %d" % (new_len, max_new), flush=True)
+    before = kept_tokens(cache)
+    out, lse, score = run(cache, new_len, q, k, v, max_new=max_new)
+    check_attention(cache, new_len, q[:n], k[:n], v[:n], out[:n], lse[:n], "padded")
+    check_scores(cache, before, new_len, q[:n], k[:n], lse[:n], score[:n], "padded")
+    for x in (out, lse, score):
+        assert bool((x[n:] == 7.0).all())

@@ -24,10 +24,16 @@ ChunkPlan chunk_plan(long long B, long long Hq, long long Hkv, long long total_n
     const long long seqs = B < total_new ? B : total_new;
     auto clamp = [](long long x, long long lo, long long hi) { return x < lo ? lo : (x > hi ? hi : x); };
     p.few_rows = total_new * Hq <= kChunkFewTotal && rows > kChunkFewRows ? rows : kChunkFewRows;
-    p.few_blocks = Hkv * clamp(rows / 16 + 2 * seqs, 0, seqs * ((p.few_rows + 31) / 32 * 2));  // (in blocks of 32: two each)
-    p.few_split = B * Hkv < kRowPieces;  // (not by the rows: a workspace for many serves calls of fewer)
+    auto blocks_of = [&](long long n) {  // (in blocks of 32: two each)
+        return Hkv * clamp(rows / 16 + 2 * n, 0, n * ((p.few_rows + 31) / 32 * 2));
+    };
+    p.few_blocks = blocks_of(seqs);
+    p.few_split = B * Hkv < kRowPieces;
+    // Room for the states of the largest batch up to this one that is split, and not by the rows: a workspace
+    // for many sequences and rows serves calls of fewer.
     // (row_piece makes at most kRowPieces and one per block of them, of 16 rows; of 32 half as many)
-    p.few_part = p.few_split ? (kRowPieces + p.few_blocks) * 16 * kChunkPart : 0;
+    const long long split = clamp((kRowPieces - 1) / Hkv, 0, seqs);
+    p.few_part = split > 0 ? (kRowPieces + blocks_of(split)) * 16 * kChunkPart : 0;
     p.bytes = align256((p.few_blocks + kTileShares) * 8) + align256(p.few_part * 4) +
               (rows > p.few_rows ? 2ll * kTileShares * kChunkRows * kChunkPart * 4 : 0);
     return p;

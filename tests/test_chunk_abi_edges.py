@@ -1,0 +1,28 @@
+"""Sizes and refusals of the chunk operators and rotary positions at the ends of their ranges (CPU only; no call
+here reaches a kernel)."""
+import os
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def dk():
+    from paper_2412_03131_amd import diffkv
+    if not os.path.exists(diffkv.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    diffkv.lib()
+    return diffkv
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(32, 8), (32, 32), (8, 1), (5, 5), (64, 8), (28, 4), (1024, 1024), (1200, 1200)])
+def test_a_workspace_for_more_sequences_serves_fewer(dk, Hq, Hkv):
+    """The size never falls as the batch grows, past the batch from which tables are not split too (1024 tables)."""
+    L = dk.layout(max_seq_len=4096)
+    border = -(-1024 // Hkv)
+    seqs = sorted({s for s in (*range(1, 70), 127, 128, 129, border - 1, border, border + 1, 4 * border) if s > 0})
+    for rows in (1, 2, 31, 32, 64, 65, 127, 128, 300, 1024, 8192, 70000):
+        need = [dk.workspace_size(dk.OP_CHUNK_ATTENTION, L, s, Hq, Hkv, rows) for s in seqs]
+        assert need == sorted(need), rows
+        need = [dk.workspace_size(dk.OP_CHUNK_SIGNIFICANCE, L, s, Hq, Hkv, rows) for s in seqs]
+        assert need == sorted(need), rows

@@ -168,13 +168,17 @@ struct Rows {
     float unit[RT];   // logit = unit * product sum (log2 units, natural ones with a score form)
     int p[RT];        // position in the sequence
     ScoreForm form[RT];
-    float m[RT], l[RT];
+    float m[RT], l[RT];  // (m: raise_max)
     f4 acc[RT][8];    // O^T: dims 16 dt + 4 quarter + r of row c
 };
 
 // One step's scores against the running softmax: sums x[rt][t][r] of tokens (t, 4 quarter + r), a
-// logit being unit * x, -> weights 2^(logit - m).  The running max is raised only when a logit
-// passes it by 8 (weights up to 2^8).  before() is called where it is, before anything is scaled.
+// logit being unit * x, -> weights 2^(logit - m), with m the running max less 7: a weight enters its
+// product as fp16, whose denormals end at 2^-24, so the offset keeps what is 2^-32 of the largest (without it
+// everything below 2^-25 was lost from the sums of values, yet counted in the normalizer).  The running max is
+// raised only when a logit passes it by 8 (weights up to 2^15).  before() is called where it is, before
+// anything is scaled.
+constexpr float kWeightBits = 7.0f, kRaiseBits = 8.0f;
 template <int RT, typename F>
 __device__ __forceinline__ void raise_max(Rows<RT>& R, const float (&unit)[RT], const float (&x)[RT][2][4], F&& before)
 {
@@ -184,13 +188,13 @@ __device__ __forceinline__ void raise_max(Rows<RT>& R, const float (&unit)[RT], 
     for (int rt = 0; rt < RT; ++rt) {
         top[rt] = max3(max3(x[rt][0][0], x[rt][0][1], x[rt][0][2]), x[rt][0][3], max3(x[rt][1][0], x[rt][1][1], x[rt][1][2]));
         top[rt] = max3(top[rt], x[rt][1][3], kLowest) * unit[rt];
-        raise |= top[rt] > R.m[rt] + 8.0f;
+        raise |= top[rt] > R.m[rt] + (kWeightBits + kRaiseBits);
     }
     if (!__any(raise)) return;
     before();
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        top[rt] = fmaxf(R.m[rt], rows_max(top[rt]));
+        top[rt] = fmaxf(R.m[rt], rows_max(top[rt]) - kWeightBits);
         const float f = __builtin_amdgcn_exp2f(R.m[rt] - top[rt]);
         R.m[rt] = top[rt];
         R.l[rt] *= f;

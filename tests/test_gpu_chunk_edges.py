@@ -10,9 +10,9 @@ torch = pytest.importorskip("torch")
 if not torch.cuda.is_available():  # pragma: no cover
     pytest.skip("needs a GPU", allow_module_level=True)
 
-from chunk_ref import D, filled, kept_tokens  # noqa: E402
+from chunk_ref import D, filled, kept_tokens, logits, softmax  # noqa: E402
 from paper_2412_03131_amd import diffkv as dk  # noqa: E402
-from test_gpu_chunk import DEV, LAYOUTS, SCALE, check_attention, check_scores, fused  # noqa: E402
+from test_gpu_chunk import DEV, H16, LAYOUTS, SCALE, check_attention, check_scores, delta, fused  # noqa: E402
 
 # Chunks that reach every kernel with eight query heads on two KV heads: single tokens (blocks of one row tile,
 # short scores), a few (two row tiles), tens (scores of long chunks), and more rows than the few-row kernel takes
@@ -97,3 +97,50 @@ def test_rows_padded_to_the_longest_chunk(max_new, new_len):
     check_scores(cache, before, new_len, q[:n], k[:n], lse[:n], score[:n], "padded")
     for x in (out, lse, score):
         assert bool((x[n:] == 7.0).all())
+
+
+def cache_of(layout, keys, values, high, scores=None, max_len=None):
+    """One table that holds the given tokens' keys and values [n, D], the `high` of the largest scores high."""
+    n = len(keys)
+    cache = dk.Cache(dk.layout(max_seq_len=max_len or n + 512, **layout), 2 * (n // 16 + 4), 1, 1, device=DEV)
+    to = lambda a, t: torch.from_numpy(np.ascontiguousarray(a, dtype=t)).to(DEV)
+    score = np.random.default_rng(n).random((n, 1)) if scores is None else np.asarray(scores)[:, None]
+    dk.quantize_append(cache, to([n], np.int32), to(keys[:, None], np.float16), to(values[:, None], np.float16),
+                       to(score, np.float32), quota=to([[[high, n - high]]], np.int32), total_new=n, max_new=n)
+    torch.cuda.synchronize()
+    assert int(cache.status.cpu()[0]) == 0 and cache.len.cpu().tolist() == [[high, n - high]]
+    return cache
+
+
+def attention_bounds(cache, new_len, q, k, v, small, **form):
+    """Per (sequence, KV head): rows, expected outputs, and bounds where a weight's error is at most `small` of its
+    row's largest weight besides its relative error (half a step of fp16) and the values' (the same)."""
+    kept, G = kept_tokens(cache), q.shape[1] // cache.num_kv_heads
+    vv = v.cpu().numpy().astype(np.float64)
+    for b, h, row, n, x, size in logits(cache, kept, new_len, q, k, SCALE, **form):
+        vals = np.concatenate([kept[b * cache.num_kv_heads + h][1], vv[row:row + n, h]])
+        p, _ = softmax(x)
+        want, A = p @ vals, p @ np.abs(vals)
+        tol = H16 * (2 * A + np.abs(want)) + 2 * delta(size)[..., None] * A + 2.0 ** -25
+        tol += small * p.max(-1)[..., None] * np.abs(vals).sum(0)
+        yield slice(row, row + n), slice(h * G, (h + 1) * G), want, tol
+
+
+@pytest.mark.parametrize("n,G", [(1, 4), (6, 4), (300, 8)])
+def test_many_small_weights_count(n, G):
+    """Tokens 2^-26.5 of their row's largest each, and fifteen of them for each large one, carry all of the value.
+    A weight is at most 2^-25 / 2^7 of its row's largest off (it is an fp16 number, 2^7 for the running max,
+    which a row's largest passes by at most 2^8)."""
+    rng = np.random.default_rng(n)
+    keys, values = np.zeros((2048, D)), np.full((2048, D), 1000.0)
+    keys[::16, 3] = 26.5 * np.log(2) / SCALE / 8.0
+    values[::16] = 0.0
+    cache = cache_of({}, keys, values, 900)
+    q, k, v = (torch.zeros((n, heads, D), dtype=torch.float16, device=DEV) for heads in (G, 1, 1))
+    q[:, :, 3] = 8.0
+    v.fill_(1000.0)
+    print("case: small weights, n %d" % n, flush=True)
+    out = run(cache, [n], q, k, v)[0].cpu().numpy().astype(np.float64)
+    for rows, heads, want, tol in attention_bounds(cache, [n], q, k, v, 2.0 ** -32):
+        assert want.min() > 1e-4 and tol.max() < 0.1 * want.min()
+        assert (np.abs(out[rows, heads].transpose(1, 0, 2) - want) <= tol).all()

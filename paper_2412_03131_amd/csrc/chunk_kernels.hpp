@@ -218,11 +218,13 @@ __device__ __forceinline__ h8 pack_weights(const float (&w)[2][4])
     }
     return __builtin_bit_cast(h8, bits);
 }
-// What the rounding left of them (two 11-bit parts hold 22 bits).  With one row tile the weights enter whole
-// (64 single tokens over 1k-4k: 44 -> 46 us): the results' error against 64 bits is then the values' and
-// their own rounding alone, 1.25 times a 32-bit computation's rounded once.  With two row tiles and in
-// chunk_tiles they are rounded once, 1.5 times it: the second products would take 2 to 13 % there (eight tokens
-// for each of 64 sequences over 2048 50 -> 56 us).
+// What the rounding left of them: two parts hold a weight to 2^-22, or to 2^-32 of its row's largest where that
+// is more (raise_max).  Weights enter all kernels whole, so a token's precision does not go by which kernel or
+// how many row tiles its neighbours in a call ask for.  The results' error against 64 bits is then the
+// values' and their own rounding alone, 1.12 to 1.28 times a 32-bit computation's rounded once; with
+// weights rounded once it was up to 1.5 times.  The second products take 2 us of 46 for 64 single tokens over
+// 1k-4k, 2 % with two row tiles, 15 % in chunk_tiles (257-512 tokens for each of 8 sequences over 0-8192: 367 ->
+// 421 us, 2048 tokens over 8192 at 64 / 8 heads: 791 -> 935).
 __device__ __forceinline__ h8 pack_rest(const float (&w)[2][4], h8 P)
 {
     float rest[2][4];
@@ -323,8 +325,9 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? kChunkLog2e : R.unit[rt];
     softmax_step<RT>(R, unit, x, P);
-    h8 rest;
-    if constexpr (RT == 1) rest = pack_rest(x[0], P[0]);
+    h8 rest[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) rest[rt] = pack_rest(x[rt], P[rt]);
 #pragma unroll
     for (int g = 0; g < kNG; ++g) {
         keep_order();
@@ -365,7 +368,8 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
             const h8 V = __builtin_bit_cast(h8, v);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, P[rt], R.acc[rt][dt]);
-            if constexpr (RT == 1) R.acc[0][dt] = mfma_k32(V, rest, R.acc[0][dt]);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, rest[rt], R.acc[rt][dt]);
         }
     }
 }
@@ -442,8 +446,9 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const RowsLds<RT>& Q, cons
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) unit[rt] = MOD ? kChunkLog2e : R.unit[rt];
     softmax_step<RT>(R, unit, x, P);
-    h8 rest;
-    if constexpr (RT == 1) rest = pack_rest(x[0], P[0]);
+    h8 rest[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) rest[rt] = pack_rest(x[rt], P[rt]);
     // values: the quarter's eight tokens of dims 16 dt + c
     bool odd = false;
 #pragma unroll
@@ -462,7 +467,8 @@ __device__ __forceinline__ void own_step(Rows<RT>& R, const RowsLds<RT>& Q, cons
         const h8 V = __builtin_bit_cast(h8, w);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, P[rt], R.acc[rt][dt]);
-        if constexpr (RT == 1) R.acc[0][dt] = mfma_k32(V, rest, R.acc[0][dt]);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, rest[rt], R.acc[rt][dt]);
     }
     if (__any(odd)) odd_values<RT>(R, x, v, i0, n, first, a, c, quarter);
 }
@@ -825,11 +831,8 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
 // their values from another and the next one is made.
 // The blocks of all tables end to end are cut into equal shares, one per CU: with a workgroup per block the
 // longest ones set the time (257-512 tokens for each of 8 sequences over 0-8192: 546 us, with shares 377).
-// Bound by issue: that case takes 366 us at 160 GFLOP, 2048 tokens over 8192 at 64 / 8 heads 788 us, 577
-// TFLOP/s (an 8192^3 fp16 library product 1137); VALU 62 % busy, 34 % of the waves' time waits on LDS
-// operands, barriers and products.
-// The weights enter as fp16 once (pack_rest's second product per tile would cost half as many matrix
-// instructions again here): the outputs' error against 64 bits is 1.5 times a 32-bit computation's.
+// Bound by issue: that case takes 421 us at 160 GFLOP, 2048 tokens over 8192 at 64 / 8 heads 935 us, 486
+// TFLOP/s (an 8192^3 fp16 library product 1137), the weights' second products not counted.
 constexpr int kTileWaves = 8;
 constexpr int kTileRows = kTileWaves * 32;
 static_assert(kTileRows == kChunkRows, "row blocks of the plan");
@@ -1138,15 +1141,17 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
     __syncthreads();
     if (begin < end) put(begin, bufs[0], slots[0], now_bad);
     bufs[2].v[wave][lane] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});  // "before" the first step
-    h8 P[RT];  // the weights of the step before, whose values are still to be added
+    h8 P[RT], rest[RT];  // the weights of the step before, whose values are still to be added
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) P[rt] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
+    for (int rt = 0; rt < RT; ++rt) P[rt] = rest[rt] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
     auto add_values = [&](const TileBuf& b) {
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) {
             const h8 V = b.v[dt][lane];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, P[rt], R.acc[rt][dt]);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, rest[rt], R.acc[rt][dt]);
         }
     };
     int at = 0;  // buffer of the step
@@ -1207,13 +1212,15 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
                 raise_max<RT>(R, unit, x, [&] {  // (the step before still has the old max)
                     add_values(before);
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) P[rt] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
+                    for (int rt = 0; rt < RT; ++rt) P[rt] = rest[rt] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
                 });
                 phase();
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V[dt], P[rt], R.acc[rt][dt]);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V[dt], rest[rt], R.acc[rt][dt]);
                     if (dt + 2 < 8) V[dt + 2] = before.v[dt + 2][lane];
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {  // a score of each row tile
@@ -1226,7 +1233,10 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
                     phase();
                 }
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) P[rt] = pack_weights(x[rt]);
+                for (int rt = 0; rt < RT; ++rt) {
+                    P[rt] = pack_weights(x[rt]);
+                    rest[rt] = pack_rest(x[rt], P[rt]);
+                }
             }
             if constexpr (mine) {
                 uint32_t odd = 0;

@@ -144,3 +144,36 @@ def test_many_small_weights_count(n, G):
     for rows, heads, want, tol in attention_bounds(cache, [n], q, k, v, 2.0 ** -32):
         assert want.min() > 1e-4 and tol.max() < 0.1 * want.min()
         assert (np.abs(out[rows, heads].transpose(1, 0, 2) - want) <= tol).all()
+
+
+@pytest.mark.parametrize("own", [False, True])
+@pytest.mark.parametrize("n,G", [(2, 4), (4, 4), (30, 4), (300, 8)])
+def test_weights_enter_whole(n, G, own):
+    """Two tokens of nearly the same weight and opposite values, and nothing else that counts: what is left of them
+    shows their weights' error.  Values are whole in fp16, weights 2^-22 off at most (two parts), products and
+    sums of fp32 far below 2^-20 of the two; with each weight rounded once it would be 2^-12."""
+    print("case: whole weights, n %d, own %s" % (n, own), flush=True)
+    a, b = 1.0, 0.94
+    if own:  # the chunk's first two tokens, over an empty cache; the others' logits are 200 below
+        cache = filled(dk, {}, 1, 1, [0], seed=1)
+    else:    # one kept high, one low
+        cache = cache_of({}, np.array([[a], [b]]) * (np.arange(D) == 3), np.array([[1.0], [-1.0]]) * np.ones(D), 1, [2.0, 1.0])
+    q, k, v = (torch.zeros((n, heads, D), dtype=torch.float16, device=DEV) for heads in (G, 1, 1))
+    q[:, :, 3] = torch.linspace(4.0, 12.0, n * G, device=DEV).reshape(n, G).half()
+    k[:, :, 3] = -6000.0
+    v.fill_(1.0)
+    if own:
+        k[0, 0, 3], k[1, 0, 3] = a, b
+        v[1] = -1.0
+    out, lse, _ = run(cache, [n], q, k, v)
+    got = out.cpu().numpy().astype(np.float64)
+    for b, h, row, _, x, size in logits(cache, kept_tokens(cache), [n], q, k, SCALE):
+        vals = np.concatenate([kept_tokens(cache)[0][1], v[:, 0].cpu().numpy().astype(np.float64)])
+        p, _ = softmax(x)
+        want = p @ vals
+        # (the others have no weight, and their logits no part in the error)
+        d = 64 * 2.0 ** -24 * np.where(p > 0, size, 0.0).max(-1) + 2.0 ** -20
+        tol = H16 * np.abs(want) + (2 * d + 2.0 ** -20)[..., None] + 2.0 ** -25
+        first = 1 if own else 0  # (from the row that sees both)
+        assert (p[:, first:] > 1e-30).sum(-1).max() == 2 and tol[:, first:].max() < 2.0 ** -14
+        assert (np.abs(got.transpose(1, 0, 2) - want) <= tol)[:, first:].all()

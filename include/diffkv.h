@@ -427,11 +427,13 @@ typedef struct diffkv_score_form {
  * sm_scale above 0 and at most 1e30 (DIFFKV_E_INVAL otherwise).  The layouts of
  * diffkv_layout_init's list, up to 8 query heads per KV head.
  * Precision: q . k_hat exact up to fp32 summation, fp32 softmax statistics;
- * v_hat is rounded to fp16 (2^-11); the weights enter in two fp16 parts (2^-22,
+ * v_hat is rounded to fp16 (2^-11, or 2^-24 where that is more; up to twice the
+ * largest fp16 it is no infinity); the weights enter in two fp16 parts (2^-22,
  * or 2^-32 of their row's largest); products are summed in fp32, and out is
  * rounded once.  That holds for every row, whatever else the call carries; the
  * order of its sums, and with it the last bits, goes by the call's lengths.
- * A NaN or infinite own key or value reaches only the rows that see its token.
+ * A NaN or infinite own key or value, or v_hat, reaches only the rows that see
+ * its token.
  */
 diffkv_status diffkv_chunk_attention(const diffkv_layout* layout, const diffkv_cache* cache,
                                      int64_t total_new, int32_t max_new, const int32_t* new_len,

@@ -52,14 +52,6 @@ __device__ __forceinline__ f4 mfma_k16(h4 a, h4 b, f4 c)
     return d;
 }
 
-// s c + z of a group's largest code can round past the largest finite fp16 (s >= 0, z finite): it
-// becomes that.  (The mode bit for it, MODE.FP16_OVFL, also loses NaN operands of matrix products.)
-__device__ __forceinline__ uint32_t finite_pair(h2 x)
-{
-    const h2 top = {(_Float16)65504.0f, (_Float16)65504.0f};
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(x, top));
-}
-
 // ---- loads -----------------------------------------------------------------------
 // Through a buffer resource: a uniform base and 32-bit offsets.  (With 64-bit addresses the
 // compiler keeps one per lane and piece of a page across the loops.)

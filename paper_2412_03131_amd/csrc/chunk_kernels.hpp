@@ -131,28 +131,30 @@ __device__ __forceinline__ void load_values(GroupValues<VB, T>& r, const uint8_t
     }
 }
 
-// Four value codes of a tile (the low 4 VB bits of w) -> s c + z as fp16 pairs of tokens
-// (0, 2) and (1, 3).  A code is read as 1024 + c (its bits under the exponent of
-// 1024, exact), the second pair as 1024 + 2^VB c; two packed steps give c and s c + z, the
-// only rounding (2^-11: values N(0, 1) of a kept token, far below their own quantization).
+// Four value codes of a tile (the low 4 VB bits of w) -> half of s c + z as fp16 pairs of tokens
+// (0, 2) and (1, 3), z given halved.  A code is read as 1024 + c (its bits under the exponent of
+// 1024, exact), the second pair as 1024 + 2^VB c; two packed steps give c / 2 and (s c + z) / 2, the
+// only rounding (2^-11: values N(0, 1) of a kept token, far below their own quantization).  Halves,
+// because s c + z of a group's largest code can round past the largest finite fp16: infinite are
+// then only those that are (a limit per pair would also hide NaN); sums of cached values are doubled once.
 template <int VB>
 __device__ __forceinline__ void value_pairs(uint32_t w, h2 s02, h2 z02, h2 s13, h2 z13, uint32_t& p02, uint32_t& p13)
 {
-    const h2 m1024 = {(_Float16)-1024.0f, (_Float16)-1024.0f};
+    const h2 half = {(_Float16)0.5f, (_Float16)0.5f}, m512 = {(_Float16)-512.0f, (_Float16)-512.0f};
     h2 y02, y13;
     if constexpr (VB == 8) {
-        y02 = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, 0x04020400u)) + m1024;
-        y13 = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030401u)) + m1024;
+        y02 = __builtin_elementwise_fma(__builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, 0x04020400u)), half, m512);
+        y13 = __builtin_elementwise_fma(__builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030401u)), half, m512);
     } else {
         constexpr uint32_t m = ((1u << VB) - 1) * 0x00010001u;
         const uint32_t x = VB == 4 ? __builtin_amdgcn_perm(0u, w, 0x0C010C00u) : (w | (w << (16 - 2 * VB)));
-        const h2 inv = {(_Float16)(1.0f / (1 << VB)), (_Float16)(1.0f / (1 << VB))};
-        const h2 off = {(_Float16)(-1024.0f / (1 << VB)), (_Float16)(-1024.0f / (1 << VB))};
-        y02 = __builtin_bit_cast(h2, (x & m) | 0x64006400u) + m1024;
+        const h2 inv = {(_Float16)(0.5f / (1 << VB)), (_Float16)(0.5f / (1 << VB))};
+        const h2 off = {(_Float16)(-512.0f / (1 << VB)), (_Float16)(-512.0f / (1 << VB))};
+        y02 = __builtin_elementwise_fma(__builtin_bit_cast(h2, (x & m) | 0x64006400u), half, m512);
         y13 = __builtin_elementwise_fma(__builtin_bit_cast(h2, (x & (m << VB)) | 0x64006400u), inv, off);
     }
-    p02 = finite_pair(__builtin_elementwise_fma(s02, y02, z02));
-    p13 = finite_pair(__builtin_elementwise_fma(s13, y13, z13));
+    p02 = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(s02, y02, z02));
+    p13 = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(s13, y13, z13));
 }
 
 // The rows a wave works on: 16 RT of them, column c of tile rt is row 16 rt + c of its block.
@@ -250,11 +252,79 @@ __device__ __forceinline__ void softmax_step(Rows<RT>& R, const float (&unit)[RT
     }
 }
 
+// ---- cached values that are not finite ------------------------------------------------
+// An infinite or NaN s c + z reaches every row of a matrix product (0 * inf is NaN), which is right while every row sees
+// every cached token: only a window hides some.  In windowed calls every step's {s, z} are looked at; a group
+// with one that is not finite (or twice the largest half) enters the products as 0, and a piece that met one adds
+// its s c + z in fp32 at the end (odd_four), each logit computed anew.
+template <int VB>
+__device__ __forceinline__ bool odd_group(uint32_t sz)
+{
+    const h2 m = __builtin_bit_cast(h2, sz);
+    return !(fabsf(__builtin_fmaf((float)m.x, (float)((1 << VB) - 1), (float)m.y)) < 131008.0f);
+}
+// A row (of the chunk's, of table t) and the cached steps u0 .. u1 - 1 that its piece went over.
+struct OddRow {
+    const ChunkArgs* args;
+    int t, row, u0, u1;
+    long long row0;  // the sequence's first token row
+    float m;         // the row's running max
+};
+template <int KB, int VB, int T>
+__device__ __forceinline__ void odd_section(f4& o, const ChunkArgs& a, const int32_t* table, bool high, int len, int u0, int u1,
+                                            const uint16_t* q, int p, const ScoreForm& form, float m, int d)
+{
+    constexpr SecOffsets O = sec_offsets(KvFmt{KB, VB, T});
+#pragma unroll 1
+    for (int token = 32 * max(u0, 0); token < min(32 * u1, len); ++token) {
+        const int slot = token % T, id = table[high ? token / T : a.p_max - 1 - token / T];
+        if ((unsigned long long)(unsigned)id >= (unsigned long long)a.num_pages) continue;
+        const uint8_t* pg = a.pool + (long long)id * a.page_bytes;
+        const uint32_t sz = *reinterpret_cast<const uint32_t*>(pg + O.vm + ((d >> 5) * T + slot) * 4);
+        const int away = p - *reinterpret_cast<const int32_t*>(pg + O.pos + 4 * slot);
+        if (!odd_group<VB>(sz) || away >= a.window) continue;
+        float x = 0.0f;
+#pragma unroll 1
+        for (int i = 0; i < kD; ++i) {
+            const int code = KB == 8 ? pg[O.kc + ((i >> 4) * T + slot) * 16 + (i & 15)]
+                                     : pg[O.kc + ((i >> 5) * T + slot) * 16 + ((i & 31) >> 1)] >> (4 * (i & 1)) & 15;
+            const h2 k = *reinterpret_cast<const h2*>(pg + O.km + slot * 16 + (i >> 5) * 4);
+            x = __builtin_fmaf(h2f(q[i]), __builtin_fmaf((float)k.x, (float)code, (float)k.y), x);
+        }
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(formed(x * a.scale, form, (float)away), kChunkLog2e, -m));
+        const h2 v = __builtin_bit_cast(h2, sz);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int byte = pg[O.vc + (d + i) * (T * VB / 8) + slot * VB / 8];
+            o[i] += w * __builtin_fmaf((float)v.x, (float)(byte >> (slot * VB % 8) & ((1 << VB) - 1)), (float)v.y);
+        }
+    }
+}
+// The sums o of four dims d .. of one group, with what odd groups add.  A function of its own that reads the launch's
+// arguments itself: inlined, or given them, it took registers from the loops (drafted tokens 34.6 -> 38 us).
+template <int LI>
+__device__ __noinline__ f4 odd_four(f4 o, OddRow r, int d)
+{
+    constexpr KvFmt hi = kLayoutFmts[LI].hi, lo = kLayoutFmts[LI].lo;
+    const ChunkArgs& a = *r.args;
+    const int G = a.Hq / a.Hkv, b = r.t / a.Hkv, j = r.row / G, hq = (r.t - b * a.Hkv) * G + r.row - j * G;
+    const SecLens len = section_lens<LI>(a, r.t);
+    const int s_hi = (len.hi + 31) >> 5, p = a.seq_len[b] + j;
+    const int32_t* table = a.page_table + (long long)r.t * a.p_max;
+    const uint16_t* q = a.q + (r.row0 + j) * a.q_stride + hq * kD;
+    const ScoreForm form{a.cap_in, a.cap, a.slopes ? a.slopes[hq] : 0.0f};
+    odd_section<hi.kb, hi.vb, hi.T>(o, a, table, true, len.hi, r.u0, r.u1, q, p, form, r.m, d);
+    odd_section<lo.kb, lo.vb, lo.T>(o, a, table, false, len.lo, r.u0 - s_hi, r.u1 - s_hi, q, p, form, r.m, d);
+    return o;
+}
+// The launch's arguments where they lie.
+__device__ __forceinline__ const ChunkArgs* chunk_args() { return (const ChunkArgs*)__builtin_amdgcn_kernarg_segment_ptr(); }
+
 // A step of cached tokens in the wave's slot; those with index >= left (in the step, by token) and
 // those of tile t where bit t of `bad` is set (a page ID outside the pool) do not exist.
-// next() is called once the slot has been read.
+// next() is called once the slot has been read.  Whether the step has odd groups (uniform).
 template <int KB, int VB, int T, int RT, bool MOD, typename F>
-__device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, const uint8_t* slot, int left, uint32_t bad,
+__device__ __forceinline__ bool cached_step(Rows<RT>& R, const RowsLds<RT>& Q, uint8_t* slot, int left, uint32_t bad,
                                             const ChunkArgs& a, int lane, F&& next)
 {
     const int c = lane & 15, quarter = lane >> 4;
@@ -305,6 +375,17 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
                 }
         }
     }
+    bool odd = false;
+    if (MOD && a.window != INT32_MAX) {  // a lane looks at {s, z} of two tokens and one group
+        constexpr SecOffsets O = sec_offsets(KvFmt{KB, VB, T});
+        uint8_t* at = slot + O.vm + (T == 16 ? (lane >> 5) * Staged<KB, VB, T, MOD>::page + 8 * (lane & 31) : 8 * lane);
+        const int token = T == 16 ? 16 * (lane >> 5) + 2 * (lane & 7) : 2 * (lane & 15);
+        const u2 sz = *reinterpret_cast<const u2*>(at);
+        const bool in = !((bad >> (T == 16 ? lane >> 5 : 0)) & 1);
+        const bool odd0 = odd_group<VB>(sz[0]) && token < left && in, odd1 = odd_group<VB>(sz[1]) && token + 1 < left && in;
+        odd = __any(odd0 || odd1);
+        if (__builtin_expect(odd, 0)) *reinterpret_cast<u2*>(at) = u2{odd0 ? 0u : sz[0], odd1 ? 0u : sz[1]};
+    }
     uint32_t keep[2] = {0xfu, 0xfu};  // which of the quarter's tokens exist
     const bool whole = left >= 32 && bad == 0;
     if (!whole) {
@@ -342,9 +423,9 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
         for (int t = 0; t < 2; ++t) {
             const u4 m = val.vm[t];
             s02[t] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x05040100u));
-            z02[t] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x07060302u));
+            z02[t] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x07060302u)) * (_Float16)0.5f;
             s13[t] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[3], m[1], 0x05040100u));
-            z13[t] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[3], m[1], 0x07060302u));
+            z13[t] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[3], m[1], 0x07060302u)) * (_Float16)0.5f;
         }
 #pragma unroll
         for (int d = 0; d < 2; ++d) {
@@ -372,6 +453,7 @@ __device__ __forceinline__ void cached_step(Rows<RT>& R, const RowsLds<RT>& Q, c
             for (int rt = 0; rt < RT; ++rt) R.acc[rt][dt] = mfma_k32(V, rest[rt], R.acc[rt][dt]);
         }
     }
+    return odd;
 }
 
 // An infinite or NaN own value must not reach the rows that do not see its token (0 * inf in a matrix
@@ -597,6 +679,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
     };
     __shared__ __align__(1024) Shared lds;
     __shared__ RowsLds<RT> Q;
+    __shared__ int odd_waves[kChunkWaves], odd_at[3];  // (the table and the piece's cached steps, kept out of the registers)
     const int lane = lane_id(), wave = wave_index();
     const int c = lane & 15, quarter = lane >> 4;
     const int G = a.Hq / a.Hkv;
@@ -708,8 +791,14 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
     }
+    if (MOD && threadIdx.x == 0) {
+        odd_at[0] = t;
+        odd_at[1] = begin;
+        odd_at[2] = cached;
+    }
     __syncthreads();
     if (u < cached) stage(u, n0, n1);
+    bool odd = false;  // whether the wave met odd groups
     {
         while (u < cached) {
             const int next = u + kChunkWaves;
@@ -722,11 +811,15 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
                 if (next < cached) stage(next, n0, n1);
             };
             staged_ready();
-            if (u < s_hi) cached_step<hi.kb, hi.vb, hi.T, RT, MOD>(R, Q, slot, len_hi - 32 * u, b, a, fresh(lane), ahead);
-            else cached_step<lo.kb, lo.vb, lo.T, RT, MOD>(R, Q, slot, len_lo - 32 * (u - s_hi), b, a, fresh(lane), ahead);
+            if (u < s_hi) odd |= cached_step<hi.kb, hi.vb, hi.T, RT, MOD>(R, Q, slot, len_hi - 32 * u, b, a, fresh(lane), ahead);
+            else odd |= cached_step<lo.kb, lo.vb, lo.T, RT, MOD>(R, Q, slot, len_lo - 32 * (u - s_hi), b, a, fresh(lane), ahead);
             u = next;
         }
     }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] *= 2.0f;  // (value_pairs)
     {
         const uint16_t* k = a.k + sb.row0 * a.k_stride + h * kD;
         const uint16_t* v = a.v + sb.row0 * a.v_stride + h * kD;
@@ -752,6 +845,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
     };
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
+        if (MOD && lane == 0) odd_waves[wave] = odd;
         __syncthreads();
         const float l = rows_sum(R.l[rt]);
         if (quarter == 0) {
@@ -774,6 +868,15 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
             for (int i = 0; i < 4; ++i) {
                 o[i] += f * x[i];
                 o[i + 4] += f * y[i];
+            }
+        }
+        if (MOD && __builtin_expect(odd_waves[0] | odd_waves[1] | odd_waves[2] | odd_waves[3], 0)) {
+            const OddRow r{chunk_args(), odd_at[0], min(r0 + 16 * rt + row, rows - 1), odd_at[1], odd_at[2], sb.row0, m};
+            const f4 x = odd_four<LI>(f4{o[0], o[1], o[2], o[3]}, r, d), y = odd_four<LI>(f4{o[4], o[5], o[6], o[7]}, r, d + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                o[i] = x[i];
+                o[i + 4] = y[i];
             }
         }
         if (splits == 1) {
@@ -850,9 +953,10 @@ struct TileBuf {
 
 // The staged pages of a step (slot) into operands: wave w makes the key operand of tile w / 4, group
 // w % 4, and the value operand of dims 16 w ..; wave 0 the metadata.  Tokens with index >= left and
-// those of tile t where bit t of `bad` is set do not exist.
+// those of tile t where bit t of `bad` is set do not exist.  Odd groups are left at 0 and noted in *odd
+// (null: not looked for).
 template <int KB, int VB, int T, bool MOD>
-__device__ __forceinline__ void tile_put(TileBuf& b, const uint8_t* slot_, int left, uint32_t bad, int wave, int lane)
+__device__ __forceinline__ void tile_put(TileBuf& b, const uint8_t* slot_, int left, uint32_t bad, int* odd, int wave, int lane)
 {
     constexpr SecOffsets O = sec_offsets(KvFmt{KB, VB, T});
     constexpr int page = T == 16 ? Staged<KB, VB, T, MOD>::page : 0;  // from one tile's page to the other's
@@ -879,9 +983,9 @@ __device__ __forceinline__ void tile_put(TileBuf& b, const uint8_t* slot_, int l
         const u4 m = *reinterpret_cast<const u4*>(slot_ + t * page + O.vm + ((wave >> 1) * T + step_slot<T>(t, 4 * quarter)) * 4);
         uint32_t p, q;
         value_pairs<VB>(codes[t], __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x05040100u)),
-                        __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x07060302u)),
+                        __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[2], m[0], 0x07060302u)) * (_Float16)0.5f,
                         __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[3], m[1], 0x05040100u)),
-                        __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[3], m[1], 0x07060302u)), p, q);
+                        __builtin_bit_cast(h2, __builtin_amdgcn_perm(m[3], m[1], 0x07060302u)) * (_Float16)0.5f, p, q);
         v[2 * t] = p;
         v[2 * t + 1] = q;
     }
@@ -893,6 +997,20 @@ __device__ __forceinline__ void tile_put(TileBuf& b, const uint8_t* slot_, int l
             };
             v[2 * t] &= (none(0) ? 0u : 0xffffu) | (none(2) ? 0u : 0xffff0000u);
             v[2 * t + 1] &= (none(1) ? 0u : 0xffffu) | (none(3) ? 0u : 0xffff0000u);
+        }
+    }
+    if (MOD && odd) {  // (a lane looks at one token's {s, z} of the wave's group)
+        const int token = lane & 31;
+        const uint32_t sz = *reinterpret_cast<const uint32_t*>(slot_ + (T == 16 ? (token >> 4) * page : 0) + O.vm +
+                                                               ((wave >> 1) * T + token % T) * 4);
+        if (__builtin_expect(__any(odd_group<VB>(sz) && token < left && !((bad >> (T == 16 ? token >> 4 : 0)) & 1)), 0)) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const u4 m = *reinterpret_cast<const u4*>(slot_ + t * page + O.vm + ((wave >> 1) * T + step_slot<T>(t, 4 * quarter)) * 4);
+                v[2 * t] &= (odd_group<VB>(m[0]) ? 0u : 0xffffu) | (odd_group<VB>(m[2]) ? 0u : 0xffff0000u);
+                v[2 * t + 1] &= (odd_group<VB>(m[1]) ? 0u : 0xffffu) | (odd_group<VB>(m[3]) ? 0u : 0xffff0000u);
+            }
+            if (lane == 0) *odd = 1;
         }
     }
     b.v[wave][lane] = __builtin_bit_cast(h8, v);
@@ -1011,7 +1129,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
         TileBuf bufs[3];
         long long scan[kTileWaves];
         long long found_at;
-        int found, last;
+        int found, last, odd;
     };
     __shared__ __align__(1024) Shared sh;
     auto& slots = sh.slots;
@@ -1129,14 +1247,16 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
         }
         return two ? (id0 < 0 ? 1u : 0u) | (id1 < 0 ? 2u : 0u) : (id0 < 0 ? 3u : 0u);
     };
+    int* const odd_word = MOD && a.window != INT32_MAX ? &sh.odd : nullptr;
     auto put = [&](int u, TileBuf& b, const uint8_t* slot, uint32_t bad) {
-        if (u < s_hi) tile_put<hi.kb, hi.vb, hi.T, MOD>(b, slot, len_hi - 32 * u, bad, wave, fresh(lane));
-        else if (u < s_hi + s_lo) tile_put<lo.kb, lo.vb, lo.T, MOD>(b, slot, len_lo - 32 * (u - s_hi), bad, wave, fresh(lane));
+        if (u < s_hi) tile_put<hi.kb, hi.vb, hi.T, MOD>(b, slot, len_hi - 32 * u, bad, odd_word, wave, fresh(lane));
+        else if (u < s_hi + s_lo) tile_put<lo.kb, lo.vb, lo.T, MOD>(b, slot, len_lo - 32 * (u - s_hi), bad, odd_word, wave, fresh(lane));
         else tile_put_own(b, slot, own - 32 * (u - s_hi - s_lo), first + 32 * (u - s_hi - s_lo), wave, fresh(lane));
     };
     // steps begin, begin + 1 on their way; `bad` of the step that is computed, the next and the one after
     uint32_t now_bad = begin < end ? load(begin, slots[0]) : 0, next_bad = begin + 1 < end ? load(begin + 1, slots[1]) : 0;
     uint32_t last_bad = 0;
+    if (MOD && threadIdx.x == 0) sh.odd = 0;
     staged_ready();
     __syncthreads();
     if (begin < end) put(begin, bufs[0], slots[0], now_bad);
@@ -1265,8 +1385,44 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
         __syncthreads();
     };
     for (int u = begin; u < min(end, s_hi + s_lo); ++u) step(u, std::false_type{});
-    for (int u = max(begin, s_hi + s_lo); u < end; ++u) step(u, std::true_type{});
-    if (!idle) add_values(bufs[at == 0 ? 2 : at - 1]);
+    if (!idle) {
+        add_values(bufs[at == 0 ? 2 : at - 1]);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            P[rt] = rest[rt] = __builtin_bit_cast(h8, u4{0, 0, 0, 0});
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) R.acc[rt][dt] *= 2.0f;  // (value_pairs)
+        }
+    }
+    if (end > s_hi + s_lo) {
+        for (int u = max(begin, s_hi + s_lo); u < end; ++u) step(u, std::true_type{});
+        if (!idle) add_values(bufs[at == 0 ? 2 : at - 1]);
+    }
+    // A wave's part of a piece's state in the workspace: its accumulators lane by lane (1 KB each), then max and sum
+    // of its rows.  A share's first piece has slot 0, the others slot 1, whose last one is read by others.
+    constexpr int kWavePart = RT * 8 * 1024 + RT * 128;
+    static_assert(kTileWaves * kWavePart <= kTileRows * kChunkPart * 4, "a piece's room in the workspace");
+    auto part_of = [&](int k, bool first_piece) {
+        return span(reinterpret_cast<uint8_t*>(a.part + (2ll * k + (first_piece ? 0 : 1)) * kTileRows * kChunkPart) +
+                        wave * kWavePart,
+                    kWavePart);
+    };
+    if (MOD && !idle && __builtin_expect(__builtin_amdgcn_readfirstlane(sh.odd), 0)) {
+        // (the sums wait in the workspace: beside them there are no registers for this)
+        const __amdgpu_buffer_rsrc_t room = part_of(share, piece == 0);
+#pragma unroll
+        for (int i = 0; i < RT * 8; ++i) put_quad(room, lane * 16, i * 1024, R.acc[i / 8][i % 8]);
+        staged_ready();
+#pragma unroll 1
+        for (int i = 0; i < RT * 8; ++i) {
+            const OddRow r{chunk_args(), t, min(r0 + 2 * (i & 8) + c, rows - 1), begin, min(end, s_hi + s_lo), sb.row0,
+                           i < 8 ? R.m[0] : R.m[1]};
+            put_quad(room, lane * 16, i * 1024, odd_four<LI>(get_quad(room, lane * 16, i * 1024), r, 16 * (i & 7) + 4 * quarter));
+        }
+        staged_ready();
+#pragma unroll
+        for (int i = 0; i < RT * 8; ++i) R.acc[i / 8][i % 8] = get_quad(room, lane * 16, i * 1024);
+    }
 
     float l[RT];
 #pragma unroll
@@ -1294,14 +1450,6 @@ __global__ __launch_bounds__(kTileWaves * kWave, 2) void chunk_tiles(ChunkArgs a
     // Cut by a share's end: the pieces' states are joined by the last of them, in order.  A share has at most
     // two pieces of cut blocks, its first (slot 0) and its last (slot 1, if it is not also the first);
     // the block's word is that of the share where it begins.
-    // A wave's part of a state: its accumulators lane by lane (1 KB each), then max and sum of its rows.
-    constexpr int kWavePart = RT * 8 * 1024 + RT * 128;
-    static_assert(kTileWaves * kWavePart <= kTileRows * kChunkPart * 4, "a piece's room in the workspace");
-    auto part_of = [&](int k, bool first_piece) {
-        return span(reinterpret_cast<uint8_t*>(a.part + (2ll * k + (first_piece ? 0 : 1)) * kTileRows * kChunkPart) +
-                        wave * kWavePart,
-                    kWavePart);
-    };
     const int k0 = (int)(from / quantum), k1 = (int)((to - 1) / quantum);
     {
         const __amdgpu_buffer_rsrc_t out = part_of(share, piece == 0);

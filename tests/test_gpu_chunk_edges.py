@@ -177,3 +177,101 @@ def test_weights_enter_whole(n, G, own):
         first = 1 if own else 0  # (from the row that sees both)
         assert (p[:, first:] > 1e-30).sum(-1).max() == 2 and tol[:, first:].max() < 2.0 ** -14
         assert (np.abs(got.transpose(1, 0, 2) - want) <= tol)[:, first:].all()
+
+
+def poke(cache, t, sec, u, group, pair, section="vmeta"):
+    """{s, z} of token u of a section of table t, as fp16."""
+    L = cache.L
+    T = L.tokens_per_page[sec]
+    page = int(cache.page_table[t, u // T if sec == 0 else L.p_max - 1 - u // T])
+    at = L.off_vmeta[sec] + (group * T + u % T) * 4 if section == "vmeta" else L.off_kmeta[sec] + (u % T * 4 + group) * 4
+    raw = torch.tensor(pair, dtype=torch.float16).view(torch.uint8).to(DEV)
+    cache.pool[page, at:at + 4] = raw
+
+
+NOT_FINITE = [(float("inf"), 0.5), (float("nan"), 0.5), (0.25, float("inf")), (0.25, float("-inf")), (0.25, float("nan"))]
+
+
+@pytest.mark.parametrize("window", [0, 150, 330], ids=lambda w: "window%d" % w)
+@pytest.mark.parametrize("layout", range(4))
+@pytest.mark.parametrize("new_len", CHUNKS, ids=str)
+def test_cached_values_that_are_not_finite(layout, new_len, window):
+    """Cached groups whose scale or zero is infinite or NaN: the rows that see such a token are not finite in that
+    group's dims, all other rows and dims are as ever."""
+    rng = np.random.default_rng(10 * layout + len(new_len))
+    cache = filled(dk, LAYOUTS[layout], 3, 2, [300, 70, 200], seed=layout)
+    lens = cache.len.cpu().numpy()
+    for i, pair in enumerate(NOT_FINITE):
+        for t in (0, 1, 5):
+            sec = int(rng.integers(2))
+            poke(cache, t, sec, int(rng.integers(lens[t, sec])), (i + t) % 4, pair)
+    q, k, v = fused(rng, sum(new_len), 8, 2)
+    form = dict(window=window) if window else {}
+    print("case: not finite, layout %d, %s, window %d" % (layout, new_len, window), flush=True)
+    with np.errstate(invalid="ignore"):
+        kept = kept_tokens(cache)
+    out, lse, _ = run(cache, new_len, q, k, v, **form)
+    got, got_lse = out.cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64)
+    vv = v.cpu().numpy().astype(np.float64)
+    mixed = False  # whether some rows see such a token and others do not
+    for b, h, row, n, x, size in logits(cache, kept, new_len, q, k, SCALE, **form):
+        vals = np.concatenate([kept[b * 2 + h][1], vv[row:row + n, h]])
+        p, want_lse = softmax(x)
+        lost = (np.isfinite(x).astype(float) @ ~np.isfinite(vals)) > 0
+        mixed |= bool((lost.any((0, 1)) & ~lost.all((0, 1))).any())
+        vals = np.where(np.isfinite(vals), vals, 0.0)
+        want, A = p @ vals, p @ np.abs(vals)
+        tol = H16 * (2 * A + np.abs(want)) + 2 * delta(size)[..., None] * A + vals.shape[0] * 2.0 ** -25 * np.abs(vals).max()
+        g = got[row:row + n, h * 4:(h + 1) * 4].transpose(1, 0, 2)
+        assert np.array_equal(np.isfinite(g), ~lost)
+        assert (np.abs(g - want) <= tol)[~lost].all()
+        assert (np.abs(got_lse[row:row + n, h * 4:(h + 1) * 4].T - want_lse) <= delta(size) + 2.0 ** -22 * np.abs(want_lse)).all()
+    assert mixed or not window or new_len[0] < 300
+
+
+@pytest.mark.parametrize("n", [1, 6, 300])
+def test_an_infinite_value_appended(n):
+    """An overflowed value at the append: its group is not finite here and in diffkv_decode_attention alike."""
+    rng = np.random.default_rng(n)
+    keys, values = rng.standard_normal((2, 200, D))
+    values[20, 40] = np.inf
+    values[150, 70] = -np.inf
+    values[151, 100:103] = np.nan
+    with np.errstate(invalid="ignore"):
+        cache = cache_of({}, keys, values, 90)
+    q, k, v = (x.contiguous() for x in fused(rng, n, 8, 1))
+    out, lse, _ = run(cache, [n], q, k, v)
+    dec, _ = dk.decode_attention(cache, q[:1].contiguous(), SCALE)
+    torch.cuda.synchronize()
+    dims = ~torch.isfinite(dec[0])
+    assert dims.any() and not dims.all() and torch.isfinite(lse).all()
+    assert torch.equal(~torch.isfinite(out), dims[:1].expand(8, -1)[None].expand(n, -1, -1))
+
+
+@pytest.mark.parametrize("form", [{}, dict(window=100), dict(cap=10.0)], ids=str)
+@pytest.mark.parametrize("new_len", CHUNKS, ids=str)
+def test_what_lies_behind_a_section_reaches_nothing(new_len, form):
+    """Slots of a page behind its section's end full of bits that are no numbers: the results are those of clean
+    pages, bit for bit."""
+    rng = np.random.default_rng(5)
+    cache = filled(dk, {}, 3, 2, [301, 70, 203], seed=3)
+    L, lens = cache.L, cache.len.cpu().numpy()
+    q, k, v = fused(rng, sum(new_len), 8, 2)
+    pool = cache.pool.clone()
+    want = run(cache, new_len, q, k, v, **form)
+    behind = pool.clone()
+    for t in range(6):
+        for sec in (0, 1):
+            T, n = L.tokens_per_page[sec], int(lens[t, sec])
+            if n % T == 0:
+                continue
+            page = int(cache.page_table[t, n // T if sec == 0 else L.p_max - 1 - n // T])
+            for off, groups in ((L.off_kmeta[sec], None), (L.off_vmeta[sec], 4)):
+                meta = behind[page, off:off + 16 * T]
+                if groups:
+                    meta.view(4, T, 4)[:, n % T:] = 0xFF
+                else:
+                    meta.view(T, 16)[n % T:] = 0xFF
+    cache.pool.copy_(behind)
+    print("case: behind the sections, %s, %s" % (new_len, form), flush=True)
+    assert same(run(cache, new_len, q, k, v, **form), want)

@@ -424,8 +424,11 @@ typedef struct diffkv_score_form {
  * The cache is read only.  A page ID outside the pool counts no tokens, and no
  * section length leads out of the table's row: the high section ends with the
  * row, the low one where the high one begins.
- * sm_scale above 0 and at most 1e30 (DIFFKV_E_INVAL otherwise).  The layouts of
+ * sm_scale above 0 and at most 65536 (DIFFKV_E_INVAL otherwise).  The layouts of
  * diffkv_layout_init's list, up to 8 query heads per KV head.
+ * Scores x up to 2^22 in magnitude, the slopes' part included: beyond, fp32's
+ * steps are no longer small against the exponential's, and a row may come out
+ * infinite or NaN.
  * Precision: q . k_hat exact up to fp32 summation, fp32 softmax statistics;
  * v_hat is rounded to fp16 (2^-11, or 2^-24 where that is more; up to twice the
  * largest fp16 it is no infinity); the weights enter in two fp16 parts (2^-22,

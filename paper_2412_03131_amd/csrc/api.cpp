@@ -260,6 +260,7 @@ bool rows_valid(const void* p, int64_t stride, int64_t heads, int64_t rows)
 {
     return p && (uintptr_t)p % 16 == 0 && stride % 8 == 0 && (stride >= heads * kD || rows <= 1) && stride >= 0;
 }
+constexpr float kMaxChunkScale = 65536.0f;
 constexpr int64_t kMaxStride = 1 << 24;  // chunk kernels: 32 rows stay within 31-bit offsets
 
 // What both chunk entry points check, and the arguments they share.
@@ -271,7 +272,7 @@ diffkv_status chunk_call(const diffkv_layout* layout, const diffkv_cache* cache,
     if (!layout_valid(layout) || !cache_valid(cache) || !cache->pool || !cache->seq_len) return DIFFKV_E_INVAL;
     if (total_new < 0 || max_new < 0 || total_new > INT32_MAX / 4) return DIFFKV_E_INVAL;
     if (num_q_heads <= 0 || num_q_heads % cache->num_kv_heads != 0) return DIFFKV_E_INVAL;
-    if (!(sm_scale > 0.0f) || sm_scale > 1e30f) return DIFFKV_E_INVAL;
+    if (!(sm_scale > 0.0f) || sm_scale > kMaxChunkScale) return DIFFKV_E_INVAL;
     if (form && (!(form->cap >= 0.0f) || form->cap > 1e30f || (form->cap > 0.0f && form->cap < 1e-30f) || form->window < 0)) return DIFFKV_E_INVAL;
     if (!layout_kernels_supported(layout)) return DIFFKV_E_UNSUPPORTED;
     if (num_q_heads / cache->num_kv_heads > 8) return DIFFKV_E_UNSUPPORTED;

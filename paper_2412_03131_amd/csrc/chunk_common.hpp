@@ -35,7 +35,7 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 constexpr float kChunkLog2e = 1.4426950408889634f;
 constexpr float kChunkLog2eRest = 1.925963034e-08f;  // log2(e) less that
 constexpr float kChunkLn2 = 0.6931471805599453f;
-constexpr float kLowest = -1e30f;  // a running max before the first key (finite: no inf - inf)
+constexpr float kLowest = -1e30f;  // a running max before the first key (finite: no inf - inf; below all scores)
 
 // The operands are named once more after the product: the compiler would otherwise place a result over an
 // operand that ends there, and what the hardware does then is not relied on.

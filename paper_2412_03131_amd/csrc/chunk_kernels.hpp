@@ -178,8 +178,8 @@ struct Rows {
 // logit being unit * x, -> weights 2^(logit - m), with m the running max less 7: a weight enters its
 // product as fp16, whose denormals end at 2^-24, so the offset keeps what is 2^-32 of the largest (without it
 // everything below 2^-25 was lost from the sums of values, yet counted in the normalizer).  The running max is
-// raised only when a logit passes it by 8 (weights up to 2^15).  before() is called where it is, before
-// anything is scaled.
+// raised only when a logit passes it by 8 (weights up to 2^15; m is rounded, the product it is taken from is not:
+// logits up to 2^22 leave them below 2^16).  before() is called where it is, before anything is scaled.
 constexpr float kWeightBits = 7.0f, kRaiseBits = 8.0f;
 template <int RT, typename F>
 __device__ __forceinline__ void raise_max(Rows<RT>& R, const float (&unit)[RT], const float (&x)[RT][2][4], F&& before)

@@ -26,3 +26,12 @@ def test_a_workspace_for_more_sequences_serves_fewer(dk, Hq, Hkv):
         assert need == sorted(need), rows
         need = [dk.workspace_size(dk.OP_CHUNK_SIGNIFICANCE, L, s, Hq, Hkv, rows) for s in seqs]
         assert need == sorted(need), rows
+
+
+def test_scales_beyond_the_range_of_scores(dk):
+    """Scores as large as the kernels' running maximum can start below: refused with their scale."""
+    from test_chunk_abi import attention, significance
+    for scale in (65537.0, 1e8, 1e30):
+        assert attention(dk, scale=scale) == dk.E_INVAL
+        assert significance(dk, scale=scale) == dk.E_INVAL
+    assert attention(dk, scale=65536.0) == dk.E_WORKSPACE  # (the next check: none is given)

@@ -275,3 +275,26 @@ def test_what_lies_behind_a_section_reaches_nothing(new_len, form):
     cache.pool.copy_(behind)
     print("case: behind the sections, %s, %s" % (new_len, form), flush=True)
     assert same(run(cache, new_len, q, k, v, **form), want)
+
+
+@pytest.mark.parametrize("form", [{}, dict(window=1000)], ids=str)
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("n", [1, 6, 300])
+def test_scores_at_the_end_of_their_range(n, sign, form):
+    """Scores of 4.1e6 in magnitude, all alike: a mean of the values seen."""
+    cache = filled(dk, {}, 1, 1, [0], seed=1)
+    q, k, v = (torch.zeros((n, heads, D), dtype=torch.float16, device=DEV) for heads in (8, 1, 1))
+    rng = np.random.default_rng(n)
+    q[:, :, 3], k[:, :, 3] = 1.0, sign * 62.5
+    v.copy_(torch.from_numpy(rng.standard_normal((n, 1, D)).astype(np.float16)))
+    nl = torch.tensor([n], dtype=torch.int32, device=DEV)
+    print("case: large scores, n %d, sign %g, %s" % (n, sign, form), flush=True)
+    out, lse = dk.chunk_attention(cache, nl, q, k, v, 65536.0, max_new=n, **form)
+    torch.cuda.synchronize()
+    vals = v[:, 0].cpu().numpy().astype(np.float64)
+    count = np.arange(1, n + 1)[:, None]
+    want, A = np.cumsum(vals, 0) / count, np.cumsum(np.abs(vals), 0) / count
+    tol = (H16 * np.abs(want) + 2.0 ** -20 * A + 2.0 ** -25)[:, None]
+    assert (np.abs(out.cpu().numpy().astype(np.float64) - want[:, None]) <= tol).all()
+    x = sign * 62.5 * 65536.0
+    assert np.allclose(lse.cpu().numpy(), x, rtol=2.0 ** -18, atol=0)

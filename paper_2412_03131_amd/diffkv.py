@@ -300,10 +300,19 @@ def prompt_significance(L, new_len, q, k, sm_scale, lse=None, score=None, max_ne
 def _rows(t, what, head_dim):
     """Address and row stride of [rows, heads, D] rows whose heads lie side by side (a slice of a
     fused projection may be given)."""
-    if t.dim() != 3 or t.dtype != torch.float16 or t.shape[2] != head_dim or t.stride(2) != 1 or (
-            t.stride(1) != head_dim and t.shape[1] > 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or t.dtype != torch.float16 or shape[2] != head_dim or stride[2] != 1 or (
+            stride[1] != head_dim and shape[1] > 1):
         raise ValueError("%s: fp16 [rows, heads, %d] with packed heads expected" % (what, head_dim))
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), stride[0]
+
+
+def _on_one_gpu(what, *tensors):
+    """All on the same GPU (None aside): an address of the host's would fault the device."""
+    at = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (at < 0 or t.get_device() != at):
+            raise ValueError("%s: tensors on one GPU expected" % what)
 
 
 def _form(cap, window, slopes):
@@ -313,7 +322,8 @@ def _form(cap, window, slopes):
 
 
 def rope_frequencies(rot_dim, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, trained_len=0, slow=1.0, fast=32.0):
-    """diffkv_rope_frequencies: (fp32 [rot_dim / 2] on the host, the scale of cosines and sines)."""
+    """diffkv_rope_frequencies: (fp32 [rot_dim / 2] on the host, the scale of cosines and sines).  rotate takes
+    them on the device."""
     freq = torch.empty(max(rot_dim // 2, 1), dtype=torch.float32)
     scale = C.c_float(0.0)
     _check(lib().diffkv_rope_frequencies(int(rot_dim), float(base), int(scaling), float(factor), int(trained_len),
@@ -341,6 +351,7 @@ def rotate(L, pos, inv_freq, q, k=None, style=ROPE_HALF, scale=1.0, q_out=None, 
     kop, kos = (None, 0) if k is None else _rows(k_out, "k_out", L.head_dim)
     qp, qs = _rows(q, "q", L.head_dim)
     qop, qos = _rows(q_out, "q_out", L.head_dim)
+    _on_one_gpu("rotate", q, k, pos, inv_freq, q_out, k_out)
     _check(lib().diffkv_rotate(C.byref(L), rows, _ptr(pos), _ptr(inv_freq), 2 * inv_freq.shape[0], int(style),
                                float(scale), Hq, qp, qs, qop, qos, Hkv, kp, ks, kop, kos, _stream(stream)),
            "diffkv_rotate")
@@ -381,6 +392,7 @@ def chunk_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, slopes
     if ws is None:
         ws = _new_ws(workspace_size(*sizes), q.device)
     (qp, qs), (kp, ks), (vp, vs) = (_rows(t, w, cache.L.head_dim) for t, w in ((q, "q"), (k, "k"), (v, "v")))
+    _on_one_gpu("chunk_attention", q, k, v, new_len, slopes, out, lse, ws)
     _check_ws(lib().diffkv_chunk_attention(
         C.byref(cache.L), _cache_struct(cache), rows, max_new, _ptr(new_len), Hq, qp, qs, kp, ks, vp, vs,
         float(sm_scale), _form(cap, window, slopes), _ptr(out), _ptr(lse), ws.data_ptr(), ws.nbytes, _stream(stream)),
@@ -403,6 +415,7 @@ def chunk_significance(cache, new_len, q, k, sm_scale, lse, cap=0.0, window=0, s
     if ws is None:
         ws = _new_ws(workspace_size(*sizes), q.device)
     (qp, qs), (kp, ks) = (_rows(t, w, cache.L.head_dim) for t, w in ((q, "q"), (k, "k")))
+    _on_one_gpu("chunk_significance", q, k, new_len, slopes, lse, score, ws)
     _check_ws(lib().diffkv_chunk_significance(
         C.byref(cache.L), _cache_struct(cache), rows, max_new, _ptr(new_len), Hq, qp, qs, kp, ks, float(sm_scale),
         _form(cap, window, slopes), _ptr(lse), _ptr(score), ws.data_ptr(), ws.nbytes, _stream(stream)),

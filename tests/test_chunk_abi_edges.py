@@ -3,6 +3,7 @@ here reaches a kernel)."""
 import os
 
 import pytest
+import torch
 
 
 @pytest.fixture(scope="module")
@@ -35,3 +36,18 @@ def test_scales_beyond_the_range_of_scores(dk):
         assert attention(dk, scale=scale) == dk.E_INVAL
         assert significance(dk, scale=scale) == dk.E_INVAL
     assert attention(dk, scale=65536.0) == dk.E_WORKSPACE  # (the next check: none is given)
+
+
+def test_binding_refuses_host_tensors(dk):
+    """What diffkv_rope_frequencies gives lies on the host; a kernel that took such an address would fault."""
+    L = dk.layout(max_seq_len=256)
+    q, kv = torch.zeros((3, 8, 128), dtype=torch.float16), torch.zeros((3, 2, 128), dtype=torch.float16)
+    freq, _ = dk.rope_frequencies(128)
+    with pytest.raises(ValueError, match="GPU"):
+        dk.rotate(L, torch.zeros(3, dtype=torch.int32), freq, q, kv)
+    cache = dk.Cache(L, 16, 1, 2, device="cpu")
+    nl, ws = torch.tensor([3], dtype=torch.int32), torch.zeros(1 << 20, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="GPU"):
+        dk.chunk_attention(cache, nl, q, kv, kv, 0.1, max_new=3, ws=ws)
+    with pytest.raises(ValueError, match="GPU"):
+        dk.chunk_significance(cache, nl, q, kv, 0.1, torch.zeros((3, 8)), max_new=3, ws=ws)

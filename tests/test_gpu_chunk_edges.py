@@ -298,3 +298,19 @@ def test_scores_at_the_end_of_their_range(n, sign, form):
     assert (np.abs(out.cpu().numpy().astype(np.float64) - want[:, None]) <= tol).all()
     x = sign * 62.5 * 65536.0
     assert np.allclose(lse.cpu().numpy(), x, rtol=2.0 ** -18, atol=0)
+
+
+def test_host_tensors_beside_device_ones_are_refused():
+    cache = filled(dk, {}, 1, 1, [50], seed=1)
+    q, k, v = fused(np.random.default_rng(1), 3, 4, 1)
+    nl = torch.tensor([3], dtype=torch.int32, device=DEV)
+    pos = torch.arange(3, dtype=torch.int32, device=DEV)
+    freq, _ = dk.rope_frequencies(128)
+    for bad in ((pos, freq), (pos.cpu(), freq.to(DEV))):
+        with pytest.raises(ValueError, match="GPU"):
+            dk.rotate(cache.L, *bad, q, k)
+    for bad in ((nl.cpu(), v, None), (nl, v.cpu(), None), (nl, v, torch.zeros(4))):
+        with pytest.raises(ValueError, match="GPU"):
+            dk.chunk_attention(cache, bad[0], q, k, bad[1], SCALE, max_new=3, slopes=bad[2])
+    with pytest.raises(ValueError, match="GPU"):
+        dk.chunk_significance(cache, nl, q, k, SCALE, torch.zeros((3, 4)), max_new=3)

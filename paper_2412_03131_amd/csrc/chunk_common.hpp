@@ -126,7 +126,7 @@ __device__ __forceinline__ SeqBlock find_block(const ChunkArgs& a, int want, int
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         const int b = b0 + lane;
         int n = b < a.B ? new_tokens(a, b) : 0;
-        const long long before = row + (wave_incl_scan(n) - n);
+        const long long before = row + (wave_incl_scan_wide(n) - n);
         const long long room = a.total_new - before;
         if (n > room) n = room > 0 ? (int)room : 0;
         const int nb = chunk_blocks(n, G, rows, lo, hi);
@@ -158,11 +158,11 @@ __device__ __forceinline__ int first_tokens(const ChunkArgs& a)
 __device__ __forceinline__ void sequence_rows(const ChunkArgs& a, SeqBlock& s, int first_n)
 {
     const int lane = lane_id();
-    int sum = lane < s.b ? first_n : 0;
+    long long sum = lane < s.b ? first_n : 0;
 #pragma unroll 4
     for (int i = lane + kWave; i < s.b; i += kWave) sum += new_tokens(a, i);
     const int n = s.b < kWave ? __builtin_amdgcn_readlane(first_n, s.b) : new_tokens(a, s.b);
-    s.row0 = __builtin_amdgcn_readlane(wave_incl_scan(sum), kWave - 1);
+    s.row0 = read_lane<long long>(wave_incl_scan_wide(sum), kWave - 1);
     const long long room = a.total_new - s.row0;
     s.n = n <= room ? n : (room > 0 ? (int)room : 0);
 }

@@ -110,6 +110,15 @@ __device__ __forceinline__ long long wave_incl_scan64(long long x)
     return (long long)(((unsigned long long)hi << 32) | lo);
 }
 
+// Inclusive prefix sum of true 64-bit values 0 <= x < 2^51 (their low 20 bits and the rest as two counters:
+// 64 low parts stay below 2^26).
+__device__ __forceinline__ long long wave_incl_scan_wide(long long x)
+{
+    constexpr int kLow = 20;
+    const long long p = wave_incl_scan64(((x >> kLow) << 32) | (x & ((1LL << kLow) - 1)));
+    return ((p >> 32) << kLow) + (p & 0xffffffffLL);
+}
+
 // Inclusive OR over a full wave, same DPP pattern as the prefix sum.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ uint32_t dpp_or_step(uint32_t x)

@@ -255,10 +255,12 @@ diffkv_status attention_call(const diffkv_layout* layout, const diffkv_cache* ca
     return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
 }
 
-// A row of `heads` heads every `stride` halfs, as the vector loads and stores need it.
-bool rows_valid(const void* p, int64_t stride, int64_t heads, int64_t rows)
+// A row of `heads` heads every `stride` halfs, as the vector loads and stores need it.  A single row's
+// stride goes to no other and becomes 0.
+bool rows_valid(const void* p, int64_t& stride, int64_t heads, int64_t rows)
 {
-    return p && (uintptr_t)p % 16 == 0 && stride % 8 == 0 && (stride >= heads * kD || rows <= 1) && stride >= 0;
+    if (rows <= 1) stride = 0;
+    return p && (uintptr_t)p % 16 == 0 && stride % 8 == 0 && (stride >= heads * kD || rows <= 1);
 }
 constexpr float kMaxChunkScale = 65536.0f;
 constexpr int64_t kMaxStride = 1 << 24;  // chunk kernels: 32 rows stay within 31-bit offsets

@@ -51,3 +51,11 @@ def test_binding_refuses_host_tensors(dk):
         dk.chunk_attention(cache, nl, q, kv, kv, 0.1, max_new=3, ws=ws)
     with pytest.raises(ValueError, match="GPU"):
         dk.chunk_significance(cache, nl, q, kv, 0.1, torch.zeros((3, 8)), max_new=3, ws=ws)
+
+
+@pytest.mark.parametrize("stride", [-1, 0, 3, 1 << 40])
+def test_a_single_row_has_any_stride(dk, stride):
+    from test_chunk_abi import attention, significance
+    strides = dict(total=1, max_new=1, qs=stride, ks=stride)
+    assert attention(dk, vs=stride, **strides) == dk.E_WORKSPACE  # (past the rows' checks: none is given)
+    assert significance(dk, **strides) == dk.E_WORKSPACE

@@ -22,9 +22,8 @@ constexpr double kTurns = 0.15915494309189533577;  // 1 / 2 pi
 // A wave takes one row's heads, eight at a time: lane = head * 8 + unit.  `waves` per row share them.
 __global__ __launch_bounds__(256) void rotate_rows(RotateArgs a, int waves_per_row)
 {
-    const long long w = (long long)blockIdx.x * 4 + wave_index();
+    for (long long w = (long long)blockIdx.x * 4 + wave_index(); w < a.rows * waves_per_row; w += (long long)gridDim.x * 4) {
     const long long row = w / waves_per_row;
-    if (row >= a.rows) return;
     const int lane = lane_id(), unit = lane & 7;
     const int half = a.rot_dim >> 1, pairs = half >> 3;  // units that turn
     float cs[8], sn[8];
@@ -75,6 +74,7 @@ __global__ __launch_bounds__(256) void rotate_rows(RotateArgs a, int waves_per_r
         *reinterpret_cast<h8*>(out + d0) = x;
         *reinterpret_cast<h8*>(out + d1) = y;
     }
+    }
 }
 
 }  // namespace
@@ -87,8 +87,8 @@ hipError_t launch_rotate(const RotateArgs& args, hipStream_t st)
     const int groups = (heads + 7) / 8;
     long long per = 8192 / a.rows;
     int waves = per < 1 ? 1 : (per < groups ? (int)per : groups);
-    const long long grid = (a.rows * waves + 3) / 4;
-    if (grid < 1 || grid > INT32_MAX) return hipErrorInvalidValue;
+    // (a launch has less than 2^32 threads: more rows than that go round)
+    const long long most = 1 << 22, grid = (a.rows * waves + 3) / 4 < most ? (a.rows * waves + 3) / 4 : most;
     void* kargs[] = {&a, &waves};
     return hipLaunchKernel(reinterpret_cast<const void*>(rotate_rows), dim3((unsigned)grid), dim3(256), kargs, 0, st);
 }

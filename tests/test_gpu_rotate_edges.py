@@ -23,3 +23,18 @@ def test_a_single_row_of_any_stride():
     want, _ = dk.rotate(L, pos, freq.to(DEV), x[:4 * D].view(1, 4, D))
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def test_more_rows_than_a_launch_has_waves():
+    """2^26 rows and a few, of one head: the last ones (and some of each part of the way) are turned as any others."""
+    rows = (1 << 26) + 5
+    x = torch.empty((rows, 1, D), dtype=torch.float16, device=DEV)
+    at = torch.tensor([0, 1, 1 << 24, (1 << 24) + 3, (1 << 25) - 1, (1 << 26) - 1, 1 << 26, rows - 1], device=DEV)
+    x[at] = torch.randn((len(at), 1, D), device=DEV).half()
+    pos = torch.arange(rows, dtype=torch.int32, device=DEV)
+    freq = dk.rope_frequencies(128)[0].to(DEV)
+    want, _ = dk.rotate(L, pos[at], freq, x[at])
+    print("case: 2^26 rows", flush=True)
+    dk.rotate(L, pos, freq, x, q_out=x)
+    torch.cuda.synchronize()
+    assert torch.equal(x[at], want)

@@ -425,7 +425,8 @@ typedef struct diffkv_score_form {
  * section length leads out of the table's row: the high section ends with the
  * row, the low one where the high one begins.
  * sm_scale above 0 and at most 65536 (DIFFKV_E_INVAL otherwise).  The layouts of
- * diffkv_layout_init's list, up to 8 query heads per KV head.
+ * diffkv_layout_init's list, up to 8 query heads per KV head, up to 2^22 tables
+ * (DIFFKV_E_UNSUPPORTED otherwise).
  * Scores x up to 2^22 in magnitude, the slopes' part included: beyond, fp32's
  * steps are no longer small against the exponential's, and a row may come out
  * infinite or NaN.

@@ -263,6 +263,7 @@ bool rows_valid(const void* p, int64_t& stride, int64_t heads, int64_t rows)
     return p && (uintptr_t)p % 16 == 0 && stride % 8 == 0 && (stride >= heads * kD || rows <= 1);
 }
 constexpr float kMaxChunkScale = 65536.0f;
+constexpr int64_t kMaxChunkTables = 1 << 22;  // a launch, a workgroup or more per table, has less than 2^32 threads
 constexpr int64_t kMaxStride = 1 << 24;  // chunk kernels: 32 rows stay within 31-bit offsets
 
 // What both chunk entry points check, and the arguments they share.
@@ -278,6 +279,7 @@ diffkv_status chunk_call(const diffkv_layout* layout, const diffkv_cache* cache,
     if (form && (!(form->cap >= 0.0f) || form->cap > 1e30f || (form->cap > 0.0f && form->cap < 1e-30f) || form->window < 0)) return DIFFKV_E_INVAL;
     if (!layout_kernels_supported(layout)) return DIFFKV_E_UNSUPPORTED;
     if (num_q_heads / cache->num_kv_heads > 8) return DIFFKV_E_UNSUPPORTED;
+    if ((int64_t)cache->num_seqs * cache->num_kv_heads > kMaxChunkTables) return DIFFKV_E_UNSUPPORTED;
     memset(&a, 0, sizeof(a));
     if (cache->num_seqs == 0 || total_new == 0 || max_new == 0) return DIFFKV_OK;
     if (!new_len || !rows_valid(q, q_stride, num_q_heads, total_new) ||

@@ -47,7 +47,7 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     float* part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(arrive) + align256((plan.few_blocks + kTileShares) * 8));
     auto launch = [&](ChunkArgs& a, int which, long long grid, int threads) {
         const void* kern = chunk_kernel(a.layout, which, mod);
-        if (!kern || grid < 1 || grid > INT32_MAX) return hipErrorInvalidValue;
+        if (!kern || grid < 1 || grid > UINT32_MAX / threads) return hipErrorInvalidValue;
         void* kargs[] = {&a};
         return hipLaunchKernel(kern, dim3((unsigned)grid), dim3((unsigned)threads), kargs, 0, st);
     };
@@ -111,7 +111,7 @@ hipError_t launch_chunk_scores(const ChunkArgs& args, bool mod, hipStream_t st)
     if (shares > most) shares = most;
     a.splits = (int)(shares < 1 ? 1 : shares);
     const long long grid = T * a.splits;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    if (grid > UINT32_MAX / (8 * kWave)) return hipErrorInvalidValue;
     void* kargs[] = {&a};
     return hipLaunchKernel(kern, dim3((unsigned)grid), dim3(8 * kWave), kargs, 0, st);
 }

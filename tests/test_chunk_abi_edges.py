@@ -59,3 +59,11 @@ def test_a_single_row_has_any_stride(dk, stride):
     strides = dict(total=1, max_new=1, qs=stride, ks=stride)
     assert attention(dk, vs=stride, **strides) == dk.E_WORKSPACE  # (past the rows' checks: none is given)
     assert significance(dk, **strides) == dk.E_WORKSPACE
+
+
+def test_more_tables_than_a_launch_can_take(dk):
+    """A launch has less than 2^32 threads, and gives no error beyond."""
+    from test_chunk_abi import attention, significance
+    for seqs, status in ((1 << 21, dk.E_WORKSPACE), ((1 << 21) + 1, dk.E_UNSUPPORTED), (1 << 28, dk.E_UNSUPPORTED)):
+        assert attention(dk, seqs=seqs) == status
+        assert significance(dk, seqs=seqs) == status

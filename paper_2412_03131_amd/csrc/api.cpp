@@ -360,7 +360,8 @@ diffkv_status diffkv_workspace_size(int32_t op, const diffkv_layout* layout, int
         return DIFFKV_OK;
     case DIFFKV_OP_CHUNK_ATTENTION:
     case DIFFKV_OP_CHUNK_SIGNIFICANCE:
-        if (num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || total_new < 0) return DIFFKV_E_INVAL;
+        if (num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || total_new < 0 || total_new > INT32_MAX / 4)
+            return DIFFKV_E_INVAL;
         *bytes = op == DIFFKV_OP_CHUNK_ATTENTION
                      ? (size_t)chunk_plan(num_seqs, num_q_heads, num_kv_heads, total_new).bytes
                      : (size_t)kScoreBytes;

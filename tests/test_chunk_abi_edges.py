@@ -67,3 +67,14 @@ def test_more_tables_than_a_launch_can_take(dk):
     for seqs, status in ((1 << 21, dk.E_WORKSPACE), ((1 << 21) + 1, dk.E_UNSUPPORTED), (1 << 28, dk.E_UNSUPPORTED)):
         assert attention(dk, seqs=seqs) == status
         assert significance(dk, seqs=seqs) == status
+
+
+def test_workspace_of_more_rows_than_a_call_takes(dk):
+    """Row counts that the calls refuse have no size either (their products would not fit 64 bits)."""
+    L = dk.layout(max_seq_len=256)
+    for op in (dk.OP_CHUNK_ATTENTION, dk.OP_CHUNK_SIGNIFICANCE):
+        for rows in ((1 << 29), 1 << 60):
+            with pytest.raises(dk.DiffKVError) as e:
+                dk.workspace_size(op, L, 4, 32, 8, rows)
+            assert e.value.code == dk.E_INVAL
+        assert dk.workspace_size(op, L, 4, 32, 8, (1 << 29) - 1) > 0

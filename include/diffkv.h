@@ -463,7 +463,9 @@ diffkv_status diffkv_chunk_attention(const diffkv_layout* layout, const diffkv_c
  *            wrote it
  *   score    device fp32 [total_new][num_kv_heads] out
  *   ws       diffkv_workspace_size(DIFFKV_OP_CHUNK_SIGNIFICANCE, ...) bytes
- * Tables of sequences without new tokens are left alone.  fp32 arithmetic.
+ * Tables of sequences without new tokens are left alone.  fp32 arithmetic.  A
+ * probability that is NaN (a NaN key that the row sees, a NaN query) counts as 0,
+ * so scores stay finite.
  * Other arguments, limits and errors as diffkv_chunk_attention.
  */
 diffkv_status diffkv_chunk_significance(const diffkv_layout* layout, const diffkv_cache* cache,

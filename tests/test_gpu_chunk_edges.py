@@ -10,7 +10,7 @@ torch = pytest.importorskip("torch")
 if not torch.cuda.is_available():  # pragma: no cover
     pytest.skip("needs a GPU", allow_module_level=True)
 
-from chunk_ref import D, filled, kept_tokens, logits, softmax  # noqa: E402
+from chunk_ref import D, filled, kept_tokens, logits, score_at, softmax  # noqa: E402
 from paper_2412_03131_amd import diffkv as dk  # noqa: E402
 from test_gpu_chunk import DEV, H16, LAYOUTS, SCALE, check_attention, check_scores, delta, fused  # noqa: E402
 
@@ -81,15 +81,16 @@ def test_single_tokens_of_a_padded_batch(new_len):
         assert bool((x[n:] == 7.0).all())
 
 
+@pytest.mark.parametrize("Hq", [16, 6])
 @pytest.mark.parametrize("max_new,new_len", [(100, [100, 1]), (300, [300, 1]), (300, [2, 16, 0, 300, 17]), (300, [0, 3]),
                                              (300, [3]), (300, [90]), (16, [16, 3, 0])], ids=str)
-def test_rows_padded_to_the_longest_chunk(max_new, new_len):
+def test_rows_padded_to_the_longest_chunk(max_new, new_len, Hq):
     """As many rows as sequences times the longest chunk, with shorter and empty chunks among them: the short
     ones' outputs and scores are there, rows that no sequence owns stay as they were."""
     rng = np.random.default_rng(len(new_len))
     B, n = len(new_len), sum(new_len)
     cache = filled(dk, {}, B, 2, [300, 70, 0, 150, 40][:B], seed=B)
-    q, k, v = fused(rng, B * max_new, 16, 2)
+    q, k, v = fused(rng, B * max_new, Hq, 2)
     print("case: %s padded to %d" % (new_len, max_new), flush=True)
     before = kept_tokens(cache)
     out, lse, score = run(cache, new_len, q, k, v, max_new=max_new)
@@ -314,3 +315,29 @@ def test_host_tensors_beside_device_ones_are_refused():
             dk.chunk_attention(cache, bad[0], q, k, bad[1], SCALE, max_new=3, slopes=bad[2])
     with pytest.raises(ValueError, match="GPU"):
         dk.chunk_significance(cache, nl, q, k, SCALE, torch.zeros((3, 4)), max_new=3)
+
+
+@pytest.mark.parametrize("form", [{}, dict(window=200)], ids=str)
+@pytest.mark.parametrize("n", [6, 60, 300])
+def test_scores_beside_nan_count_the_other_rows(n, form):
+    """A NaN key of the chunk's own, a NaN query: the rows that meet them have no part in any score."""
+    rng = np.random.default_rng(n)
+    cache = filled(dk, {}, 1, 1, [250], seed=8)
+    q, k, v = (x.contiguous() for x in fused(rng, n, 8, 1))
+    q[1, 3, 50] = float("nan")
+    k[n // 2, 0, 5] = float("nan")
+    print("case: scores beside NaN, n %d, %s" % (n, form), flush=True)
+    before = kept_tokens(cache)
+    _, lse, score = run(cache, [n], q, k, v, **form)
+    norm = lse.cpu().numpy().astype(np.float64)
+    pos, old, where = before[0][2:]
+    for b, h, row, _, x, size in logits(cache, before, [n], q, k, SCALE, **form):
+        rel = 2 * delta(np.nan_to_num(size)).max() + 2.0 ** -20
+        P = np.nan_to_num(np.exp(x - norm.T[..., None])).max(0)
+        assert np.isnan(norm[n // 2:]).any() and np.isfinite(norm[0]).all()
+        X, m = P.sum(0), len(pos)
+        left = cache.seq_len.cpu().numpy()[0] + n - pos
+        got, want = score_at(cache, where), old + (X[:m] - n * old) / left
+        assert (np.abs(got - want) <= rel * (np.abs(old) * (1 + n / left) + X[:m] / left) + 1e-30).all()
+        got, want = score.cpu().numpy().astype(np.float64)[:, 0], X[m:] / np.arange(n, 0, -1)
+        assert (np.abs(got - want) <= rel * want + 1e-30).all()

@@ -66,14 +66,12 @@ __device__ __forceinline__ int fresh(int lane)
     asm volatile("" : "+v"(lane));
     return lane;
 }
-template <int BYTES>
+template <int BYTES>  // 4, 8 or 16
 __device__ __forceinline__ auto fetch(__amdgpu_buffer_rsrc_t r, int lane_offset, int offset)
 {
     if constexpr (BYTES == 16) return __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_offset, offset, 0));
     else if constexpr (BYTES == 8) return __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(r, lane_offset, offset, 0));
-    else if constexpr (BYTES == 4) return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, lane_offset, offset, 0);
-    else if constexpr (BYTES == 2) return (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, lane_offset, offset, 0);
-    else return (uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, lane_offset, offset, 0);
+    else return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, lane_offset, offset, 0);
 }
 
 // ---- a table's sections ------------------------------------------------------------

@@ -1,5 +1,5 @@
 // k_chunk.hip -- host side of the chunk attention and score kernels (chunk_kernels.hpp,
-// instantiated per page layout in k_chunk_l<n>.hip), and the join of split rows.
+// instantiated per page layout in k_chunk_l<n>.hip): which of them takes which sequences, the workspace.
 #include "chunk_common.hpp"
 
 namespace dkv {

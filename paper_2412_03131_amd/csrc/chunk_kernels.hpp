@@ -137,6 +137,10 @@ __device__ __forceinline__ void load_values(GroupValues<VB, T>& r, const uint8_t
 // only rounding (2^-11: values N(0, 1) of a kept token, far below their own quantization).  Halves,
 // because s c + z of a group's largest code can round past the largest finite fp16: infinite are
 // then only those that are (a limit per pair would also hide NaN); sums of cached values are doubled once.
+// With a second part, as the weights have, results are as exact as a 32-bit computation's rounded once, not 1.15 to
+// 1.25 times as far off; but the conversions are most of the few-row kernel's work: 64 single tokens over 1k-4k
+// take 46 us so and 68 with two parts, one token of 16 sequences over 32k 108 and 156, parts of eight prompts 419
+// and 471, 2048 tokens over 8192 913 and 1044.
 template <int VB>
 __device__ __forceinline__ void value_pairs(uint32_t w, h2 s02, h2 z02, h2 s13, h2 z13, uint32_t& p02, uint32_t& p13)
 {
@@ -223,7 +227,7 @@ __device__ __forceinline__ h8 pack_weights(const float (&w)[2][4])
 // What the rounding left of them: two parts hold a weight to 2^-22, or to 2^-32 of its row's largest where that
 // is more (raise_max).  Weights enter all kernels whole, so a token's precision does not go by which kernel or
 // how many row tiles its neighbours in a call ask for.  The results' error against 64 bits is then the
-// values' and their own rounding alone, 1.12 to 1.28 times a 32-bit computation's rounded once; with
+// values' and their own rounding alone, 1.15 to 1.25 times a 32-bit computation's rounded once; with
 // weights rounded once it was up to 1.5 times.  The second products take 2 us of 46 for 64 single tokens over
 // 1k-4k, 2 % with two row tiles, 15 % in chunk_tiles (257-512 tokens for each of 8 sequences over 0-8192: 367 ->
 // 421 us, 2048 tokens over 8192 at 64 / 8 heads: 791 -> 935).
@@ -934,7 +938,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, RT == 1 ? (LI == 1 ? 3 : 4) : 
 // their values from another and the next one is made.
 // The blocks of all tables end to end are cut into equal shares, one per CU: with a workgroup per block the
 // longest ones set the time (257-512 tokens for each of 8 sequences over 0-8192: 546 us, with shares 377).
-// Bound by issue: that case takes 421 us at 160 GFLOP, 2048 tokens over 8192 at 64 / 8 heads 935 us, 486
+// Bound by issue: that case takes 419 us at 160 GFLOP, 2048 tokens over 8192 at 64 / 8 heads 913 us, 499
 // TFLOP/s (an 8192^3 fp16 library product 1137), the weights' second products not counted.
 constexpr int kTileWaves = 8;
 constexpr int kTileRows = kTileWaves * 32;

@@ -282,12 +282,12 @@ constexpr int kChunkPart = kD + 4;  // floats of a partial state (16-byte rows)
 // of a KV head) in blocks of 16 or 32 rows, which up to kRowPieces workgroups share; longer ones in blocks of
 // kChunkRows, all of them cut into kTileShares equal shares.  A function of what the workspace size is
 // told.  The border (8 KV heads, 4 query heads each, blocks of 32 / shares of 256 rows): 64 rows for each of
-// 64 sequences over 2048 tokens 91 / 148 us; 128 rows 168 / 155, but for 16 sequences 52 / 58 and for 4 over
-// 8192 49 / 63; 256 rows for 16 sequences 93 / 70.  Beside longer sequences only those of one block of 16 rows
+// 64 sequences over 2048 tokens 104 / 164 us; 128 rows 184 / 171, but for 16 sequences 55 / 62 and for 4 over
+// 8192 53 / 67; 256 rows for 16 sequences 103 / 81.  Beside longer sequences only those of one block of 16 rows
 // stay (a second launch: the blocks of the others would take a CU each from the shares).
 // Calls of few rows altogether (kChunkFewTotal, of all query heads) stay with the few-row kernel: one sequence's
-// 64 tokens (32 / 8 heads) over 8192 37 us, in shares 73; over 32768 80 / 106; its 128 over 8192 51 / 74, but over
-// 32768 187 / 121; 512 tokens over 8192 of 4 heads on one KV head 35 / 66.
+// 64 tokens (32 / 8 heads) over 8192 39 us, in shares 76; over 32768 90 / 114; its 128 over 8192 54 / 75, but over
+// 32768 207 / 137; 512 tokens over 8192 of 4 heads on one KV head 37 / 68.
 constexpr int kChunkFewRows = 128;
 constexpr int kChunkFewTotal = 2048;
 constexpr int kChunkRows = 256;

@@ -68,8 +68,8 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     a.rows_lo = 1;
     a.rows_hi = rows > plan.few_rows ? 16 : (int)plan.few_rows;
     a.part = part;
-    // Two row tiles share a step's dequantization (20 rows for each of 64 sequences over 2048 tokens 52 us, with
-    // one tile 67; 64 rows 91 and 117; 32 rows for 4 over 8192 30 and 40)
+    // Two row tiles share a step's dequantization (20 rows for each of 64 sequences over 2048 tokens 55 us, with
+    // one tile 62; 64 rows 104 and 123; 128 rows for 4 over 8192 53 and 62; only 32 rows for 4 31 and 29)
     const int rt = rows > 16 && rows <= plan.few_rows ? 2 : 1;
     a.splits = plan.few_split ? 0 : 1;
     a.blocks = (int)(plan.few_blocks < INT32_MAX ? plan.few_blocks : INT32_MAX);

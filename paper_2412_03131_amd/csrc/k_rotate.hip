@@ -7,8 +7,8 @@
 // before the 32-bit sine and cosine: positions of 10^5 times one radian have no digits left
 // for it in 32 bits.  fp32 products, one rounding to fp16.
 //
-// Bound by memory (each value is read and written once): 32767 rows of 48 heads take 160 us, 5.0 TB/s, as
-// a copy of that size does.  A lane owns the eight pairs of a
+// Bound by memory (each value is read and written once): 32767 rows of 48 heads take 159 us, 5.05 TB/s
+// (a copy of that size 154).  A lane owns the eight pairs of a
 // 16-dim unit and goes over heads, so their sines and cosines, which cost more than
 // the rest, serve all of them.
 #include "chunk_common.hpp"

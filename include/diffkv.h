@@ -408,9 +408,10 @@ typedef struct diffkv_score_form {
  * tokens 0 .. j in fp16:
  *   out[row][hq] = sum_c softmax_c(x) v_c,  x as in diffkv_score_form.
  *   new_len  device int32 [num_seqs], rows of sequence b follow those of b-1.
- *            They must sum to total_new with every entry in [0, max_new];
- *            lengths are clamped so that no row past total_new is read or
- *            written, and rows that no sequence owns are left as they were.
+ *            Every entry in [0, max_new], their sum at most total_new: rows
+ *            behind the last sequence's (a padded batch) are nobody's and left
+ *            as they were.  Other lengths are clamped so that no row past
+ *            total_new is read or written.
  *   q, k, v  device fp16: row r, head h at q + r*q_stride + h*head_dim (slices
  *            of a fused projection can be passed), 16-byte aligned, strides in
  *            elements, multiples of 8, at least heads*head_dim (any value with

@@ -341,3 +341,41 @@ def test_scores_beside_nan_count_the_other_rows(n, form):
         assert (np.abs(got - want) <= rel * (np.abs(old) * (1 + n / left) + X[:m] / left) + 1e-30).all()
         got, want = score.cpu().numpy().astype(np.float64)[:, 0], X[m:] / np.arange(n, 0, -1)
         assert (np.abs(got - want) <= rel * want + 1e-30).all()
+
+
+@pytest.mark.parametrize("B,Hkv,Hq,most", [(140, 8, 32, 20), (130, 8, 8, 128), (1100, 1, 8, 9)])
+def test_many_tables_of_several_blocks(B, Hkv, Hq, most):
+    """Over 1024 tables, so none is split, with up to eight row blocks each; empty chunks and padded rows among them."""
+    rng = np.random.default_rng(B)
+    new_len = rng.integers(0, most + 1, B)
+    new_len[rng.integers(0, B, B // 3)] = 0
+    new_len[B // 2] = most
+    new_len, n = new_len.tolist(), int(new_len.sum())
+    cache = filled(dk, {}, B, Hkv, rng.integers(0, 60, B), seed=B, max_len=256)
+    q, k, v = fused(rng, n + 5, Hq, Hkv)
+    print("case: %d tables, %d rows" % (B * Hkv, n), flush=True)
+    before = kept_tokens(cache)
+    out, lse, score = run(cache, new_len, q, k, v)
+    check_attention(cache, new_len, q[:n], k[:n], v[:n], out[:n], lse[:n], "many tables")
+    check_scores(cache, before, new_len, q[:n], k[:n], lse[:n], score[:n], "many tables")
+    for x in (out, lse, score):
+        assert bool((x[n:] == 7.0).all())
+
+
+@pytest.mark.parametrize("new_len", [[1, 1, 1], [3, 0, 9], [70, 1, 2]], ids=str)
+def test_a_longest_chunk_that_is_none(new_len):
+    """A program that captured its step for longer chunks than the batch now has: the results are those of the call
+    with the chunks' own length."""
+    rng = np.random.default_rng(sum(new_len))
+    cache = filled(dk, {}, 3, 2, [300, 70, 200], seed=5)
+    n = sum(new_len)
+    q, k, v = fused(rng, 600, 8, 2)
+    before, pool = kept_tokens(cache), cache.pool.clone()
+    for max_new in (max(new_len), 128, 200, 600):
+        cache.pool.copy_(pool)
+        print("case: %s of at most %d" % (new_len, max_new), flush=True)
+        out, lse, score = run(cache, new_len, q, k, v, max_new=max_new)
+        check_attention(cache, new_len, q[:n], k[:n], v[:n], out[:n], lse[:n], "at most %d" % max_new)
+        check_scores(cache, before, new_len, q[:n], k[:n], lse[:n], score[:n], "at most %d" % max_new)
+        for x in (out, lse, score):
+            assert bool((x[n:] == 7.0).all())

@@ -78,7 +78,8 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     const long long whole = args.total_new * G / per + seqs, each = seqs * ((most + per - 1) / per);
     const long long blocks = (whole < each ? whole : each) * a.Hkv;
     if (!plan.few_split) {
-        // (256 sequences' single tokens over 100-1000, 32 / 8 heads: 51 us; 54 where each workgroup searches)
+        // (256 sequences' single tokens over 100-1000, 32 / 8 heads: 53 us, 54 where each workgroup searches; 1500 of 4 / 1
+        // over 100-600 36 and 44)
         a.one_block = most <= per;
         return launch(a, rt, a.one_block ? (long long)a.B * a.Hkv : blocks, 4 * kWave);
     }

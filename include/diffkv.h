@@ -146,7 +146,8 @@ enum {
     DIFFKV_OP_GENERATION = 4,
     DIFFKV_OP_PROMPT_SIGNIFICANCE = 5,
     DIFFKV_OP_CHUNK_ATTENTION = 6,
-    DIFFKV_OP_CHUNK_SIGNIFICANCE = 7
+    DIFFKV_OP_CHUNK_SIGNIFICANCE = 7,
+    DIFFKV_OP_BLOCK_ATTENTION = 8
 };
 
 /* Bytes of device workspace the operation needs (host out-parameter).
@@ -154,8 +155,8 @@ enum {
  * num_q_heads, num_splits (0 = automatic, -1 = balanced).
  * COMPACT / ALLOC / GENERATION: num_seqs*num_kv_heads tables.
  * PROMPT_SIGNIFICANCE: num_seqs, num_q_heads, total_new.
- * CHUNK_ATTENTION / CHUNK_SIGNIFICANCE: num_seqs, num_q_heads, num_kv_heads,
- * total_new.  Unused sizes are ignored. */
+ * CHUNK_ATTENTION / CHUNK_SIGNIFICANCE / BLOCK_ATTENTION: num_seqs,
+ * num_q_heads, num_kv_heads, total_new.  Unused sizes are ignored. */
 diffkv_status diffkv_workspace_size(int32_t op, const diffkv_layout* layout,
                                     int32_t num_seqs, int32_t num_q_heads,
                                     int32_t num_kv_heads, int64_t total_new,
@@ -362,6 +363,24 @@ diffkv_status diffkv_rotate(const diffkv_layout* layout, int64_t rows, const int
                             uint16_t* k_out, int64_t k_out_stride, void* stream);
 
 /*
+ * Norms of queries and keys for each head, and their rotary positions, in one
+ * pass: with w the side's weights,
+ *   y[d] = x[d] * w[d] / sqrt(mean of the head's x^2 + eps),
+ * then y is turned as diffkv_rotate turns it (dims rot_dim .. head_dim-1 are
+ * normed and pass).
+ *   q_weight, k_weight  device fp32 [head_dim], 16-byte aligned, or NULL: ones
+ *   eps       above 0 and finite
+ * The other arguments, in-place calls, limits and errors as diffkv_rotate.  The
+ * sum of squares, the norm and all products are fp32, with one rounding to fp16.
+ */
+diffkv_status diffkv_norm_rotate(const diffkv_layout* layout, int64_t rows, const int32_t* pos,
+                                 const float* inv_freq, int32_t rot_dim, int32_t style, float scale,
+                                 float eps, int32_t num_q_heads, const uint16_t* q, int64_t q_stride,
+                                 const float* q_weight, uint16_t* q_out, int64_t q_out_stride,
+                                 int32_t num_kv_heads, const uint16_t* k, int64_t k_stride,
+                                 const float* k_weight, uint16_t* k_out, int64_t k_out_stride, void* stream);
+
+/*
  * Frequencies of rotary positions, computed on the host in 64 bits:
  * f_i = base^(-2i/rot_dim), i < rot_dim/2, for contexts longer than the trained
  * ones by `factor` (>= 1):
@@ -475,6 +494,123 @@ diffkv_status diffkv_chunk_significance(const diffkv_layout* layout, const diffk
                                         const uint16_t* k, int64_t k_stride, float sm_scale,
                                         const diffkv_score_form* form, const float* lse, float* score,
                                         void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * A uniform 8-bit cache, for layers whose tokens are not told apart by their
+ * significance (sliding windows, a model's first layers): every token is kept at
+ * 8 bits, in blocks of DIFFKV_BLOCK_TOKENS positions with one scale for a block's
+ * keys and one for its values per KV head.  Block i of a sequence holds positions
+ * 32 i .. 32 i + 31; table row b holds the IDs of sequence b's blocks, the same
+ * for all KV heads.  Positions behind the last whole block are the sequence's tail,
+ * fp16 rows as they were appended.  An ID outside the pool (-1) means that the block
+ * is not kept: appended tokens that fill it are dropped, and attention counts
+ * none there.  So a window's program gives the IDs of blocks that no row can see any
+ * more to other sequences, and gives none to the blocks of a prompt that it will
+ * never see.  The program assigns IDs and advances seq_len: the layers of a model
+ * can share both.  A sequence may be set back within its tail (seq_len not below its
+ * last whole block's end).
+ * Codes: a value is code * scale.  DIFFKV_BLOCK_E4M3: e4m3 codes (four significant
+ * bits, to 448), the scale a power of two; it suits keys with channels of
+ * different size.  DIFFKV_BLOCK_INT8: integers from -127 to 127, the scale of
+ * eight significant bits.
+ * A block of a KV head, 8192 bytes: key codes [2: token / 16][8: dim / 16]
+ * [16: token % 16][16: dim % 16], then value codes [4: dim / 32][4: r][16: dim % 16]
+ * [2: dim / 16 % 2][8: e], e < 4 token 4 r + e, e >= 4 token 12 + 4 r + e.
+ */
+enum { DIFFKV_BLOCK_TOKENS = 32 };
+enum { DIFFKV_BLOCK_E4M3 = 0, DIFFKV_BLOCK_INT8 = 1 };
+
+typedef struct diffkv_block_cache {
+    uint8_t*  pool;          /* device [num_blocks][num_kv_heads][8192], 16-byte aligned   */
+    float*    scale;         /* device [num_blocks][num_kv_heads][2]: keys, values;
+                                positive, or NaN                                     */
+    int64_t   num_blocks;    /* up to INT32_MAX                                       */
+    const int32_t* table;    /* device [num_seqs][ceil(max_seq_len / 32)] block IDs         */
+    uint16_t* tail;          /* device fp16 [num_seqs][num_kv_heads][2][32][head_dim]: keys,
+                                values of position p at p % 32; 16-byte aligned              */
+    const int32_t* seq_len;  /* device [num_seqs] tokens held, up to max_seq_len             */
+    uint32_t* status;        /* device [1] sticky DIFFKV_ST_* bits                     */
+    int32_t   num_seqs;
+    int32_t   num_kv_heads;
+    int32_t   format;        /* DIFFKV_BLOCK_E4M3 or _INT8                             */
+} diffkv_block_cache;
+
+/*
+ * Appends new tokens: positions seq_len[b] .. + new_len[b] - 1.  A block that they
+ * fill is quantized from its tail rows and new rows and stored, if its ID is in the
+ * pool; the rows behind the last whole block go to the tail.  seq_len is not
+ * advanced.  What a cache holds depends on its tokens alone, not on how they were
+ * cut into calls.
+ * With amax the largest magnitude of a block's 32 x 128 keys (or values) of a KV head:
+ *   E4M3   scale = 2^e, e the least integer with amax <= 448 * 2^e; codes are
+ *          x / scale to the nearest e4m3 value, ties to the even one
+ *   INT8   scale = amax / 127 rounded up to eight significant bits; codes are x / scale
+ *          to the nearest integer, ties to the even one
+ * exactly; scale = 1 where amax = 0.  If a value is not finite, the scale is NaN and
+ * the codes are 0: every token of the block reads NaN.
+ *   new_len  device int32 [num_seqs], rows of sequence b follow those of b-1.
+ *            Every entry in [0, max_new], their sum at most total_new (rows behind the
+ *            last sequence's are nobody's), else DIFFKV_ST_BAD_INPUT; seq_len[b] in
+ *            [0, max_seq_len - new_len[b]], else DIFFKV_ST_TABLE_OVERFLOW.  A call
+ *            that raises either changes nothing.
+ *   k, v     device fp16: row r, head h at k + r*k_stride + h*head_dim (slices of a
+ *            fused projection can be passed), 16-byte aligned, strides in elements,
+ *            multiples of 8, at least heads*head_dim (any value with one row)
+ * IDs of blocks that one call fills must differ.  head_dim 128, max_seq_len up to 2^30,
+ * total_new up to 2^25 (DIFFKV_E_UNSUPPORTED otherwise).  No workspace.
+ */
+diffkv_status diffkv_block_append(const diffkv_layout* layout, const diffkv_block_cache* cache,
+                                  int64_t total_new, int32_t max_new, const int32_t* new_len,
+                                  const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                                  void* stream);
+
+/*
+ * Reads ranges of positions back as fp16 rows, e.g. to append them to a differentiated
+ * cache, or for another sequence with the same beginning: row i of sequence b's is
+ * position start[b] + i.  Stored values are code * scale rounded once to fp16 (beyond the
+ * largest finite fp16: that one), tail rows come as they are.  A position that the cache does not
+ * hold (outside [0, seq_len), or of a block without an ID in the pool) reads zero.
+ *   start, count  device int32 [num_seqs]; rows of sequence b follow those of b-1.
+ *            Counts are clamped to [0, max_count], and so that no row past
+ *            total is written; rows behind the last sequence's are left as they
+ *            were.
+ *   k, v     device fp16 out, addressed as diffkv_block_append's inputs
+ * Limits as diffkv_block_append.  No workspace; the cache is read only.
+ */
+diffkv_status diffkv_block_read(const diffkv_layout* layout, const diffkv_block_cache* cache, int64_t total,
+                                int32_t max_count, const int32_t* start, const int32_t* count,
+                                uint16_t* k, int64_t k_stride, uint16_t* v, int64_t v_stride, void* stream);
+
+/*
+ * Attention of a chunk of new tokens over a uniform cache, before the chunk is
+ * appended: one token per sequence, drafted tokens, a prompt's next part, or any
+ * mixture.  New token j of sequence b has position p = seq_len[b] + j; its query of
+ * head hq attends to the tokens of KV head hq/(Hq/Hkv) at c <= p, the cache's
+ * (code * scale), the tail's and the chunk's own in fp16:
+ *   out[row][hq] = sum_c softmax_c(x) v_c,  x as in diffkv_score_form,
+ * where a windowed form sees the key at c if p - c < window or c < sinks: the first
+ * `sinks` tokens of a sequence stay visible (sinks >= 0; without a window it says nothing).
+ * Tiles of 32 positions that no row of a sequence sees are skipped.
+ *   new_len, q, k, v, out, lse, sm_scale, form  as diffkv_chunk_attention takes them
+ *   ws       diffkv_workspace_size(DIFFKV_OP_BLOCK_ATTENTION, ...) bytes, no clearing
+ *            needed, 16-byte aligned; calls that may overlap need one each
+ * The cache is read only.  Up to 64 query heads per KV head, head_dim 128, total_new
+ * up to 2^25, max_seq_len up to 2^30, up to 2^22 (sequence, KV head) pairs
+ * (DIFFKV_E_UNSUPPORTED otherwise).  seq_len counts clamped to [0, max_seq_len].
+ * Scores x up to 2^22 in magnitude, the slopes' part included.
+ * Precision: codes enter the products exactly, and the weights in two fp16 parts (2^-22, or 2^-37 of
+ * their row's largest, each weighed by its block's value scale); sums and softmax statistics are fp32, and out is
+ * rounded once.  The order of a row's sums, and with it the last bits, goes by the
+ * call's lengths.
+ * A NaN or infinite key or value of a tail or chunk reaches only the rows that see its token;
+ * a block whose scale is NaN, those that see one of its tokens.
+ */
+diffkv_status diffkv_block_attention(const diffkv_layout* layout, const diffkv_block_cache* cache,
+                                     int64_t total_new, int32_t max_new, const int32_t* new_len,
+                                     int32_t num_q_heads, const uint16_t* q, int64_t q_stride,
+                                     const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                                     float sm_scale, const diffkv_score_form* form, int32_t sinks,
+                                     uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Parallel free-list compaction (Sec. 5.2 recycling, Sec. 5.3): for the

@@ -14,7 +14,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libdiffkv.so")
 SOURCES = ["api.cpp", "k_memory.hip", "k_attention.hip", "k_attn_l0.hip", "k_attn_l1.hip", "k_attn_l2.hip",
            "k_attn_l3.hip", "k_generation.hip", "k_prompt.hip", "k_rotate.hip", "k_chunk.hip", "k_chunk_l0.hip",
-           "k_chunk_l1.hip", "k_chunk_l2.hip", "k_chunk_l3.hip"]
+           "k_chunk_l1.hip", "k_chunk_l2.hip", "k_chunk_l3.hip", "k_block.hip", "k_block_attn.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

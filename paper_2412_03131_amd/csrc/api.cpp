@@ -262,9 +262,82 @@ bool rows_valid(const void* p, int64_t& stride, int64_t heads, int64_t rows)
     if (rows <= 1) stride = 0;
     return p && (uintptr_t)p % 16 == 0 && stride % 8 == 0 && (stride >= heads * kD || rows <= 1);
 }
+bool form_valid(const diffkv_score_form* f)
+{
+    return !f || (f->cap >= 0.0f && f->cap <= 1e30f && (f->cap == 0.0f || f->cap >= 1e-30f) && f->window >= 0);
+}
 constexpr float kMaxChunkScale = 65536.0f;
 constexpr int64_t kMaxChunkTables = 1 << 22;  // a launch, a workgroup or more per table, has less than 2^32 threads
 constexpr int64_t kMaxStride = 1 << 24;  // chunk kernels: 32 rows stay within 31-bit offsets
+
+// What both rotating entry points check, and their arguments.
+diffkv_status rotate_call(const diffkv_layout* layout, int64_t rows, const int32_t* pos, const float* inv_freq,
+                          int32_t rot_dim, int32_t style, float scale, int32_t num_q_heads, const uint16_t* q,
+                          int64_t q_stride, uint16_t* q_out, int64_t q_out_stride, int32_t num_kv_heads,
+                          const uint16_t* k, int64_t k_stride, uint16_t* k_out, int64_t k_out_stride, RotateArgs& a)
+{
+    if (!layout_valid(layout) || rows < 0 || num_q_heads <= 0 || num_kv_heads < 0) return DIFFKV_E_INVAL;
+    if (rot_dim <= 0 || rot_dim % 2 != 0 || rot_dim > layout->head_dim) return DIFFKV_E_INVAL;
+    if (style != DIFFKV_ROPE_HALF && style != DIFFKV_ROPE_INTERLEAVED) return DIFFKV_E_INVAL;
+    if (layout->head_dim != kD || rot_dim % 16 != 0) return DIFFKV_E_UNSUPPORTED;
+    if ((num_kv_heads > 0) != (k != nullptr) || (k != nullptr) != (k_out != nullptr)) return DIFFKV_E_INVAL;
+    if ((int64_t)num_q_heads + num_kv_heads > INT32_MAX / kD || rows > ((int64_t)1 << 40)) return DIFFKV_E_INVAL;
+    if (rows == 0) return DIFFKV_OK;
+    if (!pos || !inv_freq || (uintptr_t)inv_freq % 16 != 0) return DIFFKV_E_INVAL;
+    if (!rows_valid(q, q_stride, num_q_heads, rows) || !rows_valid(q_out, q_out_stride, num_q_heads, rows))
+        return DIFFKV_E_INVAL;
+    if (k && (!rows_valid(k, k_stride, num_kv_heads, rows) || !rows_valid(k_out, k_out_stride, num_kv_heads, rows)))
+        return DIFFKV_E_INVAL;
+    if ((q == q_out && q_stride != q_out_stride && rows > 1) || (k && k == k_out && k_stride != k_out_stride && rows > 1))
+        return DIFFKV_E_INVAL;
+    memset(&a, 0, sizeof(a));
+    a.rows = rows;
+    a.pos = pos;
+    a.freq = inv_freq;
+    a.rot_dim = rot_dim;
+    a.style = style;
+    a.scale = scale;
+    a.in[0] = q;
+    a.in[1] = k;
+    a.out[0] = q_out;
+    a.out[1] = k_out;
+    a.in_stride[0] = q_stride;
+    a.in_stride[1] = k_stride;
+    a.out_stride[0] = q_out_stride;
+    a.out_stride[1] = k_out_stride;
+    a.heads[0] = num_q_heads;
+    a.heads[1] = num_kv_heads;
+    return DIFFKV_OK;
+}
+
+// What the uniform cache's entry points check, and its arguments.
+constexpr int64_t kMaxBlockRows = (int64_t)1 << 25;
+constexpr int32_t kMaxBlockLen = 1 << 30;
+constexpr int32_t kMaxBlockGroup = 64;  // query heads per KV head: a sequence's rows stay within 31 bits
+diffkv_status block_call(const diffkv_layout* layout, const diffkv_block_cache* c, int64_t rows, int32_t max_rows,
+                         BlockCacheArgs& a)
+{
+    if (!layout_valid(layout) || !c || rows < 0 || max_rows < 0) return DIFFKV_E_INVAL;
+    if (c->num_seqs < 0 || c->num_kv_heads <= 0 || c->num_blocks < 0 || c->num_blocks > INT32_MAX) return DIFFKV_E_INVAL;
+    if (c->format != DIFFKV_BLOCK_E4M3 && c->format != DIFFKV_BLOCK_INT8) return DIFFKV_E_INVAL;
+    if (!c->table || !c->tail || !c->seq_len || !c->status || (c->num_blocks > 0 && (!c->pool || !c->scale)))
+        return DIFFKV_E_INVAL;
+    if (((uintptr_t)c->pool | (uintptr_t)c->tail) % 16 != 0) return DIFFKV_E_INVAL;
+    if (layout->head_dim != kD || layout->max_seq_len > kMaxBlockLen || rows > kMaxBlockRows) return DIFFKV_E_UNSUPPORTED;
+    if ((int64_t)c->num_seqs * c->num_kv_heads > kMaxChunkTables) return DIFFKV_E_UNSUPPORTED;
+    a.pool = c->pool;
+    a.scale = c->scale;
+    a.num_blocks = c->num_blocks;
+    a.table = c->table;
+    a.width = (layout->max_seq_len + DIFFKV_BLOCK_TOKENS - 1) / DIFFKV_BLOCK_TOKENS;
+    a.tail = c->tail;
+    a.seq_len = c->seq_len;
+    a.status = c->status;
+    a.B = c->num_seqs;
+    a.Hkv = c->num_kv_heads;
+    a.max_len = layout->max_seq_len;
+    return DIFFKV_OK;
+}
 
 // What both chunk entry points check, and the arguments they share.
 diffkv_status chunk_call(const diffkv_layout* layout, const diffkv_cache* cache, int64_t total_new, int32_t max_new,
@@ -276,7 +349,7 @@ diffkv_status chunk_call(const diffkv_layout* layout, const diffkv_cache* cache,
     if (total_new < 0 || max_new < 0 || total_new > INT32_MAX / 4) return DIFFKV_E_INVAL;
     if (num_q_heads <= 0 || num_q_heads % cache->num_kv_heads != 0) return DIFFKV_E_INVAL;
     if (!(sm_scale > 0.0f) || sm_scale > kMaxChunkScale) return DIFFKV_E_INVAL;
-    if (form && (!(form->cap >= 0.0f) || form->cap > 1e30f || (form->cap > 0.0f && form->cap < 1e-30f) || form->window < 0)) return DIFFKV_E_INVAL;
+    if (!form_valid(form)) return DIFFKV_E_INVAL;
     if (!layout_kernels_supported(layout)) return DIFFKV_E_UNSUPPORTED;
     if (num_q_heads / cache->num_kv_heads > 8) return DIFFKV_E_UNSUPPORTED;
     if ((int64_t)cache->num_seqs * cache->num_kv_heads > kMaxChunkTables) return DIFFKV_E_UNSUPPORTED;
@@ -365,6 +438,11 @@ diffkv_status diffkv_workspace_size(int32_t op, const diffkv_layout* layout, int
         *bytes = op == DIFFKV_OP_CHUNK_ATTENTION
                      ? (size_t)chunk_plan(num_seqs, num_q_heads, num_kv_heads, total_new).bytes
                      : (size_t)kScoreBytes;
+        return DIFFKV_OK;
+    case DIFFKV_OP_BLOCK_ATTENTION:
+        if (num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || total_new < 0 || total_new > kMaxBlockRows)
+            return DIFFKV_E_INVAL;
+        *bytes = (size_t)block_attention_ws(num_q_heads / num_kv_heads, total_new);
         return DIFFKV_OK;
     default:
         return DIFFKV_E_INVAL;
@@ -528,38 +606,30 @@ diffkv_status diffkv_rotate(const diffkv_layout* layout, int64_t rows, const int
                             int64_t q_stride, uint16_t* q_out, int64_t q_out_stride, int32_t num_kv_heads,
                             const uint16_t* k, int64_t k_stride, uint16_t* k_out, int64_t k_out_stride, void* stream)
 {
-    if (!layout_valid(layout) || rows < 0 || num_q_heads <= 0 || num_kv_heads < 0) return DIFFKV_E_INVAL;
-    if (rot_dim <= 0 || rot_dim % 2 != 0 || rot_dim > layout->head_dim) return DIFFKV_E_INVAL;
-    if (style != DIFFKV_ROPE_HALF && style != DIFFKV_ROPE_INTERLEAVED) return DIFFKV_E_INVAL;
-    if (layout->head_dim != kD || rot_dim % 16 != 0) return DIFFKV_E_UNSUPPORTED;
-    if ((num_kv_heads > 0) != (k != nullptr) || (k != nullptr) != (k_out != nullptr)) return DIFFKV_E_INVAL;
-    if ((int64_t)num_q_heads + num_kv_heads > INT32_MAX / kD || rows > ((int64_t)1 << 40)) return DIFFKV_E_INVAL;
-    if (rows == 0) return DIFFKV_OK;
-    if (!pos || !inv_freq || (uintptr_t)inv_freq % 16 != 0) return DIFFKV_E_INVAL;
-    if (!rows_valid(q, q_stride, num_q_heads, rows) || !rows_valid(q_out, q_out_stride, num_q_heads, rows))
-        return DIFFKV_E_INVAL;
-    if (k && (!rows_valid(k, k_stride, num_kv_heads, rows) || !rows_valid(k_out, k_out_stride, num_kv_heads, rows)))
-        return DIFFKV_E_INVAL;
-    if ((q == q_out && q_stride != q_out_stride && rows > 1) || (k && k == k_out && k_stride != k_out_stride && rows > 1))
-        return DIFFKV_E_INVAL;
     RotateArgs a;
-    memset(&a, 0, sizeof(a));
-    a.rows = rows;
-    a.pos = pos;
-    a.freq = inv_freq;
-    a.rot_dim = rot_dim;
-    a.style = style;
-    a.scale = scale;
-    a.in[0] = q;
-    a.in[1] = k;
-    a.out[0] = q_out;
-    a.out[1] = k_out;
-    a.in_stride[0] = q_stride;
-    a.in_stride[1] = k_stride;
-    a.out_stride[0] = q_out_stride;
-    a.out_stride[1] = k_out_stride;
-    a.heads[0] = num_q_heads;
-    a.heads[1] = num_kv_heads;
+    const diffkv_status s = rotate_call(layout, rows, pos, inv_freq, rot_dim, style, scale, num_q_heads, q, q_stride, q_out,
+                                        q_out_stride, num_kv_heads, k, k_stride, k_out, k_out_stride, a);
+    if (s != DIFFKV_OK || rows == 0) return s;
+    hipError_t e = launch_rotate(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
+}
+
+diffkv_status diffkv_norm_rotate(const diffkv_layout* layout, int64_t rows, const int32_t* pos, const float* inv_freq,
+                                 int32_t rot_dim, int32_t style, float scale, float eps, int32_t num_q_heads,
+                                 const uint16_t* q, int64_t q_stride, const float* q_weight, uint16_t* q_out,
+                                 int64_t q_out_stride, int32_t num_kv_heads, const uint16_t* k, int64_t k_stride,
+                                 const float* k_weight, uint16_t* k_out, int64_t k_out_stride, void* stream)
+{
+    if (!(eps > 0.0f) || !isfinite(eps)) return DIFFKV_E_INVAL;
+    if (((uintptr_t)q_weight | (uintptr_t)k_weight) % 16 != 0) return DIFFKV_E_INVAL;
+    RotateArgs a;
+    const diffkv_status s = rotate_call(layout, rows, pos, inv_freq, rot_dim, style, scale, num_q_heads, q, q_stride, q_out,
+                                        q_out_stride, num_kv_heads, k, k_stride, k_out, k_out_stride, a);
+    if (s != DIFFKV_OK || rows == 0) return s;
+    a.weight[0] = q_weight;
+    a.weight[1] = k_weight;
+    a.eps = eps;
+    a.norm = true;
     hipError_t e = launch_rotate(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
 }
@@ -636,6 +706,97 @@ diffkv_status diffkv_chunk_significance(const diffkv_layout* layout, const diffk
     a.lse_in = lse;
     a.score = score;
     hipError_t e = launch_chunk_scores(a, mod, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
+}
+
+diffkv_status diffkv_block_append(const diffkv_layout* layout, const diffkv_block_cache* cache, int64_t total_new,
+                                  int32_t max_new, const int32_t* new_len, const uint16_t* k, int64_t k_stride,
+                                  const uint16_t* v, int64_t v_stride, void* stream)
+{
+    BlockAppendArgs a;
+    memset(&a, 0, sizeof(a));
+    const diffkv_status s = block_call(layout, cache, total_new, max_new, a);
+    if (s != DIFFKV_OK || a.B == 0 || total_new == 0 || max_new == 0) return s;
+    if (!new_len || !rows_valid(k, k_stride, a.Hkv, total_new) || !rows_valid(v, v_stride, a.Hkv, total_new))
+        return DIFFKV_E_INVAL;
+    a.total_new = total_new;
+    a.max_new = max_new;
+    a.new_len = new_len;
+    a.in[0] = k;
+    a.in[1] = v;
+    a.in_stride[0] = k_stride;
+    a.in_stride[1] = v_stride;
+    hipError_t e = launch_block_append(a, cache->format, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
+}
+
+diffkv_status diffkv_block_read(const diffkv_layout* layout, const diffkv_block_cache* cache, int64_t total,
+                                int32_t max_count, const int32_t* start, const int32_t* count, uint16_t* k,
+                                int64_t k_stride, uint16_t* v, int64_t v_stride, void* stream)
+{
+    BlockReadArgs a;
+    memset(&a, 0, sizeof(a));
+    const diffkv_status s = block_call(layout, cache, total, max_count, a);
+    if (s != DIFFKV_OK || a.B == 0 || total == 0 || max_count == 0) return s;
+    if (!start || !count || !rows_valid(k, k_stride, a.Hkv, total) || !rows_valid(v, v_stride, a.Hkv, total))
+        return DIFFKV_E_INVAL;
+    a.total = total;
+    a.max_count = max_count;
+    a.start = start;
+    a.count = count;
+    a.out[0] = k;
+    a.out[1] = v;
+    a.out_stride[0] = k_stride;
+    a.out_stride[1] = v_stride;
+    hipError_t e = launch_block_read(a, cache->format, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
+}
+
+diffkv_status diffkv_block_attention(const diffkv_layout* layout, const diffkv_block_cache* cache, int64_t total_new,
+                                     int32_t max_new, const int32_t* new_len, int32_t num_q_heads, const uint16_t* q,
+                                     int64_t q_stride, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                                     int64_t v_stride, float sm_scale, const diffkv_score_form* form, int32_t sinks,
+                                     uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    BlockAttnArgs a;
+    memset(&a, 0, sizeof(a));
+    const diffkv_status s = block_call(layout, cache, total_new, max_new, a);
+    if (s != DIFFKV_OK) return s;
+    if (num_q_heads <= 0 || num_q_heads % a.Hkv != 0 || sinks < 0) return DIFFKV_E_INVAL;
+    if (!(sm_scale > 0.0f) || sm_scale > kMaxChunkScale || !form_valid(form)) return DIFFKV_E_INVAL;
+    if (num_q_heads / a.Hkv > kMaxBlockGroup) return DIFFKV_E_UNSUPPORTED;
+    if (a.B == 0 || total_new == 0 || max_new == 0) return DIFFKV_OK;
+    if (!new_len || !rows_valid(q, q_stride, num_q_heads, total_new) || !rows_valid(k, k_stride, a.Hkv, total_new) ||
+        !rows_valid(v, v_stride, a.Hkv, total_new))
+        return DIFFKV_E_INVAL;
+    if (!out || (uintptr_t)out % 16 != 0) return DIFFKV_E_INVAL;
+    if (!ws || (int64_t)ws_bytes < block_attention_ws(num_q_heads / a.Hkv, total_new)) return DIFFKV_E_WORKSPACE;
+    if ((uintptr_t)ws % 16 != 0) return DIFFKV_E_INVAL;
+    a.total_new = total_new;
+    a.max_new = max_new < total_new ? max_new : (int32_t)total_new;
+    a.new_len = new_len;
+    a.Hq = num_q_heads;
+    a.G = num_q_heads / a.Hkv;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    const bool mod = form && (form->cap > 0.0f || form->slopes);
+    a.scale_x = mod ? sm_scale : sm_scale * 1.4426950408889634f;
+    if (mod && form->cap > 0.0f) {
+        a.cap = form->cap;
+        a.cap_in = 2.0f * 1.4426950408889634f / form->cap;
+    }
+    a.slopes = form ? form->slopes : nullptr;
+    a.window = form && form->window > 0 ? form->window : INT32_MAX;
+    a.sinks = form && form->window > 0 ? sinks : 0;
+    a.out = out;
+    a.lse = lse;
+    a.arrive = static_cast<unsigned long long*>(ws);
+    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kBlockRowShares * 8);
+    hipError_t e = launch_block_attention(a, cache->format, mod, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
 }
 

@@ -1,0 +1,118 @@
+// block_common.hpp -- the uniform 8-bit cache: arguments, conversions of its codes, and the operand tiles
+// of its fp16 rows.
+//
+// A cache of whole blocks of 32 positions: per block and KV head 128 x 32 key codes and as many value codes, a
+// scale for each side; the positions behind a sequence's last whole block lie in its tail as fp16 rows.  The
+// bytes of a block lie as the matrix products take them, so that a lane's operands are whole 16-byte pieces:
+//   keys    [2: token / 16][8: dim / 16][16: token % 16][16: dim % 16].  With lane = r * 16 + key and chunk 4 i + r, a
+//           wave's load i of a half is 1024 bytes in lane order.
+//   values  [4: u = dim / 32][4: r][16: dim % 16][2: dim / 16 % 2][8: e], e < 4 token 4 r + e, e >= 4 token 12 + 4 r + e.
+//           Scores come out of their product (keys as A operand) with tokens 4 r .. 4 r + 3 of each half in the lanes
+//           of r, and go into the next one (values as A operand, depth 32) as they lie; load u is 1024 bytes in
+//           lane order again and holds two tiles of 16 dims.
+#pragma once
+
+#include "chunk_common.hpp"
+
+namespace dkv {
+
+constexpr int kBT = 32;                       // positions per block
+constexpr int kBlockSide = kBT * kD;          // bytes of a block's keys (or values) of one KV head
+constexpr int kBlockBytes = 2 * kBlockSide;
+enum BlockFmt { kE4m3 = 0, kInt8 = 1 };
+constexpr float kCodeUnit = 32.0f;            // codes enter products as code / 32: at most 14 and 4
+
+// ---- conversions -------------------------------------------------------------------
+// Four codes -> four fp16 values code / 32, exactly.  e4m3: the conversion's scale is a power of two.  Integers:
+// 128 + code in the low bits of 32.0 (whose last place is 1/32), less 36.
+template <int FMT>
+__device__ __forceinline__ u2 codes4(uint32_t w)
+{
+    u2 r;
+    if constexpr (FMT == kE4m3) {
+        r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f / kCodeUnit, false));
+        r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f / kCodeUnit, true));
+    } else {
+        const uint32_t x = w ^ 0x80808080u;
+        const h2 off = {(_Float16)-36.0f, (_Float16)-36.0f};
+        r[0] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x50505050u, x, 0x04010400u)) + off);
+        r[1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x50505050u, x, 0x04030402u)) + off);
+    }
+    return r;
+}
+template <int FMT>
+__device__ __forceinline__ h8 codes8(uint32_t lo, uint32_t hi)
+{
+    const u2 a = codes4<FMT>(lo), b = codes4<FMT>(hi);
+    return __builtin_bit_cast(h8, u4{a[0], a[1], b[0], b[1]});
+}
+
+__device__ __forceinline__ float read_lane_f(float x, int l)  // l uniform
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), l));
+}
+
+// ---- the cache --------------------------------------------------------------------------
+// Block ID of a sequence's block, -1 where it is none of the pool's.
+__device__ __forceinline__ int block_id(const BlockCacheArgs& c, int b, int tile)
+{
+    const int id = tile < c.width ? c.table[(long long)b * c.width + tile] : -1;
+    return id >= 0 && id < c.num_blocks ? id : -1;
+}
+__device__ __forceinline__ int seq_tokens(const BlockCacheArgs& c, int b)
+{
+    const int L = c.seq_len[b];
+    return L < 0 ? 0 : (L > c.max_len ? c.max_len : L);
+}
+// Tail rows of (sequence, KV head): 32 rows of keys, 32 of values.
+__device__ __forceinline__ const uint16_t* tail_rows(const BlockCacheArgs& c, int b, int h)
+{
+    return c.tail + ((long long)b * c.Hkv + h) * (2 * kBlockSide);
+}
+
+// ---- the item of a wave ----------------------------------------------------------------
+// Sequences in order, each with a number of items; a wave goes over them 64 at a time (a lane a
+// sequence) and finds the one that holds a given item.  Loads(b, n, L) gives a sequence's rows and tokens, unclamped;
+// Items(n, L) its items.  Rows are clamped to [0, most] and to the rows left of `total`.
+struct SeqItem {
+    int b, n, L;          // b < 0: there is none
+    long long row0;       // the sequence's first row
+    long long item0;      // and first item
+    bool bad;             // some sequence's length lies outside its range (of those passed)
+    long long items;      // up to the end of those passed: of all, if b < 0
+};
+template <typename Loads, typename Items>
+__device__ __forceinline__ SeqItem find_item(int B, long long total, int most, long long want, Loads loads, Items items)
+{
+    SeqItem s{-1, 0, 0, 0, 0, false, 0};
+    const int lane = lane_id();
+    long long row = 0, item = 0;
+    for (int b0 = 0; b0 < B; b0 += kWave) {
+        const int b = b0 + lane;
+        int n = 0, L = 0;
+        if (b < B) loads(b, n, L);
+        s.bad = s.bad || __ballot(n < 0 || n > most) != 0;
+        n = n < 0 ? 0 : (n > most ? most : n);
+        const long long before = row + (wave_incl_scan_wide(n) - n);
+        const long long room = total - before;
+        s.bad = s.bad || __ballot(n > room && n > 0) != 0;
+        if (n > room) n = room > 0 ? (int)room : 0;
+        const long long it = b < B ? items(n, L) : 0;
+        const long long incl = item + wave_incl_scan_wide(it);
+        const unsigned long long past = __ballot(incl > want);
+        if (past && s.b < 0) {
+            const int l = __builtin_ctzll(past);
+            s.b = b0 + l;
+            s.n = __builtin_amdgcn_readlane(n, l);
+            s.L = __builtin_amdgcn_readlane(L, l);
+            s.row0 = read_lane<long long>(before, l);
+            s.item0 = read_lane<long long>(incl - it, l);
+        }
+        row = read_lane<long long>(before + n, kWave - 1);
+        item = read_lane<long long>(incl, kWave - 1);
+    }
+    s.items = item;
+    return s;
+}
+
+}  // namespace dkv

@@ -325,8 +325,65 @@ struct RotateArgs {
     uint16_t* out[2];
     long long in_stride[2], out_stride[2];
     int heads[2];
+    const float* weight[2];  // norms: [kD] or null (ones)
+    float eps;
+    bool norm;
 };
 hipError_t launch_rotate(const RotateArgs& a, hipStream_t st);
+
+// The uniform 8-bit cache (blocks of 32 positions) and its operators.
+struct BlockCacheArgs {
+    uint8_t* pool;         // [num_blocks][Hkv][2][32 * kD]
+    float* scale;          // [num_blocks][Hkv][2]
+    long long num_blocks;
+    const int32_t* table;  // [B][width]
+    int width;             // blocks of max_len positions
+    uint16_t* tail;        // [B][Hkv][2][32][kD]
+    const int32_t* seq_len;
+    uint32_t* status;
+    int B, Hkv, max_len;
+};
+struct BlockAppendArgs : BlockCacheArgs {
+    long long total_new;
+    int max_new;
+    const int32_t* new_len;
+    const uint16_t* in[2];     // keys, values
+    long long in_stride[2];
+};
+struct BlockReadArgs : BlockCacheArgs {
+    long long total;
+    int max_count;
+    const int32_t* start;
+    const int32_t* count;
+    uint16_t* out[2];
+    long long out_stride[2];
+};
+struct BlockAttnArgs : BlockCacheArgs {
+    long long total_new;
+    int max_new;
+    const int32_t* new_len;
+    int Hq, G;
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    long long q_stride, k_stride, v_stride;
+    float scale_x;         // sm_scale, times log2(e) without a score form
+    float cap_in, cap;     // 2 log2(e) / cap and cap; 0: no cap
+    const float* slopes;   // [Hq] or null
+    int window;            // INT32_MAX: none
+    int sinks;             // 0 without a window
+    uint16_t* out;
+    float* lse;
+    unsigned long long* arrive;  // [shares] arrival word of the split tile that starts in a share
+    float* part;                 // [shares][2][rows] partial states {acc[kD], reference, sum, -, -}
+    int shares;                  // workgroups, most shares of the call
+};
+constexpr int kBlockRowShares = 1024;  // most workgroups of the few-row kernel
+constexpr long long kBlockRowBytes = kBlockRowShares * (8ll + 2 * 16 * kChunkPart * 4);
+inline long long block_attention_ws(long long, long long) { return kBlockRowBytes; }
+hipError_t launch_block_append(const BlockAppendArgs& a, int format, hipStream_t st);
+hipError_t launch_block_read(const BlockReadArgs& a, int format, hipStream_t st);
+hipError_t launch_block_attention(const BlockAttnArgs& a, int format, bool mod, hipStream_t st);
 
 // Fixed device scratch of diffkv_decode_attention_noalloc, one per device.
 constexpr long long kNoAllocScratchBytes = 8ll << 20;

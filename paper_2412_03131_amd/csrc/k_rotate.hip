@@ -19,7 +19,19 @@ namespace {
 
 constexpr double kTurns = 0.15915494309189533577;  // 1 / 2 pi
 
+// Sum over the eight lanes of a head, in all of them (fixed order: neighbours, then pairs, then fours).
+__device__ __forceinline__ float head_sum(float x)
+{
+    x += __uint_as_float(dpp_u32<0xB1, 0xF>(__float_as_uint(x)));   // quad_perm 1, 0, 3, 2
+    x += __uint_as_float(dpp_u32<0x4E, 0xF>(__float_as_uint(x)));   // quad_perm 2, 3, 0, 1
+    x += __uint_as_float(dpp_u32<0x141, 0xF>(__float_as_uint(x)));  // row_half_mirror: 7 - lane of eight
+    return x;
+}
+
 // A wave takes one row's heads, eight at a time: lane = head * 8 + unit.  `waves` per row share them.
+// NORM: each head is divided by its root mean square first, and multiplied by its side's weights; the head
+// is whole in the eight lanes' registers, so the row is still read once.
+template <bool NORM>
 __global__ __launch_bounds__(256) void rotate_rows(RotateArgs a, int waves_per_row)
 {
     for (long long w = (long long)blockIdx.x * 4 + wave_index(); w < a.rows * waves_per_row; w += (long long)gridDim.x * 4) {
@@ -49,9 +61,53 @@ __global__ __launch_bounds__(256) void rotate_rows(RotateArgs a, int waves_per_r
             // dims of the unit's two 16-byte pieces
             const int d0 = a.style == 0 && turns ? unit * 8 : unit * 16;
             const int d1 = a.style == 0 && turns ? half + unit * 8 : unit * 16 + 8;
-            if (!turns && in == out) continue;
+            if (!NORM && !turns && in == out) continue;
             h8 x = *reinterpret_cast<const h8*>(in + d0), y = *reinterpret_cast<const h8*>(in + d1);
-            if (turns) {
+            if constexpr (NORM) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    sum = __builtin_fmaf((float)x[i], (float)x[i], sum);
+                    sum = __builtin_fmaf((float)y[i], (float)y[i], sum);
+                }
+                const float m = 1.0f / __builtin_sqrtf(head_sum(sum) * (1.0f / kD) + a.eps);
+                const float* weight = a.weight[which];
+                float p[8], q[8];
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    const f4 one = {1.0f, 1.0f, 1.0f, 1.0f};
+                    const f4 wp = weight ? *reinterpret_cast<const f4*>(weight + d0 + i) : one;
+                    const f4 wq = weight ? *reinterpret_cast<const f4*>(weight + d1 + i) : one;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        p[i + j] = (float)x[i + j] * m * wp[j];
+                        q[i + j] = (float)y[i + j] * m * wq[j];
+                    }
+                }
+                if (turns && a.style == 0) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float t = p[i] * cs[i] - q[i] * sn[i];
+                        q[i] = q[i] * cs[i] + p[i] * sn[i];
+                        p[i] = t;
+                    }
+                } else if (turns) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float t = p[2 * i] * cs[i] - p[2 * i + 1] * sn[i];
+                        p[2 * i + 1] = p[2 * i + 1] * cs[i] + p[2 * i] * sn[i];
+                        p[2 * i] = t;
+                        t = q[2 * i] * cs[i + 4] - q[2 * i + 1] * sn[i + 4];
+                        q[2 * i + 1] = q[2 * i + 1] * cs[i + 4] + q[2 * i] * sn[i + 4];
+                        q[2 * i] = t;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] = (_Float16)p[i];
+                    y[i] = (_Float16)q[i];
+                }
+            } else if (turns) {
                 if (a.style == 0) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -90,7 +146,8 @@ hipError_t launch_rotate(const RotateArgs& args, hipStream_t st)
     // (a launch has less than 2^32 threads: more rows than that go round)
     const long long most = 1 << 22, grid = (a.rows * waves + 3) / 4 < most ? (a.rows * waves + 3) / 4 : most;
     void* kargs[] = {&a, &waves};
-    return hipLaunchKernel(reinterpret_cast<const void*>(rotate_rows), dim3((unsigned)grid), dim3(256), kargs, 0, st);
+    const void* kernel = a.norm ? reinterpret_cast<const void*>(rotate_rows<true>) : reinterpret_cast<const void*>(rotate_rows<false>);
+    return hipLaunchKernel(kernel, dim3((unsigned)grid), dim3(256), kargs, 0, st);
 }
 
 }  // namespace dkv

@@ -16,10 +16,12 @@ LIB_PATH = os.path.join(_HERE, "libdiffkv.so")
 OK, E_INVAL, E_UNSUPPORTED, E_WORKSPACE, E_LAUNCH, E_SCRATCH = 0, 1, 2, 3, 4, 5
 ST_OUT_OF_PAGES, ST_TABLE_OVERFLOW, ST_BAD_INPUT = 1, 2, 4
 OP_APPEND, OP_ATTENTION, OP_COMPACT, OP_ALLOC, OP_GENERATION, OP_PROMPT_SIGNIFICANCE = 0, 1, 2, 3, 4, 5
-OP_CHUNK_ATTENTION, OP_CHUNK_SIGNIFICANCE = 6, 7
+OP_CHUNK_ATTENTION, OP_CHUNK_SIGNIFICANCE, OP_BLOCK_ATTENTION = 6, 7, 8
 HIGH, LOW = 0, 1
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
+BLOCK_TOKENS = 32
+BLOCK_E4M3, BLOCK_INT8 = 0, 1
 
 _lib = None
 
@@ -57,10 +59,19 @@ class ScoreForm(C.Structure):
     _fields_ = [("cap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p)]
 
 
+class BlockCacheStruct(C.Structure):
+    _fields_ = [
+        ("pool", C.c_void_p), ("scale", C.c_void_p), ("num_blocks", C.c_int64), ("table", C.c_void_p),
+        ("tail", C.c_void_p), ("seq_len", C.c_void_p), ("status", C.c_void_p), ("num_seqs", C.c_int32),
+        ("num_kv_heads", C.c_int32), ("format", C.c_int32),
+    ]
+
+
 EXPORTS = ("diffkv_layout_init", "diffkv_workspace_size", "diffkv_quantize_append",
            "diffkv_decode_attention", "diffkv_decode_attention_noalloc", "diffkv_update_significance",
            "diffkv_prompt_significance", "diffkv_rotate", "diffkv_rope_frequencies", "diffkv_chunk_attention",
-           "diffkv_chunk_significance", "diffkv_compact_free_list", "diffkv_alloc_pages",
+           "diffkv_chunk_significance", "diffkv_norm_rotate", "diffkv_block_append", "diffkv_block_read",
+           "diffkv_block_attention", "diffkv_compact_free_list", "diffkv_alloc_pages",
            "diffkv_generation_step", "diffkv_status_str")
 
 
@@ -90,6 +101,13 @@ def lib():
                                              vp, sz, vp]
         L.diffkv_chunk_significance.argtypes = [PL, PC, i64, i32, vp, i32, vp, i64, vp, i64, f32, PF, vp, vp,
                                                 vp, sz, vp]
+        PB = C.POINTER(BlockCacheStruct)
+        L.diffkv_norm_rotate.argtypes = [PL, i64, vp, vp, i32, i32, f32, f32, i32, vp, i64, vp, vp, i64,
+                                         i32, vp, i64, vp, vp, i64, vp]
+        L.diffkv_block_append.argtypes = [PL, PB, i64, i32, vp, vp, i64, vp, i64, vp]
+        L.diffkv_block_read.argtypes = [PL, PB, i64, i32, vp, vp, vp, i64, vp, i64, vp]
+        L.diffkv_block_attention.argtypes = [PL, PB, i64, i32, vp, i32, vp, i64, vp, i64, vp, i64, f32, PF, i32, vp, vp,
+                                             vp, sz, vp]
         L.diffkv_compact_free_list.argtypes = [PL, PC, i32, vp, vp, sz, vp]
         L.diffkv_alloc_pages.argtypes = [PL, PC, i32, vp, vp, sz, vp]
         L.diffkv_generation_step.argtypes = [PL, PC, f32, f32, i32, vp, sz, vp]
@@ -332,10 +350,9 @@ def rope_frequencies(rot_dim, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, trai
     return freq, scale.value
 
 
-def rotate(L, pos, inv_freq, q, k=None, style=ROPE_HALF, scale=1.0, q_out=None, k_out=None, stream=None):
-    """Rotary positions: q fp16 [rows, Hq, D], k fp16 [rows, Hkv, D] or None (rows may be strided), pos int32
-    [rows], inv_freq fp32 [rot_dim / 2] (device) -> (q_out, k_out), contiguous unless given; q_out=q turns in
-    place."""
+def _rotate_args(what, L, pos, inv_freq, q, k, q_out, k_out):
+    """Checked arguments of both rotating calls, their outputs allocated unless given:
+    (rows, q_out, k_out, (q, stride, out, stride), (heads of k, k, stride, out, stride))."""
     rows, Hq = q.shape[0], q.shape[1]
     if pos.dtype != torch.int32 or pos.shape != (rows,) or not pos.is_contiguous():
         raise ValueError("pos: contiguous int32 [rows] expected")
@@ -346,15 +363,37 @@ def rotate(L, pos, inv_freq, q, k=None, style=ROPE_HALF, scale=1.0, q_out=None, 
     if k is not None and k_out is None:
         k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
     if q_out.shape != q.shape or (k is not None and (k_out.shape != k.shape or k.shape[0] != rows)):
-        raise ValueError("rotate: outputs shaped as their inputs expected")
-    kp, ks, Hkv = (None, 0, 0) if k is None else (*_rows(k, "k", L.head_dim), k.shape[1])
-    kop, kos = (None, 0) if k is None else _rows(k_out, "k_out", L.head_dim)
-    qp, qs = _rows(q, "q", L.head_dim)
-    qop, qos = _rows(q_out, "q_out", L.head_dim)
+        raise ValueError("%s: outputs shaped as their inputs expected" % what)
+    ka = (0, None, 0, None, 0) if k is None else (
+        k.shape[1], *_rows(k, "k", L.head_dim), *_rows(k_out, "k_out", L.head_dim))
+    qa = (*_rows(q, "q", L.head_dim), *_rows(q_out, "q_out", L.head_dim))
+    return rows, q_out, k_out, qa, ka
+
+
+def rotate(L, pos, inv_freq, q, k=None, style=ROPE_HALF, scale=1.0, q_out=None, k_out=None, stream=None):
+    """Rotary positions: q fp16 [rows, Hq, D], k fp16 [rows, Hkv, D] or None (rows may be strided), pos int32
+    [rows], inv_freq fp32 [rot_dim / 2] (device) -> (q_out, k_out), contiguous unless given; q_out=q turns in
+    place."""
+    rows, q_out, k_out, qa, (Hkv, kp, ks, kop, kos) = _rotate_args("rotate", L, pos, inv_freq, q, k, q_out, k_out)
     _on_one_gpu("rotate", q, k, pos, inv_freq, q_out, k_out)
     _check(lib().diffkv_rotate(C.byref(L), rows, _ptr(pos), _ptr(inv_freq), 2 * inv_freq.shape[0], int(style),
-                               float(scale), Hq, qp, qs, qop, qos, Hkv, kp, ks, kop, kos, _stream(stream)),
+                               float(scale), q.shape[1], *qa, Hkv, kp, ks, kop, kos, _stream(stream)),
            "diffkv_rotate")
+    return q_out, k_out
+
+
+def norm_rotate(L, pos, inv_freq, q, k=None, q_weight=None, k_weight=None, eps=1e-6, style=ROPE_HALF, scale=1.0,
+                q_out=None, k_out=None, stream=None):
+    """Each head over its root mean square times its side's weights (fp32 [D] or None: ones), then rotated:
+    arguments and results as rotate."""
+    rows, q_out, k_out, (qp, qs, qop, qos), (Hkv, kp, ks, kop, kos) = _rotate_args(
+        "norm_rotate", L, pos, inv_freq, q, k, q_out, k_out)
+    _dense(q_weight, "q_weight", torch.float32, L.head_dim)
+    _dense(k_weight, "k_weight", torch.float32, L.head_dim)
+    _on_one_gpu("norm_rotate", q, k, pos, inv_freq, q_weight, k_weight, q_out, k_out)
+    _check(lib().diffkv_norm_rotate(C.byref(L), rows, _ptr(pos), _ptr(inv_freq), 2 * inv_freq.shape[0], int(style),
+                                    float(scale), float(eps), q.shape[1], qp, qs, _ptr(q_weight), qop, qos, Hkv, kp, ks,
+                                    _ptr(k_weight), kop, kos, _stream(stream)), "diffkv_norm_rotate")
     return q_out, k_out
 
 
@@ -421,6 +460,119 @@ def chunk_significance(cache, new_len, q, k, sm_scale, lse, cap=0.0, window=0, s
         _form(cap, window, slopes), _ptr(lse), _ptr(score), ws.data_ptr(), ws.nbytes, _stream(stream)),
         "diffkv_chunk_significance", *sizes)
     return score
+
+
+_BLOCK_CACHE = struct.Struct("PPqPPPPiii")
+assert _BLOCK_CACHE.size <= C.sizeof(BlockCacheStruct)
+
+
+class BlockCache:
+    """Device tensors of one uniform 8-bit cache (diffkv_block_cache); the library owns none of them.  `table` int32
+    [num_seqs, ceil(max_seq_len / 32)] (block IDs, -1: not kept) and `seq_len` int32 [num_seqs] are the program's to
+    write.  `buffers`: (pool, scale, table, tail, seq_len, status) to use instead of new ones (caches of a model's
+    layers share table and seq_len)."""
+
+    def __init__(self, L, num_blocks, num_seqs, num_kv_heads, fmt=BLOCK_E4M3, device="cuda", buffers=None):
+        self.L = L
+        self.num_blocks, self.num_seqs, self.num_kv_heads = int(num_blocks), int(num_seqs), int(num_kv_heads)
+        self.fmt = int(fmt)
+        width = -(-L.max_seq_len // BLOCK_TOKENS)
+        D = L.head_dim
+        if buffers is None:
+            dev = torch.device(device)
+            z = lambda *shape, dtype: torch.zeros(shape, dtype=dtype, device=dev)
+            buffers = (z(self.num_blocks, self.num_kv_heads, 2, BLOCK_TOKENS * D, dtype=torch.uint8),
+                       torch.ones((self.num_blocks, self.num_kv_heads, 2), dtype=torch.float32, device=dev),
+                       torch.full((self.num_seqs, width), -1, dtype=torch.int32, device=dev),
+                       z(self.num_seqs, self.num_kv_heads, 2, BLOCK_TOKENS, D, dtype=torch.float16),
+                       z(self.num_seqs, dtype=torch.int32), z(1, dtype=torch.int32))
+        self.pool, self.scale, self.table, self.tail, self.seq_len, self.status = buffers
+        for t, what, dtype, shape in (
+                (self.pool, "pool", torch.uint8, (self.num_blocks, self.num_kv_heads, 2, BLOCK_TOKENS * D)),
+                (self.scale, "scale", torch.float32, (self.num_blocks, self.num_kv_heads, 2))):
+            if t.dtype != dtype or not t.is_contiguous() or t.shape[0] < shape[0] or t.shape[1:] != shape[1:]:
+                raise ValueError("%s: contiguous %s %s expected" % (what, dtype, list(shape)))
+        _dense(self.table, "table", torch.int32, self.num_seqs, width)
+        _dense(self.tail, "tail", torch.float16, self.num_seqs, self.num_kv_heads, 2, BLOCK_TOKENS, D)
+        _dense(self.seq_len, "seq_len", torch.int32, self.num_seqs)
+        _dense(self.status, "status", torch.int32, 1)
+
+    def tensors(self):
+        return self.pool, self.scale, self.table, self.tail, self.seq_len, self.status
+
+    def struct(self):
+        return BlockCacheStruct.from_buffer_copy(_BLOCK_CACHE.pack(
+            self.pool.data_ptr(), self.scale.data_ptr(), self.num_blocks, self.table.data_ptr(), self.tail.data_ptr(),
+            self.seq_len.data_ptr(), self.status.data_ptr(), self.num_seqs, self.num_kv_heads,
+            self.fmt).ljust(C.sizeof(BlockCacheStruct), b"\0"))
+
+
+def _block_rows(cache, lens, most, what, *rows):
+    """Checked lengths and rows of a uniform cache's call; the longest length."""
+    for t in (lens if isinstance(lens, tuple) else (lens,)):
+        if t.dtype != torch.int32 or t.shape != (cache.num_seqs,) or not t.is_contiguous():
+            raise ValueError("%s: lengths: contiguous int32 [num_seqs] expected" % what)
+        last = t
+    if most is None:
+        most = int(last.max().item()) if last.shape[0] else 0
+    for t in rows:
+        if t.shape[0] != rows[0].shape[0] or t.shape[1] != cache.num_kv_heads:
+            raise ValueError("%s: [rows, num_kv_heads, head_dim] keys and values expected" % what)
+    return int(most)
+
+
+def block_append(cache, new_len, k, v, max_new=None, stream=None):
+    """diffkv_block_append: k, v fp16 [rows, Hkv, D] (device, rows concatenated per sequence, may be strided), new_len
+    int32 [B] (device), into cache (a BlockCache) at seq_len, which is not advanced."""
+    max_new = _block_rows(cache, new_len, max_new, "block_append", k, v)
+    (kp, ks), (vp, vs) = (_rows(t, w, cache.L.head_dim) for t, w in ((k, "k"), (v, "v")))
+    _on_one_gpu("block_append", k, v, new_len, *cache.tensors())
+    _check(lib().diffkv_block_append(C.byref(cache.L), cache.struct(), k.shape[0], max_new, _ptr(new_len), kp, ks, vp,
+                                     vs, _stream(stream)), "diffkv_block_append")
+
+
+def block_read(cache, start, count, total, max_count=None, k_out=None, v_out=None, stream=None):
+    """diffkv_block_read: positions start[b] .. + count[b] - 1 of each sequence (int32 [B], device) as fp16 rows
+    [total, Hkv, D], one sequence's behind the other's -> (k_out, v_out)."""
+    shape = (int(total), cache.num_kv_heads, cache.L.head_dim)
+    k_out, v_out = (torch.empty(shape, dtype=torch.float16, device=cache.tail.device) if t is None else t
+                    for t in (k_out, v_out))
+    if k_out.shape != shape or v_out.shape != shape:
+        raise ValueError("block_read: outputs [total, num_kv_heads, head_dim] expected")
+    max_count = _block_rows(cache, (start, count), max_count, "block_read", k_out, v_out)
+    (kp, ks), (vp, vs) = (_rows(t, w, cache.L.head_dim) for t, w in ((k_out, "k_out"), (v_out, "v_out")))
+    _on_one_gpu("block_read", k_out, v_out, start, count, *cache.tensors())
+    _check(lib().diffkv_block_read(C.byref(cache.L), cache.struct(), shape[0], max_count, _ptr(start), _ptr(count), kp,
+                                   ks, vp, vs, _stream(stream)), "diffkv_block_read")
+    return k_out, v_out
+
+
+def block_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, sinks=0, slopes=None, out=None, lse=None,
+                    max_new=None, ws=None, stream=None, want_lse=True):
+    """diffkv_block_attention: q fp16 [rows, Hq, D], k, v fp16 [rows, Hkv, D] (device, rows concatenated per sequence,
+    may be strided), new_len int32 [B] (device) over cache (a BlockCache) -> out fp16 [rows, Hq, D], lse fp32
+    [rows, Hq].  With a window the first `sinks` tokens stay visible.  Call it before the rows are appended."""
+    rows, Hq, D = q.shape
+    max_new = _block_rows(cache, new_len, max_new, "block_attention", k, v)
+    if k.shape[0] != rows:
+        raise ValueError("block_attention: as many rows of keys and values as of queries expected")
+    if out is None:
+        out = torch.empty((rows, Hq, D), dtype=torch.float16, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
+    _dense(out, "out", torch.float16, rows, Hq, D)
+    _dense(lse, "lse", torch.float32, rows, Hq)
+    _dense(slopes, "slopes", torch.float32, Hq)
+    sizes = (OP_BLOCK_ATTENTION, cache.L, cache.num_seqs, Hq, cache.num_kv_heads, rows)
+    if ws is None:
+        ws = _new_ws(workspace_size(*sizes), q.device)
+    (qp, qs), (kp, ks), (vp, vs) = (_rows(t, w, cache.L.head_dim) for t, w in ((q, "q"), (k, "k"), (v, "v")))
+    _on_one_gpu("block_attention", q, k, v, new_len, slopes, out, lse, ws, *cache.tensors())
+    _check_ws(lib().diffkv_block_attention(
+        C.byref(cache.L), cache.struct(), rows, max_new, _ptr(new_len), Hq, qp, qs, kp, ks, vp, vs, float(sm_scale),
+        _form(cap, window, slopes), int(sinks), _ptr(out), _ptr(lse), ws.data_ptr(), ws.nbytes, _stream(stream)),
+        "diffkv_block_attention", *sizes)
+    return out, lse
 
 
 def compact_free_list(cache, release, num_tables=None, ws=None, stream=None):

@@ -557,7 +557,7 @@ typedef struct diffkv_block_cache {
  *            fused projection can be passed), 16-byte aligned, strides in elements,
  *            multiples of 8, at least heads*head_dim (any value with one row)
  * IDs of blocks that one call fills must differ.  head_dim 128, max_seq_len up to 2^30,
- * total_new up to 2^25 (DIFFKV_E_UNSUPPORTED otherwise).  No workspace.
+ * total_new up to 2^24 (DIFFKV_E_UNSUPPORTED otherwise).  No workspace.
  */
 diffkv_status diffkv_block_append(const diffkv_layout* layout, const diffkv_block_cache* cache,
                                   int64_t total_new, int32_t max_new, const int32_t* new_len,
@@ -595,7 +595,7 @@ diffkv_status diffkv_block_read(const diffkv_layout* layout, const diffkv_block_
  *   ws       diffkv_workspace_size(DIFFKV_OP_BLOCK_ATTENTION, ...) bytes, no clearing
  *            needed, 16-byte aligned; calls that may overlap need one each
  * The cache is read only.  Up to 64 query heads per KV head, head_dim 128, total_new
- * up to 2^25, max_seq_len up to 2^30, up to 2^22 (sequence, KV head) pairs
+ * up to 2^24, max_seq_len up to 2^30, up to 2^22 (sequence, KV head) pairs
  * (DIFFKV_E_UNSUPPORTED otherwise).  seq_len counts clamped to [0, max_seq_len].
  * Scores x up to 2^22 in magnitude, the slopes' part included.
  * Precision: codes enter the products exactly, and the weights in two fp16 parts (2^-22, or 2^-37 of

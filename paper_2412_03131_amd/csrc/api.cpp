@@ -311,7 +311,7 @@ diffkv_status rotate_call(const diffkv_layout* layout, int64_t rows, const int32
 }
 
 // What the uniform cache's entry points check, and its arguments.
-constexpr int64_t kMaxBlockRows = (int64_t)1 << 25;
+constexpr int64_t kMaxBlockRows = (int64_t)1 << 24;
 constexpr int32_t kMaxBlockLen = 1 << 30;
 constexpr int32_t kMaxBlockGroup = 64;  // query heads per KV head: a sequence's rows stay within 31 bits
 diffkv_status block_call(const diffkv_layout* layout, const diffkv_block_cache* c, int64_t rows, int32_t max_rows,
@@ -795,7 +795,10 @@ diffkv_status diffkv_block_attention(const diffkv_layout* layout, const diffkv_b
     a.out = out;
     a.lse = lse;
     a.arrive = static_cast<unsigned long long*>(ws);
-    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kBlockRowShares * 8);
+    a.part = reinterpret_cast<float*>(a.arrive + kBlockRowShares);
+    a.tile_arrive = reinterpret_cast<unsigned long long*>(static_cast<uint8_t*>(ws) + kBlockRowBytes);
+    a.tile_part = reinterpret_cast<float*>(a.tile_arrive + kBlockTileShares);
+    a.few_rows = kBlockFewRows;
     hipError_t e = launch_block_attention(a, cache->format, mod, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
 }

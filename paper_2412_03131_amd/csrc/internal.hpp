@@ -374,13 +374,25 @@ struct BlockAttnArgs : BlockCacheArgs {
     int sinks;             // 0 without a window
     uint16_t* out;
     float* lse;
-    unsigned long long* arrive;  // [shares] arrival word of the split tile that starts in a share
-    float* part;                 // [shares][2][rows] partial states {acc[kD], reference, sum, -, -}
-    int shares;                  // workgroups, most shares of the call
+    int few_rows;          // rows (new tokens x G) of a sequence up to which it is one of few
+    unsigned long long* arrive;       // few rows: [shares] arrival word of the split block that starts in a share
+    float* part;                      // [shares][2][16 rows] partial states {acc[kD], reference, sum, -, -}
+    unsigned long long* tile_arrive;  // many rows: the same
+    float* tile_part;                 // [shares][2][kTilePart]
 };
-constexpr int kBlockRowShares = 1024;  // most workgroups of the few-row kernel
+// Workgroups of the attention kernels, as many as run at once: two for each CU (few rows: of eight waves, many: of four).
+constexpr int kBlockRowShares = 512;
+constexpr int kBlockTileShares = 512;
+constexpr int kTilePart = 4 * 17 * 64 * 4;  // floats of a 128-row block's state: four waves, a lane's 64 sums and {reference, sum, -, -}
+// Rows up to which a sequence goes to the few-row kernel.
+constexpr int kBlockFewRows = 64;
 constexpr long long kBlockRowBytes = kBlockRowShares * (8ll + 2 * 16 * kChunkPart * 4);
-inline long long block_attention_ws(long long, long long) { return kBlockRowBytes; }
+constexpr long long kBlockTileBytes = kBlockTileShares * (8ll + 2 * kTilePart * 4);
+// A function of the query heads per KV head and the rows alone: one for more rows serves fewer.
+inline long long block_attention_ws(long long G, long long total_new)
+{
+    return kBlockRowBytes + (total_new * G > kBlockFewRows ? kBlockTileBytes : 0);
+}
 hipError_t launch_block_append(const BlockAppendArgs& a, int format, hipStream_t st);
 hipError_t launch_block_read(const BlockReadArgs& a, int format, hipStream_t st);
 hipError_t launch_block_attention(const BlockAttnArgs& a, int format, bool mod, hipStream_t st);

@@ -5,9 +5,9 @@
 // blocks, the others are fp16 rows (the tail's up to L, the call's own behind it).  A key at c is seen
 // from p >= c if p - c < window or c < sinks.
 //
-// Scores come from v_mfma_f32_16x16x32_f16 with the keys as A operand (codes / 32 are fp16 values, exactly; the
-// block's scale multiplies the fp32 sum), so a lane's eight scores of a tile lie in one row; their weights go into the
-// second product as they lie, in two fp16 parts (2^-22), with the values as A operand.
+// Keys are the first product's A operand (codes / 32 are fp16 values, exactly; the block's scale multiplies the fp32 sum),
+// so a lane's scores of a tile lie in one row; their weights go into the second product as they lie, in two fp16 parts
+// (2^-22), with the values as A operand.  Sequences of few rows go to block_rows, the others to block_tiles.
 // A value block's scale s enters the weights: u = exp2(x + log2 s - R) for a row's reference R, so that the
 // products of all blocks add up as they are, and the normalizer takes u / s.  R is twelve below the
 // largest exponent so far, which the next ones may pass by three before R is raised: fp16 (to 2^16, in steps of 2^-24 at
@@ -53,31 +53,32 @@ __device__ __forceinline__ const uint16_t* row_of(const RowSource& s, int side, 
 {
     return pos < s.L ? s.tail[side] + (pos & (kBT - 1)) * kD : s.own[side] + (long long)(pos - s.L) * s.stride[side];
 }
-// Pieces of a tile: keys 512 (token, 16 bytes), values 128 (r, four dims).
-__device__ __forceinline__ void stage_key(const RowSource& s, int pos0, uint8_t* lds, int piece)
+// Pieces of a tile: keys 512 (token, eight dims), values 128 (r, four dims of r's eight tokens).
+__device__ __forceinline__ void put_key(u4 x, uint8_t* lds, int piece)
 {
     const int c = piece & 15, token = piece >> 4;  // c: dims 8 c ..
-    u4 x = {0, 0, 0, 0};
-    if (pos0 + token < s.end) x = *reinterpret_cast<const u4*>(row_of(s, 0, pos0 + token) + c * 8);
     const int step = (c >> 3) * 2 + (c & 1), r = (c >> 1) & 3;
     *reinterpret_cast<u4*>(lds + (token >> 4) * 4096 + step * 1024 + r * 256 + (token & 15) * 16) = x;
 }
-__device__ __forceinline__ void stage_value(const RowSource& s, int pos0, uint8_t* lds, int piece, uint32_t* odd)
+// Returns the bits of the tokens with values that are not finite among the wave's pieces.
+__device__ __forceinline__ uint32_t put_value(u2 (&x)[8], uint8_t* lds, int piece)
 {
     const int dq = piece & 31, r = piece >> 5;  // dims 4 dq ..
-    u2 x[8];
+    uint32_t bad = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int token = (e >> 2) * 16 + 4 * r + (e & 3);
-        x[e] = u2{0, 0};
-        if (pos0 + token < s.end) x[e] = *reinterpret_cast<const u2*>(row_of(s, 1, pos0 + token) + dq * 4);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            // (an exponent of ones: adding one there carries into the sign's place)
+            const uint32_t full = ((x[e][i] & 0x7fff7fffu) + 0x04000400u) & 0x80008000u;
+            bad |= full ? 1u << ((e >> 2) * 16 + 4 * r + (e & 3)) : 0u;
+        }
     }
+    uint32_t odd = 0;
+    if (__any(bad != 0)) {
+        odd = wave_or_u32(bad);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t m0 = x[e][0] & 0x7fff7fffu, m1 = x[e][1] & 0x7fff7fffu;
-        const bool bad = (m0 & 0xffffu) >= 0x7c00u || (m0 >> 16) >= 0x7c00u || (m1 & 0xffffu) >= 0x7c00u || (m1 >> 16) >= 0x7c00u;
-        if (bad) {
-            atomicOr(odd, 1u << ((e >> 2) * 16 + 4 * r + (e & 3)));
+        for (int e = 0; e < 8; ++e) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 if ((x[e][i] & 0x7c00u) == 0x7c00u) x[e][i] &= 0xffff0000u;
@@ -94,20 +95,165 @@ __device__ __forceinline__ void stage_value(const RowSource& s, int pos0, uint8_
         const int dim = dq * 4 + i;
         *reinterpret_cast<u4*>(lds + 8192 + (dim >> 5) * 2048 + ((dim >> 4) & 1) * 1024 + r * 256 + (dim & 15) * 16) = y;
     }
+    return odd;
+}
+__device__ __forceinline__ u4 key_piece(const RowSource& s, int pos0, int piece)
+{
+    const int pos = pos0 + (piece >> 4);
+    return pos < s.end ? *reinterpret_cast<const u4*>(row_of(s, 0, pos) + (piece & 15) * 8) : u4{0, 0, 0, 0};
+}
+__device__ __forceinline__ u2 value_piece(const RowSource& s, int pos0, int piece, int e)
+{
+    const int pos = pos0 + (e >> 2) * 16 + 4 * (piece >> 5) + (e & 3);
+    return pos < s.end ? *reinterpret_cast<const u2*>(row_of(s, 1, pos) + (piece & 31) * 4) : u2{0, 0};
+}
+
+// ---- scores to weights ----------------------------------------------------------------
+// One tile's scores (natural units with a form, else log2) -> weights for the values' product.
+struct TileScale {
+    float ks;       // of the fp32 product: a code's unit, scales, without a form log2(e)
+    float add;      // log2 of the values' scale (natural units with a form)
+    float rs;       // 1 / the values' scale
+};
+struct TileView {
+    int pos0, end;  // tokens from position `end` on are not there
+    bool whole;     // all rows see all 32 tokens
+};
+// A tile for rows at p_lo .. p_hi: whether all of them see all of it, and whether none sees any of it.
+__device__ __forceinline__ bool all_seen(const BlockAttnArgs& a, int pos0, int p_lo, int p_hi)
+{
+    return pos0 + kBT - 1 <= p_lo && (p_hi - pos0 < a.window || pos0 + kBT <= a.sinks);
+}
+__device__ __forceinline__ bool none_seen(const BlockAttnArgs& a, int pos0, int p_lo, int p_hi)
+{
+    return pos0 > p_hi || (p_lo - (pos0 + kBT - 1) >= a.window && pos0 >= a.sinks);
+}
+__device__ __forceinline__ float pairs_max(float v)  // over lanes l, l + 32
+{
+    auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ __forceinline__ float pairs_sum(float v)
+{
+    auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(x[0]) + __uint_as_float(x[1]);
+}
+
+// N scores of a lane (8: tiles of 16 rows, token (i / 4) 16 + 4 r + i % 4; 16: tiles of 32, token 8 (i / 4) + 4 half +
+// i % 4) become weights; acc are the row's sums of values, raised with its reference.
+template <bool MOD, int N, typename Acc, int A>
+__device__ __forceinline__ void weights(const BlockAttnArgs& a, const TileScale& t, const TileView& w, float (&y)[N], int p,
+                                        const ScoreForm& form, Acc (&acc)[A], float& ref, float& sum)
+{
+    constexpr float unit = MOD ? kChunkLn2 : 1.0f;
+    const int group = N == 8 ? lane_id() >> 4 : lane_id() >> 5;
+    float top = -INFINITY;
+    if (MOD || !w.whole) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = w.pos0 + (i >> 2) * (N == 8 ? 16 : 8) + 4 * group + (i & 3);
+            if constexpr (MOD) y[i] = formed(y[i] * t.ks, form, (float)(p - c)) + t.add;
+            else y[i] = __builtin_fmaf(y[i], t.ks, t.add);
+            if (!w.whole) {
+                const bool seen = c <= p && c < w.end && (p - c < a.window || c < a.sinks);
+                y[i] = seen ? y[i] : -INFINITY;
+            }
+            top = fmaxf(top, y[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            y[i] = __builtin_fmaf(y[i], t.ks, t.add);
+            top = fmaxf(top, y[i]);
+        }
+    }
+    if (__any(top > ref + kRefRoom * unit)) {
+        const float now = N == 8 ? rows_max(top) : pairs_max(top);
+        const float up = now > ref + kRefRoom * unit ? now - kRefBelow * unit : ref;
+        const float f = __builtin_amdgcn_exp2f((ref - up) * (MOD ? kChunkLog2e : 1.0f));
+        ref = up;
+        sum *= f;
+#pragma unroll
+        for (int i = 0; i < A; ++i) acc[i] *= f;
+    }
+    float total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        y[i] = __builtin_amdgcn_exp2f(MOD ? (y[i] - ref) * kChunkLog2e : y[i] - ref);
+        total += y[i];
+    }
+    sum = __builtin_fmaf(total, t.rs, sum);
+}
+// Eight weights as two fp16 parts.
+struct Parts {
+    h8 hi, lo;
+};
+__device__ __forceinline__ Parts parts(float a, float b, float c, float d, float e, float f, float g, float h)
+{
+    const float u[8] = {a, b, c, d, e, f, g, h};
+    Parts r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.hi[i] = (_Float16)u[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.lo[i] = (_Float16)__builtin_fmaf((float)r.hi[i], -1.0f, u[i]);
+    return r;
+}
+
+// Block IDs and scales of 64 steps of a wave, a lane each (step = first + lane * stride < end); those whose block is there.
+struct StepList {
+    int id;
+    TileScale scale;
+    unsigned long long there;
+};
+template <bool MOD>
+__device__ __forceinline__ StepList list_steps(const BlockAttnArgs& a, const Tiles& tl, int b, int h, int first, int stride, int end)
+{
+    StepList s;
+    const int step = first + lane_id() * stride;
+    s.id = step < end ? block_id(a, b, tl.at(step)) : -1;
+    s.there = __ballot(s.id >= 0);
+    float ks = 1.0f, vs = 1.0f;
+    if (s.id >= 0) {
+        const float* sc = a.scale + ((long long)s.id * a.Hkv + h) * 2;
+        ks = sc[0];
+        vs = sc[1];
+    }
+    vs *= kCodeUnit;
+    s.scale.ks = ks * kCodeUnit * a.scale_x;
+    s.scale.add = __builtin_amdgcn_logf(vs) * (MOD ? kChunkLn2 : 1.0f);
+    s.scale.rs = vs > 0.0f && vs < INFINITY ? 1.0f / vs : 1.0f;  // (a NaN scale: rows that see nothing of the block keep their sums)
+    return s;
+}
+__device__ __forceinline__ TileScale scale_of(const StepList& s, int i)
+{
+    return TileScale{read_lane_f(s.scale.ks, i), read_lane_f(s.scale.add, i), read_lane_f(s.scale.rs, i)};
+}
+
+__device__ __forceinline__ RowSource row_source(const BlockAttnArgs& a, const SeqItem& sq, int h)
+{
+    const uint16_t* tail = tail_rows(a, sq.b, h);
+    return RowSource{{tail, tail + kBlockSide},
+                     {a.k + sq.row0 * a.k_stride + h * kD, a.v + sq.row0 * a.v_stride + h * kD},
+                     {a.k_stride, a.v_stride}, sq.L, sq.L + sq.n};
+}
+// Steps whose tiles are blocks of the cache: they come first.
+__device__ __forceinline__ int coded_steps(const Tiles& tl, int L)
+{
+    const int held = L / kBT;
+    return held <= tl.sb ? held : min(max(held - tl.w0, 0) + tl.sb, tl.count());
 }
 
 // ---- few rows: a workgroup on 16 rows -------------------------------------------------
 // Eight waves on the tiles of a piece, one tile each at a time; their states meet in LDS.  All (sequence, KV head, 16
 // rows) are laid end to end by their tiles and cut into equal pieces, one for each workgroup; one that is
 // split has its pieces' states joined by the last to arrive.
+//
+// Bound by memory.  A wave asks for a tile's keys again as soon as their codes are operands, and for its values likewise, so 8 KB
+// of the next tile are always on their way.
 constexpr int kRowWaves = 8;
 constexpr int kRowStart = 2;    // a 16-row block's start, in tiles
+constexpr int kRowShare = 16;  // least units of a piece: two tiles a wave
 constexpr int kStaged = 4;      // tiles of fp16 rows in LDS at once
-
-struct RowState {               // of a wave: lane = r * 16 + row
-    f4 acc[8];                  // [u * 2 + j]: dims u 32 + j 16 + 4 r ..
-    float ref, sum;             // reference (the same in all four lanes of a row), the lane's part of the normalizer
-};
 
 struct RowLds {
     union {
@@ -119,73 +265,23 @@ struct RowLds {
     int last;
 };
 
-// One tile's scores (natural units with a form, else log2) -> weights into the values' product.
-struct RowTile {
-    float ks;       // of the fp32 product: a code's unit, scales, without a form log2(e)
-    float add;      // log2 of the values' scale (natural units with a form)
-    float rs;       // 1 / the values' scale
-    int pos0;
-    bool whole;     // all rows see all 32 tokens
-    int end;        // tokens from here on are not there
-};
-
-template <bool MOD>
-__device__ __forceinline__ void row_weights(const BlockAttnArgs& a, const RowTile& t, const f4 (&s)[2], int p, const ScoreForm& form,
-                                            RowState& st, h8& hi, h8& lo, float (&u)[8])
-{
-    const int r = lane_id() >> 4;
-    float y[8], top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int c = t.pos0 + (i >> 2) * 16 + 4 * r + (i & 3);
-        if constexpr (MOD) {
-            y[i] = formed(s[i >> 2][i & 3] * t.ks, form, (float)(p - c)) + t.add;
-        } else {
-            y[i] = __builtin_fmaf(s[i >> 2][i & 3], t.ks, t.add);
-        }
-        if (!t.whole) {
-            const bool seen = c <= p && c < t.end && (p - c < a.window || c < a.sinks);
-            y[i] = seen ? y[i] : -INFINITY;
-        }
-        top = fmaxf(top, y[i]);
-    }
-    constexpr float unit = MOD ? kChunkLn2 : 1.0f;
-    if (__any(top > st.ref + kRefRoom * unit)) {
-        const float now = rows_max(top);
-        const float ref = now > st.ref + kRefRoom * unit ? now - kRefBelow * unit : st.ref;
-        const float f = __builtin_amdgcn_exp2f((st.ref - ref) * (MOD ? kChunkLog2e : 1.0f));
-        st.ref = ref;
-        st.sum *= f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) st.acc[i] *= f;
-    }
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        u[i] = __builtin_amdgcn_exp2f(MOD ? (y[i] - st.ref) * kChunkLog2e : y[i] - st.ref);
-        sum += u[i];
-        hi[i] = (_Float16)u[i];
-        lo[i] = (_Float16)(u[i] - (float)hi[i]);
-    }
-    st.sum = __builtin_fmaf(sum, t.rs, st.sum);
-}
-
 template <int FMT, bool MOD>
 __global__ __launch_bounds__(64 * kRowWaves, 4) void block_rows(BlockAttnArgs a)
 {
     __shared__ RowLds lds;
     const int lane = lane_id(), wave = wave_index(), r = lane >> 4, col = lane & 15;
+    const int first_n = lane < a.B ? a.new_len[lane] : 0, first_L = lane < a.B ? seq_tokens(a, lane) : 0;
     const auto loads = [&](int b, int& n, int& L) {
-        n = a.new_len[b];
-        L = seq_tokens(a, b);
+        n = b < kWave ? first_n : a.new_len[b];
+        L = b < kWave ? first_L : seq_tokens(a, b);
     };
     // units of a sequence: 16-row blocks times their tiles and start
     const auto units = [&](int n, int L) {
-        return n > 0 ? (long long)a.Hkv * (((long long)n * a.G + 15) / 16) * (tiles_of(a, n, L).count() + kRowStart) : 0LL;
+        return n > 0 && n * a.G <= a.few_rows ? (long long)a.Hkv * ((n * a.G + 15) / 16) * (tiles_of(a, n, L).count() + kRowStart) : 0LL;
     };
     const long long all = find_item(a.B, a.total_new, a.max_new, INT64_MAX, loads, units).items;
-    long long share = (all + a.shares - 1) / a.shares;
-    share = share < 16 ? 16 : share;
+    long long share = (all + gridDim.x - 1) / gridDim.x;
+    share = share < kRowShare ? kRowShare : share;
     long long x = (long long)blockIdx.x * share;
     const long long x_end = min(x + share, all);
 
@@ -193,21 +289,20 @@ __global__ __launch_bounds__(64 * kRowWaves, 4) void block_rows(BlockAttnArgs a)
         const SeqItem sq = find_item(a.B, a.total_new, a.max_new, x, loads, units);
         if (sq.b < 0) break;
         const Tiles tl = tiles_of(a, sq.n, sq.L);
-        const int steps = tl.count(), blk_units = steps + kRowStart;
-        const int blocks = (int)(((long long)sq.n * a.G + 15) / 16);
+        const int blk_units = tl.count() + kRowStart, coded = coded_steps(tl, sq.L);
+        const int blocks = (sq.n * a.G + 15) / 16;
         // 16-row block of the sequence: KV head major
-        long long which = (x - sq.item0) / blk_units;
-        const long long seq_end = sq.item0 + (long long)a.Hkv * blocks * blk_units;
-        for (; x < x_end && x < seq_end; ++which) {
-            const long long t0 = sq.item0 + which * blk_units;  // the block's first unit
-            const int h = (int)(which / blocks), row_first = (int)(which - (long long)h * blocks) * 16;
+        int which = (int)((x - sq.item0) / blk_units);
+        for (; x < x_end && which < a.Hkv * blocks; ++which) {
+            const long long t0 = sq.item0 + (long long)which * blk_units;  // the block's first unit
+            const int h = which / blocks, row_first = (which - h * blocks) * 16;
             const int s0 = (int)max(x - t0 - kRowStart, 0LL);
             const int s1 = (int)(min(x_end, t0 + blk_units) - t0) - kRowStart;
             x = min(x_end, t0 + blk_units);
             if (s1 <= s0) continue;
 
             // this lane's row
-            const int rows = (int)min((long long)sq.n * a.G - row_first, 16LL);
+            const int rows = min(sq.n * a.G - row_first, 16);
             const int row = row_first + min(col, rows - 1), token = row / a.G, hq = h * a.G + row % a.G, p = sq.L + token;
             h8 q[4];
             {
@@ -218,194 +313,498 @@ __global__ __launch_bounds__(64 * kRowWaves, 4) void block_rows(BlockAttnArgs a)
             ScoreForm form{0.0f, 0.0f, 0.0f};
             if constexpr (MOD) form = ScoreForm{a.cap_in, a.cap, a.slopes ? a.slopes[hq] : 0.0f};
             const int p_lo = sq.L + row_first / a.G, p_hi = sq.L + (row_first + rows - 1) / a.G;
-            RowState st;
+            f4 acc[8];  // [u * 2 + j]: dims u 32 + j 16 + 4 r ..
+            float ref = kLowest, sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) st.acc[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-            st.ref = kLowest;
-            st.sum = 0.0f;
+            for (int i = 0; i < 8; ++i) acc[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
             // steps of the cache's blocks, then those of fp16 rows
-            const int blocks_held = sq.L / kBT;
-            const int coded = blocks_held <= tl.sb ? min(blocks_held, tl.sb)
-                                                   : min(max(blocks_held - tl.w0, 0) + tl.sb, steps);
             const int c1 = min(s1, coded);
-            for (int base = s0; base < c1; base += kRowWaves * kWave) {
-                // this wave's next 64 tiles: block IDs and scales, a lane each
-                const int mine = base + wave + lane * kRowWaves;
-                int id = -1;
-                float ks = 0.0f, vs = 1.0f;
-                if (mine < c1) id = block_id(a, sq.b, tl.at(mine));
-                if (id >= 0) {
-                    const float* sc = a.scale + ((long long)id * a.Hkv + h) * 2;
-                    ks = sc[0];
-                    vs = sc[1] * kCodeUnit;
-                }
-                const float rs = vs > 0.0f && vs < INFINITY ? 1.0f / vs : 1.0f;
-                const float add = __builtin_amdgcn_logf(vs) * (MOD ? kChunkLn2 : 1.0f);
-                ks *= kCodeUnit * a.scale_x;
-                const int here = min(kWave, (c1 - base - wave + kRowWaves - 1) / kRowWaves);
-                for (int i = 0; i < here; ++i) {
-                    const int bid = __builtin_amdgcn_readlane(id, i);
-                    if (bid < 0) continue;
-                    RowTile t;
-                    t.ks = read_lane_f(ks, i);
-                    t.add = read_lane_f(add, i);
-                    t.rs = read_lane_f(rs, i);
-                    t.pos0 = tl.at(base + wave + i * kRowWaves) * kBT;
-                    t.end = INT32_MAX;
-                    t.whole = t.pos0 + kBT - 1 <= p_lo && (p_hi - t.pos0 < a.window || t.pos0 + kBT <= a.sinks);
-                    const auto src = span(a.pool + ((long long)bid * a.Hkv + h) * kBlockBytes, kBlockBytes);
+            for (int base = s0 + wave; base < c1; base += kRowWaves * kWave) {
+                const StepList list = list_steps<MOD>(a, tl, sq.b, h, base, kRowWaves, c1);
+                unsigned long long todo = list.there;
+                if (!todo) continue;
+                int i = __builtin_ctzll(todo);
+                const auto block = [&](int at) {
+                    const int id = __builtin_amdgcn_readlane(list.id, at);
+                    return span(a.pool + ((long long)id * a.Hkv + h) * kBlockBytes, kBlockBytes);
+                };
+                auto src = block(i);
+                u4 k[4], v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k[j] = fetch<16>(src, lane * 16, j * 1024);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = fetch<16>(src, lane * 16, kBlockSide + j * 1024);
+                while (todo) {
+                    todo &= todo - 1;
+                    const int next = todo ? __builtin_ctzll(todo) : i;
+                    const TileScale ts = scale_of(list, i);
+                    TileView view{tl.at(base + i * kRowWaves) * kBT, INT32_MAX, false};
+                    view.whole = all_seen(a, view.pos0, p_lo, p_hi);
+                    src = block(next);
                     f4 s[2] = {f4{0.0f, 0.0f, 0.0f, 0.0f}, f4{0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-                    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-                        for (int i2 = 0; i2 < 2; ++i2) {
-                            const u4 w = fetch<16>(src, lane * 16, (tt * 2 + i2) * 1024);
-                            s[tt] = mfma_k32(codes8<FMT>(w[0], w[1]), q[i2 * 2], s[tt]);
-                            s[tt] = mfma_k32(codes8<FMT>(w[2], w[3]), q[i2 * 2 + 1], s[tt]);
-                        }
-                    h8 hi, lo;
-                    float u[8];
-                    row_weights<MOD>(a, t, s, p, form, st, hi, lo, u);
-#pragma unroll
-                    for (int uu = 0; uu < 4; ++uu) {
-                        const u4 w = fetch<16>(src, lane * 16, kBlockSide + uu * 1024);
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const h8 v = codes8<FMT>(w[2 * j], w[2 * j + 1]);
-                            st.acc[uu * 2 + j] = mfma_k32(v, hi, st.acc[uu * 2 + j]);
-                            st.acc[uu * 2 + j] = mfma_k32(v, lo, st.acc[uu * 2 + j]);
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        s[j >> 1] = mfma_k32(codes8<FMT>(k[j][0], k[j][1]), q[(j & 1) * 2], s[j >> 1]);
+                        s[j >> 1] = mfma_k32(codes8<FMT>(k[j][2], k[j][3]), q[(j & 1) * 2 + 1], s[j >> 1]);
                     }
+                    if (todo) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) k[j] = fetch<16>(src, lane * 16, j * 1024);
+                    }
+                    float y[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) y[j] = s[j >> 2][j & 3];
+                    weights<MOD>(a, ts, view, y, p, form, acc, ref, sum);
+                    const Parts w = parts(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const h8 x8 = codes8<FMT>(v[j >> 1][(j & 1) * 2], v[j >> 1][(j & 1) * 2 + 1]);
+                        acc[j] = mfma_k32(x8, w.hi, acc[j]);
+                        acc[j] = mfma_k32(x8, w.lo, acc[j]);
+                    }
+                    if (todo) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] = fetch<16>(src, lane * 16, kBlockSide + j * 1024);
+                    }
+                    i = next;
                 }
             }
 
-            const int f0 = max(s0, coded);
-            if (f0 < s1) {
-                const uint16_t* tail = tail_rows(a, sq.b, h);
-                const RowSource src{{tail, tail + kBlockSide},
-                                    {a.k + sq.row0 * a.k_stride + h * kD, a.v + sq.row0 * a.v_stride + h * kD},
-                                    {a.k_stride, a.v_stride}, sq.L, sq.L + sq.n};
-                for (int base = f0; base < s1; base += kStaged) {
-                    const int here = min(kStaged, s1 - base);
-                    __syncthreads();
-                    if (threadIdx.x < kStaged) lds.odd[threadIdx.x] = 0;
-                    __syncthreads();
-                    for (int piece = threadIdx.x; piece < here * 512; piece += 64 * kRowWaves)
-                        stage_key(src, tl.at(base + piece / 512) * kBT, lds.rows + piece / 512 * kRowTileBytes, piece & 511);
-                    for (int piece = threadIdx.x; piece < here * 128; piece += 64 * kRowWaves)
-                        stage_value(src, tl.at(base + piece / 128) * kBT, lds.rows + piece / 128 * kRowTileBytes, piece & 127,
-                                    &lds.odd[piece / 128]);
-                    __syncthreads();
-                    if (wave < here) {
-                        const uint8_t* tile = lds.rows + wave * kRowTileBytes;
-                        RowTile t;
-                        t.ks = a.scale_x;
-                        t.add = 0.0f;
-                        t.rs = 1.0f;
-                        t.pos0 = tl.at(base + wave) * kBT;
-                        t.end = sq.L + sq.n;
-                        t.whole = t.pos0 + kBT - 1 <= p_lo && (p_hi - t.pos0 < a.window || t.pos0 + kBT <= a.sinks);
-                        f4 s[2] = {f4{0.0f, 0.0f, 0.0f, 0.0f}, f4{0.0f, 0.0f, 0.0f, 0.0f}};
+            for (int base = max(s0, coded); base < s1; base += kStaged) {
+                const RowSource src = row_source(a, sq, h);
+                const int here = min(kStaged, s1 - base);
+                __syncthreads();
+                if (threadIdx.x < kStaged) lds.odd[threadIdx.x] = 0;
+                __syncthreads();
+#pragma unroll 1
+                for (int piece = threadIdx.x; piece < here * 512; piece += 64 * kRowWaves) {
+                    const int t = piece / 512;
+                    put_key(key_piece(src, tl.at(base + t) * kBT, piece & 511), lds.rows + t * kRowTileBytes, piece & 511);
+                }
+#pragma unroll 1
+                for (int piece = threadIdx.x; piece < here * 128; piece += 64 * kRowWaves) {
+                    const int t = piece / 128;
+                    u2 v8[8];
 #pragma unroll
-                        for (int tt = 0; tt < 2; ++tt)
+                    for (int e = 0; e < 8; ++e) v8[e] = value_piece(src, tl.at(base + t) * kBT, piece & 127, e);
+                    const uint32_t odd = put_value(v8, lds.rows + t * kRowTileBytes, piece & 127);
+                    if (odd && lane == 0) atomicOr(&lds.odd[t], odd);
+                }
+                __syncthreads();
+                if (wave < here) {
+                    const uint8_t* tile = lds.rows + wave * kRowTileBytes;
+                    TileView view{tl.at(base + wave) * kBT, sq.L + sq.n, false};
+                    view.whole = all_seen(a, view.pos0, p_lo, p_hi);
+                    f4 s[2] = {f4{0.0f, 0.0f, 0.0f, 0.0f}, f4{0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                s[tt] = mfma_k32(*reinterpret_cast<const h8*>(tile + tt * 4096 + i * 1024 + lane * 16), q[i], s[tt]);
-                        h8 hi, lo;
-                        float u[8];
-                        row_weights<MOD>(a, t, s, p, form, st, hi, lo, u);
+                    for (int j = 0; j < 8; ++j)
+                        s[j >> 2] = mfma_k32(*reinterpret_cast<const h8*>(tile + j * 1024 + lane * 16), q[j & 3], s[j >> 2]);
+                    float y[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const h8 v = *reinterpret_cast<const h8*>(tile + 8192 + i * 1024 + lane * 16);
-                            st.acc[i] = mfma_k32(v, hi, st.acc[i]);
-                            st.acc[i] = mfma_k32(v, lo, st.acc[i]);
-                        }
-                        // values that are not finite, to the rows that see their token
-                        for (uint32_t odd = __builtin_amdgcn_readfirstlane(lds.odd[wave]); odd; odd &= odd - 1) {
-                            const int token_odd = __builtin_ctz(odd), c = t.pos0 + token_odd;
-                            const int from = ((token_odd & 15) >> 2) * 16 + col, reg = (token_odd >> 4) * 4 + (token_odd & 3);
-                            float w = 0.0f;
+                    for (int j = 0; j < 8; ++j) y[j] = s[j >> 2][j & 3];
+                    weights<MOD>(a, TileScale{a.scale_x, 0.0f, 1.0f}, view, y, p, form, acc, ref, sum);
+                    const Parts w = parts(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) w = i == reg ? u[i] : w;
-                            w = __shfl(w, from);
-                            const bool seen = c <= p && (p - c < a.window || c < a.sinks);
-                            const uint16_t* vr = row_of(src, 1, c);
+                    for (int j = 0; j < 8; ++j) {
+                        const h8 x8 = *reinterpret_cast<const h8*>(tile + 8192 + j * 1024 + lane * 16);
+                        acc[j] = mfma_k32(x8, w.hi, acc[j]);
+                        acc[j] = mfma_k32(x8, w.lo, acc[j]);
+                    }
+                    // values that are not finite, to the rows that see their token
+                    for (uint32_t odd = __builtin_amdgcn_readfirstlane(lds.odd[wave]); odd; odd &= odd - 1) {
+                        const int tok = __builtin_ctz(odd), c = view.pos0 + tok;
+                        const int from = ((tok & 15) >> 2) * 16 + col, reg = (tok >> 4) * 4 + (tok & 3);
+                        float wt = 0.0f;
 #pragma unroll
-                            for (int i = 0; i < 8; ++i)
+                        for (int j = 0; j < 8; ++j) wt = j == reg ? y[j] : wt;
+                        wt = __shfl(wt, from);
+                        const bool seen = c <= p && (p - c < a.window || c < a.sinks);
+                        const uint16_t* vr = row_of(src, 1, c);
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    const float v = h2f(vr[(i >> 1) * 32 + (i & 1) * 16 + 4 * r + j]);
-                                    if (seen && !(fabsf(v) < INFINITY)) st.acc[i][j] = __builtin_fmaf(w, v, st.acc[i][j]);
-                                }
+                        for (int j = 0; j < 32; ++j) {
+                            const float v1 = h2f(vr[(j >> 3) * 32 + ((j >> 2) & 1) * 16 + 4 * r + (j & 3)]);
+                            if (seen && !(fabsf(v1) < INFINITY)) acc[j >> 2][j & 3] = __builtin_fmaf(wt, v1, acc[j >> 2][j & 3]);
                         }
                     }
                 }
             }
 
             // the waves' states
-            st.sum = rows_sum(st.sum);
+            sum = rows_sum(sum);
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<f4*>(&lds.state[wave][col][(i >> 1) * 32 + (i & 1) * 16 + 4 * r]) = st.acc[i];
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<f4*>(&lds.state[wave][col][(i >> 1) * 32 + (i & 1) * 16 + 4 * r]) = acc[i];
             if (r == 0) {
-                lds.ref[wave][col] = st.ref;
-                lds.sum[wave][col] = st.sum;
+                lds.ref[wave][col] = ref;
+                lds.sum[wave][col] = sum;
             }
             __syncthreads();
             const int my_row = threadIdx.x >> 5, dim = (threadIdx.x & 31) * 4;
             constexpr float to_log2 = MOD ? kChunkLog2e : 1.0f;
-            float ref = kLowest, sum = 0.0f;
-            f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+            ref = kLowest, sum = 0.0f;
+            f4 out = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int w = 0; w < kRowWaves; ++w) ref = fmaxf(ref, lds.ref[w][my_row]);
 #pragma unroll
             for (int w = 0; w < kRowWaves; ++w) {
                 const float f = __builtin_amdgcn_exp2f((lds.ref[w][my_row] - ref) * to_log2);
                 sum = __builtin_fmaf(lds.sum[w][my_row], f, sum);
-                acc += *reinterpret_cast<const f4*>(&lds.state[w][my_row][dim]) * f;
+                out += *reinterpret_cast<const f4*>(&lds.state[w][my_row][dim]) * f;
             }
-            const auto finish = [&]() {
-                if (my_row < rows) {
-                    const int orow = row_first + my_row, otoken = orow / a.G, ohq = h * a.G + orow % a.G;
-                    const long long at = (sq.row0 + otoken) * a.Hq + ohq;
-                    const float inv = 1.0f / sum;
+            const long long first_share = (t0 + kRowStart) / share, last_share = (t0 + blk_units - 1) / share;
+            bool whole = first_share == last_share;
+            if (!whole) {
+                // split: slot 1 of the share where the block starts, slot 0 of the others
+                const auto slot = [&](long long sh) {
+                    return span(a.part + (sh * 2 + (sh == first_share ? 1 : 0)) * 16 * kChunkPart, 16 * kChunkPart * 4);
+                };
+                const int at = my_row * kChunkPart * 4;
+                {
+                    const auto to = slot(blockIdx.x);
+                    put_quad(to, at + dim * 4, 0, out);
+                    if (dim == 0) put_quad(to, at + kD * 4, 0, f4{ref, sum, 0.0f, 0.0f});
+                }
+                whole = split_last(a.arrive + first_share, (int)(last_share - first_share) + 1, &lds.last);
+                if (whole) {
+                    ref = kLowest, sum = 0.0f;
+                    out = f4{0.0f, 0.0f, 0.0f, 0.0f};
+                    for (long long sh = first_share; sh <= last_share; ++sh) ref = fmaxf(ref, get_quad(slot(sh), at + kD * 4, 0)[0]);
+                    for (long long sh = first_share; sh <= last_share; ++sh) {
+                        const auto from = slot(sh);
+                        const f4 m = get_quad(from, at + kD * 4, 0), part = get_quad(from, at + dim * 4, 0);
+                        const float f = __builtin_amdgcn_exp2f((m[0] - ref) * to_log2);
+                        sum = __builtin_fmaf(m[1], f, sum);
+                        out += part * f;
+                    }
+                }
+            }
+            if (whole && my_row < rows) {
+                const int orow = row_first + my_row, otoken = orow / a.G, ohq = h * a.G + orow % a.G;
+                const long long at = (sq.row0 + otoken) * a.Hq + ohq;
+                const float inv = 1.0f / sum;
+                h4 y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = (_Float16)(out[j] * inv);
+                *reinterpret_cast<h4*>(a.out + at * kD + dim) = y;
+                if (a.lse && dim == 0) a.lse[at] = MOD ? ref + __logf(sum) : (ref + __log2f(sum)) * kChunkLn2;
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// ---- many rows: a workgroup on 128 rows -------------------------------------------------
+// Four waves of 32 rows each go over the same tiles.  A tile is brought into LDS once, as fp16 operands (a block's
+// codes are converted on the way), one step ahead of its use: its loads are asked for before a step's products and
+// written behind them.  v_mfma_f32_32x32x16_f16: A lane l holds row l % 32, k 8 (l / 32) .. + 7, B the same with columns, C
+// lane l in register i row 8 (i / 4) + i % 4 + 4 (l / 32) of column l % 32.
+//
+// All (sequence, KV head, 128 rows) are laid end to end and cut into equal shares, one for each workgroup; shares that follow
+// each other run on one XCD, so that its L2 serves their tiles.
+constexpr int kTileRows = 128, kTileWaves = 4;
+constexpr int kTileShare = 16; // least units of a share
+constexpr int kTileStart = 4;  // a 128-row block's start, in tiles
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f16v mfma_32(h8 a, h8 b, f16v c)
+{
+    f16v d = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    asm("" : "+v"(d) : "v"(a), "v"(b));
+    return d;
+}
+
+// Units of a sequence's 128-row blocks up to block t: each counts about as many as it has tiles.  They grow with the rows'
+// positions until the window is full; between its ends a sum of that shape in closed form stands for them.
+struct TileUnits {
+    int blocks, full;        // 128-row blocks; from `full` on all have as many tiles
+    long long first, most;   // units of block 0, of those from `full` on
+    __device__ __forceinline__ long long upto(long long t) const
+    {
+        const long long g = t < full ? t : full;
+        return first * g + (most - first) * g * (g - 1) / (2 * (long long)max(full, 1)) + most * (t - g);
+    }
+};
+__device__ __forceinline__ TileUnits tile_units(const BlockAttnArgs& a, int n, int L)
+{
+    TileUnits u;
+    u.blocks = (n * a.G + kTileRows - 1) / kTileRows;
+    const int step = (kTileRows + a.G - 1) / a.G;  // tokens of a block, about
+    u.first = tiles_of(a, min(n, step), L).count() + kTileStart;
+    const int last = max(0, n - step);
+    const int late = a.window < L + last ? max(0, min(last, a.window - L)) : last;
+    u.full = late / step;
+    u.most = max((long long)tiles_of(a, min(n - late, step), L + late).count() + kTileStart, u.first);
+    return u;
+}
+
+struct TileLds {
+    uint8_t rows[2][kRowTileBytes];
+    uint32_t odd[2][2];
+    int last;
+};
+// A step's tile on its way: a block's codes (keys, values: 16 bytes each) or pieces of rows.
+struct TileLoad {
+    u4 x[4];
+};
+
+template <int FMT, bool MOD>
+__global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs a)
+{
+    __shared__ TileLds lds;
+    const int lane = lane_id(), wave = wave_index(), half = lane >> 5, col = lane & 31;
+    const auto loads = [&](int b, int& n, int& L) {
+        n = a.new_len[b];
+        L = seq_tokens(a, b);
+    };
+    const auto units = [&](int n, int L) {
+        if (n <= 0 || n * a.G <= a.few_rows) return 0LL;
+        const TileUnits u = tile_units(a, n, L);
+        return a.Hkv * u.upto(u.blocks);
+    };
+    const long long all = find_item(a.B, a.total_new, a.max_new, INT64_MAX, loads, units).items;
+    long long share = (all + gridDim.x - 1) / gridDim.x;
+    share = share < kTileShare ? kTileShare : share;
+    // (workgroup i runs on XCD i % 8)
+    const int me = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+    long long x = (long long)me * share;
+    const long long x_end = min(x + share, all);
+
+    while (x < x_end) {
+        const SeqItem sq = find_item(a.B, a.total_new, a.max_new, x, loads, units);
+        if (sq.b < 0) break;
+        const TileUnits tu = tile_units(a, sq.n, sq.L);
+        const long long head_units = tu.upto(tu.blocks);
+        int h = (int)((x - sq.item0) / head_units), blk;
+        {
+            const long long y = x - sq.item0 - h * head_units;
+            int lo = 0, hi = tu.blocks - 1;  // the last block that starts at y or before
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (tu.upto(mid) <= y) lo = mid;
+                else hi = mid - 1;
+            }
+            blk = lo;
+        }
+        for (; x < x_end && h < a.Hkv;) {
+            // the block's tiles, and this share's of them
+            const long long t0 = sq.item0 + h * head_units + tu.upto(blk), t1 = sq.item0 + h * head_units + tu.upto(blk + 1);
+            const int row_first = blk * kTileRows, rows = min(sq.n * a.G - row_first, kTileRows);
+            const int my_h = h, j0 = row_first / a.G, j1 = (row_first + rows - 1) / a.G;
+            const Tiles tl = tiles_of(a, j1 - j0 + 1, sq.L + j0);
+            const int steps = tl.count();
+            // (a block's units and its tiles differ: unit y of w stands for its first tiles up to y steps / w)
+            const auto step_at = [&](long long y) { return (int)((y - t0) * steps / (t1 - t0)); };
+            const int s0 = step_at(x), s1 = step_at(min(x_end, t1));
+            x = min(x_end, t1);
+            if (++blk == tu.blocks) blk = 0, ++h;
+            if (s1 <= s0) continue;
+
+            const int wrow = row_first + wave * 32, wrows = min(max(sq.n * a.G - wrow, 0), 32);  // the wave's
+            const int row = min(wrow + col, sq.n * a.G - 1), token = row / a.G, hq = my_h * a.G + row % a.G, p = sq.L + token;
+            const int p_lo = sq.L + wrow / a.G, p_hi = wrows ? sq.L + (wrow + wrows - 1) / a.G : -1;
+            h8 q[8];  // [2 s + rr], s = 2 i + w: dims (4 i + 2 rr + half) 16 + 8 w ..
+            {
+                const uint16_t* at = a.q + (sq.row0 + token) * a.q_stride + (long long)hq * kD;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    q[i] = *reinterpret_cast<const h8*>(at + ((i >> 2) * 4 + (i & 1) * 2 + half) * 16 + ((i >> 1) & 1) * 8);
+            }
+            ScoreForm form{0.0f, 0.0f, 0.0f};
+            if constexpr (MOD) form = ScoreForm{a.cap_in, a.cap, a.slopes ? a.slopes[hq] : 0.0f};
+            f16v acc[4];  // dims u 32 + 8 (i / 4) + 4 half + i % 4
+            float ref = kLowest, sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
+
+            const int coded = coded_steps(tl, sq.L);
+            const RowSource src = row_source(a, sq, my_h);
+            int list_base = s0;
+            StepList list = list_steps<MOD>(a, tl, sq.b, my_h, s0, 1, min(s1, coded));
+
+            // tile of step s: its loads, its way into LDS
+            const auto load = [&](int s) {
+                TileLoad t;
+                if (s < coded) {
+                    const int id = __builtin_amdgcn_readlane(list.id, s - list_base);
+                    if (id >= 0) {
+                        const auto from = span(a.pool + ((long long)id * a.Hkv + my_h) * kBlockBytes, kBlockBytes);
+                        t.x[0] = fetch<16>(from, threadIdx.x * 16, 0);
+                        t.x[1] = fetch<16>(from, threadIdx.x * 16, kBlockSide);
+                    }
+                } else {
+                    const int pos0 = tl.at(s) * kBT;
+                    if (wave < 2) {  // values: piece (r, four dims)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const u2 y = value_piece(src, pos0, threadIdx.x, e);
+                            t.x[e >> 1][(e & 1) * 2] = y[0];
+                            t.x[e >> 1][(e & 1) * 2 + 1] = y[1];
+                        }
+                    } else {  // keys: four pieces (token, eight dims)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) t.x[i] = key_piece(src, pos0, i * 128 + threadIdx.x - 128);
+                    }
+                }
+                return t;
+            };
+            const auto store = [&](int s, TileLoad t, int buf) {
+                uint8_t* to = lds.rows[buf];
+                if (s < coded) {
+                    const int piece = threadIdx.x, c = (piece >> 4) & 7;
+                    uint8_t* k = to + (piece >> 7) * 4096 + (c >> 2) * 2048 + (c & 3) * 256 + (piece & 15) * 16;
+                    *reinterpret_cast<h8*>(k) = codes8<FMT>(t.x[0][0], t.x[0][1]);
+                    *reinterpret_cast<h8*>(k + 1024) = codes8<FMT>(t.x[0][2], t.x[0][3]);
+                    uint8_t* v = to + 8192 + (piece >> 6) * 2048 + ((piece >> 4) & 3) * 256 + (piece & 15) * 16;
+                    *reinterpret_cast<h8*>(v) = codes8<FMT>(t.x[1][0], t.x[1][1]);
+                    *reinterpret_cast<h8*>(v + 1024) = codes8<FMT>(t.x[1][2], t.x[1][3]);
+                } else if (wave < 2) {
+                    u2 y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = u2{t.x[e >> 1][(e & 1) * 2], t.x[e >> 1][(e & 1) * 2 + 1]};
+                    const uint32_t odd = put_value(y, to, threadIdx.x);
+                    if (lane == 0) lds.odd[buf][wave] = odd;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) put_key(t.x[i], to, i * 128 + threadIdx.x - 128);
+                }
+            };
+            const auto there = [&](int s) { return s >= coded || ((list.there >> (s - list_base)) & 1); };
+
+            if (there(s0)) store(s0, load(s0), 0);
+            __syncthreads();
+            for (int s = s0; s < s1; ++s) {
+                const int buf = (s - s0) & 1;
+                const bool now = there(s);
+                TileScale ts{a.scale_x, 0.0f, 1.0f};
+                if (s < coded) ts = scale_of(list, s - list_base);
+                const bool more = s + 1 < s1;
+                if (more && s + 1 < coded && s + 1 - list_base == kWave) {
+                    list_base = s + 1;
+                    list = list_steps<MOD>(a, tl, sq.b, my_h, s + 1, 1, min(s1, coded));
+                }
+                const bool ahead = more && there(s + 1);
+                TileLoad next;
+                if (ahead) next = load(s + 1);
+                TileView view{tl.at(s) * kBT, s < coded ? INT32_MAX : src.end, false};
+                if (now && !none_seen(a, view.pos0, p_lo, p_hi)) {
+                    view.whole = all_seen(a, view.pos0, p_lo, p_hi);
+                    const uint8_t* tile = lds.rows[buf];
+                    f16v sc;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sc[j] = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        sc = mfma_32(*reinterpret_cast<const h8*>(tile + (col >> 4) * 4096 + (i >> 1) * 1024 + ((i & 1) * 2 + half) * 256 + (col & 15) * 16),
+                                     q[i], sc);
+                    float y[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) y[j] = sc[j];
+                    weights<MOD>(a, ts, view, y, p, form, acc, ref, sum);
+                    const Parts w[2] = {parts(y[0], y[1], y[2], y[3], y[8], y[9], y[10], y[11]),
+                                        parts(y[4], y[5], y[6], y[7], y[12], y[13], y[14], y[15])};
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const h8 v = *reinterpret_cast<const h8*>(tile + 8192 + u * 2048 + (col >> 4) * 1024 + (2 * k + half) * 256 + (col & 15) * 16);
+                            acc[u] = mfma_32(v, w[k].hi, acc[u]);
+                            acc[u] = mfma_32(v, w[k].lo, acc[u]);
+                        }
+                    if (s >= coded) {
+                        // values that are not finite, to the rows that see their token
+                        for (uint32_t odd = __builtin_amdgcn_readfirstlane(lds.odd[buf][0] | lds.odd[buf][1]); odd; odd &= odd - 1) {
+                            const int tok = __builtin_ctz(odd), c = view.pos0 + tok;
+                            const int at = ((tok >> 2) & 1) * 32 + col, reg = (tok >> 3) * 4 + (tok & 3);
+                            float wt = 0.0f;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) wt = j == reg ? y[j] : wt;
+                            wt = __shfl(wt, at);
+                            const bool seen = c <= p && (p - c < a.window || c < a.sinks);
+                            const uint16_t* vr = row_of(src, 1, c);
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) {
+                                    const float v1 = h2f(vr[u * 32 + 8 * (j >> 2) + 4 * half + (j & 3)]);
+                                    if (seen && !(fabsf(v1) < INFINITY)) acc[u][j] = __builtin_fmaf(wt, v1, acc[u][j]);
+                                }
+                        }
+                    }
+                }
+                if (ahead) store(s + 1, next, buf ^ 1);
+                __syncthreads();
+            }
+
+            sum = pairs_sum(sum);
+            constexpr float to_log2 = MOD ? kChunkLog2e : 1.0f;
+            // the first and last share that has a tile of this block
+            const auto share_of = [&](int s) {  // of step s: that of the first unit behind it
+                const long long w = t1 - t0;
+                // the least unit y with (y + 1) steps / w > s
+                const long long y = ((long long)(s + 1) * w + steps - 1) / steps - 1;
+                return (int)((t0 + y) / share);
+            };
+            const int first_share = share_of(0), last_share = share_of(steps - 1);
+            // (where a share has less units than a tile stands for, it may have no tile)
+            const auto has = [&](int sh) {
+                return share * steps >= t1 - t0 || step_at(min((sh + 1) * share, t1)) > step_at(max(sh * share, t0));
+            };
+            bool whole = first_share == last_share;
+            if (!whole) {
+                int pieces = last_share - first_share + 1;
+                if (share * steps < t1 - t0) {
+                    pieces = 0;
+                    for (int sh = first_share; sh <= last_share; ++sh) pieces += has(sh) ? 1 : 0;
+                }
+                const auto slot = [&](int sh) {
+                    return span(a.tile_part + (long long)(sh * 2 + (sh == first_share ? 1 : 0)) * kTilePart + wave * (kTilePart / kTileWaves), kTilePart / kTileWaves * 4);
+                };
+                {
+                    const auto to = slot(me);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        put_quad(to, lane * 16, i * 1024, f4{acc[i >> 2][(i & 3) * 4], acc[i >> 2][(i & 3) * 4 + 1], acc[i >> 2][(i & 3) * 4 + 2], acc[i >> 2][(i & 3) * 4 + 3]});
+                    put_quad(to, lane * 16, 16 * 1024, f4{ref, sum, 0.0f, 0.0f});
+                }
+                whole = split_last(a.tile_arrive + first_share, pieces, &lds.last);
+                if (whole) {
+                    float top = kLowest;
+                    for (int sh = first_share; sh <= last_share; ++sh)
+                        if (has(sh)) top = fmaxf(top, get_quad(slot(sh), lane * 16, 16 * 1024)[0]);
+                    ref = top, sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
+                    for (int sh = first_share; sh <= last_share; ++sh) {
+                        if (!has(sh)) continue;
+                        const auto from_slot = slot(sh);
+                        const f4 m = get_quad(from_slot, lane * 16, 16 * 1024);
+                        const float f = __builtin_amdgcn_exp2f((m[0] - ref) * to_log2);
+                        sum = __builtin_fmaf(m[1], f, sum);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const f4 part = get_quad(from_slot, lane * 16, i * 1024);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) acc[i >> 2][(i & 3) * 4 + j] = __builtin_fmaf(part[j], f, acc[i >> 2][(i & 3) * 4 + j]);
+                        }
+                    }
+                }
+            }
+            if (whole && col < wrows) {
+                const long long at = (sq.row0 + token) * a.Hq + hq;
+                const float inv = 1.0f / sum;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
                     h4 y;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) y[j] = (_Float16)(acc[j] * inv);
-                    *reinterpret_cast<h4*>(a.out + at * kD + dim) = y;
-                    if (a.lse && dim == 0) a.lse[at] = MOD ? ref + __logf(sum) : (ref + __log2f(sum)) * kChunkLn2;
+                    for (int j = 0; j < 4; ++j) y[j] = (_Float16)(acc[i >> 2][(i & 3) * 4 + j] * inv);
+                    *reinterpret_cast<h4*>(a.out + at * kD + (i >> 2) * 32 + (i & 3) * 8 + 4 * half) = y;
                 }
-            };
-            const long long first_share = (t0 + kRowStart) / share, last_share = (t0 + blk_units - 1) / share;
-            if (first_share == last_share) {
-                finish();
-                __syncthreads();
-                continue;
-            }
-            // split: slot 1 of the share where the block starts, slot 0 of the others
-            const auto slot = [&](long long sh) {
-                return span(a.part + (sh * 2 + (sh == first_share ? 1 : 0)) * 16 * kChunkPart, 16 * kChunkPart * 4);
-            };
-            {
-                const auto to = slot(blockIdx.x);
-                put_quad(to, (my_row * kChunkPart + dim) * 4, 0, acc);
-                if (dim == 0) put_quad(to, (my_row * kChunkPart + kD) * 4, 0, f4{ref, sum, 0.0f, 0.0f});
-            }
-            if (split_last(a.arrive + first_share, (int)(last_share - first_share) + 1, &lds.last)) {
-                ref = kLowest;
-                for (long long sh = first_share; sh <= last_share; ++sh)
-                    ref = fmaxf(ref, get_quad(slot(sh), (my_row * kChunkPart + kD) * 4, 0)[0]);
-                sum = 0.0f;
-                acc = f4{0.0f, 0.0f, 0.0f, 0.0f};
-                for (long long sh = first_share; sh <= last_share; ++sh) {
-                    const auto from = slot(sh);
-                    const f4 m = get_quad(from, (my_row * kChunkPart + kD) * 4, 0), part = get_quad(from, (my_row * kChunkPart + dim) * 4, 0);
-                    const float f = __builtin_amdgcn_exp2f((m[0] - ref) * to_log2);
-                    sum = __builtin_fmaf(m[1], f, sum);
-                    acc += part * f;
-                }
-                finish();
+                if (a.lse && half == 0) a.lse[at] = MOD ? ref + __logf(sum) : (ref + __log2f(sum)) * kChunkLn2;
             }
             __syncthreads();
         }
@@ -414,10 +813,15 @@ __global__ __launch_bounds__(64 * kRowWaves, 4) void block_rows(BlockAttnArgs a)
 
 }  // namespace
 
-hipError_t launch_block_attention(const BlockAttnArgs& args, int format, bool mod, hipStream_t st)
+hipError_t launch_block_attention(const BlockAttnArgs& a, int format, bool mod, hipStream_t st)
 {
-    BlockAttnArgs a = args;
-    a.shares = kBlockRowShares;
+    // (sequences of many rows there are none, or no others)
+    if ((long long)a.max_new * a.G > a.few_rows) {
+        void (*kernel)(BlockAttnArgs) = format == kE4m3 ? (mod ? block_tiles<kE4m3, true> : block_tiles<kE4m3, false>)
+                                                        : (mod ? block_tiles<kInt8, true> : block_tiles<kInt8, false>);
+        const hipError_t e = launch1(kernel, kBlockTileShares, 64 * kTileWaves, st, a);
+        if (e != hipSuccess || a.B == 1) return e;
+    }
     void (*kernel)(BlockAttnArgs) = format == kE4m3 ? (mod ? block_rows<kE4m3, true> : block_rows<kE4m3, false>)
                                                     : (mod ? block_rows<kInt8, true> : block_rows<kInt8, false>);
     return launch1(kernel, kBlockRowShares, 64 * kRowWaves, st, a);

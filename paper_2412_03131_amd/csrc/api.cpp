@@ -769,6 +769,7 @@ diffkv_status diffkv_block_attention(const diffkv_layout* layout, const diffkv_b
     if (!new_len || !rows_valid(q, q_stride, num_q_heads, total_new) || !rows_valid(k, k_stride, a.Hkv, total_new) ||
         !rows_valid(v, v_stride, a.Hkv, total_new))
         return DIFFKV_E_INVAL;
+    if (k_stride > kMaxStride || v_stride > kMaxStride) return DIFFKV_E_UNSUPPORTED;
     if (!out || (uintptr_t)out % 16 != 0) return DIFFKV_E_INVAL;
     if (!ws || (int64_t)ws_bytes < block_attention_ws(num_q_heads / a.Hkv, total_new)) return DIFFKV_E_WORKSPACE;
     if ((uintptr_t)ws % 16 != 0) return DIFFKV_E_INVAL;

@@ -97,6 +97,11 @@ __device__ __forceinline__ uint32_t put_value(u2 (&x)[8], uint8_t* lds, int piec
     }
     return odd;
 }
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b)  // of two unsigned halves each
+{
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
+}
 __device__ __forceinline__ u4 key_piece(const RowSource& s, int pos0, int piece)
 {
     const int pos = pos0 + (piece >> 4);
@@ -139,34 +144,39 @@ __device__ __forceinline__ float pairs_sum(float v)
     return __uint_as_float(x[0]) + __uint_as_float(x[1]);
 }
 
-// N scores of a lane (8: tiles of 16 rows, token (i / 4) 16 + 4 r + i % 4; 16: tiles of 32, token 8 (i / 4) + 4 half +
-// i % 4) become weights; acc are the row's sums of values, raised with its reference.
+// N products of a lane (8: tiles of 16 rows, token (i / 4) 16 + 4 r + i % 4; 16: tiles of 32, token 8 (i / 4) + 4 half +
+// i % 4) become weights; acc are the row's sums of values, raised with its reference.  Hidden tokens' products become -inf
+// at once, so that all tiles go one way from there.
 template <bool MOD, int N, typename Acc, int A>
-__device__ __forceinline__ void weights(const BlockAttnArgs& a, const TileScale& t, const TileView& w, float (&y)[N], int p,
+__device__ __forceinline__ void weights(const BlockAttnArgs& a, TileScale t, const TileView& w, float (&y)[N], int p,
                                         const ScoreForm& form, Acc (&acc)[A], float& ref, float& sum)
 {
     constexpr float unit = MOD ? kChunkLn2 : 1.0f;
     const int group = N == 8 ? lane_id() >> 4 : lane_id() >> 5;
-    float top = -INFINITY;
-    if (MOD || !w.whole) {
+    if (__builtin_isnan(t.ks + t.add)) {  // (uniform: a block that reads NaN, to the rows that see one of its tokens)
+        t.ks = 1.0f, t.add = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = __builtin_nanf("");
+    }
+    if constexpr (MOD) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = w.pos0 + (i >> 2) * (N == 8 ? 16 : 8) + 4 * group + (i & 3);
-            if constexpr (MOD) y[i] = formed(y[i] * t.ks, form, (float)(p - c)) + t.add;
-            else y[i] = __builtin_fmaf(y[i], t.ks, t.add);
-            if (!w.whole) {
-                const bool seen = c <= p && c < w.end && (p - c < a.window || c < a.sinks);
-                y[i] = seen ? y[i] : -INFINITY;
-            }
-            top = fmaxf(top, y[i]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            y[i] = __builtin_fmaf(y[i], t.ks, t.add);
-            top = fmaxf(top, y[i]);
+            y[i] = formed(y[i] * t.ks, form, (float)(p - c));
         }
     }
+    if (!w.whole) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = w.pos0 + (i >> 2) * (N == 8 ? 16 : 8) + 4 * group + (i & 3);
+            const bool seen = c <= p && c < w.end && (p - c < a.window || c < a.sinks);
+            y[i] = seen ? y[i] : -INFINITY;
+        }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) top = max3(top, y[i], y[i + 1]);
+    top = MOD ? top + t.add : __builtin_fmaf(top, t.ks, t.add);
     if (__any(top > ref + kRefRoom * unit)) {
         const float now = N == 8 ? rows_max(top) : pairs_max(top);
         const float up = now > ref + kRefRoom * unit ? now - kRefBelow * unit : ref;
@@ -176,12 +186,12 @@ __device__ __forceinline__ void weights(const BlockAttnArgs& a, const TileScale&
 #pragma unroll
         for (int i = 0; i < A; ++i) acc[i] *= f;
     }
-    float total = 0.0f;
+    const float less = t.add - ref;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        y[i] = __builtin_amdgcn_exp2f(MOD ? (y[i] - ref) * kChunkLog2e : y[i] - ref);
-        total += y[i];
-    }
+    for (int i = 0; i < N; ++i) y[i] = __builtin_amdgcn_exp2f(MOD ? (y[i] + less) * kChunkLog2e : __builtin_fmaf(y[i], t.ks, less));
+    float total = y[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) total += y[i];
     sum = __builtin_fmaf(total, t.rs, sum);
 }
 // Eight weights as two fp16 parts.
@@ -191,12 +201,17 @@ struct Parts {
 __device__ __forceinline__ Parts parts(float a, float b, float c, float d, float e, float f, float g, float h)
 {
     const float u[8] = {a, b, c, d, e, f, g, h};
-    Parts r;
+    u4 hi, lo;
+    float minus = -1.0f;  // (hidden: a product that takes the half as it is, where a subtraction would convert it first)
+    asm("" : "+s"(minus));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r.hi[i] = (_Float16)u[i];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.lo[i] = (_Float16)__builtin_fmaf((float)r.hi[i], -1.0f, u[i]);
-    return r;
+    for (int i = 0; i < 4; ++i) {
+        const h2 top = {(_Float16)u[2 * i], (_Float16)u[2 * i + 1]};
+        hi[i] = __builtin_bit_cast(uint32_t, top);
+        const h2 rest = {(_Float16)__builtin_fmaf((float)top.x, minus, u[2 * i]), (_Float16)__builtin_fmaf((float)top.y, minus, u[2 * i + 1])};
+        lo[i] = __builtin_bit_cast(uint32_t, rest);
+    }
+    return Parts{__builtin_bit_cast(h8, hi), __builtin_bit_cast(h8, lo)};
 }
 
 // Block IDs and scales of 64 steps of a wave, a lane each (step = first + lane * stride < end); those whose block is there.
@@ -221,7 +236,7 @@ __device__ __forceinline__ StepList list_steps(const BlockAttnArgs& a, const Til
     vs *= kCodeUnit;
     s.scale.ks = ks * kCodeUnit * a.scale_x;
     s.scale.add = __builtin_amdgcn_logf(vs) * (MOD ? kChunkLn2 : 1.0f);
-    s.scale.rs = vs > 0.0f && vs < INFINITY ? 1.0f / vs : 1.0f;  // (a NaN scale: rows that see nothing of the block keep their sums)
+    s.scale.rs = vs > 0.0f && vs < INFINITY ? 1.0f / vs : 1.0f;  // (a NaN scale: see weights)
     return s;
 }
 __device__ __forceinline__ TileScale scale_of(const StepList& s, int i)
@@ -540,14 +555,9 @@ __device__ __forceinline__ TileUnits tile_units(const BlockAttnArgs& a, int n, i
 
 struct TileLds {
     uint8_t rows[2][kRowTileBytes];
-    uint32_t odd[2][2];
+    uint32_t odd[2][kTileWaves];
     int last;
 };
-// A step's tile on its way: a block's codes (keys, values: 16 bytes each) or pieces of rows.
-struct TileLoad {
-    u4 x[4];
-};
-
 template <int FMT, bool MOD>
 __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs a)
 {
@@ -620,102 +630,147 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
                 for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
 
             const int coded = coded_steps(tl, sq.L);
-            const RowSource src = row_source(a, sq, my_h);
-            int list_base = s0;
-            StepList list = list_steps<MOD>(a, tl, sq.b, my_h, s0, 1, min(s1, coded));
+            // A tile in LDS: scores, weights, values.  (Its operands are asked for together: the scheduler would
+            // wait for each by itself.)
+            const uint32_t at_k = (col >> 4) * 4096 + half * 256 + (col & 15) * 16, at_v = 8192 + (col >> 4) * 1024 + half * 256 + (col & 15) * 16;
+            float y[16];
+            const auto tile_step = [&](const uint8_t* tile, const TileScale& ts, const TileView& view) {
+                h8 x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const h8*>(tile + at_k + (i >> 1) * 1024 + (i & 1) * 512);
+                __builtin_amdgcn_sched_barrier(0);
+                f16v sc;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sc[j] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sc = mfma_32(x[i], q[i], sc);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const h8*>(tile + at_v + (i >> 1) * 2048 + (i & 1) * 512);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) y[j] = sc[j];
+                weights<MOD>(a, ts, view, y, p, form, acc, ref, sum);
+                const Parts w[2] = {parts(y[0], y[1], y[2], y[3], y[8], y[9], y[10], y[11]),
+                                    parts(y[4], y[5], y[6], y[7], y[12], y[13], y[14], y[15])};
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) acc[u] = mfma_32(x[2 * u + k], w[k].hi, acc[u]);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) acc[u] = mfma_32(x[2 * u + k], w[k].lo, acc[u]);
+                }
+            };
 
-            // tile of step s: its loads, its way into LDS
-            const auto load = [&](int s) {
-                TileLoad t;
-                if (s < coded) {
-                    const int id = __builtin_amdgcn_readlane(list.id, s - list_base);
-                    if (id >= 0) {
-                        const auto from = span(a.pool + ((long long)id * a.Hkv + my_h) * kBlockBytes, kBlockBytes);
-                        t.x[0] = fetch<16>(from, threadIdx.x * 16, 0);
-                        t.x[1] = fetch<16>(from, threadIdx.x * 16, kBlockSide);
+            // the cache's blocks: a block's loads are asked for a step before it is written to LDS, and that a step before its use
+            const int c1 = min(s1, coded);
+            for (int base = s0; base < c1; base += kWave) {
+                const StepList list = list_steps<MOD>(a, tl, sq.b, my_h, base, 1, c1);
+                unsigned long long todo = list.there, loaded = todo;
+                if (!todo) continue;
+                u4 raw_k, raw_v;
+                const auto load = [&]() {
+                    if (!loaded) return;
+                    const int id = __builtin_amdgcn_readlane(list.id, __builtin_ctzll(loaded));
+                    loaded &= loaded - 1;
+                    const auto from = span(a.pool + ((long long)id * a.Hkv + my_h) * kBlockBytes, kBlockBytes);
+                    raw_k = fetch<16>(from, threadIdx.x * 16, 0);
+                    raw_v = fetch<16>(from, threadIdx.x * 16, kBlockSide);
+                };
+                const auto store = [&](int buf) {
+                    const int piece = threadIdx.x, c = (piece >> 4) & 7;
+                    uint8_t* k = lds.rows[buf] + (piece >> 7) * 4096 + (c >> 2) * 2048 + (c & 3) * 256 + (piece & 15) * 16;
+                    *reinterpret_cast<h8*>(k) = codes8<FMT>(raw_k[0], raw_k[1]);
+                    *reinterpret_cast<h8*>(k + 1024) = codes8<FMT>(raw_k[2], raw_k[3]);
+                    uint8_t* v = lds.rows[buf] + 8192 + (piece >> 6) * 2048 + ((piece >> 4) & 3) * 256 + (piece & 15) * 16;
+                    *reinterpret_cast<h8*>(v) = codes8<FMT>(raw_v[0], raw_v[1]);
+                    *reinterpret_cast<h8*>(v + 1024) = codes8<FMT>(raw_v[2], raw_v[3]);
+                };
+                load();
+                store(0);
+                load();
+                __syncthreads();
+                for (int buf = 0; todo; buf ^= 1) {
+                    const int i = __builtin_ctzll(todo);
+                    todo &= todo - 1;
+                    if (todo) store(buf ^ 1);
+                    load();
+                    TileView view{tl.at(base + i) * kBT, INT32_MAX, false};
+                    if (!none_seen(a, view.pos0, p_lo, p_hi)) {
+                        view.whole = all_seen(a, view.pos0, p_lo, p_hi);
+                        tile_step(lds.rows[buf], scale_of(list, i), view);
                     }
-                } else {
+                    __syncthreads();
+                }
+            }
+
+            // rows in fp16
+            if (max(s0, coded) < s1) {
+                const RowSource src = row_source(a, sq, my_h);
+                // keys: two pieces (token, eight dims) of a thread; values: r = the wave, two dims of a lane
+                u4 kx[2];
+                uint32_t vx[8];
+                const int k_lane = (threadIdx.x >> 4) * (int)a.k_stride * 2 + (threadIdx.x & 15) * 16;
+                const auto load = [&](int s) {
                     const int pos0 = tl.at(s) * kBT;
-                    if (wave < 2) {  // values: piece (r, four dims)
+                    if (pos0 >= src.L) {  // the call's own rows alone: rows behind the last lie outside the span and read zero
+                        const int n = min(src.end - pos0, kBT);
+                        const auto kr = span(src.own[0] + (long long)(pos0 - src.L) * a.k_stride, (uint32_t)((n - 1) * (int)a.k_stride * 2 + kD * 2));
+                        const auto vr = span(src.own[1] + (long long)(pos0 - src.L) * a.v_stride, (uint32_t)((n - 1) * (int)a.v_stride * 2 + kD * 2));
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) kx[i] = fetch<16>(kr, k_lane, i * 16 * (int)a.k_stride * 2);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) vx[e] = fetch<4>(vr, lane * 4, ((e >> 2) * 16 + 4 * wave + (e & 3)) * (int)a.v_stride * 2);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) kx[i] = key_piece(src, pos0, i * 256 + threadIdx.x);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            const u2 y = value_piece(src, pos0, threadIdx.x, e);
-                            t.x[e >> 1][(e & 1) * 2] = y[0];
-                            t.x[e >> 1][(e & 1) * 2 + 1] = y[1];
+                            const int pos = pos0 + (e >> 2) * 16 + 4 * wave + (e & 3);
+                            vx[e] = pos < src.end ? *reinterpret_cast<const uint32_t*>(row_of(src, 1, pos) + lane * 2) : 0u;
                         }
-                    } else {  // keys: four pieces (token, eight dims)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) t.x[i] = key_piece(src, pos0, i * 128 + threadIdx.x - 128);
                     }
-                }
-                return t;
-            };
-            const auto store = [&](int s, TileLoad t, int buf) {
-                uint8_t* to = lds.rows[buf];
-                if (s < coded) {
-                    const int piece = threadIdx.x, c = (piece >> 4) & 7;
-                    uint8_t* k = to + (piece >> 7) * 4096 + (c >> 2) * 2048 + (c & 3) * 256 + (piece & 15) * 16;
-                    *reinterpret_cast<h8*>(k) = codes8<FMT>(t.x[0][0], t.x[0][1]);
-                    *reinterpret_cast<h8*>(k + 1024) = codes8<FMT>(t.x[0][2], t.x[0][3]);
-                    uint8_t* v = to + 8192 + (piece >> 6) * 2048 + ((piece >> 4) & 3) * 256 + (piece & 15) * 16;
-                    *reinterpret_cast<h8*>(v) = codes8<FMT>(t.x[1][0], t.x[1][1]);
-                    *reinterpret_cast<h8*>(v + 1024) = codes8<FMT>(t.x[1][2], t.x[1][3]);
-                } else if (wave < 2) {
-                    u2 y[8];
+                };
+                const auto store = [&](int buf) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = u2{t.x[e >> 1][(e & 1) * 2], t.x[e >> 1][(e & 1) * 2 + 1]};
-                    const uint32_t odd = put_value(y, to, threadIdx.x);
-                    if (lane == 0) lds.odd[buf][wave] = odd;
-                } else {
+                    for (int i = 0; i < 2; ++i) put_key(kx[i], lds.rows[buf], i * 256 + threadIdx.x);
+                    uint32_t top = 0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) put_key(t.x[i], to, i * 128 + threadIdx.x - 128);
-                }
-            };
-            const auto there = [&](int s) { return s >= coded || ((list.there >> (s - list_base)) & 1); };
-
-            if (there(s0)) store(s0, load(s0), 0);
-            __syncthreads();
-            for (int s = s0; s < s1; ++s) {
-                const int buf = (s - s0) & 1;
-                const bool now = there(s);
-                TileScale ts{a.scale_x, 0.0f, 1.0f};
-                if (s < coded) ts = scale_of(list, s - list_base);
-                const bool more = s + 1 < s1;
-                if (more && s + 1 < coded && s + 1 - list_base == kWave) {
-                    list_base = s + 1;
-                    list = list_steps<MOD>(a, tl, sq.b, my_h, s + 1, 1, min(s1, coded));
-                }
-                const bool ahead = more && there(s + 1);
-                TileLoad next;
-                if (ahead) next = load(s + 1);
-                TileView view{tl.at(s) * kBT, s < coded ? INT32_MAX : src.end, false};
-                if (now && !none_seen(a, view.pos0, p_lo, p_hi)) {
-                    view.whole = all_seen(a, view.pos0, p_lo, p_hi);
-                    const uint8_t* tile = lds.rows[buf];
-                    f16v sc;
+                    for (int e = 0; e < 8; ++e) top = pk_max(top, vx[e] & 0x7fff7fffu);
+                    uint32_t odd = 0;
+                    if (__any((top & 0xffffu) >= 0x7c00u || top >= 0x7c000000u)) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) sc[j] = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        sc = mfma_32(*reinterpret_cast<const h8*>(tile + (col >> 4) * 4096 + (i >> 1) * 1024 + ((i & 1) * 2 + half) * 256 + (col & 15) * 16),
-                                     q[i], sc);
-                    float y[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) y[j] = sc[j];
-                    weights<MOD>(a, ts, view, y, p, form, acc, ref, sum);
-                    const Parts w[2] = {parts(y[0], y[1], y[2], y[3], y[8], y[9], y[10], y[11]),
-                                        parts(y[4], y[5], y[6], y[7], y[12], y[13], y[14], y[15])};
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const h8 v = *reinterpret_cast<const h8*>(tile + 8192 + u * 2048 + (col >> 4) * 1024 + (2 * k + half) * 256 + (col & 15) * 16);
-                            acc[u] = mfma_32(v, w[k].hi, acc[u]);
-                            acc[u] = mfma_32(v, w[k].lo, acc[u]);
+                        for (int e = 0; e < 8; ++e) {
+                            const bool bad = (vx[e] & 0x7c00u) == 0x7c00u || (vx[e] & 0x7c000000u) == 0x7c000000u;
+                            if (__any(bad)) odd |= 1u << ((e >> 2) * 16 + 4 * wave + (e & 3));
+                            if ((vx[e] & 0x7c00u) == 0x7c00u) vx[e] &= 0xffff0000u;
+                            if ((vx[e] & 0x7c000000u) == 0x7c000000u) vx[e] &= 0xffffu;
                         }
-                    if (s >= coded) {
+                    }
+                    if (lane == 0) lds.odd[buf][wave] = odd;
+                    uint8_t* to = lds.rows[buf] + 8192 + (lane >> 4) * 2048 + ((lane >> 3) & 1) * 1024 + wave * 256 + (lane & 7) * 32;
+                    u4 y[2];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        y[0][e] = __builtin_amdgcn_perm(vx[2 * e + 1], vx[2 * e], 0x05040100u);
+                        y[1][e] = __builtin_amdgcn_perm(vx[2 * e + 1], vx[2 * e], 0x07060302u);
+                    }
+                    *reinterpret_cast<u4*>(to) = y[0];
+                    *reinterpret_cast<u4*>(to + 16) = y[1];
+                };
+                load(max(s0, coded));
+                store(0);
+                if (max(s0, coded) + 1 < s1) load(max(s0, coded) + 1);
+                __syncthreads();
+                int buf = 0;
+                for (int s = max(s0, coded); s < s1; ++s, buf ^= 1) {
+                    if (s + 1 < s1) store(buf ^ 1);
+                    if (s + 2 < s1) load(s + 2);
+                    TileView view{tl.at(s) * kBT, src.end, false};
+                    if (!none_seen(a, view.pos0, p_lo, p_hi)) {
+                        view.whole = all_seen(a, view.pos0, p_lo, p_hi);
+                        tile_step(lds.rows[buf], TileScale{a.scale_x, 0.0f, 1.0f}, view);
                         // values that are not finite, to the rows that see their token
-                        for (uint32_t odd = __builtin_amdgcn_readfirstlane(lds.odd[buf][0] | lds.odd[buf][1]); odd; odd &= odd - 1) {
+                        for (uint32_t odd = __builtin_amdgcn_readfirstlane(lds.odd[buf][0] | lds.odd[buf][1] | lds.odd[buf][2] | lds.odd[buf][3]); odd; odd &= odd - 1) {
                             const int tok = __builtin_ctz(odd), c = view.pos0 + tok;
                             const int at = ((tok >> 2) & 1) * 32 + col, reg = (tok >> 3) * 4 + (tok & 3);
                             float wt = 0.0f;
@@ -733,9 +788,8 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
                                 }
                         }
                     }
+                    __syncthreads();
                 }
-                if (ahead) store(s + 1, next, buf ^ 1);
-                __syncthreads();
             }
 
             sum = pairs_sum(sum);

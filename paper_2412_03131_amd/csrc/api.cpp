@@ -799,7 +799,7 @@ diffkv_status diffkv_block_attention(const diffkv_layout* layout, const diffkv_b
     a.part = reinterpret_cast<float*>(a.arrive + kBlockRowShares);
     a.tile_arrive = reinterpret_cast<unsigned long long*>(static_cast<uint8_t*>(ws) + kBlockRowBytes);
     a.tile_part = reinterpret_cast<float*>(a.tile_arrive + kBlockTileShares);
-    a.few_rows = kBlockFewRows;
+    a.few_rows = block_few_rows(num_q_heads, total_new);
     hipError_t e = launch_block_attention(a, cache->format, mod, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DIFFKV_OK : DIFFKV_E_LAUNCH;
 }

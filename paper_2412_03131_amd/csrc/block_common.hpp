@@ -70,6 +70,12 @@ __device__ __forceinline__ const uint16_t* tail_rows(const BlockCacheArgs& c, in
     return c.tail + ((long long)b * c.Hkv + h) * (2 * kBlockSide);
 }
 
+// One number of a state with agent scope, as get_quad.
+__device__ __forceinline__ float get_one(__amdgpu_buffer_rsrc_t r, int lane_offset, int offset)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, lane_offset, offset, 16));
+}
+
 // ---- the item of a wave ----------------------------------------------------------------
 // Sequences in order, each with a number of items; a wave goes over them 64 at a time (a lane a
 // sequence) and finds the one that holds a given item.  Loads(b, n, L) gives a sequence's rows and tokens, unclamped;
@@ -114,5 +120,61 @@ __device__ __forceinline__ SeqItem find_item(int B, long long total, int most, l
     s.items = item;
     return s;
 }
+
+// The same with the lanes' 64 sequences kept from one search to the next: a call of up to 64 reads their lengths once.
+template <typename Args>
+struct SeqScan {
+    const Args& a;
+    int base = -1, n, L;             // the lanes' sequences: base + lane; rows and tokens
+    long long before, incl, items;   // rows before the lane's sequence; items up to its end; its items
+    long long row_end, item_end;     // behind the 64
+
+    __device__ __forceinline__ explicit SeqScan(const Args& args) : a(args) {}
+    template <typename Items>
+    __device__ __forceinline__ void load(int from, long long row, long long item, Items count)
+    {
+        base = from;
+        const int b = base + lane_id();
+        n = L = 0;
+        if (b < a.B) {
+            n = a.new_len[b];
+            L = seq_tokens(a, b);
+        }
+        n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
+        before = row + (wave_incl_scan_wide(n) - n);
+        const long long room = a.total_new - before;
+        if (n > room) n = room > 0 ? (int)room : 0;
+        items = count(n, L);
+        incl = item + wave_incl_scan_wide(items);
+        row_end = read_lane<long long>(before + n, kWave - 1);
+        item_end = read_lane<long long>(incl, kWave - 1);
+    }
+    template <typename Items>
+    __device__ __forceinline__ long long total(Items count)
+    {
+        load(0, 0, 0, count);
+        while (base + kWave < a.B) load(base + kWave, row_end, item_end, count);
+        return item_end;
+    }
+    // The sequence that holds item `want`; b < 0: there is none.  Calls go forward from one to the next.
+    template <typename Items>
+    __device__ __forceinline__ SeqItem find(long long want, Items count)
+    {
+        const long long first = read_lane<long long>(incl - items, 0);
+        if (want < first) load(0, 0, 0, count);
+        while (want >= item_end && base + kWave < a.B) load(base + kWave, row_end, item_end, count);
+        SeqItem s{-1, 0, 0, 0, 0, false, 0};
+        const unsigned long long past = __ballot(incl > want);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            s.b = base + l;
+            s.n = __builtin_amdgcn_readlane(n, l);
+            s.L = __builtin_amdgcn_readlane(L, l);
+            s.row0 = read_lane<long long>(before, l);
+            s.item0 = read_lane<long long>(incl - items, l);
+        }
+        return s;
+    }
+};
 
 }  // namespace dkv

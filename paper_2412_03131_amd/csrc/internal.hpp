@@ -376,17 +376,22 @@ struct BlockAttnArgs : BlockCacheArgs {
     float* lse;
     int few_rows;          // rows (new tokens x G) of a sequence up to which it is one of few
     unsigned long long* arrive;       // few rows: [shares] arrival word of the split block that starts in a share
-    float* part;                      // [shares][2][16 rows] partial states {acc[kD], reference, sum, -, -}
+    float* part;                      // [shares][2][kRowPart] partial states
     unsigned long long* tile_arrive;  // many rows: the same
     float* tile_part;                 // [shares][2][kTilePart]
 };
-// Workgroups of the attention kernels, as many as run at once: two for each CU (few rows: of eight waves, many: of four).
-constexpr int kBlockRowShares = 512;
+// Shares of the attention kernels, as many as run at once: few rows, two waves for each SIMD; many, two workgroups for each CU.
+constexpr int kBlockRowShares = 2048;
 constexpr int kBlockTileShares = 512;
-constexpr int kTilePart = 4 * 17 * 64 * 4;  // floats of a 128-row block's state: four waves, a lane's 64 sums and {reference, sum, -, -}
-// Rows up to which a sequence goes to the few-row kernel.
-constexpr int kBlockFewRows = 64;
-constexpr long long kBlockRowBytes = kBlockRowShares * (8ll + 2 * 16 * kChunkPart * 4);
+constexpr int kRowPart = 16 * kChunkPart;   // floats of a 16-row block's state: its sums, then {reference, sum, -, -} of each row
+constexpr int kTilePart = 4 * 17 * 64 * 4;  // of a 128-row block's: four waves, a lane's 64 sums and {reference, sum, -, -}
+// Rows up to which a sequence goes to the few-row kernel: in calls of few rows altogether (of all query heads) its many pieces
+// fill the device where blocks of 128 rows do not.  (us, few-row kernel / many-row kernel, 32 / 8 heads) 64 tokens of one sequence over
+// 8192 42 / 59, of 16 over 2048 77 / 87, of 64 over 2048 335 / 256; 16 tokens of 64 over 2048 90 / 120, 32 tokens 169 / 134.
+constexpr int kBlockFewRows = 64, kBlockFewRowsSmall = 256;
+constexpr long long kBlockSmall = 32768;  // rows of all query heads
+inline int block_few_rows(long long Hq, long long total_new) { return total_new * Hq <= kBlockSmall ? kBlockFewRowsSmall : kBlockFewRows; }
+constexpr long long kBlockRowBytes = kBlockRowShares * (8ll + 2 * kRowPart * 4);
 constexpr long long kBlockTileBytes = kBlockTileShares * (8ll + 2 * kTilePart * 4);
 // A function of the query heads per KV head and the rows alone: one for more rows serves fewer.
 inline long long block_attention_ws(long long G, long long total_new)

@@ -61,7 +61,7 @@ __device__ __forceinline__ void put_key(u4 x, uint8_t* lds, int piece)
     *reinterpret_cast<u4*>(lds + (token >> 4) * 4096 + step * 1024 + r * 256 + (token & 15) * 16) = x;
 }
 // Returns the bits of the tokens with values that are not finite among the wave's pieces.
-__device__ __forceinline__ uint32_t put_value(u2 (&x)[8], uint8_t* lds, int piece)
+__device__ __forceinline__ uint32_t put_value(u2 (&x)[8], uint8_t* values, int piece)
 {
     const int dq = piece & 31, r = piece >> 5;  // dims 4 dq ..
     uint32_t bad = 0;
@@ -93,7 +93,7 @@ __device__ __forceinline__ uint32_t put_value(u2 (&x)[8], uint8_t* lds, int piec
         for (int e = 0; e < 4; ++e)
             y[e] = __builtin_amdgcn_perm(x[2 * e + 1][i >> 1], x[2 * e][i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
         const int dim = dq * 4 + i;
-        *reinterpret_cast<u4*>(lds + 8192 + (dim >> 5) * 2048 + ((dim >> 4) & 1) * 1024 + r * 256 + (dim & 15) * 16) = y;
+        *reinterpret_cast<u4*>(values + (dim >> 5) * 2048 + ((dim >> 4) & 1) * 1024 + r * 256 + (dim & 15) * 16) = y;
     }
     return odd;
 }
@@ -113,25 +113,35 @@ __device__ __forceinline__ u2 value_piece(const RowSource& s, int pos0, int piec
     return pos < s.end ? *reinterpret_cast<const u2*>(row_of(s, 1, pos) + (piece & 31) * 4) : u2{0, 0};
 }
 
+// A value that all lanes have alike, where the compiler has computed it in vector registers (quotients).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // ---- scores to weights ----------------------------------------------------------------
 // One tile's scores (natural units with a form, else log2) -> weights for the values' product.
 struct TileScale {
     float ks;       // of the fp32 product: a code's unit, scales, without a form log2(e)
     float add;      // log2 of the values' scale (natural units with a form)
     float rs;       // 1 / the values' scale
+    bool nan;       // a scale is NaN
 };
 struct TileView {
     int pos0, end;  // tokens from position `end` on are not there
     bool whole;     // all rows see all 32 tokens
 };
-// A tile for rows at p_lo .. p_hi: whether all of them see all of it, and whether none sees any of it.
-__device__ __forceinline__ bool all_seen(const BlockAttnArgs& a, int pos0, int p_lo, int p_hi)
+// The steps whose tiles all rows at p_lo .. p_hi see whole: below `sinks`, or from `first` on, up to `last`.
+struct TileRange {
+    int sinks, first, last;
+    __device__ __forceinline__ bool whole(int step) const { return (step < sinks || step >= first) && step <= last; }
+};
+__device__ __forceinline__ TileRange tile_range(const BlockAttnArgs& a, const Tiles& tl, int p_lo, int p_hi)
 {
-    return pos0 + kBT - 1 <= p_lo && (p_hi - pos0 < a.window || pos0 + kBT <= a.sinks);
-}
-__device__ __forceinline__ bool none_seen(const BlockAttnArgs& a, int pos0, int p_lo, int p_hi)
-{
-    return pos0 > p_hi || (p_lo - (pos0 + kBT - 1) >= a.window && pos0 >= a.sinks);
+    TileRange r;
+    r.sinks = min(a.sinks / kBT, tl.sb);
+    // tiles that start behind p_hi - window, and those that end at p_lo or before
+    const int from = (p_hi - a.window + kBT) >> 5, to = (p_lo + 1) / kBT - 1;
+    r.first = tl.sb + max(0, from - tl.w0);
+    r.last = to < tl.sb ? to : (to < tl.w0 ? tl.sb - 1 : to - tl.w0 + tl.sb);
+    return r;
 }
 __device__ __forceinline__ float pairs_max(float v)  // over lanes l, l + 32
 {
@@ -145,15 +155,15 @@ __device__ __forceinline__ float pairs_sum(float v)
 }
 
 // N products of a lane (8: tiles of 16 rows, token (i / 4) 16 + 4 r + i % 4; 16: tiles of 32, token 8 (i / 4) + 4 half +
-// i % 4) become weights; acc are the row's sums of values, raised with its reference.  Hidden tokens' products become -inf
-// at once, so that all tiles go one way from there.
+// i % 4) become weights in two steps: here forms, masks and the row's reference, with which acc, its sums of values, are raised.
+// Hidden tokens' products become -inf at once, so that all tiles go one way from there.
 template <bool MOD, int N, typename Acc, int A>
-__device__ __forceinline__ void weights(const BlockAttnArgs& a, TileScale t, const TileView& w, float (&y)[N], int p,
-                                        const ScoreForm& form, Acc (&acc)[A], float& ref, float& sum)
+__device__ __forceinline__ void raise(const BlockAttnArgs& a, TileScale& t, const TileView& w, float (&y)[N], int p,
+                                      const ScoreForm& form, Acc (&acc)[A], float& ref, float& sum)
 {
     constexpr float unit = MOD ? kChunkLn2 : 1.0f;
     const int group = N == 8 ? lane_id() >> 4 : lane_id() >> 5;
-    if (__builtin_isnan(t.ks + t.add)) {  // (uniform: a block that reads NaN, to the rows that see one of its tokens)
+    if (t.nan) {  // (a block that reads NaN, to the rows that see one of its tokens)
         t.ks = 1.0f, t.add = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i) y[i] = __builtin_nanf("");
@@ -173,9 +183,10 @@ __device__ __forceinline__ void weights(const BlockAttnArgs& a, TileScale t, con
             y[i] = seen ? y[i] : -INFINITY;
         }
     }
-    float top = -INFINITY;
+    float top = max3(y[0], y[1], y[2]);
 #pragma unroll
-    for (int i = 0; i < N; i += 2) top = max3(top, y[i], y[i + 1]);
+    for (int i = 3; i + 1 < N; i += 2) top = max3(top, y[i], y[i + 1]);
+    top = fmaxf(top, y[N - 1]);
     top = MOD ? top + t.add : __builtin_fmaf(top, t.ks, t.add);
     if (__any(top > ref + kRefRoom * unit)) {
         const float now = N == 8 ? rows_max(top) : pairs_max(top);
@@ -186,15 +197,16 @@ __device__ __forceinline__ void weights(const BlockAttnArgs& a, TileScale t, con
 #pragma unroll
         for (int i = 0; i < A; ++i) acc[i] *= f;
     }
+}
+// ... and here the exponents of 2.
+template <bool MOD, int N>
+__device__ __forceinline__ void exponents(const TileScale& t, float (&y)[N], float ref)
+{
     const float less = t.add - ref;
 #pragma unroll
-    for (int i = 0; i < N; ++i) y[i] = __builtin_amdgcn_exp2f(MOD ? (y[i] + less) * kChunkLog2e : __builtin_fmaf(y[i], t.ks, less));
-    float total = y[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) total += y[i];
-    sum = __builtin_fmaf(total, t.rs, sum);
+    for (int i = 0; i < N; ++i) y[i] = MOD ? (y[i] + less) * kChunkLog2e : __builtin_fmaf(y[i], t.ks, less);
 }
-// Eight weights as two fp16 parts.
+// Weights as two fp16 parts, four at a time.
 struct Parts {
     h8 hi, lo;
 };
@@ -208,40 +220,44 @@ __device__ __forceinline__ Parts parts(float a, float b, float c, float d, float
     for (int i = 0; i < 4; ++i) {
         const h2 top = {(_Float16)u[2 * i], (_Float16)u[2 * i + 1]};
         hi[i] = __builtin_bit_cast(uint32_t, top);
-        const h2 rest = {(_Float16)__builtin_fmaf((float)top.x, minus, u[2 * i]), (_Float16)__builtin_fmaf((float)top.y, minus, u[2 * i + 1])};
+        asm("" : "+v"(hi[i]));  // (else each half is converted once more by itself)
+        const h2 back = __builtin_bit_cast(h2, (uint32_t)hi[i]);
+        const h2 rest = {(_Float16)__builtin_fmaf((float)back.x, minus, u[2 * i]), (_Float16)__builtin_fmaf((float)back.y, minus, u[2 * i + 1])};
         lo[i] = __builtin_bit_cast(uint32_t, rest);
     }
     return Parts{__builtin_bit_cast(h8, hi), __builtin_bit_cast(h8, lo)};
 }
 
-// Block IDs and scales of 64 steps of a wave, a lane each (step = first + lane * stride < end); those whose block is there.
-struct StepList {
-    int id;
-    TileScale scale;
-    unsigned long long there;
+// 64 steps of the cache from `first` on (below `end`), a lane each: their block's ID (-1: none), and its scales.
+__device__ __forceinline__ int step_id(const BlockAttnArgs& a, const Tiles& tl, int b, int first, int end)
+{
+    const int step = first + lane_id();
+    return step < end ? block_id(a, b, tl.at(step)) : -1;
+}
+struct StepScales {
+    float ks, add, rs;
+    unsigned long long nan;
+    __device__ __forceinline__ TileScale at(int i) const
+    {
+        return TileScale{read_lane_f(ks, i), read_lane_f(add, i), read_lane_f(rs, i), ((nan >> i) & 1) != 0};
+    }
 };
 template <bool MOD>
-__device__ __forceinline__ StepList list_steps(const BlockAttnArgs& a, const Tiles& tl, int b, int h, int first, int stride, int end)
+__device__ __forceinline__ StepScales step_scales(const BlockAttnArgs& a, int id, int h)
 {
-    StepList s;
-    const int step = first + lane_id() * stride;
-    s.id = step < end ? block_id(a, b, tl.at(step)) : -1;
-    s.there = __ballot(s.id >= 0);
     float ks = 1.0f, vs = 1.0f;
-    if (s.id >= 0) {
-        const float* sc = a.scale + ((long long)s.id * a.Hkv + h) * 2;
+    if (id >= 0) {
+        const float* sc = a.scale + ((long long)id * a.Hkv + h) * 2;
         ks = sc[0];
         vs = sc[1];
     }
+    StepScales s;
     vs *= kCodeUnit;
-    s.scale.ks = ks * kCodeUnit * a.scale_x;
-    s.scale.add = __builtin_amdgcn_logf(vs) * (MOD ? kChunkLn2 : 1.0f);
-    s.scale.rs = vs > 0.0f && vs < INFINITY ? 1.0f / vs : 1.0f;  // (a NaN scale: see weights)
+    s.nan = __ballot(__builtin_isnan(ks + vs));
+    s.ks = ks * kCodeUnit * a.scale_x;
+    s.add = __builtin_amdgcn_logf(vs) * (MOD ? kChunkLn2 : 1.0f);
+    s.rs = vs > 0.0f && vs < INFINITY ? 1.0f / vs : 1.0f;
     return s;
-}
-__device__ __forceinline__ TileScale scale_of(const StepList& s, int i)
-{
-    return TileScale{read_lane_f(s.scale.ks, i), read_lane_f(s.scale.add, i), read_lane_f(s.scale.rs, i)};
 }
 
 __device__ __forceinline__ RowSource row_source(const BlockAttnArgs& a, const SeqItem& sq, int h)
@@ -258,67 +274,66 @@ __device__ __forceinline__ int coded_steps(const Tiles& tl, int L)
     return held <= tl.sb ? held : min(max(held - tl.w0, 0) + tl.sb, tl.count());
 }
 
-// ---- few rows: a workgroup on 16 rows -------------------------------------------------
-// Eight waves on the tiles of a piece, one tile each at a time; their states meet in LDS.  All (sequence, KV head, 16
-// rows) are laid end to end by their tiles and cut into equal pieces, one for each workgroup; one that is
-// split has its pieces' states joined by the last to arrive.
+// ---- few rows: a wave on 16 rows ---------------------------------------------------------
+// All (sequence, KV head, 16 rows) are laid end to end by their tiles and cut into equal pieces, one for each wave that the
+// device holds; a block of rows that is split has its pieces' states joined by the last to arrive.  Waves of a SIMD do not run
+// alike (the older is served first), so none waits for another: with pieces of eight waves that met in LDS, 64 ragged requests
+// took 102 us, half of it at barriers.
 //
 // Bound by memory.  A wave asks for a tile's keys again as soon as their codes are operands, and for its values likewise, so 8 KB
 // of the next tile are always on their way.
-constexpr int kRowWaves = 8;
-constexpr int kRowStart = 2;    // a 16-row block's start, in tiles
-constexpr int kRowShare = 16;  // least units of a piece: two tiles a wave
-constexpr int kStaged = 4;      // tiles of fp16 rows in LDS at once
-
-struct RowLds {
-    union {
-        uint8_t rows[kStaged * kRowTileBytes];
-        float state[kRowWaves][16][kChunkPart];
-    };
-    float ref[kRowWaves][16], sum[kRowWaves][16];
-    uint32_t odd[kStaged];
-    int last;
-};
+constexpr int kRowWaves = 4;    // of a workgroup
+constexpr int kRowStart = 3;    // units of a block's start, in tiles of the cache
+constexpr int kRowTile = 4;     // and of a tile of fp16 rows
+constexpr int kQuads = 4;      // quads of a lane in a join
+constexpr int kRowShare = 6;    // least units of a piece
 
 template <int FMT, bool MOD>
-__global__ __launch_bounds__(64 * kRowWaves, 4) void block_rows(BlockAttnArgs a)
+__global__ __launch_bounds__(64 * kRowWaves, 2) void block_rows(BlockAttnArgs a)
 {
-    __shared__ RowLds lds;
+    __shared__ uint8_t staged[kRowWaves][2 * kBlockSide];  // a wave's tile of fp16 values
     const int lane = lane_id(), wave = wave_index(), r = lane >> 4, col = lane & 15;
-    const int first_n = lane < a.B ? a.new_len[lane] : 0, first_L = lane < a.B ? seq_tokens(a, lane) : 0;
-    const auto loads = [&](int b, int& n, int& L) {
-        n = b < kWave ? first_n : a.new_len[b];
-        L = b < kWave ? first_L : seq_tokens(a, b);
+    SeqScan<BlockAttnArgs> scan(a);
+    // units of a sequence: those of its blocks of rows
+    const auto block_units = [&](const Tiles& tl, int L) {
+        const int coded = coded_steps(tl, L);
+        return coded + (tl.count() - coded) * kRowTile + kRowStart;
     };
-    // units of a sequence: 16-row blocks times their tiles and start
     const auto units = [&](int n, int L) {
-        return n > 0 && n * a.G <= a.few_rows ? (long long)a.Hkv * ((n * a.G + 15) / 16) * (tiles_of(a, n, L).count() + kRowStart) : 0LL;
+        return n > 0 && n * a.G <= a.few_rows ? (long long)a.Hkv * ((n * a.G + 15) / 16) * block_units(tiles_of(a, n, L), L) : 0LL;
     };
-    const long long all = find_item(a.B, a.total_new, a.max_new, INT64_MAX, loads, units).items;
-    long long share = (all + gridDim.x - 1) / gridDim.x;
-    share = share < kRowShare ? kRowShare : share;
-    long long x = (long long)blockIdx.x * share;
+    const long long all = scan.total(units);
+    const int shares = (int)gridDim.x * kRowWaves;
+    const long long share = max((all + shares - 1) / shares, (long long)kRowShare);
+    // (workgroup i runs on XCD i % 8: pieces that follow each other share an L2)
+    const int me = ((int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3)) * kRowWaves + wave;
+    long long x = me * share;
     const long long x_end = min(x + share, all);
 
     while (x < x_end) {
-        const SeqItem sq = find_item(a.B, a.total_new, a.max_new, x, loads, units);
+        const SeqItem sq = scan.find(x, units);
         if (sq.b < 0) break;
         const Tiles tl = tiles_of(a, sq.n, sq.L);
-        const int blk_units = tl.count() + kRowStart, coded = coded_steps(tl, sq.L);
+        const int steps = tl.count(), coded = coded_steps(tl, sq.L), blk_units = block_units(tl, sq.L);
         const int blocks = (sq.n * a.G + 15) / 16;
-        // 16-row block of the sequence: KV head major
-        int which = (int)((x - sq.item0) / blk_units);
+        // steps that start before unit u of a block
+        const auto step_at = [&](long long u) {
+            const int v = (int)u - kRowStart;
+            return v <= coded ? max(v, 0) : coded + (v - coded + kRowTile - 1) / kRowTile;
+        };
+        // block of the sequence: KV head major
+        int which = uniform((int)((x - sq.item0) / blk_units));
         for (; x < x_end && which < a.Hkv * blocks; ++which) {
             const long long t0 = sq.item0 + (long long)which * blk_units;  // the block's first unit
             const int h = which / blocks, row_first = (which - h * blocks) * 16;
-            const int s0 = (int)max(x - t0 - kRowStart, 0LL);
-            const int s1 = (int)(min(x_end, t0 + blk_units) - t0) - kRowStart;
+            const int s0 = uniform(step_at(x - t0)), s1 = uniform(step_at(min(x_end - t0, (long long)blk_units)));
             x = min(x_end, t0 + blk_units);
             if (s1 <= s0) continue;
 
             // this lane's row
             const int rows = min(sq.n * a.G - row_first, 16);
             const int row = row_first + min(col, rows - 1), token = row / a.G, hq = h * a.G + row % a.G, p = sq.L + token;
+            const long long out_row = (sq.row0 + token) * a.Hq + hq;
             h8 q[4];
             {
                 const uint16_t* at = a.q + (sq.row0 + token) * a.q_stride + (long long)hq * kD;
@@ -327,22 +342,38 @@ __global__ __launch_bounds__(64 * kRowWaves, 4) void block_rows(BlockAttnArgs a)
             }
             ScoreForm form{0.0f, 0.0f, 0.0f};
             if constexpr (MOD) form = ScoreForm{a.cap_in, a.cap, a.slopes ? a.slopes[hq] : 0.0f};
-            const int p_lo = sq.L + row_first / a.G, p_hi = sq.L + (row_first + rows - 1) / a.G;
+            const TileRange range = tile_range(a, tl, sq.L + row_first / a.G, sq.L + (row_first + rows - 1) / a.G);
             f4 acc[8];  // [u * 2 + j]: dims u 32 + j 16 + 4 r ..
             float ref = kLowest, sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+            // a tile's products -> weights
+            const auto weigh = [&](const f4 (&s)[2], TileScale ts, int step, int end, float (&y)[8]) {
+                TileView view{0, end, range.whole(step)};
+                if (!view.whole || MOD) view.pos0 = tl.at(step) * kBT;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = s[j >> 2][j & 3];
+                raise<MOD>(a, ts, view, y, p, form, acc, ref, sum);
+                exponents<MOD>(ts, y, ref);
+                float total = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    y[j] = __builtin_amdgcn_exp2f(y[j]);
+                    total += y[j];
+                }
+                sum = __builtin_fmaf(total, ts.rs, sum);
+                return parts(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
+            };
 
-            // steps of the cache's blocks, then those of fp16 rows
+            // the cache's blocks
             const int c1 = min(s1, coded);
-            for (int base = s0 + wave; base < c1; base += kRowWaves * kWave) {
-                const StepList list = list_steps<MOD>(a, tl, sq.b, h, base, kRowWaves, c1);
-                unsigned long long todo = list.there;
+            for (int base = s0; base < c1; base += kWave) {
+                const int id = step_id(a, tl, sq.b, base, c1);
+                unsigned long long todo = __ballot(id >= 0);
                 if (!todo) continue;
                 int i = __builtin_ctzll(todo);
                 const auto block = [&](int at) {
-                    const int id = __builtin_amdgcn_readlane(list.id, at);
-                    return span(a.pool + ((long long)id * a.Hkv + h) * kBlockBytes, kBlockBytes);
+                    return span(a.pool + ((long long)__builtin_amdgcn_readlane(id, at) * a.Hkv + h) * kBlockBytes, kBlockBytes);
                 };
                 auto src = block(i);
                 u4 k[4], v[4];
@@ -350,28 +381,21 @@ __global__ __launch_bounds__(64 * kRowWaves, 4) void block_rows(BlockAttnArgs a)
                 for (int j = 0; j < 4; ++j) k[j] = fetch<16>(src, lane * 16, j * 1024);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = fetch<16>(src, lane * 16, kBlockSide + j * 1024);
+                const StepScales scales = step_scales<MOD>(a, id, h);
                 while (todo) {
                     todo &= todo - 1;
                     const int next = todo ? __builtin_ctzll(todo) : i;
-                    const TileScale ts = scale_of(list, i);
-                    TileView view{tl.at(base + i * kRowWaves) * kBT, INT32_MAX, false};
-                    view.whole = all_seen(a, view.pos0, p_lo, p_hi);
                     src = block(next);
                     f4 s[2] = {f4{0.0f, 0.0f, 0.0f, 0.0f}, f4{0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        s[j >> 1] = mfma_k32(codes8<FMT>(k[j][0], k[j][1]), q[(j & 1) * 2], s[j >> 1]);
-                        s[j >> 1] = mfma_k32(codes8<FMT>(k[j][2], k[j][3]), q[(j & 1) * 2 + 1], s[j >> 1]);
-                    }
+                    for (int j = 0; j < 8; ++j)
+                        s[j >> 2] = mfma_k32(codes8<FMT>(k[j >> 1][(j & 1) * 2], k[j >> 1][(j & 1) * 2 + 1]), q[j & 3], s[j >> 2]);
                     if (todo) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) k[j] = fetch<16>(src, lane * 16, j * 1024);
                     }
                     float y[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y[j] = s[j >> 2][j & 3];
-                    weights<MOD>(a, ts, view, y, p, form, acc, ref, sum);
-                    const Parts w = parts(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
+                    const Parts w = weigh(s, scales.at(i), base + i, INT32_MAX, y);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const h8 x8 = codes8<FMT>(v[j >> 1][(j & 1) * 2], v[j >> 1][(j & 1) * 2 + 1]);
@@ -386,125 +410,159 @@ __global__ __launch_bounds__(64 * kRowWaves, 4) void block_rows(BlockAttnArgs a)
                 }
             }
 
-            for (int base = max(s0, coded); base < s1; base += kStaged) {
+            // rows in fp16: keys straight from their rows, values through LDS
+#pragma unroll 1
+            for (int step = max(s0, coded); step < s1; ++step) {
                 const RowSource src = row_source(a, sq, h);
-                const int here = min(kStaged, s1 - base);
-                __syncthreads();
-                if (threadIdx.x < kStaged) lds.odd[threadIdx.x] = 0;
-                __syncthreads();
-#pragma unroll 1
-                for (int piece = threadIdx.x; piece < here * 512; piece += 64 * kRowWaves) {
-                    const int t = piece / 512;
-                    put_key(key_piece(src, tl.at(base + t) * kBT, piece & 511), lds.rows + t * kRowTileBytes, piece & 511);
+                const int pos0 = tl.at(step) * kBT;
+                h8 k[8];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint16_t* at = row_of(src, 0, min(pos0 + j * 16 + col, src.end - 1)) + r * 16;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) k[j * 4 + i] = *reinterpret_cast<const h8*>(at + (i >> 1) * 64 + (i & 1) * 8);
                 }
+                uint32_t odd = 0;
+                wave_lds_sync();  // (the last tile's values are read)
 #pragma unroll 1
-                for (int piece = threadIdx.x; piece < here * 128; piece += 64 * kRowWaves) {
-                    const int t = piece / 128;
+                for (int piece = lane; piece < 128; piece += kWave) {
                     u2 v8[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v8[e] = value_piece(src, tl.at(base + t) * kBT, piece & 127, e);
-                    const uint32_t odd = put_value(v8, lds.rows + t * kRowTileBytes, piece & 127);
-                    if (odd && lane == 0) atomicOr(&lds.odd[t], odd);
+                    for (int e = 0; e < 8; ++e) v8[e] = value_piece(src, pos0, piece, e);
+                    odd |= put_value(v8, staged[wave], piece);
                 }
-                __syncthreads();
-                if (wave < here) {
-                    const uint8_t* tile = lds.rows + wave * kRowTileBytes;
-                    TileView view{tl.at(base + wave) * kBT, sq.L + sq.n, false};
-                    view.whole = all_seen(a, view.pos0, p_lo, p_hi);
-                    f4 s[2] = {f4{0.0f, 0.0f, 0.0f, 0.0f}, f4{0.0f, 0.0f, 0.0f, 0.0f}};
+                wave_lds_sync();
+                f4 s[2] = {f4{0.0f, 0.0f, 0.0f, 0.0f}, f4{0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        s[j >> 2] = mfma_k32(*reinterpret_cast<const h8*>(tile + j * 1024 + lane * 16), q[j & 3], s[j >> 2]);
-                    float y[8];
+                for (int j = 0; j < 8; ++j) s[j >> 2] = mfma_k32(k[j], q[j & 3], s[j >> 2]);
+                float y[8];
+                const Parts w = weigh(s, TileScale{a.scale_x, 0.0f, 1.0f, false}, step, src.end, y);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) y[j] = s[j >> 2][j & 3];
-                    weights<MOD>(a, TileScale{a.scale_x, 0.0f, 1.0f}, view, y, p, form, acc, ref, sum);
-                    const Parts w = parts(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
+                for (int j = 0; j < 8; ++j) {
+                    const h8 x8 = *reinterpret_cast<const h8*>(staged[wave] + j * 1024 + lane * 16);
+                    acc[j] = mfma_k32(x8, w.hi, acc[j]);
+                    acc[j] = mfma_k32(x8, w.lo, acc[j]);
+                }
+                // values that are not finite, to the rows that see their token
+                for (odd = __builtin_amdgcn_readfirstlane(odd); odd; odd &= odd - 1) {
+                    const int tok = __builtin_ctz(odd), c = pos0 + tok;
+                    const int reg = (tok >> 4) * 4 + (tok & 3);
+                    float wt = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) wt = j == reg ? y[j] : wt;
+                    wt = __shfl(wt, ((tok & 15) >> 2) * 16 + col);
+                    const bool seen = c <= p && (p - c < a.window || c < a.sinks);
+                    const uint16_t* vr = row_of(src, 1, c) + 4 * r;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const h8 x8 = *reinterpret_cast<const h8*>(tile + 8192 + j * 1024 + lane * 16);
-                        acc[j] = mfma_k32(x8, w.hi, acc[j]);
-                        acc[j] = mfma_k32(x8, w.lo, acc[j]);
-                    }
-                    // values that are not finite, to the rows that see their token
-                    for (uint32_t odd = __builtin_amdgcn_readfirstlane(lds.odd[wave]); odd; odd &= odd - 1) {
-                        const int tok = __builtin_ctz(odd), c = view.pos0 + tok;
-                        const int from = ((tok & 15) >> 2) * 16 + col, reg = (tok >> 4) * 4 + (tok & 3);
-                        float wt = 0.0f;
+                        const u2 w2 = *reinterpret_cast<const u2*>(vr + (j >> 1) * 32 + (j & 1) * 16);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) wt = j == reg ? y[j] : wt;
-                        wt = __shfl(wt, from);
-                        const bool seen = c <= p && (p - c < a.window || c < a.sinks);
-                        const uint16_t* vr = row_of(src, 1, c);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float v1 = h2f(vr[(j >> 3) * 32 + ((j >> 2) & 1) * 16 + 4 * r + (j & 3)]);
-                            if (seen && !(fabsf(v1) < INFINITY)) acc[j >> 2][j & 3] = __builtin_fmaf(wt, v1, acc[j >> 2][j & 3]);
+                        for (int e = 0; e < 4; ++e) {
+                            const float v1 = h2f((w2[e >> 1] >> ((e & 1) * 16)) & 0xffffu);
+                            if (seen && !(fabsf(v1) < INFINITY)) acc[j][e] = __builtin_fmaf(wt, v1, acc[j][e]);
                         }
                     }
                 }
             }
 
-            // the waves' states
-            sum = rows_sum(sum);
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<f4*>(&lds.state[wave][col][(i >> 1) * 32 + (i & 1) * 16 + 4 * r]) = acc[i];
-            if (r == 0) {
-                lds.ref[wave][col] = ref;
-                lds.sum[wave][col] = sum;
-            }
-            __syncthreads();
-            const int my_row = threadIdx.x >> 5, dim = (threadIdx.x & 31) * 4;
             constexpr float to_log2 = MOD ? kChunkLog2e : 1.0f;
-            ref = kLowest, sum = 0.0f;
-            f4 out = {0.0f, 0.0f, 0.0f, 0.0f};
+            sum = rows_sum(sum);
+            const int last_unit = steps > coded ? coded + (steps - 1 - coded) * kRowTile : steps - 1;
+            const int first_share = uniform((int)((t0 + kRowStart) / share)), last_share = uniform((int)((t0 + kRowStart + last_unit) / share));
+            if (first_share == last_share) {
+                const float inv = 1.0f / sum;
+                if (col < rows) {
 #pragma unroll
-            for (int w = 0; w < kRowWaves; ++w) ref = fmaxf(ref, lds.ref[w][my_row]);
+                    for (int i = 0; i < 8; ++i) {
+                        h4 y;
 #pragma unroll
-            for (int w = 0; w < kRowWaves; ++w) {
-                const float f = __builtin_amdgcn_exp2f((lds.ref[w][my_row] - ref) * to_log2);
-                sum = __builtin_fmaf(lds.sum[w][my_row], f, sum);
-                out += *reinterpret_cast<const f4*>(&lds.state[w][my_row][dim]) * f;
-            }
-            const long long first_share = (t0 + kRowStart) / share, last_share = (t0 + blk_units - 1) / share;
-            bool whole = first_share == last_share;
-            if (!whole) {
-                // split: slot 1 of the share where the block starts, slot 0 of the others
-                const auto slot = [&](long long sh) {
-                    return span(a.part + (sh * 2 + (sh == first_share ? 1 : 0)) * 16 * kChunkPart, 16 * kChunkPart * 4);
-                };
-                const int at = my_row * kChunkPart * 4;
-                {
-                    const auto to = slot(blockIdx.x);
-                    put_quad(to, at + dim * 4, 0, out);
-                    if (dim == 0) put_quad(to, at + kD * 4, 0, f4{ref, sum, 0.0f, 0.0f});
+                        for (int j = 0; j < 4; ++j) y[j] = (_Float16)(acc[i][j] * inv);
+                        *reinterpret_cast<h4*>(a.out + out_row * kD + (i >> 1) * 32 + (i & 1) * 16 + 4 * r) = y;
+                    }
+                    if (a.lse && r == 0) a.lse[out_row] = MOD ? ref + __logf(sum) : (ref + __log2f(sum)) * kChunkLn2;
                 }
-                whole = split_last(a.arrive + first_share, (int)(last_share - first_share) + 1, &lds.last);
-                if (whole) {
-                    ref = kLowest, sum = 0.0f;
-                    out = f4{0.0f, 0.0f, 0.0f, 0.0f};
-                    for (long long sh = first_share; sh <= last_share; ++sh) ref = fmaxf(ref, get_quad(slot(sh), at + kD * 4, 0)[0]);
-                    for (long long sh = first_share; sh <= last_share; ++sh) {
-                        const auto from = slot(sh);
-                        const f4 m = get_quad(from, at + kD * 4, 0), part = get_quad(from, at + dim * 4, 0);
-                        const float f = __builtin_amdgcn_exp2f((m[0] - ref) * to_log2);
-                        sum = __builtin_fmaf(m[1], f, sum);
-                        out += part * f;
+                continue;
+            }
+            // split: slot 1 of the share where the block starts, slot 0 of the others.  A state: rows of sums, then a quad
+            // {reference, sum, -, -} per row.
+            const auto slot = [&](int sh) {
+                return span(a.part + ((long long)sh * 2 + (sh == first_share ? 1 : 0)) * kRowPart, kRowPart * 4);
+            };
+            if (col < rows) {
+                const auto to = slot(me);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) put_quad(to, col * (kD * 4) + r * 16, (i >> 1) * 128 + (i & 1) * 64, acc[i]);
+                if (r == 0) put_quad(to, 16 * kD * 4 + col * 16, 0, f4{ref, sum, 0.0f, 0.0f});
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            int arrived = 0;
+            if (lane == 0) arrived = (int)arrive_count(a.arrive + first_share, call_tag());
+            if (__builtin_amdgcn_readfirstlane(arrived) != last_share - first_share + 1) continue;
+            // All of the block's pieces, in order: first every row's reference and normalizer (a lane a row), then the sums, a lane
+            // a quad of dims of several rows, four pieces' asked for at once.
+            const int my_row = min(lane, rows - 1);
+            float top = kLowest, total = 0.0f;
+#pragma unroll 1
+            for (int sh = first_share; sh <= last_share; sh += 8) {
+                f4 m[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m[i] = get_quad(slot(min(sh + i, last_share)), 16 * kD * 4 + my_row * 16, 0);
+                float up = top;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) up = fmaxf(up, m[i][0]);
+                total *= __builtin_amdgcn_exp2f((top - up) * to_log2);
+                top = up;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (sh + i <= last_share) total = __builtin_fmaf(m[i][1], __builtin_amdgcn_exp2f((m[i][0] - top) * to_log2), total);
+            }
+            if (a.lse && lane < rows) {
+                const int orow = row_first + lane;
+                a.lse[(sq.row0 + orow / a.G) * a.Hq + h * a.G + orow % a.G] = MOD ? top + __logf(total) : (top + __log2f(total)) * kChunkLn2;
+            }
+#pragma unroll 1
+            for (int first = 0; first < rows * 32; first += kQuads * kWave) {
+                f4 out[kQuads];
+                float up[kQuads];
+                int at[kQuads];
+#pragma unroll
+                for (int i = 0; i < kQuads; ++i) {
+                    at[i] = min(first + i * kWave + lane, rows * 32 - 1);
+                    up[i] = __shfl(top, at[i] >> 5);
+                    out[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+                }
+#pragma unroll 1
+                for (int sh = first_share; sh <= last_share; sh += 4) {
+                    f4 part[kQuads][4];
+                    float m[kQuads][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const auto from = slot(min(sh + j, last_share));
+#pragma unroll
+                        for (int i = 0; i < kQuads; ++i) {
+                            m[i][j] = get_one(from, 16 * kD * 4 + (at[i] >> 5) * 16, 0);
+                            part[i][j] = get_quad(from, at[i] * 16, 0);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (sh + j <= last_share) {
+#pragma unroll
+                            for (int i = 0; i < kQuads; ++i) out[i] += part[i][j] * __builtin_amdgcn_exp2f((m[i][j] - up[i]) * to_log2);
+                        }
                     }
                 }
-            }
-            if (whole && my_row < rows) {
-                const int orow = row_first + my_row, otoken = orow / a.G, ohq = h * a.G + orow % a.G;
-                const long long at = (sq.row0 + otoken) * a.Hq + ohq;
-                const float inv = 1.0f / sum;
-                h4 y;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = (_Float16)(out[j] * inv);
-                *reinterpret_cast<h4*>(a.out + at * kD + dim) = y;
-                if (a.lse && dim == 0) a.lse[at] = MOD ? ref + __logf(sum) : (ref + __log2f(sum)) * kChunkLn2;
+                for (int i = 0; i < kQuads; ++i) {
+                    const float inv = 1.0f / __shfl(total, at[i] >> 5);
+                    if (first + i * kWave + lane >= rows * 32) continue;
+                    const int orow = row_first + (at[i] >> 5);
+                    h4 y;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) y[j] = (_Float16)(out[i][j] * inv);
+                    *reinterpret_cast<h4*>(a.out + ((sq.row0 + orow / a.G) * a.Hq + h * a.G + orow % a.G) * kD + (at[i] & 31) * 4) = y;
+                }
             }
-            __syncthreads();
         }
     }
 }
@@ -518,7 +576,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 4) void block_rows(BlockAttnArgs a)
 // All (sequence, KV head, 128 rows) are laid end to end and cut into equal shares, one for each workgroup; shares that follow
 // each other run on one XCD, so that its L2 serves their tiles.
 constexpr int kTileRows = 128, kTileWaves = 4;
-constexpr int kTileShare = 16; // least units of a share
+constexpr int kTileShare = 8;  // least units of a share
 constexpr int kTileStart = 4;  // a 128-row block's start, in tiles
 
 typedef float f16v __attribute__((ext_vector_type(16)));
@@ -563,29 +621,25 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
 {
     __shared__ TileLds lds;
     const int lane = lane_id(), wave = wave_index(), half = lane >> 5, col = lane & 31;
-    const auto loads = [&](int b, int& n, int& L) {
-        n = a.new_len[b];
-        L = seq_tokens(a, b);
-    };
+    SeqScan<BlockAttnArgs> scan(a);
     const auto units = [&](int n, int L) {
         if (n <= 0 || n * a.G <= a.few_rows) return 0LL;
         const TileUnits u = tile_units(a, n, L);
         return a.Hkv * u.upto(u.blocks);
     };
-    const long long all = find_item(a.B, a.total_new, a.max_new, INT64_MAX, loads, units).items;
-    long long share = (all + gridDim.x - 1) / gridDim.x;
-    share = share < kTileShare ? kTileShare : share;
+    const long long all = scan.total(units);
+    const long long share = max((all + gridDim.x - 1) / gridDim.x, (long long)kTileShare);
     // (workgroup i runs on XCD i % 8)
     const int me = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
     long long x = (long long)me * share;
     const long long x_end = min(x + share, all);
 
     while (x < x_end) {
-        const SeqItem sq = find_item(a.B, a.total_new, a.max_new, x, loads, units);
+        const SeqItem sq = scan.find(x, units);
         if (sq.b < 0) break;
         const TileUnits tu = tile_units(a, sq.n, sq.L);
         const long long head_units = tu.upto(tu.blocks);
-        int h = (int)((x - sq.item0) / head_units), blk;
+        int h = uniform((int)((x - sq.item0) / head_units)), blk;
         {
             const long long y = x - sq.item0 - h * head_units;
             int lo = 0, hi = tu.blocks - 1;  // the last block that starts at y or before
@@ -605,7 +659,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
             const int steps = tl.count();
             // (a block's units and its tiles differ: unit y of w stands for its first tiles up to y steps / w)
             const auto step_at = [&](long long y) { return (int)((y - t0) * steps / (t1 - t0)); };
-            const int s0 = step_at(x), s1 = step_at(min(x_end, t1));
+            const int s0 = uniform(step_at(x)), s1 = uniform(step_at(min(x_end, t1)));
             x = min(x_end, t1);
             if (++blk == tu.blocks) blk = 0, ++h;
             if (s1 <= s0) continue;
@@ -630,49 +684,70 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
                 for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
 
             const int coded = coded_steps(tl, sq.L);
-            // A tile in LDS: scores, weights, values.  (Its operands are asked for together: the scheduler would
-            // wait for each by itself.)
+            const TileRange range = tile_range(a, tl, p_lo, p_hi);
             const uint32_t at_k = (col >> 4) * 4096 + half * 256 + (col & 15) * 16, at_v = 8192 + (col >> 4) * 1024 + half * 256 + (col & 15) * 16;
-            float y[16];
-            const auto tile_step = [&](const uint8_t* tile, const TileScale& ts, const TileView& view) {
-                h8 x[8];
+            f16v sc;     // a tile's products
+            float y[16]; // its exponents, then weights
+            h8 x[8];     // operands: asked for together (the scheduler would wait for each by itself)
+            const auto read_keys = [&](int buf) {
+                const uint8_t* tile = lds.rows[buf] + at_k;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const h8*>(tile + at_k + (i >> 1) * 1024 + (i & 1) * 512);
-                __builtin_amdgcn_sched_barrier(0);
-                f16v sc;
+                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const h8*>(tile + (i >> 1) * 1024 + (i & 1) * 512);
+            };
+            const auto scores = [&]() {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) sc[j] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sc = mfma_32(x[i], q[i], sc);
+            };
+            // A tile in LDS.  Its values are asked for beside its products.
+            const auto tile_step = [&](int buf, TileScale ts, int s, int end) {
+                TileView view{0, end, range.whole(s)};
+                if (!view.whole || MOD) view.pos0 = tl.at(s) * kBT;
+                read_keys(buf);
+                __builtin_amdgcn_sched_barrier(0);
+                scores();
+                const uint8_t* tile = lds.rows[buf] + at_v;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const h8*>(tile + at_v + (i >> 1) * 2048 + (i & 1) * 512);
+                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const h8*>(tile + (i & 3) * 2048 + (i >> 2) * 512);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) y[j] = sc[j];
-                weights<MOD>(a, ts, view, y, p, form, acc, ref, sum);
-                const Parts w[2] = {parts(y[0], y[1], y[2], y[3], y[8], y[9], y[10], y[11]),
-                                    parts(y[4], y[5], y[6], y[7], y[12], y[13], y[14], y[15])};
+                raise<MOD>(a, ts, view, y, p, form, acc, ref, sum);
+                exponents<MOD>(ts, y, ref);
+                float total[2] = {0.0f, 0.0f};
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) acc[u] = mfma_32(x[2 * u + k], w[k].hi, acc[u]);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) acc[u] = mfma_32(x[2 * u + k], w[k].lo, acc[u]);
+                for (int j = 0; j < 16; ++j) {
+                    y[j] = __builtin_amdgcn_exp2f(y[j]);
+                    total[j & 1] += y[j];
                 }
+                sum = __builtin_fmaf(total[0] + total[1], ts.rs, sum);
+                const Parts w0 = parts(y[0], y[1], y[2], y[3], y[8], y[9], y[10], y[11]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) acc[u] = mfma_32(x[u], w0.hi, acc[u]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) acc[u] = mfma_32(x[u], w0.lo, acc[u]);
+                const Parts w1 = parts(y[4], y[5], y[6], y[7], y[12], y[13], y[14], y[15]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) acc[u] = mfma_32(x[4 + u], w1.hi, acc[u]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) acc[u] = mfma_32(x[4 + u], w1.lo, acc[u]);
             };
 
-            // the cache's blocks: a block's loads are asked for a step before it is written to LDS, and that a step before its use
+            // the cache's blocks: a block's loads are asked for a step before it is written to LDS, and that two steps before its
+            // values' use
             const int c1 = min(s1, coded);
             for (int base = s0; base < c1; base += kWave) {
-                const StepList list = list_steps<MOD>(a, tl, sq.b, my_h, base, 1, c1);
-                unsigned long long todo = list.there, loaded = todo;
+                const int id = step_id(a, tl, sq.b, base, c1);
+                const StepScales scales = step_scales<MOD>(a, id, my_h);
+                unsigned long long todo = __ballot(id >= 0), loaded = todo;
                 if (!todo) continue;
                 u4 raw_k, raw_v;
                 const auto load = [&]() {
                     if (!loaded) return;
-                    const int id = __builtin_amdgcn_readlane(list.id, __builtin_ctzll(loaded));
+                    const int now = __builtin_amdgcn_readlane(id, __builtin_ctzll(loaded));
                     loaded &= loaded - 1;
-                    const auto from = span(a.pool + ((long long)id * a.Hkv + my_h) * kBlockBytes, kBlockBytes);
+                    const auto from = span(a.pool + ((long long)now * a.Hkv + my_h) * kBlockBytes, kBlockBytes);
                     raw_k = fetch<16>(from, threadIdx.x * 16, 0);
                     raw_v = fetch<16>(from, threadIdx.x * 16, kBlockSide);
                 };
@@ -694,11 +769,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
                     todo &= todo - 1;
                     if (todo) store(buf ^ 1);
                     load();
-                    TileView view{tl.at(base + i) * kBT, INT32_MAX, false};
-                    if (!none_seen(a, view.pos0, p_lo, p_hi)) {
-                        view.whole = all_seen(a, view.pos0, p_lo, p_hi);
-                        tile_step(lds.rows[buf], scale_of(list, i), view);
-                    }
+                    tile_step(buf, scales.at(i), base + i, INT32_MAX);
                     __syncthreads();
                 }
             }
@@ -757,36 +828,33 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
                     *reinterpret_cast<u4*>(to) = y[0];
                     *reinterpret_cast<u4*>(to + 16) = y[1];
                 };
-                load(max(s0, coded));
+                const int f0 = max(s0, coded);
+                load(f0);
                 store(0);
-                if (max(s0, coded) + 1 < s1) load(max(s0, coded) + 1);
+                if (f0 + 1 < s1) load(f0 + 1);
                 __syncthreads();
                 int buf = 0;
-                for (int s = max(s0, coded); s < s1; ++s, buf ^= 1) {
+                for (int s = f0; s < s1; ++s, buf ^= 1) {
                     if (s + 1 < s1) store(buf ^ 1);
                     if (s + 2 < s1) load(s + 2);
-                    TileView view{tl.at(s) * kBT, src.end, false};
-                    if (!none_seen(a, view.pos0, p_lo, p_hi)) {
-                        view.whole = all_seen(a, view.pos0, p_lo, p_hi);
-                        tile_step(lds.rows[buf], TileScale{a.scale_x, 0.0f, 1.0f}, view);
-                        // values that are not finite, to the rows that see their token
-                        for (uint32_t odd = __builtin_amdgcn_readfirstlane(lds.odd[buf][0] | lds.odd[buf][1] | lds.odd[buf][2] | lds.odd[buf][3]); odd; odd &= odd - 1) {
-                            const int tok = __builtin_ctz(odd), c = view.pos0 + tok;
-                            const int at = ((tok >> 2) & 1) * 32 + col, reg = (tok >> 3) * 4 + (tok & 3);
-                            float wt = 0.0f;
+                    tile_step(buf, TileScale{a.scale_x, 0.0f, 1.0f, false}, s, src.end);
+                    // values that are not finite, to the rows that see their token
+                    for (uint32_t odd = __builtin_amdgcn_readfirstlane(lds.odd[buf][0] | lds.odd[buf][1] | lds.odd[buf][2] | lds.odd[buf][3]); odd; odd &= odd - 1) {
+                        const int tok = __builtin_ctz(odd), c = tl.at(s) * kBT + tok;
+                        const int at = ((tok >> 2) & 1) * 32 + col, reg = (tok >> 3) * 4 + (tok & 3);
+                        float wt = 0.0f;
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) wt = j == reg ? y[j] : wt;
-                            wt = __shfl(wt, at);
-                            const bool seen = c <= p && (p - c < a.window || c < a.sinks);
-                            const uint16_t* vr = row_of(src, 1, c);
+                        for (int j = 0; j < 16; ++j) wt = j == reg ? y[j] : wt;
+                        wt = __shfl(wt, at);
+                        const bool seen = c <= p && (p - c < a.window || c < a.sinks);
+                        const uint16_t* vr = row_of(src, 1, c);
 #pragma unroll
-                            for (int u = 0; u < 4; ++u)
+                        for (int u = 0; u < 4; ++u)
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) {
-                                    const float v1 = h2f(vr[u * 32 + 8 * (j >> 2) + 4 * half + (j & 3)]);
-                                    if (seen && !(fabsf(v1) < INFINITY)) acc[u][j] = __builtin_fmaf(wt, v1, acc[u][j]);
-                                }
-                        }
+                            for (int j = 0; j < 16; ++j) {
+                                const float v1 = h2f(vr[u * 32 + 8 * (j >> 2) + 4 * half + (j & 3)]);
+                                if (seen && !(fabsf(v1) < INFINITY)) acc[u][j] = __builtin_fmaf(wt, v1, acc[u][j]);
+                            }
                     }
                     __syncthreads();
                 }
@@ -801,7 +869,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
                 const long long y = ((long long)(s + 1) * w + steps - 1) / steps - 1;
                 return (int)((t0 + y) / share);
             };
-            const int first_share = share_of(0), last_share = share_of(steps - 1);
+            const int first_share = uniform(share_of(0)), last_share = uniform(share_of(steps - 1));
             // (where a share has less units than a tile stands for, it may have no tile)
             const auto has = [&](int sh) {
                 return share * steps >= t1 - t0 || step_at(min((sh + 1) * share, t1)) > step_at(max(sh * share, t0));
@@ -825,25 +893,50 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
                 }
                 whole = split_last(a.tile_arrive + first_share, pieces, &lds.last);
                 if (whole) {
-                    float top = kLowest;
-                    for (int sh = first_share; sh <= last_share; ++sh)
-                        if (has(sh)) top = fmaxf(top, get_quad(slot(sh), lane * 16, 16 * 1024)[0]);
-                    ref = top, sum = 0.0f;
+                    // All pieces in order: references and normalizers first, then the sums, eight quads of four pieces asked
+                    // for at once.
+                    ref = kLowest, sum = 0.0f;
+#pragma unroll 1
+                    for (int sh = first_share; sh <= last_share; sh += 8) {
+                        f4 m[8];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                        for (int i = 0; i < 8; ++i) m[i] = get_quad(slot(min(sh + i, last_share)), lane * 16, 16 * 1024);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
-                    for (int sh = first_share; sh <= last_share; ++sh) {
-                        if (!has(sh)) continue;
-                        const auto from_slot = slot(sh);
-                        const f4 m = get_quad(from_slot, lane * 16, 16 * 1024);
-                        const float f = __builtin_amdgcn_exp2f((m[0] - ref) * to_log2);
-                        sum = __builtin_fmaf(m[1], f, sum);
+                        for (int i = 0; i < 8; ++i) {
+                            if (sh + i <= last_share && has(sh + i)) {
+                                const float up = fmaxf(ref, m[i][0]);
+                                sum = __builtin_fmaf(m[i][1], __builtin_amdgcn_exp2f((m[i][0] - up) * to_log2), sum * __builtin_amdgcn_exp2f((ref - up) * to_log2));
+                                ref = up;
+                            }
+                        }
+                    }
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const f4 part = get_quad(from_slot, lane * 16, i * 1024);
+                    for (int u = 0; u < 4; u += 2) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) acc[i >> 2][(i & 3) * 4 + j] = __builtin_fmaf(part[j], f, acc[i >> 2][(i & 3) * 4 + j]);
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) acc[u + i][j] = 0.0f;
+#pragma unroll 1
+                        for (int sh = first_share; sh <= last_share; sh += 4) {
+                            f4 part[4][8], m[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const auto from = slot(min(sh + k, last_share));
+                                m[k] = get_quad(from, lane * 16, 16 * 1024);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) part[k][i] = get_quad(from, lane * 16, (u * 4 + i) * 1024);
+                            }
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                if (sh + k <= last_share && has(sh + k)) {
+                                    const float f = __builtin_amdgcn_exp2f((m[k][0] - ref) * to_log2);
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                                        for (int j = 0; j < 4; ++j)
+                                            acc[u + (i >> 2)][(i & 3) * 4 + j] = __builtin_fmaf(part[k][i][j], f, acc[u + (i >> 2)][(i & 3) * 4 + j]);
+                                }
+                            }
                         }
                     }
                 }
@@ -878,7 +971,7 @@ hipError_t launch_block_attention(const BlockAttnArgs& a, int format, bool mod, 
     }
     void (*kernel)(BlockAttnArgs) = format == kE4m3 ? (mod ? block_rows<kE4m3, true> : block_rows<kE4m3, false>)
                                                     : (mod ? block_rows<kInt8, true> : block_rows<kInt8, false>);
-    return launch1(kernel, kBlockRowShares, 64 * kRowWaves, st, a);
+    return launch1(kernel, kBlockRowShares / kRowWaves, 64 * kRowWaves, st, a);
 }
 
 }  // namespace dkv

@@ -363,7 +363,7 @@ def test_single_tokens(fmt, G):
     dict(window=1), dict(window=1, sinks=4), dict(window=45), dict(window=45, sinks=1), dict(window=64, sinks=33),
     dict(window=200, sinks=100), dict(window=10 ** 9, sinks=3), dict(window=33, sinks=10 ** 9), dict(sinks=5), dict(cap=20.0),
     dict(cap=5.0, window=130, sinks=2, slopes=True), dict(slopes=True), dict(window=2 ** 31 - 1, sinks=2 ** 31 - 1)], ids=str)
-@pytest.mark.parametrize("n", [1, 6, 70])
+@pytest.mark.parametrize("n", [1, 6, 70, 300])
 def test_forms(form, n):
     form = dict(form)
     if form.get("slopes"):

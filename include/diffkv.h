@@ -369,7 +369,7 @@ diffkv_status diffkv_rotate(const diffkv_layout* layout, int64_t rows, const int
  * then y is turned as diffkv_rotate turns it (dims rot_dim .. head_dim-1 are
  * normed and pass).
  *   q_weight, k_weight  device fp32 [head_dim], 16-byte aligned, or NULL: ones
- *   eps       above 0 and finite
+ *   eps       finite, at least the smallest normal fp32 (2^-126)
  * The other arguments, in-place calls, limits and errors as diffkv_rotate.  The
  * sum of squares, the norm and all products are fp32, with one rounding to fp16.
  */

@@ -620,7 +620,7 @@ diffkv_status diffkv_norm_rotate(const diffkv_layout* layout, int64_t rows, cons
                                  int64_t q_out_stride, int32_t num_kv_heads, const uint16_t* k, int64_t k_stride,
                                  const float* k_weight, uint16_t* k_out, int64_t k_out_stride, void* stream)
 {
-    if (!(eps > 0.0f) || !isfinite(eps)) return DIFFKV_E_INVAL;
+    if (!(eps >= 1.17549435e-38f) || !isfinite(eps)) return DIFFKV_E_INVAL;
     if (((uintptr_t)q_weight | (uintptr_t)k_weight) % 16 != 0) return DIFFKV_E_INVAL;
     RotateArgs a;
     const diffkv_status s = rotate_call(layout, rows, pos, inv_freq, rot_dim, style, scale, num_q_heads, q, q_stride, q_out,

@@ -77,93 +77,57 @@ __device__ __forceinline__ float get_one(__amdgpu_buffer_rsrc_t r, int lane_offs
 }
 
 // ---- the item of a wave ----------------------------------------------------------------
-// Sequences in order, each with a number of items; a wave goes over them 64 at a time (a lane a
-// sequence) and finds the one that holds a given item.  Loads(b, n, L) gives a sequence's rows and tokens, unclamped;
-// Items(n, L) its items.  Rows are clamped to [0, most] and to the rows left of `total`.
+// Sequences in order, each with a number of items; a wave finds the one that holds a given item, 64 sequences at a time
+// (a lane a sequence).  The last 64 are kept from one search to the next: a call of up to 64 sequences reads their
+// lengths once.  Loads(b, n, L) gives a sequence's rows and tokens, unclamped; rows are clamped to [0, most] and to those
+// left of `total`.  Items(n, L): a sequence's items.
 struct SeqItem {
     int b, n, L;          // b < 0: there is none
     long long row0;       // the sequence's first row
     long long item0;      // and first item
-    bool bad;             // some sequence's length lies outside its range (of those passed)
-    long long items;      // up to the end of those passed: of all, if b < 0
 };
 template <typename Loads, typename Items>
-__device__ __forceinline__ SeqItem find_item(int B, long long total, int most, long long want, Loads loads, Items items)
-{
-    SeqItem s{-1, 0, 0, 0, 0, false, 0};
-    const int lane = lane_id();
-    long long row = 0, item = 0;
-    for (int b0 = 0; b0 < B; b0 += kWave) {
-        const int b = b0 + lane;
-        int n = 0, L = 0;
-        if (b < B) loads(b, n, L);
-        s.bad = s.bad || __ballot(n < 0 || n > most) != 0;
-        n = n < 0 ? 0 : (n > most ? most : n);
-        const long long before = row + (wave_incl_scan_wide(n) - n);
-        const long long room = total - before;
-        s.bad = s.bad || __ballot(n > room && n > 0) != 0;
-        if (n > room) n = room > 0 ? (int)room : 0;
-        const long long it = b < B ? items(n, L) : 0;
-        const long long incl = item + wave_incl_scan_wide(it);
-        const unsigned long long past = __ballot(incl > want);
-        if (past && s.b < 0) {
-            const int l = __builtin_ctzll(past);
-            s.b = b0 + l;
-            s.n = __builtin_amdgcn_readlane(n, l);
-            s.L = __builtin_amdgcn_readlane(L, l);
-            s.row0 = read_lane<long long>(before, l);
-            s.item0 = read_lane<long long>(incl - it, l);
-        }
-        row = read_lane<long long>(before + n, kWave - 1);
-        item = read_lane<long long>(incl, kWave - 1);
-    }
-    s.items = item;
-    return s;
-}
-
-// The same with the lanes' 64 sequences kept from one search to the next: a call of up to 64 reads their lengths once.
-template <typename Args>
 struct SeqScan {
-    const Args& a;
+    int B, most;
+    long long rows;
+    Loads loads;
+    Items items;
+    bool bad = false;                // some length lay outside its range
     int base = -1, n, L;             // the lanes' sequences: base + lane; rows and tokens
-    long long before, incl, items;   // rows before the lane's sequence; items up to its end; its items
+    long long before, incl, count;   // rows before the lane's sequence; items up to its end; its items
     long long row_end, item_end;     // behind the 64
 
-    __device__ __forceinline__ explicit SeqScan(const Args& args) : a(args) {}
-    template <typename Items>
-    __device__ __forceinline__ void load(int from, long long row, long long item, Items count)
+    __device__ __forceinline__ SeqScan(int B_, int most_, long long rows_, Loads l, Items i) : B(B_), most(most_), rows(rows_), loads(l), items(i) {}
+    __device__ __forceinline__ void load(int from, long long row, long long item)
     {
         base = from;
         const int b = base + lane_id();
         n = L = 0;
-        if (b < a.B) {
-            n = a.new_len[b];
-            L = seq_tokens(a, b);
-        }
-        n = n < 0 ? 0 : (n > a.max_new ? a.max_new : n);
+        if (b < B) loads(b, n, L);
+        bad = bad || __ballot(n < 0 || n > most) != 0;
+        n = n < 0 ? 0 : (n > most ? most : n);
         before = row + (wave_incl_scan_wide(n) - n);
-        const long long room = a.total_new - before;
+        const long long room = rows - before;
+        bad = bad || __ballot(n > room && n > 0) != 0;
         if (n > room) n = room > 0 ? (int)room : 0;
-        items = count(n, L);
-        incl = item + wave_incl_scan_wide(items);
+        count = b < B ? items(n, L) : 0;
+        incl = item + wave_incl_scan_wide(count);
         row_end = read_lane<long long>(before + n, kWave - 1);
         item_end = read_lane<long long>(incl, kWave - 1);
     }
-    template <typename Items>
-    __device__ __forceinline__ long long total(Items count)
+    // All sequences' items.
+    __device__ __forceinline__ long long total()
     {
-        load(0, 0, 0, count);
-        while (base + kWave < a.B) load(base + kWave, row_end, item_end, count);
+        load(0, 0, 0);
+        while (base + kWave < B) load(base + kWave, row_end, item_end);
         return item_end;
     }
-    // The sequence that holds item `want`; b < 0: there is none.  Calls go forward from one to the next.
-    template <typename Items>
-    __device__ __forceinline__ SeqItem find(long long want, Items count)
+    // The sequence that holds item `want` (after total()).
+    __device__ __forceinline__ SeqItem find(long long want)
     {
-        const long long first = read_lane<long long>(incl - items, 0);
-        if (want < first) load(0, 0, 0, count);
-        while (want >= item_end && base + kWave < a.B) load(base + kWave, row_end, item_end, count);
-        SeqItem s{-1, 0, 0, 0, 0, false, 0};
+        if (want < read_lane<long long>(incl - count, 0)) load(0, 0, 0);
+        while (want >= item_end && base + kWave < B) load(base + kWave, row_end, item_end);
+        SeqItem s{-1, 0, 0, 0, 0};
         const unsigned long long past = __ballot(incl > want);
         if (past) {
             const int l = __builtin_ctzll(past);
@@ -171,7 +135,7 @@ struct SeqScan {
             s.n = __builtin_amdgcn_readlane(n, l);
             s.L = __builtin_amdgcn_readlane(L, l);
             s.row0 = read_lane<long long>(before, l);
-            s.item0 = read_lane<long long>(incl - items, l);
+            s.item0 = read_lane<long long>(incl - count, l);
         }
         return s;
     }

@@ -124,6 +124,9 @@ __device__ __forceinline__ float put_keys(const Source& src, int first, uint8_t*
     return s.fine ? s.s : __builtin_nanf("");
 }
 
+// From the lane whose number differs by two.
+__device__ __forceinline__ u2 pair_swap(u2 x) { return u2{dpp_u32<0x4E, 0xF>(x[0]), dpp_u32<0x4E, 0xF>(x[1])}; }
+
 // A whole block of values: lane = r * 16 + group of eight dims, which takes the eight tokens of r.
 template <int FMT>
 __device__ __forceinline__ float put_values(const Source& src, int first, uint8_t* to)
@@ -136,18 +139,25 @@ __device__ __forceinline__ float put_values(const Source& src, int first, uint8_
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = top_of(top, x[e]);
     const Scale s = block_scale<FMT>(wave_top(top));
-    uint8_t* at = to + (dg >> 2) * 1024 + r * 256 + (dg & 1) * 128 + ((dg >> 1) & 1) * 8;
+    u2 w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        u2 w = {0, 0};
+        w[i] = u2{0, 0};
         if (s.fine) {
             float f[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] = h2f((x[e][i >> 1] >> ((i & 1) * 16)) & 0xffffu);
-            w[0] = code4<FMT>(f[0], f[1], f[2], f[3], s.inv);
-            w[1] = code4<FMT>(f[4], f[5], f[6], f[7], s.inv);
+            w[i][0] = code4<FMT>(f[0], f[1], f[2], f[3], s.inv);
+            w[i][1] = code4<FMT>(f[4], f[5], f[6], f[7], s.inv);
         }
-        *reinterpret_cast<u2*>(at + i * 16) = w;
+    }
+    // lanes dg and dg ^ 2 have the two halves of eight 16-byte pieces: the lower one takes the first four
+    const bool upper = (dg & 2) != 0;
+    uint8_t* at = to + (dg >> 2) * 1024 + r * 256 + (dg & 1) * 128 + (upper ? 64 : 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const u2 mine = upper ? w[4 + i] : w[i], theirs = pair_swap(upper ? w[i] : w[4 + i]);
+        *reinterpret_cast<u4*>(at + i * 16) = upper ? u4{theirs[0], theirs[1], mine[0], mine[1]} : u4{mine[0], mine[1], theirs[0], theirs[1]};
     }
     return s.fine ? s.s : __builtin_nanf("");
 }
@@ -158,25 +168,28 @@ __device__ __forceinline__ float put_values(const Source& src, int first, uint8_
 template <int FMT>
 __global__ __launch_bounds__(256) void block_append(BlockAppendArgs a)
 {
+    bool over = false;  // of the lane's sequences, some has more tokens than a sequence may
     const auto loads = [&](int b, int& n, int& L) {
         n = a.new_len[b];
         L = a.seq_len[b];
+        over = over || L < 0 || L > a.max_len || (n > 0 && n > a.max_len - L);
     };
     const auto spans = [&](int n, int L) { return n > 0 ? max((long long)((L + (long long)n) / kBT - L / kBT), 1LL) : 0LL; };
-    const auto over = [&](int n, int L) { return (L < 0 || L > a.max_len || n > a.max_len - L) ? 1LL : 0LL; };
+    SeqScan scan(a.B, a.max_new, a.total_new, loads, spans);
+    const long long jobs = scan.total() * 2 * a.Hkv;
     // a call with lengths out of their range changes nothing
-    const SeqItem any = find_item(a.B, a.total_new, a.max_new, 0, loads, over);
-    if (any.bad || any.items) {
-        if (blockIdx.x == 0 && threadIdx.x == 0)
-            atomicOr(a.status, (any.bad ? (unsigned)DIFFKV_ST_BAD_INPUT : 0u) | (any.items ? (unsigned)DIFFKV_ST_TABLE_OVERFLOW : 0u));
+    if (scan.bad || __any(over)) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            if (scan.bad) atomicOr(a.status, (unsigned)DIFFKV_ST_BAD_INPUT);
+            else atomicOr(a.status, (unsigned)DIFFKV_ST_TABLE_OVERFLOW);
+        }
         return;
     }
     const int lane = lane_id();
-    for (long long job = (long long)blockIdx.x * 4 + wave_index();; job += (long long)gridDim.x * 4) {
+    for (long long job = (long long)blockIdx.x * 4 + wave_index(); job < jobs; job += (long long)gridDim.x * 4) {
         const long long want = job / (2 * a.Hkv);
         const int side = (int)(job - want * (2 * a.Hkv)) / a.Hkv, h = (int)(job % a.Hkv);
-        const SeqItem s = find_item(a.B, a.total_new, a.max_new, want, loads, spans);
-        if (s.b < 0) break;
+        const SeqItem s = scan.find(want);
         const int first = s.L / kBT, whole = (s.L + s.n) / kBT - first, i = (int)(want - s.item0);
         uint16_t* tail = a.tail + (((long long)s.b * a.Hkv + h) * 2 + side) * kBlockSide;
         const Source src{tail, a.in[side] + s.row0 * a.in_stride[side] + h * kD, a.in_stride[side], s.L};
@@ -229,15 +242,14 @@ __global__ __launch_bounds__(256) void block_read(BlockReadArgs a)
         L = a.start[b];
     };
     // (a range's first and last position in 64 bits: any start is allowed)
-    const auto spans = [&](int n, int L) {
-        return n > 0 ? (((long long)L + n - 1) >> 5) - ((long long)L >> 5) + 1 : 0LL;
-    };
+    const auto spans = [&](int n, int L) { return n > 0 ? (((long long)L + n - 1) >> 5) - ((long long)L >> 5) + 1 : 0LL; };
+    SeqScan scan(a.B, a.max_count, a.total, loads, spans);
+    const long long jobs = scan.total() * 2 * a.Hkv;
     const int lane = lane_id();
-    for (long long job = (long long)blockIdx.x * 4 + wave_index();; job += (long long)gridDim.x * 4) {
+    for (long long job = (long long)blockIdx.x * 4 + wave_index(); job < jobs; job += (long long)gridDim.x * 4) {
         const long long want = job / (2 * a.Hkv);
         const int side = (int)(job - want * (2 * a.Hkv)) / a.Hkv, h = (int)(job % a.Hkv);
-        const SeqItem s = find_item(a.B, a.total, a.max_count, want, loads, spans);
-        if (s.b < 0) break;
+        const SeqItem s = scan.find(want);
         const int held = seq_tokens(a, s.b);
         const long long tile = ((long long)s.L >> 5) + (want - s.item0), pos0 = tile * kBT;
         const long long lo = s.L, hi = (long long)s.L + s.n;
@@ -252,28 +264,29 @@ __global__ __launch_bounds__(256) void block_read(BlockReadArgs a)
             const uint8_t* from = a.pool + (((long long)id * a.Hkv + h) * 2 + side) * kBlockSide;
             const float scale = a.scale[((long long)id * a.Hkv + h) * 2 + side];
             if (side == 0) {
-                const int c = lane & 7, t = lane >> 3;
-                u4 w[4];
+                // lane: eight dims of a token, so that 16 lanes write a whole row
+                const int c = lane & 15, t = lane >> 4;
+                u2 w[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int token = t + 8 * i;
-                    w[i] = *reinterpret_cast<const u4*>(from + (token >> 4) * 2048 + c * 256 + (token & 15) * 16);
+                for (int i = 0; i < 8; ++i) {
+                    const int token = t + 4 * i;
+                    w[i] = *reinterpret_cast<const u2*>(from + (token >> 4) * 2048 + (c >> 1) * 256 + (token & 15) * 16 + (c & 1) * 8);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const uint32_t x = w[i][2 * j], y = w[i][2 * j + 1];
-                        put(t + 8 * i, c * 16 + j * 8,
-                            u4{value2<FMT>(x, 0, scale), value2<FMT>(x, 1, scale), value2<FMT>(y, 0, scale), value2<FMT>(y, 1, scale)});
-                    }
-                }
+                for (int i = 0; i < 8; ++i)
+                    put(t + 4 * i, c * 8, u4{value2<FMT>(w[i][0], 0, scale), value2<FMT>(w[i][0], 1, scale), value2<FMT>(w[i][1], 0, scale), value2<FMT>(w[i][1], 1, scale)});
             } else {
                 const int dg = lane & 15, r = lane >> 4;
-                const uint8_t* at = from + (dg >> 2) * 1024 + r * 256 + (dg & 1) * 128 + ((dg >> 1) & 1) * 8;
-                u2 w[8];  // dim i: tokens 0 .. 7 of r
+                const bool upper = (dg & 2) != 0;
+                const uint8_t* at = from + (dg >> 2) * 1024 + r * 256 + (dg & 1) * 128 + (upper ? 64 : 0);
+                u2 w[8];  // dim i: tokens 0 .. 7 of r; lanes dg and dg ^ 2 read half of both's pieces each
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const u2*>(at + i * 16);
+                for (int i = 0; i < 4; ++i) {
+                    const u4 x = *reinterpret_cast<const u4*>(at + i * 16);
+                    const u2 lo = {x[0], x[1]}, hi = {x[2], x[3]}, theirs = pair_swap(upper ? lo : hi);
+                    w[i] = upper ? theirs : lo;
+                    w[4 + i] = upper ? hi : theirs;
+                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     u4 y;

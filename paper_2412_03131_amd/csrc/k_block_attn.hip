@@ -267,6 +267,13 @@ __device__ __forceinline__ RowSource row_source(const BlockAttnArgs& a, const Se
                      {a.k + sq.row0 * a.k_stride + h * kD, a.v + sq.row0 * a.v_stride + h * kD},
                      {a.k_stride, a.v_stride}, sq.L, sq.L + sq.n};
 }
+__device__ __forceinline__ auto lengths_of(const BlockAttnArgs& a)
+{
+    return [&a](int b, int& n, int& L) {
+        n = a.new_len[b];
+        L = seq_tokens(a, b);
+    };
+}
 // Steps whose tiles are blocks of the cache: they come first.
 __device__ __forceinline__ int coded_steps(const Tiles& tl, int L)
 {
@@ -293,7 +300,6 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void block_rows(BlockAttnArgs a)
 {
     __shared__ uint8_t staged[kRowWaves][2 * kBlockSide];  // a wave's tile of fp16 values
     const int lane = lane_id(), wave = wave_index(), r = lane >> 4, col = lane & 15;
-    SeqScan<BlockAttnArgs> scan(a);
     // units of a sequence: those of its blocks of rows
     const auto block_units = [&](const Tiles& tl, int L) {
         const int coded = coded_steps(tl, L);
@@ -302,7 +308,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void block_rows(BlockAttnArgs a)
     const auto units = [&](int n, int L) {
         return n > 0 && n * a.G <= a.few_rows ? (long long)a.Hkv * ((n * a.G + 15) / 16) * block_units(tiles_of(a, n, L), L) : 0LL;
     };
-    const long long all = scan.total(units);
+    SeqScan scan(a.B, a.max_new, a.total_new, lengths_of(a), units);
+    const long long all = scan.total();
     const int shares = (int)gridDim.x * kRowWaves;
     const long long share = max((all + shares - 1) / shares, (long long)kRowShare);
     // (workgroup i runs on XCD i % 8: pieces that follow each other share an L2)
@@ -311,7 +318,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void block_rows(BlockAttnArgs a)
     const long long x_end = min(x + share, all);
 
     while (x < x_end) {
-        const SeqItem sq = scan.find(x, units);
+        const SeqItem sq = scan.find(x);
         if (sq.b < 0) break;
         const Tiles tl = tiles_of(a, sq.n, sq.L);
         const int steps = tl.count(), coded = coded_steps(tl, sq.L), blk_units = block_units(tl, sq.L);
@@ -621,13 +628,13 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
 {
     __shared__ TileLds lds;
     const int lane = lane_id(), wave = wave_index(), half = lane >> 5, col = lane & 31;
-    SeqScan<BlockAttnArgs> scan(a);
     const auto units = [&](int n, int L) {
         if (n <= 0 || n * a.G <= a.few_rows) return 0LL;
         const TileUnits u = tile_units(a, n, L);
         return a.Hkv * u.upto(u.blocks);
     };
-    const long long all = scan.total(units);
+    SeqScan scan(a.B, a.max_new, a.total_new, lengths_of(a), units);
+    const long long all = scan.total();
     const long long share = max((all + gridDim.x - 1) / gridDim.x, (long long)kTileShare);
     // (workgroup i runs on XCD i % 8)
     const int me = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
@@ -635,7 +642,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
     const long long x_end = min(x + share, all);
 
     while (x < x_end) {
-        const SeqItem sq = scan.find(x, units);
+        const SeqItem sq = scan.find(x);
         if (sq.b < 0) break;
         const TileUnits tu = tile_units(a, sq.n, sq.L);
         const long long head_units = tu.upto(tu.blocks);

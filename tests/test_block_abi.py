@@ -163,7 +163,7 @@ def norm_rotate(dk, **c):
                                  dict(rot=33), dict(rot=144), dict(style=2), dict(Hq=0), dict(Hkv=-1), dict(Hkv=0),
                                  dict(k=None), dict(ko=None), dict(q=None), dict(qo=None), dict(q=FAKE + 2),
                                  dict(qs=504), dict(qs=516), dict(kos=64), dict(qos=1024), dict(kos=256), dict(eps=0.0),
-                                 dict(eps=-1e-6), dict(eps=math.nan), dict(eps=math.inf), dict(qw=FAKE + 4), dict(kw=FAKE + 8)],
+                                 dict(eps=-1e-6), dict(eps=1e-39), dict(eps=math.nan), dict(eps=math.inf), dict(qw=FAKE + 4), dict(kw=FAKE + 8)],
                          ids=str)
 def test_refused_norms(dk, bad):
     assert norm_rotate(dk, **bad) == dk.E_INVAL

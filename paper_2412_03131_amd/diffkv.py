@@ -462,15 +462,12 @@ def chunk_significance(cache, new_len, q, k, sm_scale, lse, cap=0.0, window=0, s
     return score
 
 
-_BLOCK_CACHE = struct.Struct("PPqPPPPiii")
-assert _BLOCK_CACHE.size <= C.sizeof(BlockCacheStruct)
-
-
 class BlockCache:
     """Device tensors of one uniform 8-bit cache (diffkv_block_cache); the library owns none of them.  `table` int32
     [num_seqs, ceil(max_seq_len / 32)] (block IDs, -1: not kept) and `seq_len` int32 [num_seqs] are the program's to
     write.  `buffers`: (pool, scale, table, tail, seq_len, status) to use instead of new ones (caches of a model's
-    layers share table and seq_len)."""
+    layers share table and seq_len).  The tensors are the handle's for its life: their contents may be written, but
+    others need another handle."""
 
     def __init__(self, L, num_blocks, num_seqs, num_kv_heads, fmt=BLOCK_E4M3, device="cuda", buffers=None):
         self.L = L
@@ -486,49 +483,67 @@ class BlockCache:
                        torch.full((self.num_seqs, width), -1, dtype=torch.int32, device=dev),
                        z(self.num_seqs, self.num_kv_heads, 2, BLOCK_TOKENS, D, dtype=torch.float16),
                        z(self.num_seqs, dtype=torch.int32), z(1, dtype=torch.int32))
-        self.pool, self.scale, self.table, self.tail, self.seq_len, self.status = buffers
+        self._tensors = tuple(buffers)
+        pool, scale, table, tail, seq_len, status = self._tensors
         for t, what, dtype, shape in (
-                (self.pool, "pool", torch.uint8, (self.num_blocks, self.num_kv_heads, 2, BLOCK_TOKENS * D)),
-                (self.scale, "scale", torch.float32, (self.num_blocks, self.num_kv_heads, 2))):
+                (pool, "pool", torch.uint8, (self.num_blocks, self.num_kv_heads, 2, BLOCK_TOKENS * D)),
+                (scale, "scale", torch.float32, (self.num_blocks, self.num_kv_heads, 2))):
             if t.dtype != dtype or not t.is_contiguous() or t.shape[0] < shape[0] or t.shape[1:] != shape[1:]:
                 raise ValueError("%s: contiguous %s %s expected" % (what, dtype, list(shape)))
-        _dense(self.table, "table", torch.int32, self.num_seqs, width)
-        _dense(self.tail, "tail", torch.float16, self.num_seqs, self.num_kv_heads, 2, BLOCK_TOKENS, D)
-        _dense(self.seq_len, "seq_len", torch.int32, self.num_seqs)
-        _dense(self.status, "status", torch.int32, 1)
+        _dense(table, "table", torch.int32, self.num_seqs, width)
+        _dense(tail, "tail", torch.float16, self.num_seqs, self.num_kv_heads, 2, BLOCK_TOKENS, D)
+        _dense(seq_len, "seq_len", torch.int32, self.num_seqs)
+        _dense(status, "status", torch.int32, 1)
+        if any(t.device != pool.device for t in self._tensors):
+            raise ValueError("BlockCache: tensors on one device expected")
+        self._struct = BlockCacheStruct(pool.data_ptr(), scale.data_ptr(), self.num_blocks, table.data_ptr(),
+                                        tail.data_ptr(), seq_len.data_ptr(), status.data_ptr(), self.num_seqs,
+                                        self.num_kv_heads, self.fmt)
+
+    def _same(self, i, t):  # (what `cache.seq_len += n` ends with)
+        if t is not self._tensors[i]:
+            raise AttributeError("a BlockCache's tensors are its handle's for life: write into them, or make another")
+
+    pool, scale, table, tail, seq_len, status = (
+        property(lambda self, i=i: self._tensors[i], lambda self, t, i=i: self._same(i, t)) for i in range(6))
 
     def tensors(self):
-        return self.pool, self.scale, self.table, self.tail, self.seq_len, self.status
+        return self._tensors
 
     def struct(self):
-        return BlockCacheStruct.from_buffer_copy(_BLOCK_CACHE.pack(
-            self.pool.data_ptr(), self.scale.data_ptr(), self.num_blocks, self.table.data_ptr(), self.tail.data_ptr(),
-            self.seq_len.data_ptr(), self.status.data_ptr(), self.num_seqs, self.num_kv_heads,
-            self.fmt).ljust(C.sizeof(BlockCacheStruct), b"\0"))
+        return self._struct
 
 
-def _block_rows(cache, lens, most, what, *rows):
-    """Checked lengths and rows of a uniform cache's call; the longest length."""
-    for t in (lens if isinstance(lens, tuple) else (lens,)):
-        if t.dtype != torch.int32 or t.shape != (cache.num_seqs,) or not t.is_contiguous():
-            raise ValueError("%s: lengths: contiguous int32 [num_seqs] expected" % what)
-        last = t
-    if most is None:
-        most = int(last.max().item()) if last.shape[0] else 0
-    for t in rows:
-        if t.shape[0] != rows[0].shape[0] or t.shape[1] != cache.num_kv_heads:
-            raise ValueError("%s: [rows, num_kv_heads, head_dim] keys and values expected" % what)
-    return int(most)
+def _block_lens(cache, t, what):
+    if t.dtype != torch.int32 or t.shape != (cache.num_seqs,) or not t.is_contiguous():
+        raise ValueError("%s: lengths: contiguous int32 [num_seqs] expected" % what)
+
+
+def _block_rows(cache, k, v, what, rows):
+    """Addresses and row strides of keys and values [rows, num_kv_heads, head_dim]."""
+    D = cache.L.head_dim
+    kp, ks = _rows(k, "k", D)
+    vp, vs = _rows(v, "v", D)
+    if k.shape != (rows, cache.num_kv_heads, D) or v.shape != k.shape:
+        raise ValueError("%s: [rows, num_kv_heads, head_dim] keys and values expected" % what)
+    return kp, ks, vp, vs
+
+
+def _longest(lens):
+    return int(lens.max().item()) if lens.shape[0] else 0
 
 
 def block_append(cache, new_len, k, v, max_new=None, stream=None):
     """diffkv_block_append: k, v fp16 [rows, Hkv, D] (device, rows concatenated per sequence, may be strided), new_len
     int32 [B] (device), into cache (a BlockCache) at seq_len, which is not advanced."""
-    max_new = _block_rows(cache, new_len, max_new, "block_append", k, v)
-    (kp, ks), (vp, vs) = (_rows(t, w, cache.L.head_dim) for t, w in ((k, "k"), (v, "v")))
-    _on_one_gpu("block_append", k, v, new_len, *cache.tensors())
-    _check(lib().diffkv_block_append(C.byref(cache.L), cache.struct(), k.shape[0], max_new, _ptr(new_len), kp, ks, vp,
-                                     vs, _stream(stream)), "diffkv_block_append")
+    _block_lens(cache, new_len, "block_append")
+    rows = k.shape[0]
+    kv = _block_rows(cache, k, v, "block_append", rows)
+    _on_one_gpu("block_append", k, v, new_len, cache.pool)
+    if max_new is None:
+        max_new = _longest(new_len)
+    _check(lib().diffkv_block_append(cache.L, cache.struct(), rows, int(max_new), new_len.data_ptr(), *kv, _stream(stream)),
+           "diffkv_block_append")
 
 
 def block_read(cache, start, count, total, max_count=None, k_out=None, v_out=None, stream=None):
@@ -537,13 +552,14 @@ def block_read(cache, start, count, total, max_count=None, k_out=None, v_out=Non
     shape = (int(total), cache.num_kv_heads, cache.L.head_dim)
     k_out, v_out = (torch.empty(shape, dtype=torch.float16, device=cache.tail.device) if t is None else t
                     for t in (k_out, v_out))
-    if k_out.shape != shape or v_out.shape != shape:
-        raise ValueError("block_read: outputs [total, num_kv_heads, head_dim] expected")
-    max_count = _block_rows(cache, (start, count), max_count, "block_read", k_out, v_out)
-    (kp, ks), (vp, vs) = (_rows(t, w, cache.L.head_dim) for t, w in ((k_out, "k_out"), (v_out, "v_out")))
-    _on_one_gpu("block_read", k_out, v_out, start, count, *cache.tensors())
-    _check(lib().diffkv_block_read(C.byref(cache.L), cache.struct(), shape[0], max_count, _ptr(start), _ptr(count), kp,
-                                   ks, vp, vs, _stream(stream)), "diffkv_block_read")
+    _block_lens(cache, start, "block_read")
+    _block_lens(cache, count, "block_read")
+    kv = _block_rows(cache, k_out, v_out, "block_read", shape[0])
+    _on_one_gpu("block_read", k_out, v_out, start, count, cache.pool)
+    if max_count is None:
+        max_count = _longest(count)
+    _check(lib().diffkv_block_read(cache.L, cache.struct(), shape[0], int(max_count), start.data_ptr(), count.data_ptr(), *kv,
+                                   _stream(stream)), "diffkv_block_read")
     return k_out, v_out
 
 
@@ -553,9 +569,9 @@ def block_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, sinks=
     may be strided), new_len int32 [B] (device) over cache (a BlockCache) -> out fp16 [rows, Hq, D], lse fp32
     [rows, Hq].  With a window the first `sinks` tokens stay visible.  Call it before the rows are appended."""
     rows, Hq, D = q.shape
-    max_new = _block_rows(cache, new_len, max_new, "block_attention", k, v)
-    if k.shape[0] != rows:
-        raise ValueError("block_attention: as many rows of keys and values as of queries expected")
+    _block_lens(cache, new_len, "block_attention")
+    kv = _block_rows(cache, k, v, "block_attention", rows)
+    qp, qs = _rows(q, "q", cache.L.head_dim)
     if out is None:
         out = torch.empty((rows, Hq, D), dtype=torch.float16, device=q.device)
     if lse is None and want_lse:
@@ -566,11 +582,12 @@ def block_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, sinks=
     sizes = (OP_BLOCK_ATTENTION, cache.L, cache.num_seqs, Hq, cache.num_kv_heads, rows)
     if ws is None:
         ws = _new_ws(workspace_size(*sizes), q.device)
-    (qp, qs), (kp, ks), (vp, vs) = (_rows(t, w, cache.L.head_dim) for t, w in ((q, "q"), (k, "k"), (v, "v")))
-    _on_one_gpu("block_attention", q, k, v, new_len, slopes, out, lse, ws, *cache.tensors())
+    _on_one_gpu("block_attention", q, k, v, new_len, slopes, out, lse, ws, cache.pool)
+    if max_new is None:
+        max_new = _longest(new_len)
     _check_ws(lib().diffkv_block_attention(
-        C.byref(cache.L), cache.struct(), rows, max_new, _ptr(new_len), Hq, qp, qs, kp, ks, vp, vs, float(sm_scale),
-        _form(cap, window, slopes), int(sinks), _ptr(out), _ptr(lse), ws.data_ptr(), ws.nbytes, _stream(stream)),
+        cache.L, cache.struct(), rows, int(max_new), new_len.data_ptr(), Hq, qp, qs, *kv, float(sm_scale),
+        _form(cap, window, slopes), int(sinks), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes, _stream(stream)),
         "diffkv_block_attention", *sizes)
     return out, lse
 

@@ -148,6 +148,10 @@ def test_binding_checks_its_tensors(dk):
                    (5, t[5].long())):
         with pytest.raises(ValueError):
             dk.BlockCache(L, 16, 2, 2, buffers=t[:i] + [bad] + t[i + 1:])
+    c.seq_len += 3  # (in place: the same tensor)
+    assert c.seq_len.tolist() == [3, 3] and c.seq_len is t[4]
+    with pytest.raises(AttributeError):
+        c.seq_len = torch.zeros(2, dtype=torch.int32)
 
 
 def norm_rotate(dk, **c):

@@ -980,7 +980,9 @@ hipError_t launch_block_attention(const BlockAttnArgs& a, int format, bool mod, 
     if ((long long)a.max_new * a.G > a.few_rows) {
         void (*kernel)(BlockAttnArgs) = format == kE4m3 ? (mod ? block_tiles<kE4m3, true> : block_tiles<kE4m3, false>)
                                                         : (mod ? block_tiles<kInt8, true> : block_tiles<kInt8, false>);
-        const hipError_t e = launch1(kernel, kBlockTileShares, 64 * kTileWaves, st, a);
+        BlockAttnArgs t = a;
+        if (a.B == 1) t.few_rows = 0;  // (a lone sequence is this kernel's, also where it has less rows than max_new says)
+        const hipError_t e = launch1(kernel, kBlockTileShares, 64 * kTileWaves, st, t);
         if (e != hipSuccess || a.B == 1) return e;
     }
     void (*kernel)(BlockAttnArgs) = format == kE4m3 ? (mod ? block_rows<kE4m3, true> : block_rows<kE4m3, false>)

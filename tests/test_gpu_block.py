@@ -534,6 +534,21 @@ def test_padded_batch_and_strides():
         assert (out[2 * n:] == 5).all() and (lse[2 * n:] == 5).all()
 
 
+@pytest.mark.parametrize("n", [0, 1, 5, 63, 64, 65])
+def test_a_lone_sequence_with_less_rows_than_max_new(n):
+    rng = np.random.default_rng(24)
+    plain = plain_of(rng, [100], 2, INT8)
+    c = ref.filled(dk, plain, 800, DEV)
+    q, k, v = rows_of(rng, 400, 8, 2)
+    out = torch.full((400, 8, D), 5.0, dtype=torch.float16, device=DEV)
+    lse = torch.full((400, 8), 5.0, device=DEV)
+    dk.block_attention(c, ints([n]), q, k, v, SCALE, out=out, lse=lse, max_new=400)
+    torch.cuda.synchronize()
+    if n:
+        check(plain, c, [n], q[:n], k[:n], v[:n], out[:n], lse[:n], "padded")
+    assert (out[n:] == 5).all() and (lse[n:] == 5).all()
+
+
 def test_lengths_out_of_range_are_clamped():
     rng = np.random.default_rng(18)
     plain = plain_of(rng, [70, 40, 33], 2, INT8)

@@ -596,7 +596,7 @@ diffkv_status diffkv_block_read(const diffkv_layout* layout, const diffkv_block_
  *            needed, 16-byte aligned; calls that may overlap need one each
  *            (strides of k and v at most 2^24)
  * The cache is read only.  Up to 64 query heads per KV head, head_dim 128, total_new
- * up to 2^24, max_seq_len up to 2^30, up to 2^22 (sequence, KV head) pairs
+ * up to 2^23, max_seq_len up to 2^30, up to 2^22 (sequence, KV head) pairs
  * (DIFFKV_E_UNSUPPORTED otherwise).  seq_len counts clamped to [0, max_seq_len].
  * Scores x up to 2^22 in magnitude, the slopes' part included.
  * Precision: codes enter the products exactly, and the weights in two fp16 parts (2^-22, or 2^-37 of

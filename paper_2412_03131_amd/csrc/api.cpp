@@ -312,6 +312,7 @@ diffkv_status rotate_call(const diffkv_layout* layout, int64_t rows, const int32
 
 // What the uniform cache's entry points check, and its arguments.
 constexpr int64_t kMaxBlockRows = (int64_t)1 << 24;
+constexpr int64_t kMaxBlockAttnRows = (int64_t)1 << 23;  // (units of a sequence's blocks of rows: products stay below 2^62)
 constexpr int32_t kMaxBlockLen = 1 << 30;
 constexpr int32_t kMaxBlockGroup = 64;  // query heads per KV head: a sequence's rows stay within 31 bits
 diffkv_status block_call(const diffkv_layout* layout, const diffkv_block_cache* c, int64_t rows, int32_t max_rows,
@@ -440,7 +441,7 @@ diffkv_status diffkv_workspace_size(int32_t op, const diffkv_layout* layout, int
                      : (size_t)kScoreBytes;
         return DIFFKV_OK;
     case DIFFKV_OP_BLOCK_ATTENTION:
-        if (num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || total_new < 0 || total_new > kMaxBlockRows)
+        if (num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || total_new < 0 || total_new > kMaxBlockAttnRows)
             return DIFFKV_E_INVAL;
         *bytes = (size_t)block_attention_ws(num_q_heads / num_kv_heads, total_new);
         return DIFFKV_OK;
@@ -764,7 +765,7 @@ diffkv_status diffkv_block_attention(const diffkv_layout* layout, const diffkv_b
     if (s != DIFFKV_OK) return s;
     if (num_q_heads <= 0 || num_q_heads % a.Hkv != 0 || sinks < 0) return DIFFKV_E_INVAL;
     if (!(sm_scale > 0.0f) || sm_scale > kMaxChunkScale || !form_valid(form)) return DIFFKV_E_INVAL;
-    if (num_q_heads / a.Hkv > kMaxBlockGroup) return DIFFKV_E_UNSUPPORTED;
+    if (num_q_heads / a.Hkv > kMaxBlockGroup || total_new > kMaxBlockAttnRows) return DIFFKV_E_UNSUPPORTED;
     if (a.B == 0 || total_new == 0 || max_new == 0) return DIFFKV_OK;
     if (!new_len || !rows_valid(q, q_stride, num_q_heads, total_new) || !rows_valid(k, k_stride, a.Hkv, total_new) ||
         !rows_valid(v, v_stride, a.Hkv, total_new))

@@ -601,6 +601,7 @@ struct TileUnits {
     long long first, most;   // units of block 0, of those from `full` on
     __device__ __forceinline__ long long upto(long long t) const
     {
+        // (up to 2^23 tokens of up to 64 heads: g <= 2^22, and most - first <= 2^18, so the product is below 2^62)
         const long long g = t < full ? t : full;
         return first * g + (most - first) * g * (g - 1) / (2 * (long long)max(full, 1)) + most * (t - g);
     }

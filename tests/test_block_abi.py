@@ -86,7 +86,8 @@ def test_not_implemented(dk):
         assert f(dk, seqs=(1 << 21) + 1) == dk.E_UNSUPPORTED
     assert attention(dk, Hq=130, qs=130 * 128) == dk.E_UNSUPPORTED
     assert attention(dk, Hq=128, qs=128 * 128) == dk.E_WORKSPACE
-    assert attention(dk, total=1 << 24) == dk.E_WORKSPACE
+    assert attention(dk, total=(1 << 23) + 1) == dk.E_UNSUPPORTED  # (its units of work would pass 64 bits)
+    assert attention(dk, total=1 << 23) == dk.E_WORKSPACE
 
 
 def test_nothing_to_do(dk):
@@ -105,11 +106,11 @@ def test_a_single_row_has_any_stride(dk, stride):
 def test_workspace(dk):
     L = dk.layout(max_seq_len=8192)
     for G, Hkv in ((1, 1), (4, 8), (8, 8), (64, 2)):
-        need = [dk.workspace_size(dk.OP_BLOCK_ATTENTION, L, 64, G * Hkv, Hkv, rows) for rows in (0, 1, 64, 500, 4000, 1 << 24)]
+        need = [dk.workspace_size(dk.OP_BLOCK_ATTENTION, L, 64, G * Hkv, Hkv, rows) for rows in (0, 1, 64, 500, 4000, 1 << 23)]
         assert need == sorted(need) and need[-1] < 192 << 20  # (one for more rows serves fewer)
         for seqs in (1, 1000):
             assert dk.workspace_size(dk.OP_BLOCK_ATTENTION, L, seqs, G * Hkv, Hkv, 500) == need[3]
-    for bad in ((0, 1, 1), (4, 0, 1), (4, 8, 1), (8, 2, -1), (8, 2, (1 << 24) + 1)):
+    for bad in ((0, 1, 1), (4, 0, 1), (4, 8, 1), (8, 2, -1), (8, 2, (1 << 23) + 1)):
         with pytest.raises(dk.DiffKVError) as e:
             dk.workspace_size(dk.OP_BLOCK_ATTENTION, L, 1, *bad)
         assert e.value.code == dk.E_INVAL

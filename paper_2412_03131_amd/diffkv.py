@@ -333,6 +333,13 @@ def _on_one_gpu(what, *tensors):
             raise ValueError("%s: tensors on one GPU expected" % what)
 
 
+def _stream_at(what, stream, t):
+    """A stream's address; it has to be one of the GPU that t is on (a kernel runs where its stream is)."""
+    if (torch._C._cuda_getDevice() if stream is None else stream.device.index) != t.get_device():
+        raise ValueError("%s: a stream of the tensors' GPU expected (None: the current GPU's)" % what)
+    return _stream(stream)
+
+
 def _form(cap, window, slopes):
     if cap == 0.0 and window == 0 and slopes is None:
         return None
@@ -393,7 +400,7 @@ def norm_rotate(L, pos, inv_freq, q, k=None, q_weight=None, k_weight=None, eps=1
     _on_one_gpu("norm_rotate", q, k, pos, inv_freq, q_weight, k_weight, q_out, k_out)
     _check(lib().diffkv_norm_rotate(C.byref(L), rows, _ptr(pos), _ptr(inv_freq), 2 * inv_freq.shape[0], int(style),
                                     float(scale), float(eps), q.shape[1], qp, qs, _ptr(q_weight), qop, qos, Hkv, kp, ks,
-                                    _ptr(k_weight), kop, kos, _stream(stream)), "diffkv_norm_rotate")
+                                    _ptr(k_weight), kop, kos, _stream_at("norm_rotate", stream, q)), "diffkv_norm_rotate")
     return q_out, k_out
 
 
@@ -542,8 +549,8 @@ def block_append(cache, new_len, k, v, max_new=None, stream=None):
     _on_one_gpu("block_append", k, v, new_len, cache.pool)
     if max_new is None:
         max_new = _longest(new_len)
-    _check(lib().diffkv_block_append(cache.L, cache.struct(), rows, int(max_new), new_len.data_ptr(), *kv, _stream(stream)),
-           "diffkv_block_append")
+    _check(lib().diffkv_block_append(cache.L, cache.struct(), rows, int(max_new), new_len.data_ptr(), *kv,
+                                     _stream_at("block_append", stream, k)), "diffkv_block_append")
 
 
 def block_read(cache, start, count, total, max_count=None, k_out=None, v_out=None, stream=None):
@@ -559,7 +566,7 @@ def block_read(cache, start, count, total, max_count=None, k_out=None, v_out=Non
     if max_count is None:
         max_count = _longest(count)
     _check(lib().diffkv_block_read(cache.L, cache.struct(), shape[0], int(max_count), start.data_ptr(), count.data_ptr(), *kv,
-                                   _stream(stream)), "diffkv_block_read")
+                                   _stream_at("block_read", stream, k_out)), "diffkv_block_read")
     return k_out, v_out
 
 
@@ -587,8 +594,8 @@ def block_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, sinks=
         max_new = _longest(new_len)
     _check_ws(lib().diffkv_block_attention(
         cache.L, cache.struct(), rows, int(max_new), new_len.data_ptr(), Hq, qp, qs, *kv, float(sm_scale),
-        _form(cap, window, slopes), int(sinks), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes, _stream(stream)),
-        "diffkv_block_attention", *sizes)
+        _form(cap, window, slopes), int(sinks), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes,
+        _stream_at("block_attention", stream, q)), "diffkv_block_attention", *sizes)
     return out, lse
 
 

@@ -519,6 +519,86 @@ def test_values_that_are_not_finite(bad, n):
         assert torch.equal(out[:n][free], out0[:n][free]) and torch.equal(out[n:], out0[n:]), where
 
 
+@pytest.mark.parametrize("n", [6, 200])
+def test_queries_that_are_not_finite(n):
+    """A NaN or infinite query is its own row's alone."""
+    rng = np.random.default_rng(23)
+    plain = plain_of(rng, [75, 64], 1, INT8)
+    c = ref.filled(dk, plain, 400, DEV)
+    q, k, v = (x.clone() for x in rows_of(rng, 2 * n, 4, 1))
+    want, want_lse = dk.block_attention(c, ints([n, n]), q, k, v, SCALE)
+    q[3, 1, 5], q[n + 1, 0, 9] = float("nan"), float("inf")
+    out, lse = dk.block_attention(c, ints([n, n]), q, k, v, SCALE)
+    torch.cuda.synchronize()
+    hit = torch.zeros((2 * n, 4), dtype=torch.bool, device=DEV)
+    hit[3, 1] = hit[n + 1, 0] = True
+    assert torch.isnan(out[hit]).all()
+    assert torch.equal(out[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
+
+
+def test_nothing_to_do_and_nothing_kept():
+    """No rows, no blocks, a sequence's tail alone, no lse."""
+    c = dk.BlockCache(dk.layout(max_seq_len=100), 0, 2, 1, device=DEV)
+    rng = np.random.default_rng(25)
+    plain = ref.Plain(2, 1, E4M3)
+    q, k, v = rows_of(rng, 5, 2, 1)
+    dk.block_append(c, ints([4, 1]), k, v)
+    plain.append([4, 1], k.cpu().numpy(), v.cpu().numpy())
+    c.seq_len += ints([4, 1])
+    kb, vb = dk.block_read(c, ints([0, 0]), ints([4, 1]), 5)
+    out, lse = dk.block_attention(c, ints([2, 3]), q, k, v, SCALE)
+    alone, none = dk.block_attention(c, ints([2, 3]), q, k, v, SCALE, want_lse=False)
+    torch.cuda.synchronize()
+    assert torch.equal(kb, k) and torch.equal(vb, v) and none is None and torch.equal(alone, out)
+    check(plain, c, [2, 3], q, k, v, out, lse, "tails")
+    out, lse = dk.block_attention(c, ints([0, 0]), q[:0], k[:0], v[:0], SCALE)
+    assert out.shape == (0, 2, D) and lse.shape == (0, 2)
+    dk.block_append(c, ints([0, 0]), k, v)
+    kb, _ = dk.block_read(c, ints([3, 0]), ints([0, 0]), 0)
+    torch.cuda.synchronize()
+    assert kb.shape == (0, 1, D) and int(c.status) == 0 and c.seq_len.tolist() == [4, 1]
+
+
+def test_two_calls_at_once():
+    """Attention on two streams, each with its own workspace, over one cache."""
+    rng = np.random.default_rng(26)
+    plain = plain_of(rng, [900, 300], 2, E4M3)
+    c = ref.filled(dk, plain, 1200, DEV)
+    rows = [rows_of(rng, 2 * n, 8, 2) for n in (1, 150)]
+    want = [dk.block_attention(c, ints([n, n]), *x, SCALE) for n, x in zip((1, 150), rows)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in rows]
+    lens = [ints([1, 1]), ints([150, 150])]
+    sizes = [dk.workspace_size(dk.OP_BLOCK_ATTENTION, c.L, 2, 8, 2, len(x[0])) for x in rows]
+    ws = [torch.zeros(s, dtype=torch.uint8, device=DEV) for s in sizes]
+    got = [[], []]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            out, lse = torch.empty_like(want[i][0]), torch.empty_like(want[i][1])
+            dk.block_attention(c, lens[i], *rows[i], SCALE, out=out, lse=lse, max_new=(1, 150)[i], ws=ws[i], stream=s)
+            got[i].append((out, lse))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(o, want[i][0]) and torch.equal(e, want[i][1]) for o, e in got[i])
+
+
+def test_a_stream_of_another_gpu_is_refused():
+    c = dk.BlockCache(dk.layout(max_seq_len=64), 4, 1, 1, device=DEV)
+    k = torch.zeros((1, 1, D), dtype=torch.float16, device=DEV)
+
+    class Elsewhere:
+        device, cuda_stream = torch.device("cuda", 1), 0
+
+    freq = dk.rope_frequencies(128)[0].to(DEV)
+    for call in (lambda s: dk.block_append(c, ints([1]), k, k, stream=s),
+                 lambda s: dk.block_read(c, ints([0]), ints([1]), 1, stream=s),
+                 lambda s: dk.block_attention(c, ints([1]), k, k, k, SCALE, stream=s),
+                 lambda s: dk.norm_rotate(c.L, ints([1]), freq, k, stream=s)):
+        with pytest.raises(ValueError, match="stream"):
+            call(Elsewhere())
+
+
 def test_padded_batch_and_strides():
     """Rows behind the last sequence's are left as they were; a single row has any stride."""
     rng = np.random.default_rng(17)

@@ -380,7 +380,8 @@ struct BlockAttnArgs : BlockCacheArgs {
     unsigned long long* tile_arrive;  // many rows: the same
     float* tile_part;                 // [shares][2][kTilePart]
 };
-// Shares of the attention kernels, as many as run at once: few rows, two waves for each SIMD; many, two workgroups for each CU.
+// Shares of the attention kernels, as many as run at once on 256 CUs: a wave each with few rows, two for each SIMD; a workgroup each
+// with many, two for each CU.
 constexpr int kBlockRowShares = 2048;
 constexpr int kBlockTileShares = 512;
 constexpr int kRowPart = 16 * kChunkPart;   // floats of a 16-row block's state: its sums, then {reference, sum, -, -} of each row
@@ -388,6 +389,7 @@ constexpr int kTilePart = 4 * 17 * 64 * 4;  // of a 128-row block's: four waves,
 // Rows up to which a sequence goes to the few-row kernel: in calls of few rows altogether (of all query heads) its many pieces
 // fill the device where blocks of 128 rows do not.  (us, few-row kernel / many-row kernel, 32 / 8 heads) 64 tokens of one sequence over
 // 8192 42 / 59, of 16 over 2048 77 / 87, of 64 over 2048 335 / 256; 16 tokens of 64 over 2048 90 / 120, 32 tokens 169 / 134.
+// One sequence's 64 tokens over 32768, which the host cannot tell from those over 8192: 128 / 104.
 constexpr int kBlockFewRows = 64, kBlockFewRowsSmall = 256;
 constexpr long long kBlockSmall = 32768;  // rows of all query heads
 inline int block_few_rows(long long Hq, long long total_new) { return total_new * Hq <= kBlockSmall ? kBlockFewRowsSmall : kBlockFewRows; }

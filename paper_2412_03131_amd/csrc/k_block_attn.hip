@@ -40,7 +40,7 @@ __device__ __forceinline__ Tiles tiles_of(const BlockAttnArgs& a, int n, int L)
 // A tile of fp16 rows in LDS (16 KB): keys [2: token / 16][4: s = 2 i + w][4: r][16: token % 16][8 dims], dims
 // (4 i + r) 16 + 8 w ..; values [4: u][2: j][4: r][16: dim][8 tokens], both as a block's codes are taken.  Tokens from
 // `end` on are zero, and so are values that are not finite (0 * inf would reach the rows that do
-// not see them): their tokens' bits go into *odd.
+// not see them): put_value returns their tokens' bits, and their products follow one by one.
 constexpr int kRowTileBytes = 4 * kBlockSide;
 
 struct RowSource {
@@ -288,7 +288,8 @@ __device__ __forceinline__ int coded_steps(const Tiles& tl, int L)
 // took 102 us, half of it at barriers.
 //
 // Bound by memory.  A wave asks for a tile's keys again as soon as their codes are operands, and for its values likewise, so 8 KB
-// of the next tile are always on their way.
+// of the next tile are always on their way.  64 single tokens over 1024 .. 4096, 32 / 8 heads: 72 us, 345 MB at 4.8 TB/s; two
+// tiles ahead gained nothing, two row tiles for a wave took 41 us instead of 28 (24 requests' drafts over a window of 2048).
 constexpr int kRowWaves = 4;    // of a workgroup
 constexpr int kRowStart = 3;    // units of a block's start, in tiles of the cache
 constexpr int kRowTile = 4;     // and of a tile of fp16 rows
@@ -576,12 +577,16 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void block_rows(BlockAttnArgs a)
 
 // ---- many rows: a workgroup on 128 rows -------------------------------------------------
 // Four waves of 32 rows each go over the same tiles.  A tile is brought into LDS once, as fp16 operands (a block's
-// codes are converted on the way), one step ahead of its use: its loads are asked for before a step's products and
-// written behind them.  v_mfma_f32_32x32x16_f16: A lane l holds row l % 32, k 8 (l / 32) .. + 7, B the same with columns, C
-// lane l in register i row 8 (i / 4) + i % 4 + 4 (l / 32) of column l % 32.
+// codes are converted on the way), one step ahead of its use, and its loads are asked for a step before that.
+// v_mfma_f32_32x32x16_f16: A lane l holds row l % 32, k 8 (l / 32) .. + 7, B the same with columns, C lane l in register i row
+// 8 (i / 4) + i % 4 + 4 (l / 32) of column l % 32.
 //
 // All (sequence, KV head, 128 rows) are laid end to end and cut into equal shares, one for each workgroup; shares that follow
 // each other run on one XCD, so that its L2 serves their tiles.
+//
+// Bound by issue, the matrix products before the rest: 2048 tokens over 8192, 64 / 8 heads, take 896 us, 691 TFLOP/s of the two
+// products; the weights' second part adds half as many again (weights rounded once: 770 us, where this took 932).  A third wave
+// on a SIMD does not fit its registers (spilled: 1117 us).
 constexpr int kTileRows = 128, kTileWaves = 4;
 constexpr int kTileShare = 8;  // least units of a share
 constexpr int kTileStart = 4;  // a 128-row block's start, in tiles

@@ -89,7 +89,7 @@ __device__ __forceinline__ float head_sum(float x)
 // The same with each head over its root mean square first, times its side's weights w: a head is whole in its eight lanes'
 // registers, so the row is still read once.  Queries, then keys; a side's weights enter the cosines and sines, once per row:
 //   a' = m (a (w_a cos) - b (w_b sin)), b' = m (b (w_b cos) + a (w_a sin)), m = 1 / sqrt(mean + eps).
-// Bound by memory as the rotation: 32767 rows of 48 heads take 160 us (weights read for every head: 175).
+// Bound by memory as the rotation: 32767 rows of 48 heads take 158 us (weights read for every head: 175).
 __global__ __launch_bounds__(256) void norm_rotate_rows(RotateArgs a, int waves_per_row)
 {
     for (long long w = (long long)blockIdx.x * 4 + wave_index(); w < a.rows * waves_per_row; w += (long long)gridDim.x * 4) {

@@ -79,7 +79,8 @@ __device__ __forceinline__ float get_one(__amdgpu_buffer_rsrc_t r, int lane_offs
 // ---- the item of a wave ----------------------------------------------------------------
 // Sequences in order, each with a number of items; a wave finds the one that holds a given item, 64 sequences at a time
 // (a lane a sequence).  The last 64 are kept from one search to the next: a call of up to 64 sequences reads their
-// lengths once.  Loads(b, n, L) gives a sequence's rows and tokens, unclamped; rows are clamped to [0, most] and to those
+// lengths once.  In larger ones four 64s' lengths are asked for at once, and where each 64 (or a few of them) starts is kept, a
+// lane each, so that a search reads one 64 again.  Loads(b, n, L) gives a sequence's rows and tokens, unclamped; rows are clamped to [0, most] and to those
 // left of `total`.  Items(n, L): a sequence's items.
 struct SeqItem {
     int b, n, L;          // b < 0: there is none
@@ -96,14 +97,22 @@ struct SeqScan {
     int base = -1, n, L;             // the lanes' sequences: base + lane; rows and tokens
     long long before, incl, count;   // rows before the lane's sequence; items up to its end; its items
     long long row_end, item_end;     // behind the 64
+    int stride;                      // 64s from one kept start to the next
+    long long row_at, item_at;       // the lane's start: rows and items before it
 
     __device__ __forceinline__ SeqScan(int B_, int most_, long long rows_, Loads l, Items i) : B(B_), most(most_), rows(rows_), loads(l), items(i) {}
     __device__ __forceinline__ void load(int from, long long row, long long item)
     {
+        int n0 = 0, L0 = 0;
+        if (from + lane_id() < B) loads(from + lane_id(), n0, L0);
+        take(from, n0, L0, row, item);
+    }
+    __device__ __forceinline__ void take(int from, int n0, int L0, long long row, long long item)
+    {
         base = from;
+        n = n0;
+        L = L0;
         const int b = base + lane_id();
-        n = L = 0;
-        if (b < B) loads(b, n, L);
         bad = bad || __ballot(n < 0 || n > most) != 0;
         n = n < 0 ? 0 : (n > most ? most : n);
         before = row + (wave_incl_scan_wide(n) - n);
@@ -118,14 +127,41 @@ struct SeqScan {
     // All sequences' items.
     __device__ __forceinline__ long long total()
     {
-        load(0, 0, 0);
-        while (base + kWave < B) load(base + kWave, row_end, item_end);
+        constexpr int kAtOnce = 4;
+        stride = (B - 1) / (kWave * kWave) + 1;
+        row_at = 0;
+        item_at = INT64_MAX;
+        row_end = item_end = 0;
+        int kept = 0, left = 0;
+        for (int from = 0; from < B; from += kAtOnce * kWave) {
+            int n4[kAtOnce], L4[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                const int b = from + i * kWave + lane_id();
+                n4[i] = L4[i] = 0;
+                if (b < B) loads(b, n4[i], L4[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                if (from + i * kWave >= B) break;
+                if (left == 0) {
+                    if (lane_id() == kept) row_at = row_end, item_at = item_end;
+                    ++kept;
+                    left = stride;
+                }
+                --left;
+                take(from + i * kWave, n4[i], L4[i], row_end, item_end);
+            }
+        }
         return item_end;
     }
     // The sequence that holds item `want` (after total()).
     __device__ __forceinline__ SeqItem find(long long want)
     {
-        if (want < read_lane<long long>(incl - count, 0)) load(0, 0, 0);
+        if (want < read_lane<long long>(incl - count, 0) || want >= item_end) {
+            const int at = __popcll(__ballot(item_at <= want)) - 1;  // the last that starts at `want` or before
+            load(at * stride * kWave, read_lane<long long>(row_at, at), read_lane<long long>(item_at, at));
+        }
         while (want >= item_end && base + kWave < B) load(base + kWave, row_end, item_end);
         SeqItem s{-1, 0, 0, 0, 0};
         const unsigned long long past = __ballot(incl > want);

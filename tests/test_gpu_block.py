@@ -403,6 +403,37 @@ def test_many_sequences():
     attend(plain_of(rng, lens, 1, E4M3), new, 4, "many sequences")
 
 
+@pytest.mark.parametrize("B", [64, 65, 256, 257, 4096, 4097, 8300])
+def test_numbers_of_sequences(B):
+    """Both sides of the numbers of sequences that a wave reads at once, and keeps the starts of: attention, append, read."""
+    rng = np.random.default_rng(27 + B)
+    lens = [int(n) for n in rng.integers(0, 40, B)]
+    new = [int(n) for n in (rng.random(B) < 0.4) * rng.integers(1, 4, B)]
+    idle = min(128, B // 4)  # (in large calls a whole 64 of them)
+    new[B // 3:B // 3 + idle] = [0] * idle
+    new[B // 2], new[B - 1] = 70, 1
+    plain = plain_of(rng, lens, 1, INT8)
+    c, q, k, v, _, _ = attend(plain, new, 4, "%d sequences" % B)
+    free = sorted(set(range(c.num_blocks)) - set(c.table.cpu().numpy().ravel().tolist()))
+    table = c.table.cpu().numpy()
+    for b in range(B):  # (blocks that the call fills and that find no ID are dropped)
+        for i in range(lens[b] // T, (lens[b] + new[b]) // T):
+            if free:
+                table[b, i] = free.pop()
+    c.table.copy_(to(table))
+    dk.block_append(c, ints(new), k, v)
+    plain.append(new, k.cpu().numpy(), v.cpu().numpy())
+    c.seq_len += ints(new)
+    same_cache(c, plain, "append to %d sequences" % B)
+    start, count = [len(r[0]) // T * T for r in plain.rows], [len(r[0]) % T for r in plain.rows]
+    kb, vb = dk.block_read(c, ints(start), ints(count), sum(count))
+    torch.cuda.synchronize()
+    assert int(c.status) == 0
+    for side, x in enumerate((kb, vb)):
+        want = np.concatenate([r[side][s:] for r, s in zip(plain.rows, start)])
+        assert np.array_equal(x.cpu().numpy().view(np.int16), want.view(np.int16))
+
+
 def test_one_long_among_single_tokens():
     rng = np.random.default_rng(14)
     new = [1] * 20

@@ -81,8 +81,8 @@ __device__ __forceinline__ float get_one(__amdgpu_buffer_rsrc_t r, int lane_offs
 // (a lane a sequence).  The last 64 are kept from one search to the next: a call of up to 64 sequences reads their
 // lengths once.  In larger ones four 64s' lengths are asked for at once, and where each 64 (or a few of them) starts is kept, a
 // lane each, so that a search reads one 64 again (attention of 4096 sequences' single tokens over 128, 8 / 1 heads:
-// 99 -> 74 us; of 1024 over 64, 32 / 8 heads: 56 -> 49).  Loads(b, n, L) gives a sequence's rows and tokens, unclamped; rows are clamped to [0, most] and to those
-// left of `total`.  Items(n, L): a sequence's items.
+// 99 -> 74 us; of 1024 over 64, 32 / 8 heads: 56 -> 49).  Loads(b, n, L) gives a sequence's rows and tokens, unclamped; rows are
+// clamped to [0, most] and to those left of `total`.  Items(n, L): a sequence's items.
 struct SeqItem {
     int b, n, L;          // b < 0: there is none
     long long row0;       // the sequence's first row

@@ -614,6 +614,41 @@ def test_two_calls_at_once():
         assert all(torch.equal(o, want[i][0]) and torch.equal(e, want[i][1]) for o, e in got[i])
 
 
+@pytest.mark.parametrize("n", [2, 150])  # (few rows, many)
+def test_addresses_past_32_bits(n):
+    """Blocks behind 4 GiB of pool, rows 2^24 elements apart: as near ones, bit for bit."""
+    rng = np.random.default_rng(28)
+    H, lens = 8, [150, 64]
+    L = dk.layout(max_seq_len=300)
+    k0, v0 = to(keys_of(rng, sum(lens), H)), to(halves(rng, sum(lens), H, D))
+    q, k, v = (x.contiguous() for x in rows_of(rng, 2 * n, 2 * H, H))
+    far = torch.empty((2 * n - 1) * (1 << 24) + 4 * H * D, dtype=torch.float16, device=DEV)
+    apart = [far[at * D:].as_strided(x.shape, (1 << 24, D, 1)) for x, at in ((q, 0), (k, 2 * H), (v, 3 * H))]
+    for to_, x in zip(apart, (q, k, v)):
+        to_.copy_(x)
+    got = []
+    for blocks, rows in ((40, (q, k, v)), (66000, apart)):
+        c = dk.BlockCache(L, blocks, 2, H, fmt=INT8, device=DEV)
+        c.table.copy_(blocks - 1 - torch.arange(c.table.numel(), dtype=torch.int32, device=DEV).view(c.table.shape))
+        dk.block_append(c, ints(lens), k0, v0)
+        c.seq_len += ints(lens)
+        out, lse = dk.block_attention(c, ints([n, n]), *rows, SCALE)
+        dk.block_append(c, ints([n, n]), *rows[1:])
+        c.seq_len += n
+        total = sum(lens) + 2 * n
+        got.append((out, lse, *dk.block_read(c, ints([0, 0]), ints([x + n for x in lens]), total), c.scale[-1]))
+        assert int(c.status) == 0
+    torch.cuda.synchronize()
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+    assert got[0][2][:150].abs().sum() > 0
+    freq = dk.rope_frequencies(128)[0].to(DEV)
+    pos = torch.arange(2 * n, dtype=torch.int32, device=DEV)
+    near = dk.norm_rotate(L, pos, freq, q, k)
+    dk.norm_rotate(L, pos, freq, apart[0], apart[1], q_out=apart[0], k_out=apart[1])
+    assert torch.equal(near[0], apart[0]) and torch.equal(near[1], apart[1])
+
+
 def test_a_stream_of_another_gpu_is_refused():
     c = dk.BlockCache(dk.layout(max_seq_len=64), 4, 1, 1, device=DEV)
     k = torch.zeros((1, 1, D), dtype=torch.float16, device=DEV)

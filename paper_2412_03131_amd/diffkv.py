@@ -1,9 +1,13 @@
 """Thin ctypes binding of libdiffkv.so (the C ABI declared in include/diffkv.h).
 
 Argument marshalling only: every step of the hot path runs in the HIP
-kernels of the library.  PyTorch provides device memory and the stream.
+kernels of the library.  PyTorch provides device memory and the stream: the
+current one, or the one that a call is given.  Buffers that a call is not given
+come from its stream; a result that another stream uses is ordered by the
+program, as torch's own are (wait_stream, record_stream).
 Loading fails loudly when the library has not been built.
 """
+import contextlib
 import ctypes as C
 import os
 import struct
@@ -171,8 +175,27 @@ def _cache_struct(c):
         c.num_kv_heads))
 
 
-def _new_ws(nbytes, device):
-    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+_HERE = contextlib.nullcontext()
+
+
+def _on(stream):
+    """What a call does by itself before its launch is done on the stream that it runs on."""
+    if stream is None or (stream.cuda_stream == _stream(None) and stream.device.index == torch._C._cuda_getDevice()):
+        return _HERE
+    return torch.cuda.stream(stream)
+
+
+def _new(stream, shape, dtype, device):
+    """A buffer that a call is not given, taken from its stream: the bytes of one taken from another may be in use there
+    as the call's kernels start, or that stream's next buffer before they end."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _on(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _new_ws(nbytes, device, stream):
+    return _new(stream, max(nbytes, 256), torch.uint8, device)
 
 
 def _check_ws(code, what, *sizes):
@@ -250,7 +273,7 @@ def quantize_append(cache, new_len, k, v, score, quota=None, alpha_h=0.0, alpha_
         max_new = int(nl.max()) if max_new is None else max_new
     sizes = (OP_APPEND, L, cache.num_seqs, 0, cache.num_kv_heads, total_new)
     if ws is None:
-        ws = _new_ws(workspace_size(*sizes), cache.pool.device)
+        ws = _new_ws(workspace_size(*sizes), cache.pool.device, stream)
     _check_ws(lib().diffkv_quantize_append(
         C.byref(L), _cache_struct(cache), int(total_new), int(max_new), _ptr(new_len), _ptr(_bits16(k)),
         _ptr(_bits16(v)), _ptr(score), _ptr(quota), float(alpha_h), float(alpha_l), int(window),
@@ -264,12 +287,12 @@ def decode_attention(cache, q, sm_scale, out=None, lse=None, num_splits=0, ws=No
     L = cache.L
     B, Hq, D = q.shape
     if out is None:
-        out = torch.empty((B, Hq, D), dtype=torch.float32, device=q.device)
+        out = _new(stream, (B, Hq, D), torch.float32, q.device)
     if lse is None and want_lse:
-        lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
+        lse = _new(stream, (B, Hq), torch.float32, q.device)
     sizes = (OP_ATTENTION, L, cache.num_seqs, Hq, cache.num_kv_heads, 0, num_splits)
     if ws is None:
-        ws = _new_ws(workspace_size(*sizes), q.device)
+        ws = _new_ws(workspace_size(*sizes), q.device, stream)
     _check_ws(lib().diffkv_decode_attention(
         C.byref(L), _cache_struct(cache), Hq, _ptr(_bits16(q)), float(sm_scale), _ptr(out), _ptr(lse),
         int(num_splits), ws.data_ptr(), ws.nbytes, _stream(stream)), "diffkv_decode_attention", *sizes)
@@ -304,10 +327,10 @@ def prompt_significance(L, new_len, q, k, sm_scale, lse=None, score=None, max_ne
     if max_new is None:
         max_new = int(new_len.max().item()) if B else 0
     if score is None:
-        score = torch.empty((rows, Hkv), dtype=torch.float32, device=q.device)
+        score = _new(stream, (rows, Hkv), torch.float32, q.device)
     sizes = (OP_PROMPT_SIGNIFICANCE, L, B, Hq, Hkv, rows)
     if ws is None:
-        ws = _new_ws(workspace_size(*sizes), q.device)
+        ws = _new_ws(workspace_size(*sizes), q.device, stream)
     _check_ws(lib().diffkv_prompt_significance(C.byref(L), B, rows, int(max_new), _ptr(new_len), Hq, Hkv,
                                                _ptr(_bits16(q)), _ptr(_bits16(k)), float(sm_scale), _ptr(lse),
                                                _ptr(score), ws.data_ptr(), ws.nbytes, _stream(stream)),
@@ -334,7 +357,10 @@ def _on_one_gpu(what, *tensors):
 
 
 def _stream_at(what, stream, t):
-    """A stream's address; it has to be one of the GPU that t is on (a kernel runs where its stream is)."""
+    """A stream's address; it has to be one of the GPU that t is on (a kernel runs where its stream is).  Asked for
+    before a call allocates: buffers come from its stream."""
+    if t.get_device() < 0:
+        raise ValueError("%s: tensors on one GPU expected" % what)
     if (torch._C._cuda_getDevice() if stream is None else stream.device.index) != t.get_device():
         raise ValueError("%s: a stream of the tensors' GPU expected (None: the current GPU's)" % what)
     return _stream(stream)
@@ -357,7 +383,7 @@ def rope_frequencies(rot_dim, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, trai
     return freq, scale.value
 
 
-def _rotate_args(what, L, pos, inv_freq, q, k, q_out, k_out):
+def _rotate_args(what, L, pos, inv_freq, q, k, q_out, k_out, stream):
     """Checked arguments of both rotating calls, their outputs allocated unless given:
     (rows, q_out, k_out, (q, stride, out, stride), (heads of k, k, stride, out, stride))."""
     rows, Hq = q.shape[0], q.shape[1]
@@ -366,9 +392,9 @@ def _rotate_args(what, L, pos, inv_freq, q, k, q_out, k_out):
     if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq: contiguous fp32 expected")
     if q_out is None:
-        q_out = torch.empty((rows, Hq, q.shape[2]), dtype=q.dtype, device=q.device)
+        q_out = _new(stream, (rows, Hq, q.shape[2]), q.dtype, q.device)
     if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        k_out = _new(stream, k.shape, k.dtype, k.device)
     if q_out.shape != q.shape or (k is not None and (k_out.shape != k.shape or k.shape[0] != rows)):
         raise ValueError("%s: outputs shaped as their inputs expected" % what)
     ka = (0, None, 0, None, 0) if k is None else (
@@ -381,7 +407,8 @@ def rotate(L, pos, inv_freq, q, k=None, style=ROPE_HALF, scale=1.0, q_out=None, 
     """Rotary positions: q fp16 [rows, Hq, D], k fp16 [rows, Hkv, D] or None (rows may be strided), pos int32
     [rows], inv_freq fp32 [rot_dim / 2] (device) -> (q_out, k_out), contiguous unless given; q_out=q turns in
     place."""
-    rows, q_out, k_out, qa, (Hkv, kp, ks, kop, kos) = _rotate_args("rotate", L, pos, inv_freq, q, k, q_out, k_out)
+    rows, q_out, k_out, qa, (Hkv, kp, ks, kop, kos) = _rotate_args(
+        "rotate", L, pos, inv_freq, q, k, q_out, k_out, stream)
     _on_one_gpu("rotate", q, k, pos, inv_freq, q_out, k_out)
     _check(lib().diffkv_rotate(C.byref(L), rows, _ptr(pos), _ptr(inv_freq), 2 * inv_freq.shape[0], int(style),
                                float(scale), q.shape[1], *qa, Hkv, kp, ks, kop, kos, _stream(stream)),
@@ -393,14 +420,15 @@ def norm_rotate(L, pos, inv_freq, q, k=None, q_weight=None, k_weight=None, eps=1
                 q_out=None, k_out=None, stream=None):
     """Each head over its root mean square times its side's weights (fp32 [D] or None: ones), then rotated:
     arguments and results as rotate."""
+    at = _stream_at("norm_rotate", stream, q)
     rows, q_out, k_out, (qp, qs, qop, qos), (Hkv, kp, ks, kop, kos) = _rotate_args(
-        "norm_rotate", L, pos, inv_freq, q, k, q_out, k_out)
+        "norm_rotate", L, pos, inv_freq, q, k, q_out, k_out, stream)
     _dense(q_weight, "q_weight", torch.float32, L.head_dim)
     _dense(k_weight, "k_weight", torch.float32, L.head_dim)
     _on_one_gpu("norm_rotate", q, k, pos, inv_freq, q_weight, k_weight, q_out, k_out)
     _check(lib().diffkv_norm_rotate(C.byref(L), rows, _ptr(pos), _ptr(inv_freq), 2 * inv_freq.shape[0], int(style),
                                     float(scale), float(eps), q.shape[1], qp, qs, _ptr(q_weight), qop, qos, Hkv, kp, ks,
-                                    _ptr(k_weight), kop, kos, _stream_at("norm_rotate", stream, q)), "diffkv_norm_rotate")
+                                    _ptr(k_weight), kop, kos, at), "diffkv_norm_rotate")
     return q_out, k_out
 
 
@@ -428,15 +456,15 @@ def chunk_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, slopes
     rows, Hq, D = q.shape
     max_new = _chunk(cache, new_len, max_new, "chunk_attention", q, k, v)
     if out is None:
-        out = torch.empty((rows, Hq, D), dtype=torch.float16, device=q.device)
+        out = _new(stream, (rows, Hq, D), torch.float16, q.device)
     if lse is None and want_lse:
-        lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
+        lse = _new(stream, (rows, Hq), torch.float32, q.device)
     _dense(out, "out", torch.float16, rows, Hq, D)
     _dense(lse, "lse", torch.float32, rows, Hq)
     _dense(slopes, "slopes", torch.float32, Hq)
     sizes = (OP_CHUNK_ATTENTION, cache.L, cache.num_seqs, Hq, cache.num_kv_heads, rows)
     if ws is None:
-        ws = _new_ws(workspace_size(*sizes), q.device)
+        ws = _new_ws(workspace_size(*sizes), q.device, stream)
     (qp, qs), (kp, ks), (vp, vs) = (_rows(t, w, cache.L.head_dim) for t, w in ((q, "q"), (k, "k"), (v, "v")))
     _on_one_gpu("chunk_attention", q, k, v, new_len, slopes, out, lse, ws)
     _check_ws(lib().diffkv_chunk_attention(
@@ -453,13 +481,13 @@ def chunk_significance(cache, new_len, q, k, sm_scale, lse, cap=0.0, window=0, s
     rows, Hq = q.shape[0], q.shape[1]
     max_new = _chunk(cache, new_len, max_new, "chunk_significance", q, k)
     if score is None:
-        score = torch.empty((rows, cache.num_kv_heads), dtype=torch.float32, device=q.device)
+        score = _new(stream, (rows, cache.num_kv_heads), torch.float32, q.device)
     _dense(lse, "lse", torch.float32, rows, Hq)
     _dense(score, "score", torch.float32, rows, cache.num_kv_heads)
     _dense(slopes, "slopes", torch.float32, Hq)
     sizes = (OP_CHUNK_SIGNIFICANCE, cache.L, cache.num_seqs, Hq, cache.num_kv_heads, rows)
     if ws is None:
-        ws = _new_ws(workspace_size(*sizes), q.device)
+        ws = _new_ws(workspace_size(*sizes), q.device, stream)
     (qp, qs), (kp, ks) = (_rows(t, w, cache.L.head_dim) for t, w in ((q, "q"), (k, "k")))
     _on_one_gpu("chunk_significance", q, k, new_len, slopes, lse, score, ws)
     _check_ws(lib().diffkv_chunk_significance(
@@ -557,7 +585,8 @@ def block_read(cache, start, count, total, max_count=None, k_out=None, v_out=Non
     """diffkv_block_read: positions start[b] .. + count[b] - 1 of each sequence (int32 [B], device) as fp16 rows
     [total, Hkv, D], one sequence's behind the other's -> (k_out, v_out)."""
     shape = (int(total), cache.num_kv_heads, cache.L.head_dim)
-    k_out, v_out = (torch.empty(shape, dtype=torch.float16, device=cache.tail.device) if t is None else t
+    at = _stream_at("block_read", stream, cache.pool)
+    k_out, v_out = (_new(stream, shape, torch.float16, cache.tail.device) if t is None else t
                     for t in (k_out, v_out))
     _block_lens(cache, start, "block_read")
     _block_lens(cache, count, "block_read")
@@ -565,8 +594,8 @@ def block_read(cache, start, count, total, max_count=None, k_out=None, v_out=Non
     _on_one_gpu("block_read", k_out, v_out, start, count, cache.pool)
     if max_count is None:
         max_count = _longest(count)
-    _check(lib().diffkv_block_read(cache.L, cache.struct(), shape[0], int(max_count), start.data_ptr(), count.data_ptr(), *kv,
-                                   _stream_at("block_read", stream, k_out)), "diffkv_block_read")
+    _check(lib().diffkv_block_read(cache.L, cache.struct(), shape[0], int(max_count), start.data_ptr(), count.data_ptr(), *kv, at),
+           "diffkv_block_read")
     return k_out, v_out
 
 
@@ -579,23 +608,24 @@ def block_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, sinks=
     _block_lens(cache, new_len, "block_attention")
     kv = _block_rows(cache, k, v, "block_attention", rows)
     qp, qs = _rows(q, "q", cache.L.head_dim)
+    at = _stream_at("block_attention", stream, cache.pool)
     if out is None:
-        out = torch.empty((rows, Hq, D), dtype=torch.float16, device=q.device)
+        out = _new(stream, (rows, Hq, D), torch.float16, q.device)
     if lse is None and want_lse:
-        lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
+        lse = _new(stream, (rows, Hq), torch.float32, q.device)
     _dense(out, "out", torch.float16, rows, Hq, D)
     _dense(lse, "lse", torch.float32, rows, Hq)
     _dense(slopes, "slopes", torch.float32, Hq)
     sizes = (OP_BLOCK_ATTENTION, cache.L, cache.num_seqs, Hq, cache.num_kv_heads, rows)
     if ws is None:
-        ws = _new_ws(workspace_size(*sizes), q.device)
+        ws = _new_ws(workspace_size(*sizes), q.device, stream)
     _on_one_gpu("block_attention", q, k, v, new_len, slopes, out, lse, ws, cache.pool)
     if max_new is None:
         max_new = _longest(new_len)
     _check_ws(lib().diffkv_block_attention(
         cache.L, cache.struct(), rows, int(max_new), new_len.data_ptr(), Hq, qp, qs, *kv, float(sm_scale),
-        _form(cap, window, slopes), int(sinks), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes,
-        _stream_at("block_attention", stream, q)), "diffkv_block_attention", *sizes)
+        _form(cap, window, slopes), int(sinks), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes, at),
+        "diffkv_block_attention", *sizes)
     return out, lse
 
 
@@ -605,7 +635,7 @@ def compact_free_list(cache, release, num_tables=None, ws=None, stream=None):
     nt = cache.num_tables if num_tables is None else num_tables
     sizes = (OP_COMPACT, L, cache.num_seqs, 0, cache.num_kv_heads)
     if ws is None:
-        ws = _new_ws(workspace_size(*sizes), cache.pool.device)
+        ws = _new_ws(workspace_size(*sizes), cache.pool.device, stream)
     _check_ws(lib().diffkv_compact_free_list(C.byref(L), _cache_struct(cache), int(nt), _ptr(release), ws.data_ptr(), ws.nbytes,
                        _stream(stream)), "diffkv_compact_free_list", *sizes)
     return ws
@@ -617,7 +647,7 @@ def alloc_pages(cache, demand, num_tables=None, ws=None, stream=None):
     nt = cache.num_tables if num_tables is None else num_tables
     sizes = (OP_ALLOC, L, cache.num_seqs, 0, cache.num_kv_heads)
     if ws is None:
-        ws = _new_ws(workspace_size(*sizes), cache.pool.device)
+        ws = _new_ws(workspace_size(*sizes), cache.pool.device, stream)
     _check_ws(lib().diffkv_alloc_pages(C.byref(L), _cache_struct(cache), int(nt), _ptr(demand), ws.data_ptr(), ws.nbytes,
                        _stream(stream)), "diffkv_alloc_pages", *sizes)
     return ws
@@ -628,7 +658,7 @@ def generation_step(cache, alpha_h, alpha_l, recent_window, ws=None, stream=None
     L = cache.L
     sizes = (OP_GENERATION, L, cache.num_seqs, 0, cache.num_kv_heads)
     if ws is None:
-        ws = _new_ws(workspace_size(*sizes), cache.pool.device)
+        ws = _new_ws(workspace_size(*sizes), cache.pool.device, stream)
     _check_ws(lib().diffkv_generation_step(C.byref(L), _cache_struct(cache), float(alpha_h), float(alpha_l),
                                            int(recent_window), ws.data_ptr(), ws.nbytes, _stream(stream)),
               "diffkv_generation_step", *sizes)

@@ -179,7 +179,7 @@ _HERE = contextlib.nullcontext()
 
 
 def _on(stream):
-    """What a call does by itself before its launch is done on the stream that it runs on."""
+    """What a call does before its launch (lengths read, buffers taken) is done on the stream that it runs on."""
     if stream is None or (stream.cuda_stream == _stream(None) and stream.device.index == torch._C._cuda_getDevice()):
         return _HERE
     return torch.cuda.stream(stream)
@@ -192,6 +192,12 @@ def _new(stream, shape, dtype, device):
         return torch.empty(shape, dtype=dtype, device=device)
     with _on(stream):
         return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _longest(lens, stream):
+    """Read with a synchronization of the call's stream: where its kernels read the lengths, they are written by then."""
+    with _on(stream):
+        return int(lens.max().item()) if lens.shape[0] else 0
 
 
 def _new_ws(nbytes, device, stream):
@@ -268,7 +274,8 @@ def quantize_append(cache, new_len, k, v, score, quota=None, alpha_h=0.0, alpha_
     (read from new_len with a device sync when omitted)."""
     L = cache.L
     if total_new is None or max_new is None:
-        nl = new_len.cpu()
+        with _on(stream):
+            nl = new_len.cpu()
         total_new = int(nl.sum()) if total_new is None else total_new
         max_new = int(nl.max()) if max_new is None else max_new
     sizes = (OP_APPEND, L, cache.num_seqs, 0, cache.num_kv_heads, total_new)
@@ -325,7 +332,7 @@ def prompt_significance(L, new_len, q, k, sm_scale, lse=None, score=None, max_ne
     rows, Hq, Hkv = q.shape[0], q.shape[1], k.shape[1]
     B = new_len.shape[0]
     if max_new is None:
-        max_new = int(new_len.max().item()) if B else 0
+        max_new = _longest(new_len, stream)
     if score is None:
         score = _new(stream, (rows, Hkv), torch.float32, q.device)
     sizes = (OP_PROMPT_SIGNIFICANCE, L, B, Hq, Hkv, rows)
@@ -358,7 +365,7 @@ def _on_one_gpu(what, *tensors):
 
 def _stream_at(what, stream, t):
     """A stream's address; it has to be one of the GPU that t is on (a kernel runs where its stream is).  Asked for
-    before a call allocates: buffers come from its stream."""
+    before a call allocates or reads lengths, which it does there."""
     if t.get_device() < 0:
         raise ValueError("%s: tensors on one GPU expected" % what)
     if (torch._C._cuda_getDevice() if stream is None else stream.device.index) != t.get_device():
@@ -432,11 +439,11 @@ def norm_rotate(L, pos, inv_freq, q, k=None, q_weight=None, k_weight=None, eps=1
     return q_out, k_out
 
 
-def _chunk(cache, new_len, max_new, what, q, *rows):
+def _chunk(cache, new_len, max_new, what, stream, q, *rows):
     if new_len.dtype != torch.int32 or new_len.shape != (cache.num_seqs,) or not new_len.is_contiguous():
         raise ValueError("%s: new_len: contiguous int32 [num_seqs] expected" % what)
     if max_new is None:
-        max_new = int(new_len.max().item()) if new_len.shape[0] else 0
+        max_new = _longest(new_len, stream)
     for t in rows:
         if t.shape[0] != q.shape[0] or t.shape[1] != cache.num_kv_heads:
             raise ValueError("%s: [rows, num_kv_heads, head_dim] keys and values expected" % what)
@@ -454,7 +461,7 @@ def chunk_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, slopes
     sequence, may be strided), new_len int32 [B] (device) -> out fp16 [rows, Hq, D], lse fp32 [rows, Hq].
     Call it before the rows are appended."""
     rows, Hq, D = q.shape
-    max_new = _chunk(cache, new_len, max_new, "chunk_attention", q, k, v)
+    max_new = _chunk(cache, new_len, max_new, "chunk_attention", stream, q, k, v)
     if out is None:
         out = _new(stream, (rows, Hq, D), torch.float16, q.device)
     if lse is None and want_lse:
@@ -479,7 +486,7 @@ def chunk_significance(cache, new_len, q, k, sm_scale, lse, cap=0.0, window=0, s
     """diffkv_chunk_significance: the chunk's probabilities (lse from chunk_attention with the same q, k and
     form) enter the cached tokens' scores in place; returns the new tokens' scores, fp32 [rows, Hkv]."""
     rows, Hq = q.shape[0], q.shape[1]
-    max_new = _chunk(cache, new_len, max_new, "chunk_significance", q, k)
+    max_new = _chunk(cache, new_len, max_new, "chunk_significance", stream, q, k)
     if score is None:
         score = _new(stream, (rows, cache.num_kv_heads), torch.float32, q.device)
     _dense(lse, "lse", torch.float32, rows, Hq)
@@ -564,10 +571,6 @@ def _block_rows(cache, k, v, what, rows):
     return kp, ks, vp, vs
 
 
-def _longest(lens):
-    return int(lens.max().item()) if lens.shape[0] else 0
-
-
 def block_append(cache, new_len, k, v, max_new=None, stream=None):
     """diffkv_block_append: k, v fp16 [rows, Hkv, D] (device, rows concatenated per sequence, may be strided), new_len
     int32 [B] (device), into cache (a BlockCache) at seq_len, which is not advanced."""
@@ -575,10 +578,11 @@ def block_append(cache, new_len, k, v, max_new=None, stream=None):
     rows = k.shape[0]
     kv = _block_rows(cache, k, v, "block_append", rows)
     _on_one_gpu("block_append", k, v, new_len, cache.pool)
+    at = _stream_at("block_append", stream, k)
     if max_new is None:
-        max_new = _longest(new_len)
-    _check(lib().diffkv_block_append(cache.L, cache.struct(), rows, int(max_new), new_len.data_ptr(), *kv,
-                                     _stream_at("block_append", stream, k)), "diffkv_block_append")
+        max_new = _longest(new_len, stream)
+    _check(lib().diffkv_block_append(cache.L, cache.struct(), rows, int(max_new), new_len.data_ptr(), *kv, at),
+           "diffkv_block_append")
 
 
 def block_read(cache, start, count, total, max_count=None, k_out=None, v_out=None, stream=None):
@@ -593,7 +597,7 @@ def block_read(cache, start, count, total, max_count=None, k_out=None, v_out=Non
     kv = _block_rows(cache, k_out, v_out, "block_read", shape[0])
     _on_one_gpu("block_read", k_out, v_out, start, count, cache.pool)
     if max_count is None:
-        max_count = _longest(count)
+        max_count = _longest(count, stream)
     _check(lib().diffkv_block_read(cache.L, cache.struct(), shape[0], int(max_count), start.data_ptr(), count.data_ptr(), *kv, at),
            "diffkv_block_read")
     return k_out, v_out
@@ -621,7 +625,7 @@ def block_attention(cache, new_len, q, k, v, sm_scale, cap=0.0, window=0, sinks=
         ws = _new_ws(workspace_size(*sizes), q.device, stream)
     _on_one_gpu("block_attention", q, k, v, new_len, slopes, out, lse, ws, cache.pool)
     if max_new is None:
-        max_new = _longest(new_len)
+        max_new = _longest(new_len, stream)
     _check_ws(lib().diffkv_block_attention(
         cache.L, cache.struct(), rows, int(max_new), new_len.data_ptr(), Hq, qp, qs, *kv, float(sm_scale),
         _form(cap, window, slopes), int(sinks), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes, at),

@@ -84,3 +84,33 @@ def test_buffers_come_from_the_stream_of_the_call(calls, name, given):
     assert calls["launched"] == ["diffkv_" + name]
     assert calls["allocated"] == [HERE if given is None else given] * buffers
     assert calls["current"] == [HERE]
+
+
+@pytest.mark.parametrize("name", ["quantize_append", "prompt_significance", "chunk_attention", "chunk_significance",
+                                  "block_append", "block_read", "block_attention"])
+@pytest.mark.parametrize("given", [None, HERE, OTHER], ids=["none", "current", "other"])
+def test_lengths_are_read_on_the_stream_of_the_call(calls, monkeypatch, name, given):
+    """A program may still be writing them there."""
+    L = dk.layout(max_seq_len=256)
+    f16, i32, f32 = torch.float16, torch.int32, torch.float32
+    q, kv, lens = torch.zeros((3, 4, 128), dtype=f16), torch.zeros((3, 2, 128), dtype=f16), torch.tensor([2, 1], dtype=i32)
+    score, lse = torch.zeros((3, 2), dtype=f32), torch.zeros((3, 4), dtype=f32)
+    c, u = dk.Cache(L, 8, 2, 2, device="cpu"), dk.BlockCache(L, 8, 2, 2, device="cpu")
+    s = None if given is None else Stream(given)
+    call = {
+        "quantize_append": lambda: dk.quantize_append(c, lens, kv, kv, score, stream=s),
+        "prompt_significance": lambda: dk.prompt_significance(L, lens, q, kv, 0.1, stream=s),
+        "chunk_attention": lambda: dk.chunk_attention(c, lens, q, kv, kv, 0.1, stream=s),
+        "chunk_significance": lambda: dk.chunk_significance(c, lens, q, kv, 0.1, lse, stream=s),
+        "block_append": lambda: dk.block_append(u, lens, kv, kv, stream=s),
+        "block_read": lambda: dk.block_read(u, lens, lens, 3, stream=s),
+        "block_attention": lambda: dk.block_attention(u, lens, q, kv, kv, 0.1, stream=s),
+    }[name]
+    read, real_max, real_cpu = [], torch.Tensor.max, torch.Tensor.cpu
+    monkeypatch.setattr(torch.Tensor, "max", lambda t, *a: read.append(calls["current"][-1]) or real_max(t, *a))
+    monkeypatch.setattr(torch.Tensor, "cpu", lambda t, *a: read.append(calls["current"][-1]) or real_cpu(t, *a))
+    call()
+    assert calls["launched"] == ["diffkv_" + name]
+    # (quantize_append copies them to the host first: what it does there is no matter)
+    assert read[0] == (HERE if given is None else given)
+    assert calls["current"] == [HERE]

@@ -48,3 +48,26 @@ def test_two_streams_without_buffers():
     torch.cuda.synchronize()
     for i, results in got:
         assert all(torch.equal(x, y) for x, y in zip(results, want[i]))
+
+
+def test_lengths_written_on_the_stream_of_the_call():
+    """Without max_new the lengths are read where the call runs, behind what writes them there."""
+    rng = np.random.default_rng(32)
+    plain = ref.Plain(2, 1, dk.BLOCK_E4M3)
+    plain.append([70, 40], *(rng.standard_normal((110, 1, D)).astype(np.float16) for _ in (0, 1)))
+    c = ref.filled(dk, plain, 300, DEV)
+    q, k, v = (torch.from_numpy(rng.standard_normal((90, h, D)).astype(np.float16)).to(DEV) for h in (4, 1, 1))
+    lens = torch.tensor([80, 10], dtype=torch.int32, device=DEV)
+    want = dk.block_attention(c, lens, q, k, v, SCALE)
+    a = torch.randn((4096, 4096), device=DEV)
+    late = torch.zeros_like(lens)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(20):
+            a = a @ a
+            a = a / a.abs().max()
+        late.copy_(lens)
+    got = dk.block_attention(c, late, q, k, v, SCALE, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))

@@ -604,7 +604,7 @@ diffkv_status diffkv_block_read(const diffkv_layout* layout, const diffkv_block_
  * rounded once.  The order of a row's sums, and with it the last bits, goes by the
  * call's lengths.
  * A NaN or infinite key or value of a tail or chunk reaches only the rows that see its token;
- * a block whose scale is NaN, those that see one of its tokens.
+ * a block whose scale is NaN, those that see one of its tokens.  Values do not reach lse.
  */
 diffkv_status diffkv_block_attention(const diffkv_layout* layout, const diffkv_block_cache* cache,
                                      int64_t total_new, int32_t max_new, const int32_t* new_len,

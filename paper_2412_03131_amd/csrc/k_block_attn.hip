@@ -163,8 +163,8 @@ __device__ __forceinline__ void raise(const BlockAttnArgs& a, TileScale& t, cons
 {
     constexpr float unit = MOD ? kChunkLn2 : 1.0f;
     const int group = N == 8 ? lane_id() >> 4 : lane_id() >> 5;
-    if (t.nan) {  // (a block that reads NaN, to the rows that see one of its tokens)
-        t.ks = 1.0f, t.add = 0.0f;
+    if (t.nan && __builtin_isnan(t.ks)) {  // (keys that read NaN, to the rows that see one of their tokens)
+        t.ks = 1.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i) y[i] = __builtin_nanf("");
     }
@@ -205,6 +205,13 @@ __device__ __forceinline__ void exponents(const TileScale& t, float (&y)[N], flo
     const float less = t.add - ref;
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = MOD ? (y[i] + less) * kChunkLog2e : __builtin_fmaf(y[i], t.ks, less);
+}
+// Values that read NaN, to the rows that see one of their tokens: a NaN among a row's weights, behind their sum, reaches all of its
+// sums of values and not its normalizer.
+template <int N>
+__device__ __forceinline__ void spoil(const BlockAttnArgs& a, const TileView& w, float (&y)[N], int p)
+{
+    if (w.whole || p - (w.pos0 + kBT - 1) < a.window || w.pos0 < a.sinks) y[0] = __builtin_nanf("");
 }
 // Weights as two fp16 parts, four at a time.
 struct Parts {
@@ -254,6 +261,7 @@ __device__ __forceinline__ StepScales step_scales(const BlockAttnArgs& a, int id
     StepScales s;
     vs *= kCodeUnit;
     s.nan = __ballot(__builtin_isnan(ks + vs));
+    vs = __builtin_isnan(vs) ? kCodeUnit : vs;
     s.ks = ks * kCodeUnit * a.scale_x;
     s.add = __builtin_amdgcn_logf(vs) * (MOD ? kChunkLn2 : 1.0f);
     s.rs = vs > 0.0f && vs < INFINITY ? 1.0f / vs : 1.0f;
@@ -370,6 +378,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void block_rows(BlockAttnArgs a)
                     total += y[j];
                 }
                 sum = __builtin_fmaf(total, ts.rs, sum);
+                if (ts.nan) spoil(a, view, y, p);
                 return parts(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
             };
 
@@ -742,6 +751,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void block_tiles(BlockAttnArgs 
                     total[j & 1] += y[j];
                 }
                 sum = __builtin_fmaf(total[0] + total[1], ts.rs, sum);
+                if (ts.nan) spoil(a, view, y, p);
                 const Parts w0 = parts(y[0], y[1], y[2], y[3], y[8], y[9], y[10], y[11]);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) acc[u] = mfma_32(x[u], w0.hi, acc[u]);

@@ -1,0 +1,101 @@
+"""The uniform 8-bit cache's attention where its operands are not finite, and its ends: against the 64-bit definitions of
+block_ref.  Tolerances as test_gpu_block derives them."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():  # pragma: no cover
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import block_ref as ref  # noqa: E402
+from block_ref import D  # noqa: E402
+from paper_2412_03131_amd import diffkv as dk  # noqa: E402
+
+DEV = "cuda"
+SCALE = 1.0 / np.sqrt(128.0)
+E4M3, INT8 = dk.BLOCK_E4M3, dk.BLOCK_INT8
+FORMS = {"plain": {}, "windowed": dict(window=45, sinks=5), "formed": dict(cap=20.0, slopes=True),
+         "all": dict(cap=5.0, slopes=True, window=45, sinks=5)}
+
+
+def halves(rng, *shape, size=1.0):
+    return (rng.standard_normal(shape) * size).astype(np.float16)
+
+
+def to(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def plain_of(rng, lens, H, fmt):
+    p = ref.Plain(len(lens), H, fmt)
+    p.append(lens, halves(rng, sum(lens), H, D), halves(rng, sum(lens), H, D))
+    return p
+
+
+def form_of(name, heads):
+    form = dict(FORMS[name])
+    if form.get("slopes"):
+        form["slopes"] = (2.0 ** -np.arange(1, heads + 1)).astype(np.float32)
+    return form
+
+
+def attend(plain, new, q, k, v, scale=SCALE, room=0, drop=(), **form):
+    """Outputs and normalizers of new's rows as numpy; `room` rows more are in the call than the sequences have."""
+    c = ref.filled(dk, plain, max(len(r[0]) for r in plain.rows) + max(new), DEV, drop=drop)
+    if form.get("slopes") is not None:
+        form["slopes"] = to(form["slopes"])
+    q, k, v = (to(np.concatenate([x, np.zeros((room,) + x.shape[1:], x.dtype)])) for x in (q, k, v))
+    out, lse = dk.block_attention(c, ints(new), q, k, v, scale, max_new=max(new) + room, **form)
+    torch.cuda.synchronize()
+    return out.cpu().numpy()[:sum(new)].astype(np.float64), lse.cpu().numpy()[:sum(new)].astype(np.float64)
+
+
+def check(plain, new, q, k, v, got, what, scale=SCALE, measure=None, drop=(), **form):
+    """Values within their tolerances, and what is not finite as it should be.  `measure`: (plain, k) whose products say
+    how far the scores may be off, where those of plain and k are infinite."""
+    kept = lambda b, i: (b, i) not in drop
+    G = q.shape[1] // plain.H
+    with np.errstate(all="ignore"):
+        sizes = [x[6:] for x in ref.attention((measure or (plain, k))[0], new, q, (measure or (plain, k))[1],
+                                              np.nan_to_num(v, posinf=0, neginf=0), scale, kept, **form)]
+        for (b, h, row, n, want, want_lse, *_), (A, size, keys, V) in zip(ref.attention(plain, new, q, k, v, scale, kept, **form), sizes):
+            A, V = np.nan_to_num(A), float(np.nan_to_num(V))
+            size = np.nan_to_num(size)
+            d = 64 * 2.0 ** -24 * size + 2.0 ** -20
+            tol = 2.0 ** -11 * np.abs(want) + (2 * d[..., None] + 2.0 ** -20 + keys * 2.0 ** -28) * A + \
+                keys * 2.0 ** -31 * V * max(1.0, V) + 2.0 ** -25
+            g = got[0][row:row + n, h * G:(h + 1) * G].transpose(1, 0, 2)
+            fine = np.isfinite(want)
+            odd = np.isfinite(g) != fine
+            assert not odd.any(), "%s b=%d h=%d: %d that should (not) be finite" % (what, b, h, odd.sum())
+            bad = fine & ~(np.abs(g - want) <= tol)
+            assert not bad.any(), "%s b=%d h=%d: %d wrong, first %s: %r, expected %r" % (
+                what, b, h, bad.sum(), np.argwhere(bad)[0], g[bad][0], want[bad][0])
+            gl = got[1][row:row + n, h * G:(h + 1) * G].T
+            fine = np.isfinite(want_lse)
+            odd = np.isfinite(gl) != fine
+            assert not odd.any(), "%s b=%d h=%d: %d lse that should (not) be finite" % (what, b, h, odd.sum())
+            bad = fine & ~(np.abs(gl - want_lse) <= d + 2.0 ** -22 * np.abs(want_lse))
+            assert not bad.any(), "%s b=%d h=%d lse: %r, expected %r" % (what, b, h, gl[bad][0], want_lse[bad][0])
+
+
+@pytest.mark.parametrize("fmt", [E4M3, INT8])
+@pytest.mark.parametrize("form", sorted(FORMS))
+@pytest.mark.parametrize("n", [6, 200])  # (few rows, many)
+def test_a_block_whose_values_read_nan(fmt, form, n):
+    """The outputs of the rows that see one of its tokens are NaN; their normalizers know no values."""
+    rng = np.random.default_rng(41)
+    form = form_of(form, 4)
+    lens, new = [100, 64], [n, n]
+    plain = plain_of(rng, lens, 1, fmt)
+    plain.rows[0][1][40, 0, 17] = np.nan
+    q, k, v = halves(rng, 2 * n, 4, D), halves(rng, 2 * n, 1, D), halves(rng, 2 * n, 1, D)
+    got = attend(plain, new, q, k, v, **form)
+    assert np.isfinite(got[1]).all() and np.isnan(got[0][0]).all() and np.isfinite(got[0][n:]).all()
+    check(plain, new, q, k, v, got, "values", **form)

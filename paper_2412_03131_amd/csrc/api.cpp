@@ -786,7 +786,8 @@ diffkv_status diffkv_block_attention(const diffkv_layout* layout, const diffkv_b
     a.k_stride = k_stride;
     a.v_stride = v_stride;
     const bool mod = form && (form->cap > 0.0f || form->slopes);
-    a.scale_x = mod ? sm_scale : sm_scale * 1.4426950408889634f;
+    // (times a block's scale never zero, which would make NaN of a hidden token's -inf; products below 2^39 give no score at 2^-80)
+    a.scale_x = mod ? sm_scale : fmaxf(sm_scale * 1.4426950408889634f, 0x1p-80f);
     if (mod && form->cap > 0.0f) {
         a.cap = form->cap;
         a.cap_in = 2.0f * 1.4426950408889634f / form->cap;

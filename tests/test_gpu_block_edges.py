@@ -99,3 +99,16 @@ def test_a_block_whose_values_read_nan(fmt, form, n):
     got = attend(plain, new, q, k, v, **form)
     assert np.isfinite(got[1]).all() and np.isnan(got[0][0]).all() and np.isfinite(got[0][n:]).all()
     check(plain, new, q, k, v, got, "values", **form)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-38, 1e-42, 1.5e-45])
+@pytest.mark.parametrize("n", [6, 200])
+def test_scales_of_scores_down_to_zero(scale, n):
+    """Hidden tokens stay hidden where a score's scale rounds to nothing."""
+    rng = np.random.default_rng(42)
+    plain = plain_of(rng, [100, 0], 1, E4M3)
+    plain.rows[0][0][:] *= np.float16(2.0 ** -12)
+    new = [n, n]
+    q, k, v = halves(rng, 2 * n, 4, D), halves(rng, 2 * n, 1, D), halves(rng, 2 * n, 1, D)
+    got = attend(plain, new, q, k, v, scale=scale, window=45, sinks=5)
+    check(plain, new, q, k, v, got, "scale %g" % scale, scale=scale, window=45, sinks=5)

@@ -12,11 +12,11 @@
 //           lane order again and holds two tiles of 16 dims.
 #pragma once
 
+#include "block_units.hpp"
 #include "chunk_common.hpp"
 
 namespace dkv {
 
-constexpr int kBT = 32;                       // positions per block
 constexpr int kBlockSide = kBT * kD;          // bytes of a block's keys (or values) of one KV head
 constexpr int kBlockBytes = 2 * kBlockSide;
 enum BlockFmt { kE4m3 = 0, kInt8 = 1 };

@@ -20,22 +20,6 @@ namespace {
 
 constexpr float kRefBelow = 12.0f, kRefRoom = 15.0f;  // log2 units
 
-// The tiles that a sequence's new tokens see, in order: [0, sb) and [w0, last].
-struct Tiles {
-    int sb, w0, last;
-    __device__ __forceinline__ int count() const { return sb + last + 1 - w0; }
-    __device__ __forceinline__ int at(int step) const { return step < sb ? step : w0 + step - sb; }
-};
-__device__ __forceinline__ Tiles tiles_of(const BlockAttnArgs& a, int n, int L)
-{
-    Tiles t;
-    t.last = (L + n - 1) / kBT;
-    const int sb = a.sinks / kBT + (a.sinks % kBT != 0);
-    t.sb = min(sb, t.last + 1);
-    t.w0 = max(t.sb, max(0, L + 1 - a.window) / kBT);
-    return t;
-}
-
 // ---- fp16 rows as operands -------------------------------------------------------------
 // A tile of fp16 rows in LDS (16 KB): keys [2: token / 16][4: s = 2 i + w][4: r][16: token % 16][8 dims], dims
 // (4 i + r) 16 + 8 w ..; values [4: u][2: j][4: r][16: dim][8 tokens], both as a block's codes are taken.  Tokens from
@@ -596,9 +580,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void block_rows(BlockAttnArgs a)
 // Bound by issue, the matrix products before the rest: 2048 tokens over 8192, 64 / 8 heads, take 896 us, 691 TFLOP/s of the two
 // products; the weights' second part adds half as many again (weights rounded once: 770 us, where this took 932).  A third wave
 // on a SIMD does not fit its registers (spilled: 1117 us).
-constexpr int kTileRows = 128, kTileWaves = 4;
+constexpr int kTileWaves = 4;
 constexpr int kTileShare = 8;  // least units of a share
-constexpr int kTileStart = 4;  // a 128-row block's start, in tiles
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f16v mfma_32(h8 a, h8 b, f16v c)
@@ -606,31 +589,6 @@ __device__ __forceinline__ f16v mfma_32(h8 a, h8 b, f16v c)
     f16v d = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
     asm("" : "+v"(d) : "v"(a), "v"(b));
     return d;
-}
-
-// Units of a sequence's 128-row blocks up to block t: each counts about as many as it has tiles.  They grow with the rows'
-// positions until the window is full; between its ends a sum of that shape in closed form stands for them.
-struct TileUnits {
-    int blocks, full;        // 128-row blocks; from `full` on all have as many tiles
-    long long first, most;   // units of block 0, of those from `full` on
-    __device__ __forceinline__ long long upto(long long t) const
-    {
-        // (up to 2^23 tokens of up to 64 heads: g <= 2^22, and most - first <= 2^18, so the product is below 2^62)
-        const long long g = t < full ? t : full;
-        return first * g + (most - first) * g * (g - 1) / (2 * (long long)max(full, 1)) + most * (t - g);
-    }
-};
-__device__ __forceinline__ TileUnits tile_units(const BlockAttnArgs& a, int n, int L)
-{
-    TileUnits u;
-    u.blocks = (n * a.G + kTileRows - 1) / kTileRows;
-    const int step = (kTileRows + a.G - 1) / a.G;  // tokens of a block, about
-    u.first = tiles_of(a, min(n, step), L).count() + kTileStart;
-    const int last = max(0, n - step);
-    const int late = a.window < L + last ? max(0, min(last, a.window - L)) : last;
-    u.full = late / step;
-    u.most = max((long long)tiles_of(a, min(n - late, step), L + late).count() + kTileStart, u.first);
-    return u;
 }
 
 struct TileLds {

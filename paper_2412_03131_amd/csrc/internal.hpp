@@ -389,7 +389,9 @@ constexpr int kTilePart = 4 * 17 * 64 * 4;  // of a 128-row block's: four waves,
 // Rows up to which a sequence goes to the few-row kernel: in calls of few rows altogether (of all query heads) its many pieces
 // fill the device where blocks of 128 rows do not.  (us, few-row kernel / many-row kernel, 32 / 8 heads) 64 tokens of one sequence over
 // 8192 42 / 59, of 16 over 2048 77 / 87, of 64 over 2048 335 / 256; 16 tokens of 64 over 2048 90 / 120, 32 tokens 169 / 134.
-// One sequence's 64 tokens over 32768, which the host cannot tell from those over 8192: 128 / 104.
+// One sequence's 64 tokens over 32768, which the host cannot tell from those over 8192: 128 / 104.  Other groups: 8 / 8 heads, 64 tokens
+// of 64 over 2048 88 / 111, 200 of one over 8192 40 / 74, 200 of four 109 / 94; 64 / 8 heads, 4 tokens of 64 over 2048 78 / 103, 8 tokens
+// 81 / 108; 128 / 8 heads, 8 tokens 153 / 119.
 constexpr int kBlockFewRows = 64, kBlockFewRowsSmall = 256;
 constexpr long long kBlockSmall = 32768;  // rows of all query heads
 inline int block_few_rows(long long Hq, long long total_new) { return total_new * Hq <= kBlockSmall ? kBlockFewRowsSmall : kBlockFewRows; }

@@ -10,7 +10,7 @@
 //
 // Bound by memory, with few rows by a chain of loads.  A wave takes one block of one side and KV head, all of it in registers, so
 // the maximum needs no second read and no workgroup waits for another: 32768 tokens of 8 KV heads are appended in 46 us (201 MB at
-// 4.3 TB/s), 16 sequences of 32701 read back in 647 us (3.2 GB at 5.0 TB/s).
+// 4.3 TB/s; 37 where the last-level cache still holds the rows), 16 sequences of 32701 read back in 647 us (3.2 GB at 5.0 TB/s).
 #include "block_common.hpp"
 
 namespace dkv {

@@ -279,14 +279,18 @@ __device__ __forceinline__ int coded_steps(const Tiles& tl, int L)
 // alike (the older is served first), so none waits for another: with pieces of eight waves that met in LDS, 64 ragged requests
 // took 102 us, half of it at barriers.
 //
-// Bound by memory.  A wave asks for a tile's keys again as soon as their codes are operands, and for its values likewise, so 8 KB
-// of the next tile are always on their way.  64 single tokens over 1024 .. 4096, 32 / 8 heads: 72 us, 345 MB at 4.8 TB/s; two
-// tiles ahead gained nothing, two row tiles for a wave took 41 us instead of 28 (24 requests' drafts over a window of 2048).
+// Bound by memory where there are many sequences.  A wave asks for a tile's keys again as soon as their codes are operands, and for
+// its values likewise, so 8 KB of the next tile are always on their way.  64 single tokens over 1024 .. 4096, 32 / 8 heads: 73 us,
+// 345 MB at 4.7 TB/s; two tiles ahead gained nothing, two row tiles for a wave took 41 us instead of 28 (24 requests' drafts over a
+// window of 2048).
 constexpr int kRowWaves = 4;    // of a workgroup
 constexpr int kRowStart = 3;    // units of a block's start, in tiles of the cache
 constexpr int kRowTile = 4;     // and of a tile of fp16 rows
 constexpr int kQuads = 4;      // quads of a lane in a join
-constexpr int kRowShare = 6;    // least units of a piece
+// Least units of a piece.  A block's pieces grow in number with its length, and one wave joins them all: short contexts want small
+// pieces, lone long ones large ones.  (us with 6 / 12 / 24 / 48, one token, 32 / 8 heads) over 600 13.6 / 16.8 / 23.4 / 36.8, over 4096
+// 28 / 22 / 27 / 40, over 32768 211 / 56 / 60 / 74; 64 tokens over 2560 69.9 / 69.9 / 71.0 / 98.
+constexpr int kRowShare = 6;
 
 template <int FMT, bool MOD>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void block_rows(BlockAttnArgs a)
@@ -577,11 +581,14 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void block_rows(BlockAttnArgs a)
 // All (sequence, KV head, 128 rows) are laid end to end and cut into equal shares, one for each workgroup; shares that follow
 // each other run on one XCD, so that its L2 serves their tiles.
 //
-// Bound by issue, the matrix products before the rest: 2048 tokens over 8192, 64 / 8 heads, take 896 us, 691 TFLOP/s of the two
-// products; the weights' second part adds half as many again (weights rounded once: 770 us, where this took 932).  A third wave
-// on a SIMD does not fit its registers (spilled: 1117 us).
+// Bound by issue, the matrix products before the rest: 2048 tokens over 8192, 64 / 8 heads, take 899 us, 689 TFLOP/s of the two
+// products (867 to 970 us from card to card); the weights' second part adds half as many again (weights rounded once: 770 us, where
+// this took 932).  A cap takes 1299 us where a call without takes 869, slopes 1107, both 1395.  A third wave on a SIMD does not fit
+// its registers (spilled: 1117 us).
 constexpr int kTileWaves = 4;
-constexpr int kTileShare = 8;  // least units of a share
+// Least units of a share (us with 8 / 16 / 32, one sequence): 512 tokens alone, 32 / 8 heads, 39 / 49 / 75; 300 tokens over 8192, 4 / 1
+// heads, 70 / 58 / 69, whose blocks are cut into some 33 pieces with 8; of longer parts the same.
+constexpr int kTileShare = 8;
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f16v mfma_32(h8 a, h8 b, f16v c)
